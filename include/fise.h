@@ -456,6 +456,75 @@ int fise_masked_attention_restricted(const void* x, const void* ln_gamma, const 
                                      void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Transformer denoisers: products of a few rows with 4-bit weights, the norms
+ * around a block with its gate and modulation, attention over a cache of latent
+ * vectors.  Together they are a block whose weights, cache and conditioning are
+ * small; the masked 1x1 convolution writes the latent cache at the active tokens.
+ * ------------------------------------------------------------------------ */
+
+/* 4-bit weights W[N, K] (out, in): W[n, k] = s[n, k / group] * q[n, k], q a whole
+ * number in -8..7, s bf16, group 32, 64, 128 or 256 columns (the last one may be
+ * shorter).  N, K in 1..2^20.  `packed` (fise_w4_bytes bytes, 16-byte aligned) is laid
+ * out once for the matrix unit and belongs to the caller.
+ * fise_w4_pack: w [N, K] float or bf16.  scale NULL: the library chooses s = the
+ * largest magnitude of the group / 7, rounded to bf16, and q = the nearest whole number
+ * to w / s, so that a weight comes back within s / 2; a group with a value that is
+ * not finite comes back as NaN.  scale given (bf16 [N, ceil(K / group)], finite): q =
+ * the nearest of -8..7 to w / s (codes that exist already: w = s q in float, which is
+ * exact); where s is 0, q is 0.
+ * fise_w4_unpack: w [N, K] = s q, in float exact, in bf16 rounded once (for products of
+ * many rows, as the 1x1 convolution takes them). */
+size_t fise_w4_bytes(int N, int K, int group);
+int fise_w4_pack(const void* w, int dtype, const void* scale, int N, int K, int group, void* packed, void* stream);
+int fise_w4_unpack(const void* packed, int N, int K, int group, void* w, int dtype, void* stream);
+
+/* y[m, n] = sum_k act(x[m, k]) W[n, k] + bias[n] (+ residual[m, n]), act = SiLU with
+ * silu_in, else identity.  Made for few rows (M up to about 64: time embeddings,
+ * single tokens, the tokens a mask leaves at the deep levels); more rows are taken 64
+ * at a time, the weights read again for each.  x, y and bias have a type of their own
+ * (residual has y's); all sums are float: the products of a group first, then those
+ * sums times their scale.  x rows: K and x_stride multiples of 8, 16-byte aligned; y and
+ * residual rows: any alignment of their type.  residual may be y itself; y must not
+ * otherwise overlap an input.  M == 0 touches nothing. */
+typedef struct {
+    const void* x; int x_dtype; int64_t x_stride;           /* [M, K], rows x_stride elements apart */
+    const void* packed; int N, K, group;
+    const void* bias; int bias_dtype;                       /* [N] or NULL */
+    const void* residual; int64_t residual_stride;          /* [M, N] or NULL */
+    void* y; int y_dtype; int64_t y_stride;                 /* [M, N] */
+    int M; int silu_in;
+} fise_w4_linear_args;
+int fise_w4_linear(const fise_w4_linear_args* a /* host */, void* stream);
+
+/* The norms around a block, its gate and its modulation, in one pass over the rows:
+ *   r = res_scale * x + gate[b] * Npost(h)
+ *   y = Npre(r) * (1 + mod_scale[b]) + mod_shift[b]
+ * N(v) = v / rms(v) * w (FISE_NORM_RMS), (v - mean(v)) / std(v) * w + b
+ * (FISE_NORM_LAYER) or v (FISE_NORM_NONE), over the C channels of a row, biased
+ * variance plus eps under the root; w / b NULL = 1 / 0 (b only with FISE_NORM_LAYER).
+ * h NULL: no branch (r = res_scale * x).  gate, mod_scale, mod_shift: float [B, C],
+ * batch element b at + b * mod_stride, NULL = 1, 0, 0.  y is computed from r before r is
+ * rounded.  r or y may be NULL (not both).
+ * x and r are maps [B, H, W, C]; rows: those of the active tiles, or with tile == 0 (tile_idx
+ * ignored) all of them.  h and y are compact rows [B, M, C] in list order, tile by tile and
+ * row-major inside a tile (tile == 0: token order), or maps with h_is_map / y_is_map;
+ * rows of r and of a map y that are not active keep their value.  r may be x; y may be h or x
+ * if it has the same form; nothing else may overlap.  C a multiple of 8, at most 16384. */
+typedef enum { FISE_NORM_NONE = 0, FISE_NORM_LAYER = 1, FISE_NORM_RMS = 2 } fise_norm_kind;
+typedef struct {
+    const void* x; int B, H, W, C; int dtype;
+    const void* h; int h_is_map;
+    int post_norm; const void* post_w; const void* post_b;  /* on h */
+    const float* gate; float res_scale;
+    int pre_norm; const void* pre_w; const void* pre_b;     /* on r */
+    const float* mod_scale; const float* mod_shift; int64_t mod_stride;
+    float eps;
+    const int32_t* tile_idx; int n_active; int tile;
+    void* r; void* y; int y_is_map;
+} fise_gated_norm_args;
+int fise_masked_gated_norm(const fise_gated_norm_args* a /* host */, void* stream);
+
+/* ------------------------------------------------------------------------
  * Tracing.  With profiling enabled every launch of the gathered-GEMM and
  * attention kernels is bracketed by two HIP events on the caller's stream
  * (host objects; no device memory).  fise_profile_read(kind, ...) waits for the

@@ -58,6 +58,19 @@ class fise_transformer_args(C.Structure):
                 ("tile_idx", vp), ("n_active", i32), ("tile", i32), ("stats_fresh", i32)]
 
 
+class fise_w4_linear_args(C.Structure):
+    _fields_ = [("x", vp), ("x_dtype", i32), ("x_stride", i64), ("packed", vp), ("N", i32), ("K", i32), ("group", i32),
+                ("bias", vp), ("bias_dtype", i32), ("residual", vp), ("residual_stride", i64),
+                ("y", vp), ("y_dtype", i32), ("y_stride", i64), ("M", i32), ("silu_in", i32)]
+
+
+class fise_gated_norm_args(C.Structure):
+    _fields_ = [("x", vp), ("B", i32), ("H", i32), ("W", i32), ("C", i32), ("dtype", i32), ("h", vp), ("h_is_map", i32),
+                ("post_norm", i32), ("post_w", vp), ("post_b", vp), ("gate", vp), ("res_scale", f32),
+                ("pre_norm", i32), ("pre_w", vp), ("pre_b", vp), ("mod_scale", vp), ("mod_shift", vp), ("mod_stride", i64), ("eps", f32),
+                ("tile_idx", vp), ("n_active", i32), ("tile", i32), ("r", vp), ("y", vp), ("y_is_map", i32)]
+
+
 class fise_unet_desc(C.Structure):
     _fields_ = [("in_ch", i32), ("out_ch", i32), ("base", i32), ("n_levels", i32),
                 ("mults", i32 * FISE_MAX_LEVELS), ("attn", i32 * FISE_MAX_LEVELS), ("layers", i32),
@@ -116,6 +129,11 @@ _SIGS = {
     "fise_unet_cache_move_active": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]),
     "fise_unet_cache_move_tile_rows": (i32, [vp, vp, vp, C.POINTER(i32), i32, i32, i32, i32, vp]),
     "fise_masked_unet_step": (i32, [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, C.POINTER(i32), vp, sz, vp]),
+    "fise_w4_bytes": (sz, [i32, i32, i32]),
+    "fise_w4_pack": (i32, [vp, i32, vp, i32, i32, i32, vp, vp]),
+    "fise_w4_unpack": (i32, [vp, i32, i32, i32, vp, i32, vp]),
+    "fise_w4_linear": (i32, [C.POINTER(fise_w4_linear_args), vp]),
+    "fise_masked_gated_norm": (i32, [C.POINTER(fise_gated_norm_args), vp]),
     "fise_profile_enable": (i32, [i32]),
     "fise_profile_calibrate": (i32, [i32, vp]),
     "fise_calibrate_peaks": (i32, [vp, sz, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
@@ -376,6 +394,123 @@ def fise_masked_transformer_block_workspace_bytes(args):
 def fise_masked_transformer_block(args, workspace, stream=None):
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _ck(lib().fise_masked_transformer_block(C.byref(args), _p(workspace), nbytes, _stream(stream)))
+
+
+# --------------------------------------------------------------------------- transformer denoisers
+def _like(name, t, shape, dtype):
+    """A tensor of that shape and one of those types, contiguous in memory."""
+    if tuple(t.shape) != tuple(shape) or t.dtype not in dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype} with strides {t.stride()}")
+
+
+def _rows_of(name, t, shape):
+    """Distance between the rows of a two-dimensional tensor whose columns are neighbours."""
+    if tuple(t.shape) != tuple(shape) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected rows {tuple(shape)} with neighbouring columns, got {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def fise_w4_bytes(N, K, group):
+    n = lib().fise_w4_bytes(N, K, group)
+    if n == 0:
+        raise FiseError(-2, fise_last_error())
+    return n
+
+
+def _packed_size(packed, N, K, group):
+    if packed.numel() * packed.element_size() < fise_w4_bytes(N, K, group):
+        raise ValueError(f"packed weights of {N} x {K} in groups of {group} take {fise_w4_bytes(N, K, group)} bytes")
+
+
+def fise_w4_pack(w, packed, group, scale=None, stream=None):
+    N, K = w.shape
+    _like("w", w, (N, K), (torch.float32, torch.bfloat16))
+    _packed_size(packed, N, K, group)
+    if scale is not None:
+        _like("scale", scale, (N, -(-K // group)), (torch.bfloat16,))
+    _ck(lib().fise_w4_pack(_p(w), _dt(w), _p(scale), N, K, group, _p(packed), _stream(stream)))
+
+
+def fise_w4_unpack(packed, w, group, stream=None):
+    N, K = w.shape
+    _like("w", w, (N, K), (torch.float32, torch.bfloat16))
+    _packed_size(packed, N, K, group)
+    _ck(lib().fise_w4_unpack(_p(packed), N, K, group, _p(w), _dt(w), _stream(stream)))
+
+
+def w4_linear_args(x, packed, group, y, bias=None, residual=None, silu_in=False):
+    """Arguments of fise_w4_linear for x [M, K] and y [M, N], rows any distance apart; they keep the tensors alive."""
+    M, K = x.shape
+    N = y.shape[1]
+    _packed_size(packed, N, K, group)
+    a = fise_w4_linear_args()
+    a.x, a.x_dtype, a.x_stride = _p(x), _dt(x), _rows_of("x", x, (M, K))
+    if M == 1:
+        a.x_stride = (K + 7) // 8 * 8
+    a.packed, a.N, a.K, a.group = _p(packed), N, K, group
+    if bias is not None:
+        _like("bias", bias, (N,), (torch.float32, torch.bfloat16))
+        a.bias, a.bias_dtype = _p(bias), _dt(bias)
+    a.y, a.y_dtype, a.y_stride = _p(y), _dt(y), _rows_of("y", y, (M, N))
+    if residual is not None:
+        if residual.dtype != y.dtype:
+            raise ValueError(f"residual is {residual.dtype}, y {y.dtype}")
+        a.residual, a.residual_stride = _p(residual), _rows_of("residual", residual, (M, N))
+    a.M, a.silu_in = M, int(bool(silu_in))
+    a.keep = (x, packed, bias, residual, y)
+    return a
+
+
+def fise_w4_linear(args, stream=None):
+    _ck(lib().fise_w4_linear(C.byref(args), _stream(stream)))
+
+
+FISE_NORM_NONE, FISE_NORM_LAYER, FISE_NORM_RMS = 0, 1, 2
+_NORMS = {"none": FISE_NORM_NONE, "layer": FISE_NORM_LAYER, "rms": FISE_NORM_RMS}
+
+
+def gated_norm_args(x, h=None, post="none", post_w=None, post_b=None, gate=None, res_scale=1.0, pre="none", pre_w=None, pre_b=None,
+                    mod_scale=None, mod_shift=None, eps=1e-5, tile_idx=None, n_active=0, tile=0, r=None, y=None):
+    """Arguments of fise_masked_gated_norm; they keep the tensors alive.  x and r are maps [B, H, W, C]; h and y maps too, or compact rows [B, M, C].
+    gate, mod_scale, mod_shift: float [B, C], with the same distance between their rows."""
+    B, H, W, Cc = x.shape
+    M = n_active * tile * tile if tile else H * W
+    types = (x.dtype,)
+    a = fise_gated_norm_args()
+    _like("x", x, (B, H, W, Cc), (torch.float32, torch.bfloat16))
+    a.x, a.B, a.H, a.W, a.C, a.dtype = _p(x), B, H, W, Cc, _dt(x)
+    for name, t in (("h", h), ("y", y)):
+        if t is not None:
+            _like(name, t, (B, H, W, Cc) if t.dim() == 4 else (B, M, Cc), types)
+            setattr(a, name, _p(t))
+            setattr(a, name + "_is_map", int(t.dim() == 4))
+    if r is not None:
+        _like("r", r, (B, H, W, Cc), types)
+        a.r = _p(r)
+    for name, t in (("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b)):
+        if t is not None:
+            _like(name, t, (Cc,), types)
+            setattr(a, name, _p(t))
+    strides = set()
+    for name, t in (("gate", gate), ("mod_scale", mod_scale), ("mod_shift", mod_shift)):
+        if t is not None:
+            if t.dtype != torch.float32:
+                raise ValueError(f"{name}: float is what modulations are, got {t.dtype}")
+            strides.add(_rows_of(name, t, (B, Cc)) if B > 1 else 0)
+            setattr(a, name, _p(t))
+    if len(strides) > 1:
+        raise ValueError(f"gate, mod_scale and mod_shift: rows {sorted(strides)} apart, they share one distance")
+    a.mod_stride = strides.pop() if strides else 0
+    if tile_idx is not None and (tile_idx.dtype != torch.int32 or not tile_idx.is_contiguous() or tile_idx.numel() < n_active):
+        raise ValueError(f"tile_idx: expected {n_active} int32 numbers")
+    a.post_norm, a.pre_norm, a.res_scale, a.eps = _NORMS[post], _NORMS[pre], res_scale, eps
+    a.tile_idx, a.n_active, a.tile = _p(tile_idx), n_active, tile
+    a.keep = (x, h, post_w, post_b, gate, pre_w, pre_b, mod_scale, mod_shift, tile_idx, r, y)
+    return a
+
+
+def fise_masked_gated_norm(args, stream=None):
+    _ck(lib().fise_masked_gated_norm(C.byref(args), _stream(stream)))
 
 
 # --------------------------------------------------------------------------- UNet

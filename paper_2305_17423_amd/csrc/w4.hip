@@ -1,0 +1,333 @@
+// Products of a few rows with 4-bit weights: y[m, n] = sum_k act(x[m, k]) s[n, k / g] q[n, k] + bias[n] (+ residual[m, n]), q a whole number from -8 to 7,
+// s one bf16 number for g columns of an output.
+//
+// The weight bytes bound it (a byte holds two weights and is read once), and next to them the instructions that make bf16 of them.  So the weights are laid out
+// once as operands of the matrix unit (w4_choice.h): a wave reads 1 KB of consecutive bytes, 16 outputs x 128 columns, and a lane's 16 bytes are its part of
+// four 16x16x32 instructions.  A weight goes to float as q / 16 (v_cvt_off_f32_i4) and two of those to a bf16 pair; both are exact, and so are the
+// products; they are added in float, a group at a time, and the group's scale is applied to that sum, in float too.  Nothing is added to the
+// weights that would have to be taken off again, so an infinite x gives what the definition gives.
+// x is staged in LDS as bf16.  Float x, and x behind SiLU, is split into three bf16 numbers that add up to it exactly: three rows of the
+// instruction, of which a few rows of x leave most idle, added in the epilogue.
+#include "igemm.h"
+#include "profile.h"
+#include "w4_choice.h"
+
+namespace fise {
+
+// ---------------------------------------------------------------------------------------------------------------- packing
+__device__ __forceinline__ float w4_value(const float* p) { return *p; }
+__device__ __forceinline__ float w4_value(const bf16_t* p) { return bf2f(*p); }
+__device__ __forceinline__ size_t w4_scale_at(int n, int k, int group, int tiles_k, int groups) {
+    const size_t tn = n / W4_ROWS, row = n % W4_ROWS;
+    if (group < W4_COLS) return ((tn * tiles_k + k / W4_COLS) * W4_ROWS + row) * (W4_COLS / group) + k % W4_COLS / group;
+    return (tn * groups + k / group) * W4_ROWS + row;
+}
+
+// A lane packs eight columns of an output; the lanes of a group find its largest magnitude among them.  The scale is that / 7 in bf16, a weight the
+// nearest multiple of it: at most half a scale off (7 scales are at least 7 / (7 (1 + 2^-8)) of the largest).  Magnitudes are compared as
+// whole numbers, so that a NaN wins: a group with a value that is not finite has a scale that is not, and comes back as NaN.
+template <typename T>
+__global__ __launch_bounds__(256) void w4_pack_kernel(const T* __restrict__ w, const bf16_t* __restrict__ given, int N, int K, int group, int tiles_k, int groups,
+                                                      unsigned* __restrict__ tiles, bf16_t* __restrict__ scales) {
+    const int n = blockIdx.y, k = (blockIdx.x * 256 + threadIdx.x) * 8, cols = tiles_k * W4_COLS;
+    float v[8];
+    unsigned top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] = n < N && k + e < K ? w4_value(w + (size_t)n * K + k + e) : 0.f;
+        top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+    }
+    for (int o = 1; o < group / 8; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
+    if (k >= cols) return;
+    bf16_t s = 0;
+    if (n < N && k < K) s = given ? given[(size_t)n * groups + k / group] : f2bf(__uint_as_float(top) / 7.f);
+    const float sf = bf2f(s);
+    unsigned word = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float r = rintf(v[e] / sf);
+        const float lo = given ? -8.f : -7.f;
+        const int q = sf != 0.f && r == r ? (int)fminf(fmaxf(r, lo), 7.f) : 0;
+        word |= ((unsigned)q & 15u) << (4 * e);
+    }
+    const int in = k % W4_COLS / 8, j = in / 4, quarter = in % 4;
+    tiles[(((size_t)(n / W4_ROWS) * tiles_k + k / W4_COLS) * 64 + quarter * 16 + n % W4_ROWS) * 4 + j] = word;
+    if (k % group == 0 && (group < W4_COLS || k < K)) scales[w4_scale_at(n, k, group, tiles_k, groups)] = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void w4_unpack_kernel(const unsigned* __restrict__ tiles, const bf16_t* __restrict__ scales, int N, int K, int group, int tiles_k, int groups,
+                                                        T* __restrict__ w) {
+    const int n = blockIdx.y, k = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (k >= K) return;
+    const int in = k % W4_COLS / 8, j = in / 4, quarter = in % 4;
+    const unsigned word = tiles[(((size_t)(n / W4_ROWS) * tiles_k + k / W4_COLS) * 64 + quarter * 16 + n % W4_ROWS) * 4 + j];
+    const float s = bf2f(scales[w4_scale_at(n, k, group, tiles_k, groups)]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (k + e < K) Elem<T>::st(w + (size_t)n * K + k + e, (float)((int)(word << (28 - 4 * e)) >> 28) * s);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- product
+struct W4Args {
+    const void* x; long long x_stride; int x_f32, silu;
+    const unsigned char* tiles; const bf16_t* scales; int N, K, tiles_k, groups, group_shift;      // group_shift: tile columns of a group as a power of two (wide groups)
+    const void* bias; int bias_f32; const void* residual; long long residual_stride; void* y; long long y_stride; int y_f32;
+    int M;
+    W4Choice c;
+};
+
+__device__ __forceinline__ unsigned w4_pair(unsigned w) {              // two weights / 16 from the lowest eight bits, as a bf16 pair: exact
+#if defined(__HIP_DEVICE_COMPILE__)
+    return f2bf2(__builtin_amdgcn_cvt_off_f32_i4(w), __builtin_amdgcn_cvt_off_f32_i4(w >> 4));
+#else
+    return w;
+#endif
+}
+
+__device__ __forceinline__ void w4_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }      // (weights that are on their way stay there)
+
+// a value of x as three bf16 numbers that add up to it
+__device__ __forceinline__ void w4_split(float v, bf16_t (&p)[3]) {    // truncated, not rounded: no piece of a finite number overflows, and what is left has 8 bits in the end
+    const unsigned a = __float_as_uint(v) & 0xffff0000u;
+    p[0] = (bf16_t)(a >> 16);
+    const bool finite = (a & 0x7f800000u) != 0x7f800000u;
+    const float r1 = finite ? v - __uint_as_float(a) : 0.f;
+    const unsigned b = __float_as_uint(r1) & 0xffff0000u;
+    p[1] = (bf16_t)(b >> 16);
+    p[2] = (bf16_t)(__float_as_uint(r1 - __uint_as_float(b)) >> 16);
+    if (v != v) p[0] |= 0x40;                                          // a NaN whose bits are all in the lower half stays one
+}
+
+// MT: tiles of 16 rows of x; GS: matrix instructions a scale covers (1, 2, 4: groups of 32, 64, 128 and more).
+template <int MT, int GS>
+__global__ __launch_bounds__(1024) void w4_linear_kernel(const W4Args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    bf16_t* const xs = reinterpret_cast<bf16_t*>(lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), threads = blockDim.x;
+    const W4Choice& c = a.c;
+    const int kw = wave % c.waves_k, nw = wave / c.waves_k;
+    const int tn = blockIdx.x * c.waves_n + nw, tiles_n = (a.N + W4_ROWS - 1) / W4_ROWS;
+    const bool live = tn < tiles_n;
+    const int m0 = blockIdx.y * c.slab, rows = min(c.slab, a.M - m0), rows_x = rows * c.pieces;
+    const int l16 = lane & 15, lq = lane >> 4;
+
+    constexpr int PF = 4, NS = 4 / GS;                                 // tiles in flight; scales of a tile
+    const unsigned char* const wt = a.tiles + (size_t)(live ? tn : 0) * a.tiles_k * W4_TILE_BYTES + lane * 16;
+    const bf16_t* const st = a.scales + (size_t)(live ? tn : 0) * (GS < 4 ? a.tiles_k * NS : a.groups) * W4_ROWS;
+    u32x4_t w[PF];
+    unsigned s[PF][(NS + 1) / 2];
+    auto fetch = [&](int slot, int t) {
+        w[slot] = *reinterpret_cast<const u32x4_t*>(wt + (size_t)t * W4_TILE_BYTES);
+        if constexpr (GS == 4) s[slot][0] = st[(size_t)(t >> a.group_shift) * W4_ROWS + l16];
+        else if constexpr (GS == 2) s[slot][0] = *reinterpret_cast<const unsigned*>(st + ((size_t)t * W4_ROWS + l16) * 2);
+        else { const uint2 v = *reinterpret_cast<const uint2*>(st + ((size_t)t * W4_ROWS + l16) * 4); s[slot][0] = v.x; s[slot][1] = v.y; }
+    };
+    f32x4_t acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = f32x4_t{0, 0, 0, 0};
+    // rows of LDS that do not exist: the lane reads the first one instead, and its results are not stored
+    const bf16_t* xr[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) xr[t] = xs + (size_t)(t * 16 + l16 < rows_x ? t * 16 + l16 : 0) * c.pitch + lq * 8;
+
+    for (int t0 = 0; t0 < a.tiles_k; t0 += c.chunk) {
+        const int t1 = min(a.tiles_k, t0 + c.chunk);
+        const int first = t0 + kw, n_t = live && first < t1 ? (t1 - first + c.waves_k - 1) / c.waves_k : 0;
+#pragma unroll
+        for (int p = 0; p < PF; ++p)
+            if (p < n_t) fetch(p, first + p * c.waves_k);
+        // ---- x of this chunk: pieces of eight columns; columns past K are zeros
+        const int cols8 = (t1 - t0) * (W4_COLS / 8);
+        if (t0) w4_barrier();
+        for (int i = tid; i < rows * cols8; i += threads) {
+            const int m = i / cols8, k = t0 * W4_COLS + (i - m * cols8) * 8;
+            float v[8];
+            uint4 raw = make_uint4(0, 0, 0, 0);
+            if (a.x_f32) {
+                float4 lo = make_float4(0, 0, 0, 0), hi = lo;
+                if (k < a.K) { const float* p = (const float*)a.x + (size_t)(m0 + m) * a.x_stride + k; lo = *reinterpret_cast<const float4*>(p); hi = *reinterpret_cast<const float4*>(p + 4); }
+                v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+            } else {
+                if (k < a.K) raw = *reinterpret_cast<const uint4*>((const bf16_t*)a.x + (size_t)(m0 + m) * a.x_stride + k);
+                v[0] = lo16(raw.x); v[1] = hi16(raw.x); v[2] = lo16(raw.y); v[3] = hi16(raw.y);
+                v[4] = lo16(raw.z); v[5] = hi16(raw.z); v[6] = lo16(raw.w); v[7] = hi16(raw.w);
+            }
+            bf16_t* const to = xs + (size_t)m * c.pieces * c.pitch + (k - t0 * W4_COLS);
+            if (c.pieces == 1) { *reinterpret_cast<uint4*>(to) = raw; continue; }
+            unsigned out[3][4];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                bf16_t p[3];
+                w4_split(a.silu ? silu_f(v[e]) : v[e], p);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) out[q][e >> 1] = e & 1 ? out[q][e >> 1] | (unsigned)p[q] << 16 : p[q];
+            }
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + (size_t)q * c.pitch) = make_uint4(out[q][0], out[q][1], out[q][2], out[q][3]);
+        }
+        w4_barrier();
+        for (int i0 = 0; i0 < n_t; i0 += PF) {
+#pragma unroll
+            for (int p = 0; p < PF; ++p) {
+                const int i = i0 + p;
+                if (i < n_t) {
+                    const int kx = (first + i * c.waves_k - t0) * W4_COLS;
+                    f32x4_t part[MT];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned q = w[p][j];
+                        const u32x4_t bw = {w4_pair(q), w4_pair(q >> 8), w4_pair(q >> 16), w4_pair(q >> 24)};
+                        const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(&bw);
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) {
+                            const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(xr[t] + kx + j * 32);
+                            part[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b, j % GS ? part[t] : f32x4_t{0, 0, 0, 0}, 0, 0, 0);
+                        }
+                        if (j % GS == GS - 1) {
+                            const unsigned sw = s[p][j / GS / 2];
+                            const float sc = GS < 4 && (j / GS) % 2 ? hi16(sw) : lo16(sw);
+#pragma unroll
+                            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(part[t][e], sc, acc[t][e]);
+                        }
+                    }
+                    if (i + PF < n_t) fetch(p, first + (i + PF) * c.waves_k);
+                }
+            }
+        }
+    }
+    // ---- the waves of an output tile and the pieces of a row meet in LDS, in order
+    __syncthreads();
+    float* const red = reinterpret_cast<float*>(lds);                  // [wave][row of x][16]
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) red[((wave * MT + t) * 16 + lq * 4 + e) * 16 + l16] = acc[t][e];
+    __syncthreads();
+    for (int i = tid; i < c.waves_n * rows * 16; i += threads) {
+        const int col = i & 15, rest = i >> 4, g = rest / rows, m = rest - g * rows, n = (blockIdx.x * c.waves_n + g) * W4_ROWS + col;
+        if (n >= a.N) continue;
+        float v = 0.f;
+        for (int k = 0; k < c.waves_k; ++k)
+            for (int q = c.pieces - 1; q >= 0; --q) v += red[((g * c.waves_k + k) * MT * 16 + m * c.pieces + q) * 16 + col];
+        v *= 16.f;
+        if (a.bias) v += a.bias_f32 ? ((const float*)a.bias)[n] : bf2f(((const bf16_t*)a.bias)[n]);
+        const size_t at = (size_t)(m0 + m) * a.y_stride + n;
+        if (a.residual) {
+            const size_t ar = (size_t)(m0 + m) * a.residual_stride + n;
+            v += a.y_f32 ? ((const float*)a.residual)[ar] : bf2f(((const bf16_t*)a.residual)[ar]);
+        }
+        if (a.y_f32) ((float*)a.y)[at] = v; else ((bf16_t*)a.y)[at] = f2bf(v);
+    }
+#endif
+}
+
+template <int MT, int GS> static int launch_w4(const W4Args& a, hipStream_t st) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&w4_linear_kernel<MT, GS>), hipFuncAttributeMaxDynamicSharedMemorySize, W4_LDS);
+    if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_w4_linear: cannot raise the dynamic LDS limit");
+    const W4Choice& c = a.c;
+    {
+        const double bytes = (double)a.N * a.K / 2 + 2.0 * a.N * a.groups + (double)a.M * a.K * (a.x_f32 ? 4 : 2) + (double)a.M * a.N * (a.y_f32 ? 4 : 2);
+        ProfileScope prof(PROF_ROWS_GEMM, 2.0 * a.M * a.N * a.K, bytes, st);
+        hipLaunchKernelGGL((w4_linear_kernel<MT, GS>), dim3((unsigned)ceil_div(ceil_div(a.N, W4_ROWS), c.waves_n), (unsigned)c.slabs), dim3(64u * c.waves_n * c.waves_k), (size_t)c.lds, st, a);
+    }
+    FISE_CHECK_LAUNCH("fise_w4_linear");
+    return FISE_OK;
+}
+template <int MT> static int launch_w4(const W4Args& a, int group, hipStream_t st) {
+    return group == 32 ? launch_w4<MT, 1>(a, st) : group == 64 ? launch_w4<MT, 2>(a, st) : launch_w4<MT, 4>(a, st);
+}
+
+// sizes that pack, unpack and product share; numbers of tiles have 31 bits
+static int w4_check(const char* fn, int N, int K, int group) {
+    if (N < 1 || K < 1 || !w4_group_ok(group)) return fail(FISE_ERR_SHAPE, "%s: N=%d K=%d group=%d (32, 64, 128 or 256)", fn, N, K, group);
+    if (N > 1 << 20 || K > 1 << 20) return fail(FISE_ERR_SHAPE, "%s: N=%d K=%d beyond 2^20", fn, N, K);
+    return FISE_OK;
+}
+
+}  // namespace fise
+
+using namespace fise;
+
+extern "C" size_t fise_w4_bytes(int N, int K, int group) {
+    if (w4_check("fise_w4_bytes", N, K, group)) return 0;
+    return (size_t)w4_layout(N, K, group).bytes;
+}
+
+extern "C" int fise_w4_pack(const void* w, int dtype, const void* scale, int N, int K, int group, void* packed, void* stream) {
+    const char* fn = "fise_w4_pack";
+    if (!w || !packed) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (dtype != FISE_F32 && dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d", fn, dtype);
+    if (int e = w4_check(fn, N, K, group)) return e;
+    if (!aligned16(w) || !aligned16(scale) || !aligned16(packed)) return fail(FISE_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    const W4Layout l = w4_layout(N, K, group);
+    const dim3 block(256);
+    bf16_t* const scales = (bf16_t*)((unsigned char*)packed + l.scale_off);
+    // outputs go in the grid's second dimension, which ends at 65535
+    for (int n0 = 0; n0 < (int)l.tiles_n * W4_ROWS; n0 += 32768) {
+        const int rows = std::min((int)l.tiles_n * W4_ROWS - n0, 32768);
+        const dim3 grid((unsigned)ceil_div((int)l.tiles_k * W4_COLS, 2048), (unsigned)rows);
+        const size_t per_row = (size_t)(group < W4_COLS ? l.tiles_k * (W4_COLS / group) : l.groups);
+        unsigned* const t = (unsigned*)((unsigned char*)packed + (size_t)(n0 / W4_ROWS) * l.tiles_k * W4_TILE_BYTES);
+        bf16_t* const s = scales + (size_t)n0 * per_row;
+        const bf16_t* const given = scale ? (const bf16_t*)scale + (size_t)n0 * l.groups : nullptr;
+        if (dtype == FISE_F32)
+            hipLaunchKernelGGL(w4_pack_kernel<float>, grid, block, 0, as_stream(stream), (const float*)w + (size_t)n0 * K, given, N - n0, K, group, (int)l.tiles_k, (int)l.groups, t, s);
+        else
+            hipLaunchKernelGGL(w4_pack_kernel<bf16_t>, grid, block, 0, as_stream(stream), (const bf16_t*)w + (size_t)n0 * K, given, N - n0, K, group, (int)l.tiles_k, (int)l.groups, t, s);
+        FISE_CHECK_LAUNCH(fn);
+    }
+    return FISE_OK;
+}
+
+extern "C" int fise_w4_unpack(const void* packed, int N, int K, int group, void* w, int dtype, void* stream) {
+    const char* fn = "fise_w4_unpack";
+    if (!w || !packed) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (dtype != FISE_F32 && dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d", fn, dtype);
+    if (int e = w4_check(fn, N, K, group)) return e;
+    if (!aligned16(w) || !aligned16(packed)) return fail(FISE_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    const W4Layout l = w4_layout(N, K, group);
+    const size_t per_row = (size_t)(group < W4_COLS ? l.tiles_k * (W4_COLS / group) : l.groups);
+    for (int n0 = 0; n0 < N; n0 += 32768) {
+        const dim3 grid((unsigned)ceil_div(K, 2048), (unsigned)std::min(N - n0, 32768)), block(256);
+        const unsigned* const t = (const unsigned*)((const unsigned char*)packed + (size_t)(n0 / W4_ROWS) * l.tiles_k * W4_TILE_BYTES);
+        const bf16_t* const s = (const bf16_t*)((const unsigned char*)packed + l.scale_off) + (size_t)n0 * per_row;
+        if (dtype == FISE_F32)
+            hipLaunchKernelGGL(w4_unpack_kernel<float>, grid, block, 0, as_stream(stream), t, s, N - n0, K, group, (int)l.tiles_k, (int)l.groups, (float*)w + (size_t)n0 * K);
+        else
+            hipLaunchKernelGGL(w4_unpack_kernel<bf16_t>, grid, block, 0, as_stream(stream), t, s, N - n0, K, group, (int)l.tiles_k, (int)l.groups, (bf16_t*)w + (size_t)n0 * K);
+        FISE_CHECK_LAUNCH(fn);
+    }
+    return FISE_OK;
+}
+
+extern "C" int fise_w4_linear(const fise_w4_linear_args* g, void* stream) {
+    const char* fn = "fise_w4_linear";
+    if (!g || !g->x || !g->packed || !g->y) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    auto known = [](int d) { return d == FISE_F32 || d == FISE_BF16; };
+    if (!known(g->x_dtype) || !known(g->y_dtype) || (g->bias && !known(g->bias_dtype)))
+        return fail(FISE_ERR_DTYPE, "%s: dtypes x %d, y %d, bias %d", fn, g->x_dtype, g->y_dtype, g->bias_dtype);
+    if (int e = w4_check(fn, g->N, g->K, g->group)) return e;
+    if (g->M < 0 || g->M > 1 << 20 || g->x_stride < g->K || g->y_stride < g->N || (g->residual && g->residual_stride < g->N))
+        return fail(FISE_ERR_SHAPE, "%s: M=%d, strides x %lld, y %lld, residual %lld", fn, g->M, (long long)g->x_stride, (long long)g->y_stride, (long long)g->residual_stride);
+    if (g->K % 8 || g->x_stride % 8 || !aligned16(g->x) || !aligned16(g->packed))
+        return fail(FISE_ERR_ALIGN, "%s: K and the row stride of x must be multiples of 8, x and the weights 16-byte aligned", fn);
+    const size_t ye = g->y_dtype == FISE_F32 ? 4 : 2, be = g->bias_dtype == FISE_F32 ? 4 : 2;
+    if ((uintptr_t)g->y % ye || (uintptr_t)g->residual % ye || (g->bias && (uintptr_t)g->bias % be)) return fail(FISE_ERR_ALIGN, "%s: y, residual and bias must be aligned to their type", fn);
+    if (g->M == 0) return FISE_OK;
+    const W4Layout l = w4_layout(g->N, g->K, g->group);
+    W4Args a{};
+    a.x = g->x; a.x_stride = g->x_stride; a.x_f32 = g->x_dtype == FISE_F32; a.silu = g->silu_in != 0;
+    a.tiles = (const unsigned char*)g->packed; a.scales = (const bf16_t*)((const unsigned char*)g->packed + l.scale_off);
+    a.N = g->N; a.K = g->K; a.tiles_k = (int)l.tiles_k; a.groups = (int)l.groups; a.group_shift = g->group == 256 ? 1 : 0;
+    a.bias = g->bias; a.bias_f32 = g->bias_dtype == FISE_F32;
+    a.residual = g->residual; a.residual_stride = g->residual_stride; a.y = g->y; a.y_stride = g->y_stride; a.y_f32 = g->y_dtype == FISE_F32;
+    a.M = g->M;
+    a.c = w4_choose(g->M, g->N, g->K, a.x_f32 || a.silu);
+    if (a.c.slabs > 65535) return fail(FISE_ERR_SHAPE, "%s: M=%d rows", fn, g->M);
+    const hipStream_t st = as_stream(stream);
+    return a.c.mt == 1 ? launch_w4<1>(a, g->group, st) : a.c.mt == 2 ? launch_w4<2>(a, g->group, st) : launch_w4<4>(a, g->group, st);
+}
