@@ -524,6 +524,37 @@ typedef struct {
 } fise_gated_norm_args;
 int fise_masked_gated_norm(const fise_gated_norm_args* a /* host */, void* stream);
 
+/* Attention whose keys and values of all heads come from one latent vector c of r
+ * channels and one shared key of dr channels a token:
+ *   k[j, h] = [W_uk[h] c_j | pe_j],  v[j, h] = W_uv[h] c_j
+ *   out[b, m, h] = sum_j softmax_j(scale * q[b, m, h] . k[j, h]) v[j, h]
+ * cache [B, cache_tokens, r + dr] holds [c | pe] a token (a map: the masked 1x1
+ * convolution refreshes it at the active tokens); the first n_keys tokens of an element take
+ * part, of those the first kv_len[b] (device int32 [B], values outside 0..n_keys count as the
+ * nearest of those; NULL: n_keys).  What lies behind them is not read.  causal != 0: query m
+ * is the token at kv_len[b] - M + m and sees the keys up to itself.  A query that sees no key
+ * gives zeros; a key that it does not see has no effect on it, whatever it holds.
+ * q [B, M, heads, d + dr], w_uk [heads, d, r], w_uv [heads, dv, r] (out, in), out
+ * [B, M, heads * dv].  bf16 only; d, dv, r multiples of 8 up to 160, 160, 512, dr a multiple
+ * of 8 up to 64 (0: no shared key); scale > 0.
+ * Forms: ABSORBED brings W_uk to the queries and W_uv to the sums, and every head meets the
+ * latent vectors themselves: the cache is read once for 64 (query, head) rows.  EXPANDED
+ * makes keys and values of all heads first.  AUTO takes the one that is expected to be faster
+ * (few queries: absorbed).  They round at different places (absorbed: the queries behind W_uk,
+ * bf16; expanded: keys and values, bf16); probabilities are bf16 in both, sums and softmax
+ * statistics float.  Results of a form depend on the arguments only, not on the run.
+ * workspace: fise_latent_attention_workspace_bytes(a), which reads sizes, form and pointers but
+ * not what they point to.  M == 0 touches nothing; nothing may overlap out. */
+enum { FISE_LATENT_AUTO = 0, FISE_LATENT_ABSORBED = 1, FISE_LATENT_EXPANDED = 2 };
+typedef struct {
+    const void* q; const void* cache; const int32_t* kv_len; const void* w_uk; const void* w_uv; void* out;
+    int B, M, n_keys; int64_t cache_tokens;
+    int heads, d, dr, dv, r;
+    float scale; int causal; int form; int dtype;
+} fise_latent_attention_args;
+size_t fise_latent_attention_workspace_bytes(const fise_latent_attention_args* a /* host */);
+int fise_latent_attention(const fise_latent_attention_args* a /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------
  * Tracing.  With profiling enabled every launch of the gathered-GEMM and
  * attention kernels is bracketed by two HIP events on the caller's stream

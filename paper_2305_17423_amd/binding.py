@@ -71,6 +71,13 @@ class fise_gated_norm_args(C.Structure):
                 ("tile_idx", vp), ("n_active", i32), ("tile", i32), ("r", vp), ("y", vp), ("y_is_map", i32)]
 
 
+class fise_latent_attention_args(C.Structure):
+    _fields_ = [("q", vp), ("cache", vp), ("kv_len", vp), ("w_uk", vp), ("w_uv", vp), ("out", vp),
+                ("B", i32), ("M", i32), ("n_keys", i32), ("cache_tokens", i64),
+                ("heads", i32), ("d", i32), ("dr", i32), ("dv", i32), ("r", i32),
+                ("scale", f32), ("causal", i32), ("form", i32), ("dtype", i32)]
+
+
 class fise_unet_desc(C.Structure):
     _fields_ = [("in_ch", i32), ("out_ch", i32), ("base", i32), ("n_levels", i32),
                 ("mults", i32 * FISE_MAX_LEVELS), ("attn", i32 * FISE_MAX_LEVELS), ("layers", i32),
@@ -134,6 +141,8 @@ _SIGS = {
     "fise_w4_unpack": (i32, [vp, i32, i32, i32, vp, i32, vp]),
     "fise_w4_linear": (i32, [C.POINTER(fise_w4_linear_args), vp]),
     "fise_masked_gated_norm": (i32, [C.POINTER(fise_gated_norm_args), vp]),
+    "fise_latent_attention_workspace_bytes": (sz, [C.POINTER(fise_latent_attention_args)]),
+    "fise_latent_attention": (i32, [C.POINTER(fise_latent_attention_args), vp, sz, vp]),
     "fise_profile_enable": (i32, [i32]),
     "fise_profile_calibrate": (i32, [i32, vp]),
     "fise_calibrate_peaks": (i32, [vp, sz, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
@@ -511,6 +520,39 @@ def gated_norm_args(x, h=None, post="none", post_w=None, post_b=None, gate=None,
 
 def fise_masked_gated_norm(args, stream=None):
     _ck(lib().fise_masked_gated_norm(C.byref(args), _stream(stream)))
+
+
+FISE_LATENT_AUTO, FISE_LATENT_ABSORBED, FISE_LATENT_EXPANDED = 0, 1, 2
+
+
+def latent_attention_args(q, cache, w_uk, w_uv, out, scale, kv_len=None, n_keys=None, causal=False, form=FISE_LATENT_AUTO):
+    """Arguments of fise_latent_attention; they keep the tensors alive.  q [B, M, heads, d + dr], cache [B, cache_tokens, r + dr] or a map
+    [B, H, W, r + dr], w_uk [heads, d, r], w_uv [heads, dv, r], out [B, M, heads * dv]; kv_len: int32 [B] on the device."""
+    B, M, heads, width = q.shape
+    d, r = w_uk.shape[1:]
+    dv, dr, bf = w_uv.shape[1], width - d, (torch.bfloat16,)
+    tokens = cache.numel() // max(B * (r + dr), 1)
+    for name, t, shape in (("q", q, (B, M, heads, d + dr)), ("w_uk", w_uk, (heads, d, r)), ("w_uv", w_uv, (heads, dv, r)), ("out", out, (B, M, heads * dv)),
+                           ("cache", cache, (B, *cache.shape[1:-1], r + dr))):
+        _like(name, t, shape, bf)
+    if kv_len is not None:
+        _like("kv_len", kv_len, (B,), (torch.int32,))
+    a = fise_latent_attention_args()
+    a.q, a.cache, a.kv_len, a.w_uk, a.w_uv, a.out = _p(q), _p(cache), _p(kv_len), _p(w_uk), _p(w_uv), _p(out)
+    a.B, a.M, a.n_keys, a.cache_tokens = B, M, tokens if n_keys is None else n_keys, tokens
+    a.heads, a.d, a.dr, a.dv, a.r = heads, d, dr, dv, r
+    a.scale, a.causal, a.form, a.dtype = scale, int(bool(causal)), form, FISE_BF16
+    a.keep = (q, cache, kv_len, w_uk, w_uv, out)
+    return a
+
+
+def fise_latent_attention_workspace_bytes(args):
+    return lib().fise_latent_attention_workspace_bytes(C.byref(args))
+
+
+def fise_latent_attention(args, workspace, stream=None):
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _ck(lib().fise_latent_attention(C.byref(args), _p(workspace), nbytes, _stream(stream)))
 
 
 # --------------------------------------------------------------------------- UNet

@@ -1,0 +1,62 @@
+// What the two forms of attention over a cache of latent vectors share.  Internal.
+#pragma once
+#include "igemm.h"
+#include "latent_choice.h"
+#include "profile.h"
+
+namespace fise {
+
+struct LatentArgs {
+    const bf16_t* q; const bf16_t* cache; const int* kv_len; const bf16_t* w_uk; const bf16_t* w_uv; bf16_t* out;
+    int B, M, n, heads, d, dr, dv, r, causal; long long cache_tokens;
+    float scale_log2e;
+    // absorbed
+    int tiles, groups, workgroups, tokens;               // tiles of rows, B * tiles, workgroups of the second launch, tokens of a workgroup of the third
+    int* table; bf16_t* qa; float2* ml; float* part;
+    // expanded
+    long long n_pad; bf16_t* k; bf16_t* v;               // keys of a head [B, heads, n_pad, 16 KD], values [B, heads * dv, n_pad]
+    FastDiv d_heads, d_tiles, d_M;
+};
+
+// Keys of a batch element, and how many of them query m sees: all, or (causal) the query is the key at len - M + m and sees those up to itself.
+__device__ __forceinline__ int la_len(const LatentArgs& a, int b) { return a.kv_len ? min(max(a.kv_len[b], 0), a.n) : a.n; }
+__device__ __forceinline__ int la_limit(const LatentArgs& a, int len, int m) { return a.causal ? min(max(len - a.M + m + 1, 0), len) : len; }
+
+__device__ __forceinline__ void la_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+#if defined(__HIP_DEVICE_COMPILE__)
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+// Sixteen lanes read a block of 4 rows x 16 columns (lane i: four columns from 4 (i % 4) of row i / 4) and get it turned: lane i column i, all four rows.
+// Two blocks are the operand of a 16x16x32 product whose summed index runs down the rows: row groups `at` and `at` + second.
+__device__ __forceinline__ bf16x8_t la_turned(const unsigned char* at, int second) {
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FISE_AS3 s16x4_t*)(FISE_AS3 void*)at);
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FISE_AS3 s16x4_t*)(FISE_AS3 void*)(at + second));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// bf16 pairs whose values that are not finite are zeros
+__device__ __forceinline__ uint4 la_finite(uint4 v) {
+    auto clean = [](unsigned x) {
+        if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+        if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+        return x;
+    };
+    return make_uint4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
+}
+// over the four lanes l, l + 16, l + 32, l + 48
+__device__ __forceinline__ float la_max4(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float la_sum4(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+#endif
+
+int launch_expanded(const LatentArgs& a, int tile, hipStream_t st);
+
+}  // namespace fise

@@ -1,0 +1,439 @@
+// Attention whose keys and values come from one latent vector c_j (r channels) and one shared key (dr channels) a token:
+//   k[j, h] = [W_uk[h] c_j | k_pe_j],   v[j, h] = W_uv[h] c_j,   o[m, h] = softmax_j(q[m, h] . k[j, h] scale) v[j, h].
+//
+// Absorbed form (few queries): q . W_uk c = (W_uk^T q) . c, so W_uk goes to the queries once and W_uv to the sums at the end; in between every head reads the same
+// rows [c | k_pe], which come in from the cache once for 64 rows (query, head).  Three launches: latent_query_kernel, latent_absorbed_kernel,
+// latent_values_kernel.  Expanded form: latent_expanded.hip.
+#include <algorithm>
+#include "latent.h"
+
+namespace fise {
+
+// ---------------------------------------------------------------------------------------------------------------- queries
+// qa[b, m, h] = [W_uk[h]^T q_c | q_pe | 0]: a workgroup takes 128 latent channels of a head and 64 tokens (a wave 32 channels); W_uk's rows run along the result, so
+// they are turned on the way out of LDS.  The result is rounded to bf16, as any operand of the matrix unit.
+// The first workgroup also writes the line of key blocks: table[g] = blocks of all groups before g.
+constexpr int LQ_COLS = 128, LQ_TOKENS = 64;
+__global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, int R, int DR) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int LQ_PITCH = LQ_COLS * 2 + 32;                         // four rows of a block side by side in the banks
+    __shared__ __attribute__((aligned(16))) unsigned char lds[160 * LQ_PITCH];
+    __shared__ int sums[256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
+    const int h = blockIdx.x, c0 = blockIdx.y * LQ_COLS, t0 = blockIdx.z * LQ_TOKENS, tokens = a.B * a.M, width = R + DR;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
+        const int each = (a.groups + 255) / 256, g0 = min(tid * each, a.groups), g1 = min(g0 + each, a.groups);
+        auto blocks = [&](int g) {
+            const int b = (int)fdiv((unsigned)g, a.d_tiles), t = g - b * a.tiles;
+            const int last = min(a.M * a.heads, (t + 1) * LA_ROWS) - 1;
+            return (la_limit(a, la_len(a, b), (int)fdiv((unsigned)last, a.d_heads)) + LA_KEYS - 1) / LA_KEYS;
+        };
+        int s = 0;
+        for (int g = g0; g < g1; ++g) s += blocks(g);
+        sums[tid] = s;
+        __syncthreads();
+        for (int o = 1; o < 256; o <<= 1) {
+            const int v = tid >= o ? sums[tid - o] : 0;
+            __syncthreads();
+            sums[tid] += v;
+            __syncthreads();
+        }
+        int at = sums[tid] - s;
+        for (int g = g0; g < g1; ++g) { a.table[g] = at; at += blocks(g); }
+        if (tid == 255) a.table[a.groups] = sums[255];
+    }
+    const int steps = (a.d + 31) / 32;
+    for (int i = tid; i < steps * 32 * (LQ_COLS / 8); i += 256) {
+        const int row = i / (LQ_COLS / 8), c = (i % (LQ_COLS / 8)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < a.d && c0 + c < a.r) v = *reinterpret_cast<const uint4*>(a.w_uk + ((size_t)h * a.d + row) * a.r + c0 + c);
+        *reinterpret_cast<uint4*>(lds + row * LQ_PITCH + c * 2) = v;
+    }
+    __syncthreads();
+    const unsigned char* const from = lds + (lq * 8 + l16 / 4) * LQ_PITCH + (wave * 32 + (l16 % 4) * 4) * 2;
+#pragma unroll
+    for (int tt = 0; tt < LQ_TOKENS / 16; ++tt) {
+        const int t = t0 + tt * 16 + l16;
+        if (t0 + tt * 16 >= tokens) break;
+        const bool ok = t < tokens;
+        const bf16_t* const q = a.q + ((size_t)(ok ? t : 0) * a.heads + h) * (a.d + a.dr);
+        f32x4_t acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        for (int ks = 0; ks < steps; ++ks) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            const int c = ks * 32 + lq * 8;
+            if (ok && c < a.d) v = *reinterpret_cast<const uint4*>(q + c);
+            const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(&v);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(la_turned(from + ks * 32 * LQ_PITCH + j * 32, 4 * LQ_PITCH), x, acc[j], 0, 0, 0);
+        }
+        if (!ok) continue;
+        bf16_t* const to = a.qa + ((size_t)t * a.heads + h) * width;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            *reinterpret_cast<uint2*>(to + c0 + wave * 32 + j * 16 + lq * 4) = make_uint2(f2bf2(acc[j][0], acc[j][1]), f2bf2(acc[j][2], acc[j][3]));
+        if (blockIdx.y == 0 && wave == 0)
+            for (int c = lq * 8; c < DR; c += 32)
+                *reinterpret_cast<uint4*>(to + R + c) = c < a.dr ? *reinterpret_cast<const uint4*>(q + a.d + c) : make_uint4(0, 0, 0, 0);
+    }
+#endif
+}
+
+// ---------------------------------------------------------------------------------------------------------------- sums over the latent vectors
+// A workgroup of four waves has 64 rows (query, head) and goes through its blocks of 32 keys; a block's rows [c | k_pe] lie in LDS, in a ring, loaded there
+// directly two or three blocks ahead.  Scores: a wave has 16 rows, whose operands stay in registers, against all keys of the block.  The first index of the product is
+// the key, and a lane reads the key rows in the order that makes its eight scores those of eight consecutive keys: its probabilities are
+// then, as they stand, its part of the second product's operand.  Sums: the waves exchange probabilities and a wave has all 64 rows x a quarter
+// of the latent channels, whose operand is the same block read turned, so nothing is read twice from memory and no transposed copy exists.
+// A row's sixteen-byte pieces are stored at piece ^ la_swizzle(key): the eight lanes of a step of the score product, and the four keys that a turned
+// read takes at a time, then lie in different banks.
+template <int R_, int DR_> struct LaTile {
+    static constexpr int R = R_, DR = DR_, PIECES = (R + DR) / 8, PITCH = PIECES * 16, TILE = LA_KEYS * PITCH, PER_CU = latent_per_cu(R), RING = R == 256 && DR ? 3 : 4, AHEAD = RING - 1;
+    static constexpr int LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32, P = RING * TILE, ALPHA = P + LA_ROWS * LA_KEYS * 2, LDS = ALPHA + LA_ROWS * 4;
+    static_assert(TILE % 4096 == 0 && PIECES % 8 == 0 && PER_CU * LDS <= 160 * 1024, "whole loads of four waves; LDS of a CU");
+};
+__device__ __forceinline__ int la_swizzle(int key) { return ((key & 3) << 1) | ((key >> 3) & 1); }
+
+template <int R, int DR>
+__global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(const LatentArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    using T = LaTile<R, DR>;
+    constexpr int RT = T::RT, KS = T::KS, PITCH = T::PITCH, LPW = T::LPW, AHEAD = T::AHEAD;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // consecutive workgroups go to the eight XCDs in turn: give each XCD one run of the line
+    const int total = __builtin_amdgcn_readfirstlane(a.table[a.groups]), workgroups = min(a.workgroups, total);      // each has a block
+    int w = blockIdx.x;
+    if (w >= workgroups) return;
+    { const int chunk = workgroups >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
+    const int line0 = (int)((long long)w * total / workgroups), line1 = (int)((long long)(w + 1) * total / workgroups);
+    int g = 0;
+    for (int lo = 0, hi = a.groups - 1;;) {                            // last group that starts at or before line0
+        if (lo >= hi) { g = lo; break; }
+        const int mid = (lo + hi + 1) >> 1;
+        if (__builtin_amdgcn_readfirstlane(a.table[mid]) <= line0) lo = mid; else hi = mid - 1;
+    }
+    const int row_bytes = (a.r + a.dr) * 2, rows = a.M * a.heads;
+
+    // ---- places that depend on the lane only: loads (offset of a piece in a block of the cache; pieces that do not exist past its end), operands
+    unsigned off[LPW];
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+        const int p = (wave * LPW + j) * 64 + lane, key = p / T::PIECES, piece = (p - key * T::PIECES) ^ la_swizzle(key);
+        const int c = piece * 8, pe = c - R;
+        off[j] = c < R ? (c < a.r ? (unsigned)(key * row_bytes + c * 2) : 0x40000000u) : (pe < a.dr ? (unsigned)(key * row_bytes + (a.r + pe) * 2) : 0x40000000u);
+    }
+    const int my_key = (l16 >> 2) * 8 + (l16 & 3);                     // of the first half of a block's scores; the second half's is 4 further
+    unsigned kat[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) kat[j] = (unsigned)(my_key * PITCH + ((j * 4 + lq) ^ la_swizzle(my_key)) * 16);
+    constexpr int VB = RT < 4 ? RT : 4;
+    unsigned vat[VB];
+    {
+        const int key = lq * 8 + l16 / 4;
+#pragma unroll
+        for (int j = 0; j < VB; ++j) vat[j] = (unsigned)(key * PITCH + (((wave * RT + j) * 2 + (l16 % 4) / 2) ^ la_swizzle(key)) * 16 + (l16 & 1) * 8);
+    }
+
+    for (int at = line0; at < line1; ++g) {
+        const int g_at = __builtin_amdgcn_readfirstlane(a.table[g]), g_end = __builtin_amdgcn_readfirstlane(a.table[g + 1]);
+        const int end = min(line1, g_end);
+        if (end <= at) continue;
+        const int b = (int)fdiv((unsigned)g, a.d_tiles), row0 = (g - b * a.tiles) * LA_ROWS;
+        const int blk0 = at - g_at, blk1 = end - g_at, len = __builtin_amdgcn_readfirstlane(la_len(a, b));
+        const int row = row0 + wave * 16 + l16;
+        const int limit = row < rows ? la_limit(a, len, (int)fdiv((unsigned)row, a.d_heads)) : len;
+        const int limit_first = la_limit(a, len, (int)fdiv((unsigned)row0, a.d_heads));       // the fewest keys that a row of the tile sees
+        const unsigned char* const keys = (const unsigned char*)a.cache + (size_t)b * a.cache_tokens * row_bytes;
+
+        int put = 0, get = 0;                                          // places in the ring
+        auto load = [&](int blk) {                                     // (behind the last block: nothing but zeros, no traffic, the same count of loads)
+            const int k0 = blk * LA_KEYS, left = min(max(len - k0, 0), LA_KEYS);
+            const auto rsrc = buf(keys + (size_t)k0 * row_bytes, blk < blk1 ? (unsigned)(left * row_bytes) : 0u);
+            unsigned char* const to = lds + put + wave * LPW * 1024;
+            put = put == AHEAD * T::TILE ? 0 : put + T::TILE;
+#pragma unroll
+            for (int j = 0; j < LPW; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (FISE_AS3 void*)(to + j * 1024), 16, (int)off[j], 0, 0, 0);
+        };
+        bf16x8_t qf[KS];
+        {
+            const bf16_t* const q = a.qa + ((size_t)b * rows + min(row, rows - 1)) * (R + DR) + lq * 8;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(q + ks * 32);
+        }
+        la_barrier();                                                  // the group before has been read to its end
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(blk0 + i);
+        // the queries have arrived before the loop (the compiler's count would otherwise wait for every load in flight)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" ::"v"(qf[ks]));
+
+        f32x4_t acc[RT][4];
+#pragma unroll
+        for (int j = 0; j < RT; ++j)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[j][t] = f32x4_t{0, 0, 0, 0};
+        float m_run = -INFINITY, l_run = 0.f;                          // l: of this lane's keys until the end
+
+        for (int blk = blk0; blk < blk1; ++blk) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPW) : "memory");
+            load(blk + AHEAD);                                         // over the block before, which all waves are done with
+            const unsigned char* const tile = lds + get;
+            get = get == AHEAD * T::TILE ? 0 : get + T::TILE;
+            const int k0 = blk * LA_KEYS;
+            // ---- scores of eight keys a lane: k0 + lq * 8 + (0..7)
+            f32x4_t s[2][2];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(tile + kat[ks & 1] + (ks >> 1) * 128 + kt * 4 * PITCH);
+                    s[kt][ks & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks], ks < 2 ? f32x4_t{0, 0, 0, 0} : s[kt][ks & 1], 0, 0, 0);
+                }
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = (s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3]) * a.scale_log2e;
+            const bool partial = k0 + LA_KEYS > limit_first;           // uniform: some row of the tile does not see all of the block
+            if (partial) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k0 + lq * 8 + e >= limit) p[e] = -INFINITY;
+            }
+            float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+            mx = fmaxf(m_run, la_max4(mx));
+            const float base = mx == -INFINITY ? 0.f : mx;             // nothing seen yet: every probability is exp2(-inf) = 0
+            const float alpha = __builtin_amdgcn_exp2f(m_run - base);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(p[e] - base); sum += p[e]; }
+            l_run = fmaf(l_run, alpha, sum);
+            m_run = mx;
+            *reinterpret_cast<uint4*>(lds + T::P + tid * 16) = make_uint4(f2bf2(p[0], p[1]), f2bf2(p[2], p[3]), f2bf2(p[4], p[5]), f2bf2(p[6], p[7]));
+            if (lq == 0) *reinterpret_cast<float*>(lds + T::ALPHA + (wave * 16 + l16) * 4) = alpha;
+            la_barrier();
+            if (a.causal && partial) {
+                // a key that a row does not see takes part with probability 0: what is not finite in it must not
+                for (int i = tid; i < LA_KEYS * (R / 8); i += 256) {
+                    const int key = i / (R / 8), piece = (i - key * (R / 8)) ^ la_swizzle(key);
+                    uint4* const at16 = reinterpret_cast<uint4*>(const_cast<unsigned char*>(tile) + key * PITCH + piece * 16);
+                    *at16 = la_finite(*at16);
+                }
+                la_barrier();
+            }
+            // ---- sums of a quarter of the latent channels for all 64 rows
+            bf16x8_t pf[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                pf[t] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + (t * 64 + lane) * 16);
+                const float al = *reinterpret_cast<const float*>(lds + T::ALPHA + (t * 16 + l16) * 4);
+                if (__any(al != 1.0f)) {                               // a maximum has moved, which becomes rare
+#pragma unroll
+                    for (int j = 0; j < RT; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][t][e] *= al;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < RT; ++j) {
+                const bf16x8_t vf = la_turned(tile + vat[j % VB] + (j / VB) * 128, 4 * PITCH);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[j][t], 0, 0, 0);
+            }
+        }
+        at = end;
+        // ---- partial result of this part of the group
+        const size_t slot = (size_t)w + g;
+        l_run = la_sum4(l_run);
+        if (lq == 0) a.ml[slot * LA_ROWS + wave * 16 + l16] = make_float2(m_run, l_run);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (row0 + t * 16 + l16 >= rows) continue;
+            float* const o = a.part + (slot * LA_ROWS + t * 16 + l16) * R + wave * (RT * 16) + lq * 4;
+#pragma unroll
+            for (int j = 0; j < RT; ++j) *reinterpret_cast<float4*>(o + j * 16) = make_float4(acc[j][t][0], acc[j][t][1], acc[j][t][2], acc[j][t][3]);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // the empty loads behind the last block and the stores: the next group counts from nothing
+    }
+#endif
+}
+
+// ---------------------------------------------------------------------------------------------------------------- values
+// o[t, h] = W_uv[h] (sum over the parts).  A workgroup of eight waves has a head and `tokens` tokens (at most 16): it adds up the parts with their weights
+// exp2(m - max), divides, and leaves the sums in LDS as two bf16 numbers each (16 of the float's 24 bits, so that this product rounds only its result);
+// the waves take 16 value channels at a time.
+template <int R>
+__global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int QUADS = R / 4, PARTS = 512 / QUADS, PITCH = R + 8;   // parts: lanes that share the parts of a token, or have tokens of their own
+    __shared__ __attribute__((aligned(16))) bf16_t hi[16][PITCH], lo[16][PITCH];
+    __shared__ __attribute__((aligned(16))) float4 sums[PARTS][QUADS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
+    const int h = blockIdx.x, t0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.B * a.M - t0);
+    const int part = tid / QUADS, quad = tid - part * QUADS;
+    const int total = a.table[a.groups], workgroups = min(a.workgroups, total);
+    // the weights of the first 16 channels of this wave, on their way while the parts are added
+    const int vt = (a.dv + 15) / 16;
+    auto weights = [&](bf16x8_t (&wf)[R / 32], int v) {
+        const bf16_t* const w = a.w_uv + ((size_t)h * a.dv + v * 16 + l16) * a.r;
+#pragma unroll
+        for (int ks = 0; ks < R / 32; ++ks) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (v * 16 + l16 < a.dv && ks * 32 + lq * 8 < a.r) x = *reinterpret_cast<const uint4*>(w + ks * 32 + lq * 8);
+            wf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
+        }
+    };
+    bf16x8_t wf[R / 32];
+    if (wave < vt) weights(wf, wave);
+
+    // the sums of token t0 + i over every `step`-th part from the first + `from` on
+    auto merge = [&](int i, int from, int step) {
+        float4 o = make_float4(0, 0, 0, 0);
+        const int t = t0 + i, b = (int)fdiv((unsigned)t, a.d_M), row = (t - b * a.M) * a.heads + h, tile = row / LA_ROWS, g = b * a.tiles + tile;
+        const int g0 = a.table[g], g1 = a.table[g + 1];
+        if (i >= tokens || g1 <= g0) return o;
+        // workgroups with a part of blocks g0 .. g1 - 1: block x belongs to the largest w with w total / workgroups <= x
+        auto owner = [&](int x) { return (int)((((long long)x + 1) * workgroups - 1) / total); };
+        const int w0 = owner(g0), w1 = owner(g1 - 1);
+        const size_t at = (size_t)g * LA_ROWS + (row - tile * LA_ROWS);
+        float top = -INFINITY;
+        for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.ml[at + (size_t)w * LA_ROWS].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        float l = 0.f;
+        for (int w = w0; w <= w1; ++w) { const float2 v = a.ml[at + (size_t)w * LA_ROWS]; l = fmaf(__builtin_amdgcn_exp2f(v.x - base), v.y, l); }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;                   // no key seen: zeros
+#pragma unroll 4
+        for (int w = w0 + from; w <= w1; w += step) {
+            const float f = __builtin_amdgcn_exp2f(a.ml[at + (size_t)w * LA_ROWS].x - base) * inv;
+            const float4 v = *reinterpret_cast<const float4*>(a.part + (at + (size_t)w * LA_ROWS) * R + quad * 4);
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        }
+        return o;
+    };
+    auto put = [&](int i, float4 o) {
+        const unsigned h0 = f2bf2(o.x, o.y), h1 = f2bf2(o.z, o.w);
+        auto rest = [](float v, float high) { return (__float_as_uint(high) & 0x7f800000u) == 0x7f800000u ? 0.f : v - high; };
+        *reinterpret_cast<uint2*>(&hi[i][quad * 4]) = make_uint2(h0, h1);
+        *reinterpret_cast<uint2*>(&lo[i][quad * 4]) = make_uint2(f2bf2(rest(o.x, lo16(h0)), rest(o.y, hi16(h0))), f2bf2(rest(o.z, lo16(h1)), rest(o.w, hi16(h1))));
+    };
+    // as many lane groups as tokens, or the groups deal a token's parts out among them
+    const int share = a.tokens >= PARTS ? 1 : PARTS / a.tokens;
+    if (share == 1) {
+        if (part < PARTS)
+            for (int i = part; i < tokens; i += PARTS) put(i, merge(i, 0, 1));
+    } else {
+        const int i = part / share, mine = part - i * share;
+        const bool works = part < PARTS && i < tokens;
+        float4 o = make_float4(0, 0, 0, 0);
+        if (works) sums[part][quad] = o = merge(i, mine, share);
+        __syncthreads();
+        if (works && mine == 0) {
+            for (int k = 1; k < share; ++k) { const float4 v = sums[part + k][quad]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+            put(i, o);
+        }
+    }
+    __syncthreads();
+    const int src = l16 < tokens ? l16 : 0;                            // (tokens that do not exist: the first one's sums, not stored)
+    for (int v = wave; v < vt; v += 8) {
+        if (v != wave) weights(wf, v);
+        f32x4_t acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int ks = 0; ks < R / 32; ++ks) {
+            acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[ks], *reinterpret_cast<const bf16x8_t*>(&hi[src][ks * 32 + lq * 8]), acc[0], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[ks], *reinterpret_cast<const bf16x8_t*>(&lo[src][ks * 32 + lq * 8]), acc[1], 0, 0, 0);
+        }
+        const int c = v * 16 + lq * 4;
+        if (l16 < tokens && c < a.dv)
+            *reinterpret_cast<uint2*>(a.out + ((size_t)(t0 + l16) * a.heads + h) * a.dv + c) =
+                make_uint2(f2bf2(acc[0][0] + acc[1][0], acc[0][1] + acc[1][1]), f2bf2(acc[0][2] + acc[1][2], acc[0][3] + acc[1][3]));
+    }
+#endif
+}
+
+template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStream_t st) {
+    using T = LaTile<R, DR>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_absorbed_kernel<R, DR>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+    if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_latent_attention: cannot raise the dynamic LDS limit");
+    const int tokens = a.B * a.M;
+    hipLaunchKernelGGL(latent_query_kernel, dim3((unsigned)a.heads, R / LQ_COLS, (unsigned)ceil_div(tokens, LQ_TOKENS)), dim3(256), 0, st, a, R, DR);
+    FISE_CHECK_LAUNCH("fise_latent_attention: queries");
+    {
+        const double pairs = (double)tokens * a.heads * a.n;
+        ProfileScope prof(PROF_ATTENTION, 2.0 * pairs * (2 * a.r + a.dr), 2.0 * a.B * a.n * (a.r + a.dr), st);
+        hipLaunchKernelGGL((latent_absorbed_kernel<R, DR>), dim3((unsigned)a.workgroups), dim3(256), T::LDS, st, a);
+    }
+    FISE_CHECK_LAUNCH("fise_latent_attention: absorbed");
+    {
+        ProfileScope prof(PROF_ATTENTION_MERGE, 2.0 * tokens * a.heads * (double)a.r * a.dv, 2.0 * a.heads * (double)a.r * a.dv, st);
+        hipLaunchKernelGGL(latent_values_kernel<R>, dim3((unsigned)a.heads, (unsigned)ceil_div(tokens, a.tokens)), dim3(512), 0, st, a);
+    }
+    FISE_CHECK_LAUNCH("fise_latent_attention: values");
+    return FISE_OK;
+}
+template <int R> static int launch_absorbed(const LatentArgs& a, hipStream_t st) { return a.dr ? launch_absorbed<R, 64>(a, st) : launch_absorbed<R, 0>(a, st); }
+
+static int latent_check(const char* fn, const fise_latent_attention_args* g, LatentShape& s) {
+    if (!g || !g->q || !g->cache || !g->w_uk || !g->w_uv || !g->out) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (g->dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d (bf16 only)", fn, g->dtype);
+    if (g->B < 1 || g->M < 0 || g->n_keys < 0 || g->cache_tokens < g->n_keys || g->heads < 1 || g->d < 1 || g->d > 160 || g->dv < 1 || g->dv > 160 || g->dr < 0 || g->dr > 64 ||
+        g->r < 1 || g->r > 512 || g->form < FISE_LATENT_AUTO || g->form > FISE_LATENT_EXPANDED)
+        return fail(FISE_ERR_SHAPE, "%s: B%d M%d keys%d of %lld heads%d d%d dr%d dv%d r%d form%d", fn, g->B, g->M, g->n_keys, (long long)g->cache_tokens, g->heads, g->d, g->dr, g->dv, g->r, g->form);
+    if (g->d % 8 || g->dr % 8 || g->dv % 8 || g->r % 8) return fail(FISE_ERR_ALIGN, "%s: d %d, dr %d, dv %d and r %d must be multiples of 8", fn, g->d, g->dr, g->dv, g->r);
+    for (const void* p : {g->q, g->cache, g->w_uk, g->w_uv, (const void*)g->out})
+        if (!aligned16(p)) return fail(FISE_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
+    if (!(g->scale > 0) || g->scale > 1e30f) return fail(FISE_ERR_SHAPE, "%s: scale %g", fn, g->scale);
+    s = LatentShape{g->B, g->M, g->n_keys, g->heads, g->d, g->dr, g->dv, g->r, g->causal != 0};
+    // row numbers and key blocks are counted in 31 bits, heads and tokens are grid dimensions
+    const long long rows = (long long)g->M * g->heads, tiles = (rows + LA_ROWS - 1) / LA_ROWS, blocks = ((long long)g->n_keys + LA_KEYS - 1) / LA_KEYS;
+    if (g->n_keys > 1 << 26 || rows >= 1ll << 30 || (long long)g->B * tiles >= 1ll << 30 || (long long)g->B * tiles * (blocks + 1) >= 1ll << 31 || (long long)g->B * g->M > 1 << 20 || g->heads > 65535)
+        return fail(FISE_ERR_SHAPE, "%s: B%d M%d heads%d keys%d: too many rows or key blocks", fn, g->B, g->M, g->heads, g->n_keys);
+    if ((long long)g->B * g->heads * (std::max(g->M, g->n_keys) / 64 + 2) * 10 >= 1ll << 31) return fail(FISE_ERR_SHAPE, "%s: B%d heads%d M%d keys%d: too many tiles", fn, g->B, g->heads, g->M, g->n_keys);
+    return FISE_OK;
+}
+
+static bool expands(const fise_latent_attention_args* g, const LatentShape& s) { return g->form == FISE_LATENT_AUTO ? latent_expands(s) : g->form == FISE_LATENT_EXPANDED; }
+
+}  // namespace fise
+
+using namespace fise;
+
+extern "C" size_t fise_latent_attention_workspace_bytes(const fise_latent_attention_args* g) {
+    LatentShape s;
+    if (latent_check("fise_latent_attention_workspace_bytes", g, s)) return 0;
+    if (s.M == 0) return 256;
+    return expands(g, s) ? expanded_layout(s).total : absorbed_layout(s).total;
+}
+
+extern "C" int fise_latent_attention(const fise_latent_attention_args* g, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fise_latent_attention";
+    LatentShape s;
+    if (int e = latent_check(fn, g, s)) return e;
+    if (s.M == 0) return FISE_OK;
+    if (!workspace) return fail(FISE_ERR_NULL, "%s: null workspace", fn);
+    if ((uintptr_t)workspace & 255) return fail(FISE_ERR_ALIGN, "%s: the workspace must be 256-byte aligned", fn);
+    const bool expanded = expands(g, s);
+    const size_t need = expanded ? expanded_layout(s).total : absorbed_layout(s).total;
+    if (workspace_bytes < need) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
+    unsigned char* const ws = (unsigned char*)workspace;
+    LatentArgs a{};
+    a.q = (const bf16_t*)g->q; a.cache = (const bf16_t*)g->cache; a.kv_len = g->kv_len; a.w_uk = (const bf16_t*)g->w_uk; a.w_uv = (const bf16_t*)g->w_uv; a.out = (bf16_t*)g->out;
+    a.B = s.B; a.M = s.M; a.n = s.n; a.heads = s.heads; a.d = s.d; a.dr = s.dr; a.dv = s.dv; a.r = s.r; a.causal = s.causal; a.cache_tokens = g->cache_tokens;
+    a.scale_log2e = g->scale * 1.4426950408889634f;
+    a.d_heads = fast_div(s.heads); a.d_M = fast_div(s.M);
+    const hipStream_t st = as_stream(stream);
+    if (expanded) {
+        const ExpandedLayout l = expanded_layout(s);
+        a.n_pad = l.n_pad; a.k = (bf16_t*)(ws + l.k); a.v = (bf16_t*)(ws + l.v);
+        return launch_expanded(a, expanded_tile(s), st);
+    }
+    const AbsorbedLayout l = absorbed_layout(s);
+    a.tiles = absorbed_tiles(s); a.groups = s.B * a.tiles; a.workgroups = absorbed_workgroups(s); a.tokens = absorbed_tokens(s);
+    a.table = (int*)(ws + l.table); a.qa = (bf16_t*)(ws + l.q); a.ml = (float2*)(ws + l.ml); a.part = (float*)(ws + l.part);
+    a.d_tiles = fast_div(a.tiles);
+    switch (latent_width(s.r)) {
+    case 128: return launch_absorbed<128>(a, st);
+    case 256: return launch_absorbed<256>(a, st);
+    case 384: return launch_absorbed<384>(a, st);
+    default: return launch_absorbed<512>(a, st);
+    }
+}

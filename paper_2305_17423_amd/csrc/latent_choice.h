@@ -1,0 +1,74 @@
+// How attention over a cache of latent vectors is laid out and which form it takes: plain C++, so that a host program can ask for the form of any size.  Internal.
+#pragma once
+#include <algorithm>
+#include <cstddef>
+
+namespace fise {
+
+constexpr int LA_ROWS = 64;           // rows (query, head) of a workgroup of the absorbed form
+constexpr int LA_KEYS = 32;           // keys of a block
+constexpr int LA_CUS = 256;
+
+struct LatentShape { int B, M, n, heads, d, dr, dv, r; bool causal; };
+
+// Widths the kernels are built for: the latent vector and the shared key are filled up with zeros on their way into LDS.
+inline int latent_width(int r) { return r <= 128 ? 128 : r <= 256 ? 256 : r <= 384 ? 384 : 512; }
+constexpr int latent_per_cu(int R) { return R <= 128 ? 3 : R <= 256 ? 2 : 1; }      // workgroups whose blocks of keys a CU's LDS holds
+inline int latent_shared(int dr) { return dr ? 64 : 0; }
+
+// ---- absorbed form.  Blocks of keys of all (batch element, tile of rows) groups stand in one line, which the workgroups share evenly: workgroup w has
+// blocks w T / G .. (w + 1) T / G of T.  A workgroup's part of a group is a partial result in slot w + group, which no other pair has.
+inline int absorbed_tiles(const LatentShape& s) { return (int)(((long long)s.M * s.heads + LA_ROWS - 1) / LA_ROWS); }
+// As many workgroups as find room on the CUs at once, and two blocks each at least: a partial result costs as much to write and read as a block of keys.
+inline int absorbed_workgroups(const LatentShape& s) {
+    const long long blocks = (long long)s.B * absorbed_tiles(s) * ((s.n + LA_KEYS - 1) / LA_KEYS);
+    return (int)std::max(1ll, std::min<long long>(latent_per_cu(latent_width(s.r)) * LA_CUS, (blocks + 1) / 2));
+}
+struct AbsorbedLayout { size_t table, q, ml, part, total; };
+inline AbsorbedLayout absorbed_layout(const LatentShape& s) {
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    const size_t R = latent_width(s.r), groups = (size_t)s.B * absorbed_tiles(s), slots = groups + absorbed_workgroups(s);
+    AbsorbedLayout l;
+    l.table = 0;
+    l.q = l.table + up((groups + 1) * 4);
+    l.ml = l.q + up((size_t)s.B * s.M * s.heads * (R + latent_shared(s.dr)) * 2);
+    l.part = l.ml + up(slots * LA_ROWS * 8);
+    l.total = l.part + up(slots * LA_ROWS * R * 4);
+    return l;
+}
+// Tokens a workgroup of the last launch (merge, then the values' weights) takes
+inline int absorbed_tokens(const LatentShape& s) {
+    const long long tokens = (long long)s.B * s.M;
+    return tokens * s.heads >= 16 * 2 * LA_CUS ? 16 : tokens * s.heads >= 4 * LA_CUS ? 4 : 1;
+}
+
+// ---- expanded form.  Keys of a head are rows [W_uk c | k_pe | 0] of 16 KD channels, values are transposed, as everywhere in the library; both for whole tiles of
+// LX_KEYS keys.
+constexpr int LX_QUERIES = 128, LX_BLOCK = 64, LX_KEYS = 128;
+struct ExpandedTile { int KD, DB; };  // 16-channel steps of a key, 32-channel blocks of a value
+constexpr ExpandedTile kExpandedTiles[] = {{4, 2}, {6, 2}, {8, 2}, {8, 4}, {12, 2}, {12, 4}, {14, 5}};
+inline int expanded_tile(const LatentShape& s) {
+    for (int i = 0;; ++i)
+        if (16 * kExpandedTiles[i].KD >= s.d + s.dr && 32 * kExpandedTiles[i].DB >= s.dv) return i;      // (the last one holds the largest: 160 + 64, 160)
+}
+struct ExpandedLayout { long long n_pad; size_t k, v, total; };
+inline ExpandedLayout expanded_layout(const LatentShape& s) {
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    ExpandedLayout l;
+    l.n_pad = ((long long)s.n + LX_KEYS - 1) / LX_KEYS * LX_KEYS;
+    l.k = 0;
+    l.v = l.k + up((size_t)s.B * s.heads * l.n_pad * kExpandedTiles[expanded_tile(s)].KD * 32);
+    l.total = l.v + up((size_t)s.B * s.heads * s.dv * l.n_pad * 2) + 256;
+    return l;
+}
+
+// ---- which form.  Operations of each at the rate that its kernels reach.
+inline bool latent_expands(const LatentShape& s) {
+    const double keys = (double)s.n, pairs = (double)s.M * s.heads * (s.causal && s.M > 1 ? keys - 0.5 * std::min<double>(s.M, keys) : keys);
+    const double absorbed = pairs * (2.0 * latent_width(s.r) + latent_shared(s.dr)) + (double)s.M * s.heads * s.r * (s.d + s.dv);
+    const ExpandedTile t = kExpandedTiles[expanded_tile(s)];
+    const double expanded = pairs * (16 * t.KD + 32 * t.DB) + keys * s.heads * s.r * (s.d + s.dv);
+    return expanded < absorbed;
+}
+
+}  // namespace fise

@@ -90,3 +90,42 @@ def test_gated_norm_binding_checks_its_tensors():
                 dict(gate=mod[:, :64], mod_scale=torch.zeros((2, 64))), dict(pre_w=torch.zeros(63)), dict(tile_idx=idx[:1]), dict(tile_idx=idx.long())):
         with pytest.raises(ValueError):
             fb.gated_norm_args(x, **{**dict(tile_idx=idx, n_active=2, tile=4, r=x), **bad})
+
+
+def latent():
+    return set_all(fb.fise_latent_attention_args(), q=A, cache=A, w_uk=A, w_uv=A, out=2 * A, B=2, M=0, n_keys=100, cache_tokens=128, heads=8, d=128, dr=64, dv=128, r=512, scale=0.1,
+                   dtype=1)
+
+
+@pytest.mark.parametrize("change,code", [({}, 0), ({"q": None}, -1), ({"cache": None}, -1), ({"w_uk": None}, -1), ({"w_uv": None}, -1), ({"out": None}, -1), ({"dtype": 0}, -3),
+                                         ({"B": 0}, -2), ({"M": -1}, -2), ({"n_keys": -1}, -2), ({"cache_tokens": 99}, -2), ({"heads": 0}, -2), ({"d": 168}, -2), ({"dv": 0}, -2),
+                                         ({"dr": 72}, -2), ({"r": 520}, -2), ({"r": 0}, -2), ({"form": 3}, -2), ({"form": -1}, -2), ({"d": 36}, -4), ({"dr": 4}, -4), ({"dv": 20}, -4),
+                                         ({"r": 100}, -4), ({"q": A + 8}, -4), ({"out": A + 2}, -4), ({"scale": 0.0}, -2), ({"scale": float("nan")}, -2), ({"scale": float("inf")}, -2),
+                                         ({"M": 4}, -1), ({"heads": 70000}, -2), ({"M": 1 << 28}, -2), ({"n_keys": 1 << 27, "cache_tokens": 1 << 27}, -2)])
+def test_latent_attention(change, code):
+    assert call("fise_latent_attention", latent, change, None, 0, None) == code
+    if code:
+        assert "fise_latent_attention" in fb.fise_last_error()
+
+
+@pytest.mark.parametrize("form", [0, 1, 2])
+def test_latent_attention_workspace(form):
+    L, a = fb.lib(), set_all(latent(), M=4, form=form)
+    need = fb.fise_latent_attention_workspace_bytes(a)
+    assert need > 256
+    assert L.fise_latent_attention(ctypes.byref(a), 256, need - 1, None) == -5
+    assert L.fise_latent_attention(ctypes.byref(a), 128, need, None) == -4
+    assert L.fise_latent_attention(None, 256, need, None) == -1
+    a.r = 7
+    assert fb.fise_latent_attention_workspace_bytes(a) == 0
+
+
+def test_latent_attention_binding_checks_its_tensors():
+    bf = dict(dtype=torch.bfloat16)
+    q, c, wk, wv, out = (torch.zeros(s, **bf) for s in ((2, 3, 4, 48), (2, 5, 6, 80), (4, 32, 64), (4, 24, 64), (2, 3, 96)))
+    a = fb.latent_attention_args(q, c, wk, wv, out, 0.2)
+    assert (a.n_keys, a.cache_tokens, a.d, a.dr, a.dv, a.r) == (30, 30, 32, 16, 24, 64)
+    for bad in (dict(out=out[:, :2]), dict(cache=c[..., :72]), dict(q=q.float()), dict(w_uv=wv[:3]), dict(kv_len=torch.zeros(2)), dict(kv_len=torch.zeros(3, dtype=torch.int32)),
+                dict(cache=c.transpose(1, 2)), dict(w_uk=wk.transpose(1, 2))):
+        with pytest.raises(ValueError):
+            fb.latent_attention_args(**{**dict(q=q, cache=c, w_uk=wk, w_uv=wv, out=out, scale=0.2), **bad})
