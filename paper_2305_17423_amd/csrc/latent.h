@@ -25,6 +25,18 @@ __device__ __forceinline__ int la_limit(const LatentArgs& a, int len, int m) { r
 __device__ __forceinline__ void la_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 #if defined(__HIP_DEVICE_COMPILE__)
+// A raw buffer of `bytes` from a base that is the same for all lanes, in scalar registers whatever the compiler knows of it (see buf()).
+__device__ __forceinline__ u32x4_t la_buffer(const void* p, int bytes) {
+    const unsigned long long a = (unsigned long long)(size_t)p;
+    return u32x4_t{(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)a), (unsigned)__builtin_amdgcn_readfirstlane((int)((a >> 32) & 0xffff)), (unsigned)__builtin_amdgcn_readfirstlane(bytes),
+                   0x00020000u};
+}
+// Sixteen bytes a lane from there to LDS, the lanes side by side from `to` on; offsets that are not below the buffer's size bring zeros.  Written out because the
+// compiler waits for every load of the builtin that is in flight in front of a turned read or a write of LDS; whoever reads what it brings waits by its count.
+// (m0 is changed: nothing else in these kernels uses it.)
+__device__ __forceinline__ void la_to_lds(u32x4_t from, unsigned off, unsigned to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(from), "s"(to) : "memory");
+}
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 // Sixteen lanes read a block of 4 rows x 16 columns (lane i: four columns from 4 (i % 4) of row i / 4) and get it turned: lane i column i, all four rows.
 // Two blocks are the operand of a 16x16x32 product whose summed index runs down the rows: row groups `at` and `at` + second.

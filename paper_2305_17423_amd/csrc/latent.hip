@@ -85,14 +85,20 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
 // the key, and a lane reads the key rows in the order that makes its eight scores those of eight consecutive keys: its probabilities are
 // then, as they stand, its part of the second product's operand.  Sums: the waves exchange probabilities and a wave has all 64 rows x a quarter
 // of the latent channels, whose operand is the same block read turned, so nothing is read twice from memory and no transposed copy exists.
-// A row's sixteen-byte pieces are stored at piece ^ la_swizzle(key): the eight lanes of a step of the score product, and the four keys that a turned
-// read takes at a time, then lie in different banks.
+// A turn is the scores of one block and the sums of the block before, so that one barrier serves both and neither product waits for the softmax of its own block.
+// A row's reference moves only when a score lies 8 powers of two above it: any reference gives the same quotient, probabilities stay below 256 (a bf16 and a float have
+// the same relative steps there) and the factor for the sums before is 1 almost always.
 template <int R_, int DR_> struct LaTile {
-    static constexpr int R = R_, DR = DR_, PIECES = (R + DR) / 8, PITCH = PIECES * 16, TILE = LA_KEYS * PITCH, PER_CU = latent_per_cu(R), RING = R == 256 && DR ? 3 : 4, AHEAD = RING - 1;
-    static constexpr int LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32, P = RING * TILE, ALPHA = P + LA_ROWS * LA_KEYS * 2, LDS = ALPHA + LA_ROWS * 4;
-    static_assert(TILE % 4096 == 0 && PIECES % 8 == 0 && PER_CU * LDS <= 160 * 1024, "whole loads of four waves; LDS of a CU");
+    static constexpr int R = R_, DR = DR_, PIECES = (R + DR) / 8, PITCH = PIECES * 16, TILE = LA_KEYS * PITCH, PER_CU = latent_per_cu(R);
+    static constexpr int RING = R == 128 || (R == 256 && DR) ? 3 : 4, AHEAD = RING - 1, LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32;
+    static constexpr int P = RING * TILE, PB = LA_ROWS * LA_KEYS * 2, ALPHA = P + 2 * PB, AB = LA_ROWS * 4, LDS = ALPHA + 2 * AB;      // probabilities and factors: two of each
+    // Place of a row's pieces.  A sixteen-byte read takes lanes 0-3, 12-15, 20-23, 24-27 at once (then the other sixteen of a half wave), which are sixteen keys of the
+    // score product's operand, two neighbouring pieces alternating with key / 8; half a turned read takes two pieces of keys k .. k + 3 and k + 8 .. k + 11.  Both
+    // meet every bank once.  (Where rows are 128 bytes off a multiple of 256, odd keys are in the other half of the banks anyway.)
+    static constexpr int PERIOD = PITCH % 256 ? 8 : 16;
+    static __device__ __forceinline__ int swizzle(int key) { return (PITCH % 256 ? 0 : (key & 1) << 3) | (key & 2) << 1 | (key & 8) >> 2; }
+    static_assert(TILE % 4096 == 0 && PIECES % PERIOD == 0 && PER_CU * LDS <= 160 * 1024, "whole loads of four waves; LDS of a CU");
 };
-__device__ __forceinline__ int la_swizzle(int key) { return ((key & 3) << 1) | ((key >> 3) & 1); }
 
 template <int R, int DR>
 __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(const LatentArgs a) {
@@ -101,18 +107,19 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
     constexpr int RT = T::RT, KS = T::KS, PITCH = T::PITCH, LPW = T::LPW, AHEAD = T::AHEAD;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    const int wave = uniform(tid >> 6);
     // consecutive workgroups go to the eight XCDs in turn: give each XCD one run of the line
-    const int total = __builtin_amdgcn_readfirstlane(a.table[a.groups]), workgroups = min(a.workgroups, total);      // each has a block
+    const int total = uniform(a.table[a.groups]), workgroups = min(a.workgroups, total);      // each has a block
     int w = blockIdx.x;
     if (w >= workgroups) return;
     { const int chunk = workgroups >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
-    const int line0 = (int)((long long)w * total / workgroups), line1 = (int)((long long)(w + 1) * total / workgroups);
+    const int line0 = uniform((int)((long long)w * total / workgroups)), line1 = uniform((int)((long long)(w + 1) * total / workgroups));
     int g = 0;
     for (int lo = 0, hi = a.groups - 1;;) {                            // last group that starts at or before line0
         if (lo >= hi) { g = lo; break; }
         const int mid = (lo + hi + 1) >> 1;
-        if (__builtin_amdgcn_readfirstlane(a.table[mid]) <= line0) lo = mid; else hi = mid - 1;
+        if (uniform(a.table[mid]) <= line0) lo = mid; else hi = mid - 1;
     }
     const int row_bytes = (a.r + a.dr) * 2, rows = a.M * a.heads;
 
@@ -120,41 +127,45 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
     unsigned off[LPW];
 #pragma unroll
     for (int j = 0; j < LPW; ++j) {
-        const int p = (wave * LPW + j) * 64 + lane, key = p / T::PIECES, piece = (p - key * T::PIECES) ^ la_swizzle(key);
+        const int p = (wave * LPW + j) * 64 + lane, key = p / T::PIECES, piece = (p - key * T::PIECES) ^ T::swizzle(key);
         const int c = piece * 8, pe = c - R;
         off[j] = c < R ? (c < a.r ? (unsigned)(key * row_bytes + c * 2) : 0x40000000u) : (pe < a.dr ? (unsigned)(key * row_bytes + (a.r + pe) * 2) : 0x40000000u);
     }
     const int my_key = (l16 >> 2) * 8 + (l16 & 3);                     // of the first half of a block's scores; the second half's is 4 further
-    unsigned kat[2];
+    constexpr int KB = T::PERIOD / 4;                                  // steps after which the places repeat
+    unsigned kat[KB];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) kat[j] = (unsigned)(my_key * PITCH + ((j * 4 + lq) ^ la_swizzle(my_key)) * 16);
-    constexpr int VB = RT < 4 ? RT : 4;
+    for (int j = 0; j < KB; ++j) kat[j] = (unsigned)(my_key * PITCH + ((j * 4 + lq) ^ T::swizzle(my_key)) * 16);
+    constexpr int VB = RT < T::PERIOD / 2 ? RT : T::PERIOD / 2;
     unsigned vat[VB];
     {
         const int key = lq * 8 + l16 / 4;
 #pragma unroll
-        for (int j = 0; j < VB; ++j) vat[j] = (unsigned)(key * PITCH + (((wave * RT + j) * 2 + (l16 % 4) / 2) ^ la_swizzle(key)) * 16 + (l16 & 1) * 8);
+        for (int j = 0; j < VB; ++j) vat[j] = (unsigned)(key * PITCH + (((wave * RT + j) * 2 + (l16 % 4) / 2) ^ T::swizzle(key)) * 16 + (l16 & 1) * 8);
     }
+    const unsigned lds0 = (unsigned)(size_t)(FISE_AS3 unsigned char*)(FISE_AS3 void*)lds;
 
     for (int at = line0; at < line1; ++g) {
-        const int g_at = __builtin_amdgcn_readfirstlane(a.table[g]), g_end = __builtin_amdgcn_readfirstlane(a.table[g + 1]);
+        const int g_at = uniform(a.table[g]), g_end = uniform(a.table[g + 1]);
         const int end = min(line1, g_end);
         if (end <= at) continue;
-        const int b = (int)fdiv((unsigned)g, a.d_tiles), row0 = (g - b * a.tiles) * LA_ROWS;
-        const int blk0 = at - g_at, blk1 = end - g_at, len = __builtin_amdgcn_readfirstlane(la_len(a, b));
+        const int b = uniform((int)fdiv((unsigned)g, a.d_tiles)), row0 = (g - b * a.tiles) * LA_ROWS;
+        const int blk0 = at - g_at, blk1 = end - g_at, len = uniform(la_len(a, b));
         const int row = row0 + wave * 16 + l16;
-        const int limit = row < rows ? la_limit(a, len, (int)fdiv((unsigned)row, a.d_heads)) : len;
+        const int sees = row < rows ? la_limit(a, len, (int)fdiv((unsigned)row, a.d_heads)) : len;
+        const int limit = min(sees, blk1 * LA_KEYS);                   // (behind this part's last block: nothing)
         const int limit_first = la_limit(a, len, (int)fdiv((unsigned)row0, a.d_heads));       // the fewest keys that a row of the tile sees
         const unsigned char* const keys = (const unsigned char*)a.cache + (size_t)b * a.cache_tokens * row_bytes;
 
         int put = 0, get = 0;                                          // places in the ring
+        auto next = [](int x) { return x == AHEAD * T::TILE ? 0 : x + T::TILE; };
         auto load = [&](int blk) {                                     // (behind the last block: nothing but zeros, no traffic, the same count of loads)
             const int k0 = blk * LA_KEYS, left = min(max(len - k0, 0), LA_KEYS);
-            const auto rsrc = buf(keys + (size_t)k0 * row_bytes, blk < blk1 ? (unsigned)(left * row_bytes) : 0u);
-            unsigned char* const to = lds + put + wave * LPW * 1024;
-            put = put == AHEAD * T::TILE ? 0 : put + T::TILE;
+            const u32x4_t from = la_buffer(keys + (size_t)k0 * row_bytes, blk < blk1 ? left * row_bytes : 0);
+            const unsigned to = uniform(lds0 + put + wave * LPW * 1024);
+            put = next(put);
 #pragma unroll
-            for (int j = 0; j < LPW; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (FISE_AS3 void*)(to + j * 1024), 16, (int)off[j], 0, 0, 0);
+            for (int j = 0; j < LPW; ++j) la_to_lds(from, off[j], to + j * 1024);
         };
         bf16x8_t qf[KS];
         {
@@ -176,70 +187,104 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
             for (int t = 0; t < 4; ++t) acc[j][t] = f32x4_t{0, 0, 0, 0};
         float m_run = -INFINITY, l_run = 0.f;                          // l: of this lane's keys until the end
 
-        for (int blk = blk0; blk < blk1; ++blk) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPW) : "memory");
+        // Product m of the scores takes key rows of half m & 1, step m >> 1; reads go out LA_AHEAD products before theirs.
+        constexpr int LA_AHEAD = 6, NK = 2 * KS, RK = LA_AHEAD + 1;
+        f32x4_t s[2][2];
+        bf16x8_t kf[RK];
+        auto read_k = [&](const unsigned char* tile, int m) { return *reinterpret_cast<const bf16x8_t*>(tile + kat[(m >> 1) % KB] + (m >> 1) / KB * (T::PERIOD * 16) + (m & 1) * 4 * PITCH); };
+        auto score = [&](int m) {
+            f32x4_t& to = s[m & 1][(m >> 1) & 1];
+            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m % RK], qf[m >> 1], m < 4 ? f32x4_t{0, 0, 0, 0} : to, 0, 0, 0);
+        };
+        // softmax of a block in five pieces: scores of eight keys a lane, k0 + lq * 8 + (0..7); their maximum; the reference and the factor for the sums before;
+        // probabilities; those and the factor to LDS
+        float p[8], mx, alpha;
+        auto softmax = [&](int piece, int k0, int which) {
+            if (piece == 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[e] = (s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3]) * a.scale_log2e;
+                    if (k0 + lq * 8 + e >= limit) p[e] = -INFINITY;
+                }
+            } else if (piece == 1) {
+                mx = la_max4(fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7]))));
+            } else if (piece == 2) {
+                mx = mx > m_run + 8.f ? mx : m_run;                    // (the first block: above -inf)
+                const float base = mx == -INFINITY ? 0.f : mx;         // nothing seen yet: every probability is exp2(-inf) = 0
+                alpha = __builtin_amdgcn_exp2f(m_run - base);
+                m_run = mx;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] -= base;
+            } else if (piece == 3) {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(p[e]); sum += p[e]; }
+                l_run = fmaf(l_run, alpha, sum);
+            } else {
+                *reinterpret_cast<uint4*>(lds + T::P + which * T::PB + tid * 16) = make_uint4(f2bf2(p[0], p[1]), f2bf2(p[2], p[3]), f2bf2(p[4], p[5]), f2bf2(p[6], p[7]));
+                if (lq == 0) *reinterpret_cast<float*>(lds + T::ALPHA + which * T::AB + (wave * 16 + l16) * 4) = alpha;
+            }
+        };
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPW) : "memory");
+#pragma unroll
+        for (int m = 0; m < NK; ++m) { kf[m % RK] = read_k(lds, m); score(m); }
+#pragma unroll
+        for (int i = 0; i < 5; ++i) softmax(i, blk0 * LA_KEYS, 0);
+        int which = 0;
+        for (int blk = blk0; blk < blk1; ++blk, which ^= 1) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 2) * LPW) : "memory");
             load(blk + AHEAD);                                         // over the block before, which all waves are done with
             const unsigned char* const tile = lds + get;
-            get = get == AHEAD * T::TILE ? 0 : get + T::TILE;
-            const int k0 = blk * LA_KEYS;
-            // ---- scores of eight keys a lane: k0 + lq * 8 + (0..7)
-            f32x4_t s[2][2];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(tile + kat[ks & 1] + (ks >> 1) * 128 + kt * 4 * PITCH);
-                    s[kt][ks & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks], ks < 2 ? f32x4_t{0, 0, 0, 0} : s[kt][ks & 1], 0, 0, 0);
-                }
-            float p[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = (s[e >> 2][0][e & 3] + s[e >> 2][1][e & 3]) * a.scale_log2e;
-            const bool partial = k0 + LA_KEYS > limit_first;           // uniform: some row of the tile does not see all of the block
-            if (partial) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (k0 + lq * 8 + e >= limit) p[e] = -INFINITY;
-            }
-            float mx = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-            mx = fmaxf(m_run, la_max4(mx));
-            const float base = mx == -INFINITY ? 0.f : mx;             // nothing seen yet: every probability is exp2(-inf) = 0
-            const float alpha = __builtin_amdgcn_exp2f(m_run - base);
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(p[e] - base); sum += p[e]; }
-            l_run = fmaf(l_run, alpha, sum);
-            m_run = mx;
-            *reinterpret_cast<uint4*>(lds + T::P + tid * 16) = make_uint4(f2bf2(p[0], p[1]), f2bf2(p[2], p[3]), f2bf2(p[4], p[5]), f2bf2(p[6], p[7]));
-            if (lq == 0) *reinterpret_cast<float*>(lds + T::ALPHA + (wave * 16 + l16) * 4) = alpha;
-            la_barrier();
-            if (a.causal && partial) {
+            get = next(get);
+            if (a.causal && blk * LA_KEYS + LA_KEYS > limit_first) {
                 // a key that a row does not see takes part with probability 0: what is not finite in it must not
                 for (int i = tid; i < LA_KEYS * (R / 8); i += 256) {
-                    const int key = i / (R / 8), piece = (i - key * (R / 8)) ^ la_swizzle(key);
+                    const int key = i / (R / 8), piece = (i - key * (R / 8)) ^ T::swizzle(key);
                     uint4* const at16 = reinterpret_cast<uint4*>(const_cast<unsigned char*>(tile) + key * PITCH + piece * 16);
                     *at16 = la_finite(*at16);
                 }
                 la_barrier();
             }
-            // ---- sums of a quarter of the latent channels for all 64 rows
-            bf16x8_t pf[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                pf[t] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + (t * 64 + lane) * 16);
-                const float al = *reinterpret_cast<const float*>(lds + T::ALPHA + (t * 16 + l16) * 4);
-                if (__any(al != 1.0f)) {                               // a maximum has moved, which becomes rare
+            for (int m = 0; m < LA_AHEAD; ++m) kf[m] = read_k(lds + get, m);
+            float al[4];
 #pragma unroll
-                    for (int j = 0; j < RT; ++j)
+            for (int t = 0; t < 4; ++t) al[t] = *reinterpret_cast<const float*>(lds + T::ALPHA + which * T::AB + (t * 16 + l16) * 4);
+            if (__any(al[0] != 1.0f || al[1] != 1.0f || al[2] != 1.0f || al[3] != 1.0f)) {      // a reference has moved, which becomes rare
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][t][e] *= al;
-                }
+                for (int j = 0; j < RT; ++j)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][t][e] *= al[t];
             }
+            // ---- scores of the next block, then sums of this one (a quarter of the latent channels for all 64 rows) with the softmax of the next between them; in this
+            // order, which the compiler's own would give up for fewer registers: every product would wait for its operand
+            bf16x8_t pf[4], vf[2];
+            auto read_v = [&](int j) { return la_turned(tile + vat[j % VB] + j / VB * (T::PERIOD * 16), 4 * PITCH); };
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int m = 0; m < NK; ++m) {
+                if (m + LA_AHEAD < NK) kf[(m + LA_AHEAD) % RK] = read_k(lds + get, m + LA_AHEAD);
+                else if (m + LA_AHEAD < NK + 4) pf[m + LA_AHEAD - NK] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + which * T::PB + ((m + LA_AHEAD - NK) * 64 + lane) * 16);
+                else if (m + LA_AHEAD == NK + 4) vf[0] = read_v(0);
+                __builtin_amdgcn_sched_barrier(0);
+                score(m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            static_assert(LA_AHEAD > 4, "probabilities and the first values are read with the last scores");
 #pragma unroll
             for (int j = 0; j < RT; ++j) {
-                const bf16x8_t vf = la_turned(tile + vat[j % VB] + (j / VB) * 128, 4 * PITCH);
+                if (j + 1 < RT) vf[(j + 1) & 1] = read_v(j + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[j][t], 0, 0, 0);
+                for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pf[t], acc[j][t], 0, 0, 0);
+                if (j * 5 / RT != (j + 1) * 5 / RT || RT < 5)          // five pieces over the RT steps (fewer steps than pieces: what is left at the end)
+                    softmax(RT < 5 ? j : j * 5 / RT, (blk + 1) * LA_KEYS, which ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int i = RT; i < 5; ++i) softmax(i, (blk + 1) * LA_KEYS, which ^ 1);
         }
         at = end;
         // ---- partial result of this part of the group

@@ -7,7 +7,8 @@ namespace fise {
 
 // ---------------------------------------------------------------------------------------------------------------- keys and values
 // Tiles of 128 keys x 128 weight rows of one batch element on 32x32x16 products, four waves of 64 x 64; both operands run along the latent channels, 64 a step,
-// loaded directly to LDS, a step ahead.  Rows of 128 bytes, sixteen-byte pieces at piece ^ (row & 7).  The first index of the product is the one that runs along the
+// loaded directly to LDS, a step ahead.  Rows of 128 bytes, sixteen-byte pieces at piece ^ (row / 2 & 7): sixteen rows read at
+// once lie in different banks.  The first index of the product is the one that runs along the
 // result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.
 constexpr int LE_STEP = 64, LE_STAGE = 2 * 128 * LE_STEP * 2;
 __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs a, int KD, int key_tiles, int k_tiles, int v_tiles, FastDiv d_key_tiles, FastDiv d_tiles) {
@@ -28,19 +29,21 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 
     // a wave loads 32 rows of each operand in four loads of eight rows
     unsigned key_off[4], w_off[4];
-    const int piece = (lane & 7) ^ (lane >> 3);
+    int piece[2];                                                      // of loads of even and odd number
+#pragma unroll
+    for (int j = 0; j < 2; ++j) piece[j] = (lane & 7) ^ ((j * 8 + (lane >> 3)) >> 1);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int row = wave * 32 + j * 8 + (lane >> 3);
-        key_off[j] = (unsigned)(row * row_bytes + piece * 16);
-        w_off[j] = (unsigned)(row * a.r * 2 + piece * 16);
+        key_off[j] = (unsigned)(row * row_bytes + piece[j & 1] * 16);
+        w_off[j] = (unsigned)(row * a.r * 2 + piece[j & 1] * 16);
     }
     const int steps = (a.r + LE_STEP - 1) / LE_STEP;
     auto load = [&](int s) {
-        const bool ok = s * LE_STEP + piece * 8 < a.r;                 // channels past r: zeros on both sides
         unsigned char* const to = lds + (s & 1) * LE_STAGE + wave * 4096;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            const bool ok = s * LE_STEP + piece[j & 1] * 8 < a.r;      // channels past r: zeros on both sides
             __builtin_amdgcn_raw_ptr_buffer_load_lds(keys, (FISE_AS3 void*)(to + j * 1024), 16, (int)(ok ? key_off[j] + s * (LE_STEP * 2) : 0x40000000u), 0, 0, 0);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(weights, (FISE_AS3 void*)(to + 16384 + j * 1024), 16, (int)(ok ? w_off[j] + s * (LE_STEP * 2) : 0x40000000u), 0, 0, 0);
         }
@@ -63,7 +66,7 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
             bf16x8_t x[2], y[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int at = ((ks * 2 + hl) ^ (l32 & 7)) * 16;
+                const int at = ((ks * 2 + hl) ^ ((l32 >> 1) & 7)) * 16;
                 x[i] = *reinterpret_cast<const bf16x8_t*>(stage + first + (wr * 64 + i * 32 + l32) * 128 + at);
                 y[i] = *reinterpret_cast<const bf16x8_t*>(stage + second + (wc * 64 + i * 32 + l32) * 128 + at);
             }
@@ -105,12 +108,12 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // ---------------------------------------------------------------------------------------------------------------- attention
 // A wave has 32 queries of a head; keys come in blocks of 64 through LDS, loaded directly, a block ahead.  Scores are computed transposed (a lane keeps one query),
 // from key rows in the order that makes a lane's eight scores of a 16-key step those of eight consecutive keys: they are the operand of the second product as
-// they stand.  Key rows of 128 k bytes: pieces at piece ^ (row & 7); of 64 (2 k + 1): at piece ^ (row / 2 & 3); value rows of 128 bytes: the first.
+// they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 template <int KD, int DB>
 __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArgs a, int nqt, FastDiv d_nqt) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int PIECES = 2 * KD, PITCH = PIECES * 16, KB = LX_BLOCK * PITCH, VB = DB * 32 * 128, STAGE = KB + VB, KL = KB / 4096, VL = VB / 4096;
-    static_assert(KB % 4096 == 0 && KD % 2 == 0, "whole loads of four waves");
+    static_assert(KB % 4096 == 0 && KD % 2 == 0 && (PITCH % 256 || PIECES % 16 == 0), "whole loads of four waves");
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -123,7 +126,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArg
     const int limit = la_limit(a, len, min(m, a.M - 1)), limit_first = la_limit(a, len, qt * LX_QUERIES), limit_last = la_limit(a, len, min(qt * LX_QUERIES + LX_QUERIES, a.M) - 1);
     const int blocks = (limit_last + LX_BLOCK - 1) / LX_BLOCK;
 
-    auto swizzle = [](int row) { return PITCH % 128 ? (row >> 1) & 3 : row & 7; };
+    auto swizzle = [](int row) { return PITCH % 128 ? (row >> 2) & 3 : PITCH % 256 ? (row >> 1) & 7 : row & 15; };
     unsigned k_off[KL], v_off[VL];
 #pragma unroll
     for (int j = 0; j < KL; ++j) {
@@ -135,7 +138,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArg
     const bf16_t* const v = a.v + (size_t)bh * a.dv * a.n_pad;
 #pragma unroll
     for (int j = 0; j < VL; ++j) {
-        const int row = (wave * VL + j) * 8 + (lane >> 3), piece = (lane & 7) ^ (row & 7);
+        const int row = (wave * VL + j) * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
         v_off[j] = row < a.dv ? (unsigned)((lane >> 3) * a.n_pad * 2 + piece * 16) : 0x40000000u;
     }
     auto load = [&](int blk) {
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArg
             const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(&pw);
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
-                const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(stage + KB + (i * 32 + l32) * 128 + ((u * 2 + hl) ^ (l32 & 7)) * 16);
+                const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(stage + KB + (i * 32 + l32) * 128 + ((u * 2 + hl) ^ ((l32 >> 1) & 7)) * 16);
                 o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
             }
         }
