@@ -10,18 +10,20 @@
 namespace fise {
 
 // ---------------------------------------------------------------------------------------------------------------- queries
-// qa[b, m, h] = [W_uk[h]^T q_c | q_pe | 0]: a workgroup takes 128 latent channels of a head and 64 tokens (a wave 32 channels); W_uk's rows run along the result, so
-// they are turned on the way out of LDS.  The result is rounded to bf16, as any operand of the matrix unit.
-// The first workgroup also writes the line of key blocks: table[g] = blocks of all groups before g.
+// qa[b, m, h] = [W_uk[h]^T q_c | q_pe | 0]: a workgroup has 128 latent channels of a head (a wave 32 of them) and takes 64 tokens at a time; W_uk's rows run along the
+// result, so they are turned on the way out of LDS.  The result is rounded to bf16, as any operand of the matrix unit.  All loads of a round go out together: few
+// tokens wait for one trip to memory, not for one a step.
+// The last workgroup writes the line of key blocks instead: table[g] = blocks of all groups before g.
 constexpr int LQ_COLS = 128, LQ_TOKENS = 64;
-__global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, int R, int DR) {
+[[maybe_unused]] constexpr int LQ_STEPS = 5;                           // steps of 32 channels of d, at most 160
+__global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, int R, int DR, int rounds) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int LQ_PITCH = LQ_COLS * 2 + 32;                         // four rows of a block side by side in the banks
-    __shared__ __attribute__((aligned(16))) unsigned char lds[160 * LQ_PITCH];
-    __shared__ int sums[256];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[LQ_STEPS * 32 * LQ_PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
-    const int h = blockIdx.x, c0 = blockIdx.y * LQ_COLS, t0 = blockIdx.z * LQ_TOKENS, tokens = a.B * a.M, width = R + DR;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) {
+    if (blockIdx.x == gridDim.x - 1) {
+        if (blockIdx.y) return;
+        int* const sums = reinterpret_cast<int*>(lds);
         const int each = (a.groups + 255) / 256, g0 = min(tid * each, a.groups), g1 = min(g0 + each, a.groups);
         auto blocks = [&](int g) {
             const int b = (int)fdiv((unsigned)g, a.d_tiles), t = g - b * a.tiles;
@@ -41,40 +43,64 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
         int at = sums[tid] - s;
         for (int g = g0; g < g1; ++g) { a.table[g] = at; at += blocks(g); }
         if (tid == 255) a.table[a.groups] = sums[255];
+        return;
     }
+    const int cols = R / LQ_COLS, h = blockIdx.x / cols, c0 = (blockIdx.x - h * cols) * LQ_COLS, tokens = a.B * a.M, width = R + DR;
     const int steps = (a.d + 31) / 32;
-    for (int i = tid; i < steps * 32 * (LQ_COLS / 8); i += 256) {
-        const int row = i / (LQ_COLS / 8), c = (i % (LQ_COLS / 8)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < a.d && c0 + c < a.r) v = *reinterpret_cast<const uint4*>(a.w_uk + ((size_t)h * a.d + row) * a.r + c0 + c);
-        *reinterpret_cast<uint4*>(lds + row * LQ_PITCH + c * 2) = v;
+    uint4 qv[LQ_TOKENS / 16][LQ_STEPS];
+    auto queries = [&](int t0) {
+#pragma unroll
+        for (int tt = 0; tt < LQ_TOKENS / 16; ++tt) {
+            const int t = t0 + tt * 16 + l16;
+#pragma unroll
+            for (int ks = 0; ks < LQ_STEPS; ++ks) {
+                qv[tt][ks] = make_uint4(0, 0, 0, 0);
+                const int c = ks * 32 + lq * 8;
+                if (t < tokens && c < a.d) qv[tt][ks] = *reinterpret_cast<const uint4*>(a.q + ((size_t)t * a.heads + h) * (a.d + a.dr) + c);
+            }
+        }
+    };
+    {
+        uint4 w[LQ_STEPS * 2];
+        const int c = (tid & 15) * 8;
+#pragma unroll
+        for (int i = 0; i < LQ_STEPS * 2; ++i) {
+            const int row = i * 16 + (tid >> 4);
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (row < a.d && c0 + c < a.r) w[i] = *reinterpret_cast<const uint4*>(a.w_uk + ((size_t)h * a.d + row) * a.r + c0 + c);
+        }
+        queries(blockIdx.y * LQ_TOKENS);
+#pragma unroll
+        for (int i = 0; i < LQ_STEPS * 2; ++i) *reinterpret_cast<uint4*>(lds + (i * 16 + (tid >> 4)) * LQ_PITCH + c * 2) = w[i];
     }
     __syncthreads();
     const unsigned char* const from = lds + (lq * 8 + l16 / 4) * LQ_PITCH + (wave * 32 + (l16 % 4) * 4) * 2;
+    for (int round = 0; round < rounds; ++round) {
+        const int t0 = (round * gridDim.y + blockIdx.y) * LQ_TOKENS;
+        if (t0 >= tokens) return;
+        if (round) queries(t0);
 #pragma unroll
-    for (int tt = 0; tt < LQ_TOKENS / 16; ++tt) {
-        const int t = t0 + tt * 16 + l16;
-        if (t0 + tt * 16 >= tokens) break;
-        const bool ok = t < tokens;
-        const bf16_t* const q = a.q + ((size_t)(ok ? t : 0) * a.heads + h) * (a.d + a.dr);
-        f32x4_t acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-        for (int ks = 0; ks < steps; ++ks) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            const int c = ks * 32 + lq * 8;
-            if (ok && c < a.d) v = *reinterpret_cast<const uint4*>(q + c);
-            const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(&v);
+        for (int tt = 0; tt < LQ_TOKENS / 16; ++tt) {
+            if (t0 + tt * 16 >= tokens) return;
+            const int t = t0 + tt * 16 + l16;
+            f32x4_t acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+            for (int ks = 0; ks < LQ_STEPS; ++ks)
+                if (ks < steps) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(la_turned(from + ks * 32 * LQ_PITCH + j * 32, 4 * LQ_PITCH), *reinterpret_cast<const bf16x8_t*>(&qv[tt][ks]),
+                                                                         acc[j], 0, 0, 0);
+                }
+            if (t >= tokens) continue;
+            bf16_t* const to = a.qa + ((size_t)t * a.heads + h) * width;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(la_turned(from + ks * 32 * LQ_PITCH + j * 32, 4 * LQ_PITCH), x, acc[j], 0, 0, 0);
+                *reinterpret_cast<uint2*>(to + c0 + wave * 32 + j * 16 + lq * 4) = make_uint2(f2bf2(acc[j][0], acc[j][1]), f2bf2(acc[j][2], acc[j][3]));
+            if (c0 == 0 && wave == 0)
+                for (int c = lq * 8; c < DR; c += 32)
+                    *reinterpret_cast<uint4*>(to + R + c) = c < a.dr ? *reinterpret_cast<const uint4*>(a.q + ((size_t)t * a.heads + h) * (a.d + a.dr) + a.d + c) : make_uint4(0, 0, 0, 0);
         }
-        if (!ok) continue;
-        bf16_t* const to = a.qa + ((size_t)t * a.heads + h) * width;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            *reinterpret_cast<uint2*>(to + c0 + wave * 32 + j * 16 + lq * 4) = make_uint2(f2bf2(acc[j][0], acc[j][1]), f2bf2(acc[j][2], acc[j][3]));
-        if (blockIdx.y == 0 && wave == 0)
-            for (int c = lq * 8; c < DR; c += 32)
-                *reinterpret_cast<uint4*>(to + R + c) = c < a.dr ? *reinterpret_cast<const uint4*>(q + a.d + c) : make_uint4(0, 0, 0, 0);
     }
 #endif
 }
@@ -313,6 +339,9 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
     constexpr int QUADS = R / 4, PARTS = 512 / QUADS, PITCH = R + 8;   // parts: lanes that share the parts of a token, or have tokens of their own
     __shared__ __attribute__((aligned(16))) bf16_t hi[16][PITCH], lo[16][PITCH];
     __shared__ __attribute__((aligned(16))) float4 sums[PARTS][QUADS];
+    __shared__ float2 stats[16];                                       // of a token: reference, 1 / sum
+    __shared__ size_t first[16];                                       // its first part's place
+    __shared__ int count[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
     const int h = blockIdx.x, t0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.B * a.M - t0);
     const int part = tid / QUADS, quad = tid - part * QUADS;
@@ -331,26 +360,44 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
     bf16x8_t wf[R / 32];
     if (wave < vt) weights(wf, wave);
 
+    // ---- what the parts of each token weigh: 32 lanes a token go over its parts (workgroups that had a part of its group's blocks; block x belongs to the largest w with
+    // w total / workgroups <= x), keeping a maximum and a sum, and meet.  l == 0: no key was seen, zeros.
+    if (tid < a.tokens * 32) {
+        const int i = tid >> 5, t = t0 + i;
+        if (i < tokens) {
+            const int b = (int)fdiv((unsigned)t, a.d_M), row = (t - b * a.M) * a.heads + h, tile = row / LA_ROWS, g = b * a.tiles + tile;
+            const int g0 = a.table[g], g1 = a.table[g + 1];
+            auto owner = [&](int x) { return (int)((((long long)x + 1) * workgroups - 1) / total); };
+            const int w0 = g1 > g0 ? owner(g0) : 0, n = g1 > g0 ? owner(g1 - 1) - w0 + 1 : 0;
+            const size_t at = ((size_t)g + w0) * LA_ROWS + (row - tile * LA_ROWS);
+            float top = -INFINITY, l = 0.f;
+            for (int p = tid & 31; p < n; p += 32) {
+                const float2 v = a.ml[at + (size_t)p * LA_ROWS];
+                const float m = fmaxf(top, v.x), base = m == -INFINITY ? 0.f : m;
+                l = l * __builtin_amdgcn_exp2f(top - base) + v.y * __builtin_amdgcn_exp2f(v.x - base);
+                top = m;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const float mo = __shfl_xor(top, o), lo_ = __shfl_xor(l, o), m = fmaxf(top, mo), base = m == -INFINITY ? 0.f : m;
+                l = l * __builtin_amdgcn_exp2f(top - base) + lo_ * __builtin_amdgcn_exp2f(mo - base);
+                top = m;
+            }
+            if ((tid & 31) == 0) { stats[i] = make_float2(top == -INFINITY ? 0.f : top, l == 0.f ? 0.f : 1.0f / l); first[i] = at; count[i] = n; }
+        }
+    }
+    __syncthreads();
     // the sums of token t0 + i over every `step`-th part from the first + `from` on
     auto merge = [&](int i, int from, int step) {
         float4 o = make_float4(0, 0, 0, 0);
-        const int t = t0 + i, b = (int)fdiv((unsigned)t, a.d_M), row = (t - b * a.M) * a.heads + h, tile = row / LA_ROWS, g = b * a.tiles + tile;
-        const int g0 = a.table[g], g1 = a.table[g + 1];
-        if (i >= tokens || g1 <= g0) return o;
-        // workgroups with a part of blocks g0 .. g1 - 1: block x belongs to the largest w with w total / workgroups <= x
-        auto owner = [&](int x) { return (int)((((long long)x + 1) * workgroups - 1) / total); };
-        const int w0 = owner(g0), w1 = owner(g1 - 1);
-        const size_t at = (size_t)g * LA_ROWS + (row - tile * LA_ROWS);
-        float top = -INFINITY;
-        for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.ml[at + (size_t)w * LA_ROWS].x);
-        const float base = top == -INFINITY ? 0.f : top;
-        float l = 0.f;
-        for (int w = w0; w <= w1; ++w) { const float2 v = a.ml[at + (size_t)w * LA_ROWS]; l = fmaf(__builtin_amdgcn_exp2f(v.x - base), v.y, l); }
-        const float inv = l == 0.f ? 0.f : 1.0f / l;                   // no key seen: zeros
+        const float2 st = stats[i];
+        const int n = count[i];
+        const float2* const ml = a.ml + first[i];
+        const float* const part_o = a.part + first[i] * R + quad * 4;
 #pragma unroll 4
-        for (int w = w0 + from; w <= w1; w += step) {
-            const float f = __builtin_amdgcn_exp2f(a.ml[at + (size_t)w * LA_ROWS].x - base) * inv;
-            const float4 v = *reinterpret_cast<const float4*>(a.part + (at + (size_t)w * LA_ROWS) * R + quad * 4);
+        for (int p = from; p < n; p += step) {
+            const float f = __builtin_amdgcn_exp2f(ml[(size_t)p * LA_ROWS].x - st.x) * st.y;
+            const float4 v = *reinterpret_cast<const float4*>(part_o + (size_t)p * (LA_ROWS * R));
             o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
         }
         return o;
@@ -400,7 +447,9 @@ template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStre
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_absorbed_kernel<R, DR>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
     if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_latent_attention: cannot raise the dynamic LDS limit");
     const int tokens = a.B * a.M;
-    hipLaunchKernelGGL(latent_query_kernel, dim3((unsigned)a.heads, R / LQ_COLS, (unsigned)ceil_div(tokens, LQ_TOKENS)), dim3(256), 0, st, a, R, DR);
+    // up to three workgroups a CU, which take several rounds of tokens where there are more
+    const int cols = a.heads * (R / LQ_COLS), tiles = ceil_div(tokens, LQ_TOKENS), rounds = ceil_div(tiles, std::max(1, 3 * LA_CUS / cols));
+    hipLaunchKernelGGL(latent_query_kernel, dim3((unsigned)cols + 1, (unsigned)ceil_div(tiles, rounds)), dim3(256), 0, st, a, R, DR, rounds);
     FISE_CHECK_LAUNCH("fise_latent_attention: queries");
     {
         const double pairs = (double)tokens * a.heads * a.n;

@@ -76,22 +76,31 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
                 for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
         }
     }
+    // through LDS, column by column of the product (its pieces of eight rows at piece ^ (column & 15)), so that sixteen lanes store 256 bytes side by side
     const int width = KD * 16;
+    la_barrier();
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int row = wr * 64 + i * 32 + q * 8 + hl * 4, col = wc * 64 + j * 32 + l32;
-                const uint2 v = make_uint2(f2bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f2bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
-                if (values) {
-                    if (w0 + col < n_w) *reinterpret_cast<uint2*>(a.v + ((size_t)b * n_w + w0 + col) * a.n_pad + key0 + row) = v;
-                } else if (w0 + row < n_w) {
-                    const int c = w0 + row, h = c / a.d;
-                    *reinterpret_cast<uint2*>(a.k + (((size_t)b * a.heads + h) * a.n_pad + key0 + col) * width + (c - h * a.d)) = v;
-                }
+                const int piece = wr * 8 + i * 4 + q, col = wc * 64 + j * 32 + l32;
+                *reinterpret_cast<uint2*>(lds + col * 256 + (piece ^ (col & 15)) * 16 + hl * 8) =
+                    make_uint2(f2bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f2bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
             }
+    la_barrier();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int col = i * 16 + (tid >> 4), row = (tid & 15) * 8;
+        const uint4 v = *reinterpret_cast<const uint4*>(lds + col * 256 + ((tid & 15) ^ (col & 15)) * 16);
+        if (values) {
+            if (w0 + col < n_w) *reinterpret_cast<uint4*>(a.v + ((size_t)b * n_w + w0 + col) * a.n_pad + key0 + row) = v;
+        } else if (w0 + row < n_w) {
+            const int c = w0 + row, h = c / a.d;
+            *reinterpret_cast<uint4*>(a.k + (((size_t)b * a.heads + h) * a.n_pad + key0 + col) * width + (c - h * a.d)) = v;
+        }
+    }
     if (!values) {
         // the shared key (and zeros) behind the channels of the heads that begin in this tile
         const int h0 = (w0 + a.d - 1) / a.d, h1 = min((w0 + 127) / a.d + 1, a.heads), tail = (width - a.d) / 8;
@@ -110,16 +119,19 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // from key rows in the order that makes a lane's eight scores of a 16-key step those of eight consecutive keys: they are the operand of the second product as
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 template <int KD, int DB>
-__global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArgs a, int nqt, FastDiv d_nqt) {
+__global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArgs a, int nqt, int heads_xcd) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int PIECES = 2 * KD, PITCH = PIECES * 16, KB = LX_BLOCK * PITCH, VB = DB * 32 * 128, STAGE = KB + VB, KL = KB / 4096, VL = VB / 4096;
     static_assert(KB % 4096 == 0 && KD % 2 == 0 && (PITCH % 256 || PIECES % 16 == 0), "whole loads of four waves");
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int w = blockIdx.x;                                                // an XCD gets whole heads, the tiles with most keys first
-    { const int chunk = gridDim.x >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
-    const int bh = (int)fdiv((unsigned)w, d_nqt), qt = nqt - 1 - (w - bh * nqt), b = (int)fdiv((unsigned)bh, a.d_heads), h = bh - b * a.heads;
+    // an XCD gets whole heads (where their number allows), the tiles of all of them with most keys first; where all are on the CUs at once, two a CU, the second half
+    // the other way round, so that the two that share a CU have as many keys as any other two
+    const int per_xcd = (gridDim.x & 7) == 0 && heads_xcd, i_xcd = per_xcd ? blockIdx.x >> 3 : blockIdx.x, heads_here = per_xcd ? heads_xcd : a.B * a.heads;
+    const int rank = i_xcd / heads_here, local = i_xcd - rank * heads_here, half = nqt >> 1;
+    const int bh = (per_xcd ? (blockIdx.x & 7) * heads_xcd : 0) + local, b = (int)fdiv((unsigned)bh, a.d_heads), h = bh - b * a.heads;
+    const int qt = gridDim.x <= 2 * LA_CUS && rank >= nqt - half ? rank - (nqt - half) : nqt - 1 - rank;
     const int len = __builtin_amdgcn_readfirstlane(la_len(a, b));
     const int m = qt * LX_QUERIES + wave * 32 + l32;
     const bool ok = m < a.M;
@@ -277,7 +289,7 @@ template <int TILE> static int launch_tile(const LatentArgs& a, hipStream_t st) 
     const int nqt = ceil_div(a.M, LX_QUERIES);
     {
         ProfileScope prof(PROF_ATTENTION, 2.0 * a.B * a.M * a.heads * (double)a.n * (a.d + a.dr + a.dv), 2.0 * a.B * a.n * a.heads * (double)(a.d + a.dr + a.dv), st);
-        hipLaunchKernelGGL((latent_expanded_kernel<KD, DB>), dim3((unsigned)(a.B * a.heads * nqt)), dim3(256), lds, st, a, nqt, fast_div(nqt));
+        hipLaunchKernelGGL((latent_expanded_kernel<KD, DB>), dim3((unsigned)(a.B * a.heads * nqt)), dim3(256), lds, st, a, nqt, a.B * a.heads % 8 ? 0 : a.B * a.heads / 8);
     }
     FISE_CHECK_LAUNCH("fise_latent_attention: expanded");
     return FISE_OK;
