@@ -44,7 +44,9 @@ inline int absorbed_tokens(const LatentShape& s) {
 
 // ---- expanded form.  Keys of a head are rows [W_uk c | k_pe | 0] of 16 KD channels, values are transposed, as everywhere in the library; both for whole tiles of
 // LX_KEYS keys.
-constexpr int LX_QUERIES = 128, LX_BLOCK = 64, LX_KEYS = 128;
+constexpr int LX_BLOCK = 64, LX_KEYS = 128;
+// 64 queries a workgroup, two waves sharing 32 of them, where 128 would leave CUs without one
+inline bool expanded_halves(int B, int heads, int M) { return (long long)B * heads * ((M + 127) / 128) < LA_CUS; }
 struct ExpandedTile { int KD, DB; };  // 16-channel steps of a key, 32-channel blocks of a value
 constexpr ExpandedTile kExpandedTiles[] = {{4, 2}, {6, 2}, {8, 2}, {8, 4}, {12, 2}, {12, 4}, {14, 5}};
 inline int expanded_tile(const LatentShape& s) {

@@ -118,50 +118,55 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // A wave has 32 queries of a head; keys come in blocks of 64 through LDS, loaded directly, a block ahead.  Scores are computed transposed (a lane keeps one query),
 // from key rows in the order that makes a lane's eight scores of a 16-key step those of eight consecutive keys: they are the operand of the second product as
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
-template <int KD, int DB>
-__global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArgs a, int nqt, int heads_xcd) {
+// A turn is: scores of the next block, with the exponentials of this block between the products; sums of this block, with the maximum of the next between them.  So
+// neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
+// NB: blocks of 32 keys a wave takes of the 64.  2: 128 queries a workgroup.  1: 64, two waves share 32 queries, each has half of the keys, and meet at the end; where there
+// are fewer workgroups of 128 than CUs.
+template <int KD, int DB, int NB>
+__global__ __launch_bounds__(256, KD <= 12 ? 2 : 1) void latent_expanded_kernel(const LatentArgs a, int nqt, int heads_xcd) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int PIECES = 2 * KD, PITCH = PIECES * 16, KB = LX_BLOCK * PITCH, VB = DB * 32 * 128, STAGE = KB + VB, KL = KB / 4096, VL = VB / 4096;
+    constexpr int PIECES = 2 * KD, PITCH = PIECES * 16, KB = LX_BLOCK * PITCH, VB = DB * 32 * 128, KL = KB / 4096, VL = VB / 4096, TQ = 64 * NB;
     static_assert(KB % 4096 == 0 && KD % 2 == 0 && (PITCH % 256 || PIECES % 16 == 0), "whole loads of four waves");
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];                  // keys, keys, values, values
+    const unsigned lds0 = (unsigned)(size_t)(FISE_AS3 unsigned char*)(FISE_AS3 void*)lds;
     const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = NB == 1 ? wave >> 1 : wave, kb0 = NB == 1 ? wave & 1 : 0;
     // an XCD gets whole heads (where their number allows), the tiles of all of them with most keys first; where all are on the CUs at once, two a CU, the second half
     // the other way round, so that the two that share a CU have as many keys as any other two
     const int per_xcd = (gridDim.x & 7) == 0 && heads_xcd, i_xcd = per_xcd ? blockIdx.x >> 3 : blockIdx.x, heads_here = per_xcd ? heads_xcd : a.B * a.heads;
     const int rank = i_xcd / heads_here, local = i_xcd - rank * heads_here, half = nqt >> 1;
-    const int bh = (per_xcd ? (blockIdx.x & 7) * heads_xcd : 0) + local, b = (int)fdiv((unsigned)bh, a.d_heads), h = bh - b * a.heads;
-    const int qt = gridDim.x <= 2 * LA_CUS && rank >= nqt - half ? rank - (nqt - half) : nqt - 1 - rank;
+    const int bh = __builtin_amdgcn_readfirstlane((per_xcd ? (blockIdx.x & 7) * heads_xcd : 0) + local), b = (int)fdiv((unsigned)bh, a.d_heads), h = bh - b * a.heads;
+    const int qt = __builtin_amdgcn_readfirstlane(gridDim.x <= 2 * LA_CUS && rank >= nqt - half ? rank - (nqt - half) : nqt - 1 - rank);
     const int len = __builtin_amdgcn_readfirstlane(la_len(a, b));
-    const int m = qt * LX_QUERIES + wave * 32 + l32;
+    const int m = qt * TQ + group * 32 + l32;
     const bool ok = m < a.M;
-    const int limit = la_limit(a, len, min(m, a.M - 1)), limit_first = la_limit(a, len, qt * LX_QUERIES), limit_last = la_limit(a, len, min(qt * LX_QUERIES + LX_QUERIES, a.M) - 1);
+    const int limit = la_limit(a, len, min(m, a.M - 1)), limit_first = la_limit(a, len, qt * TQ), limit_last = la_limit(a, len, min(qt * TQ + TQ, a.M) - 1);
     const int blocks = (limit_last + LX_BLOCK - 1) / LX_BLOCK;
 
     auto swizzle = [](int row) { return PITCH % 128 ? (row >> 2) & 3 : PITCH % 256 ? (row >> 1) & 7 : row & 15; };
-    unsigned k_off[KL], v_off[VL];
+    unsigned k_off[KL], v_off[2];
 #pragma unroll
     for (int j = 0; j < KL; ++j) {
         const int p = (wave * KL + j) * 64 + lane, row = p / PIECES, piece = (p - row * PIECES) ^ swizzle(row);
         const int key = (row & 32) + 16 * (row >> 4 & 1) + 8 * (row >> 2 & 1) + 4 * (row >> 3 & 1) + (row & 3);
         k_off[j] = (unsigned)(key * PITCH + piece * 16);
     }
-    const bf16_t* const k = a.k + (size_t)bh * a.n_pad * (KD * 16);
-    const bf16_t* const v = a.v + (size_t)bh * a.dv * a.n_pad;
+    const unsigned char* const k = (const unsigned char*)(a.k + (size_t)bh * a.n_pad * (KD * 16));
+    const unsigned char* const v = (const unsigned char*)(a.v + (size_t)bh * a.dv * a.n_pad);
+    const unsigned v_pitch = (unsigned)(a.n_pad * 2);
 #pragma unroll
-    for (int j = 0; j < VL; ++j) {
-        const int row = (wave * VL + j) * 8 + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
-        v_off[j] = row < a.dv ? (unsigned)((lane >> 3) * a.n_pad * 2 + piece * 16) : 0x40000000u;
-    }
-    auto load = [&](int blk) {
-        const auto kr = buf(k + (size_t)blk * LX_BLOCK * (KD * 16), KB);
-        unsigned char* const to = lds + (blk & 1) * STAGE;
+    for (int j = 0; j < 2; ++j) v_off[j] = (unsigned)(lane >> 3) * v_pitch + (unsigned)((lane & 7) ^ ((j * 8 + (lane >> 3)) >> 1)) * 16;
+    auto load_k = [&](int blk) {                                       // (behind the last block: nothing)
+        const u32x4_t from = la_buffer(k + (size_t)blk * KB, blk < blocks ? KB : 0);
 #pragma unroll
-        for (int j = 0; j < KL; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (FISE_AS3 void*)(to + (wave * KL + j) * 1024), 16, (int)k_off[j], 0, 0, 0);
+        for (int j = 0; j < KL; ++j) la_to_lds(from, k_off[j], lds0 + (blk & 1) * KB + (wave * KL + j) * 1024);
+    };
+    auto load_v = [&](int blk) {                                       // eight rows a load, each with a base of its own: rows of a long cache lie far apart
 #pragma unroll
-        for (int j = 0; j < VL; ++j) {                                 // eight rows a load, each with a base of its own: rows of a long cache lie far apart
-            const auto vr = buf(v + (size_t)(wave * VL + j) * 8 * a.n_pad + blk * LX_BLOCK, 0x40000000u);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (FISE_AS3 void*)(to + KB + (wave * VL + j) * 1024), 16, (int)v_off[j], 0, 0, 0);
+        for (int j = 0; j < VL; ++j) {
+            const int row = (wave * VL + j) * 8;                       // rows past dv (a multiple of 8): zeros
+            const u32x4_t from = la_buffer(v + (size_t)row * v_pitch + (size_t)blk * (LX_BLOCK * 2), blk < blocks && row < a.dv ? 0x7fffffff : 0);
+            la_to_lds(from, v_off[(wave * VL + j) & 1], lds0 + 2 * KB + (blk & 1) * VB + (wave * VL + j) * 1024);
         }
     };
     bf16x8_t qf[KD];
@@ -175,92 +180,162 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArg
             qf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
         }
     }
+    load_k(0);
+    load_k(1);
+    load_v(0);
     f32x16_t o[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
-    if (blocks > 0) load(0);
+    float m_run = -INFINITY, l_run = 0.f, alpha = 1.f, base = 0.f;
+
+    constexpr int NK = NB * KD, NV = 2 * NB * DB, AHEAD = 4, RING = AHEAD + 1, NE = 16 * NB;      // products of the scores, of the sums; reads ahead of them; scores a lane
+    bf16x8_t fr[RING];
+    // where a lane's operands lie: key row l32 of a 32-key block (swizzle(l32 + 32) is that of l32), value row l32
+    constexpr int KU = PITCH % 256 ? (PITCH % 128 ? 2 : 4) : 8;        // steps after which the places repeat
+    unsigned k_at[KU], v_at[4];
 #pragma unroll
-    for (int ks = 0; ks < KD; ++ks) asm volatile("" ::"v"(qf[ks]));
-    for (int blk = 0; blk < blocks; ++blk) {
+    for (int u = 0; u < KU; ++u) k_at[u] = (unsigned)(l32 * PITCH + ((u * 2 + hl) ^ swizzle(l32)) * 16);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v_at[u] = (unsigned)(l32 * 128 + ((u * 2 + hl) ^ ((l32 >> 1) & 7)) * 16);
+    auto read_k = [&](const unsigned char* tile, int p) {              // product p: step p % KD of block p / KD
+        const int ks = p % KD;
+        return *reinterpret_cast<const bf16x8_t*>(tile + k_at[ks % KU] + (ks / KU) * (KU * 32) + (kb0 + p / KD) * (32 * PITCH));
+    };
+    // product p: value rows of block p % DB, keys of step p / DB (16 of them)
+    auto read_v = [&](const unsigned char* tile, int p) {
+        const int u = p / DB;
+        return *reinterpret_cast<const bf16x8_t*>(tile + (NB == 1 ? v_at[u] ^ (unsigned)(kb0 * 64) : v_at[u]) + p % DB * 4096);
+    };
+    auto score = [&](f32x16_t (&s)[NB], int p) {
+        if (p % KD == 0) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[p / KD][e] = 0.f;
+        }
+        s[p / KD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[p % RING], qf[p % KD], s[p / KD], 0, 0, 0);
+    };
+    auto mask = [&](f32x16_t (&s)[NB], int blk) {
+        if (blk * LX_BLOCK + LX_BLOCK > limit_first) {                 // uniform: some query of the tile does not see all of the block
+#pragma unroll
+            for (int e = 0; e < NE; ++e)
+                if (blk * LX_BLOCK + (kb0 + e / 16) * 32 + (e >> 3 & 1) * 16 + hl * 8 + (e & 7) >= limit) s[e / 16][e % 16] = -INFINITY;
+        }
+    };
+    float top;
+    auto maximum = [&](const f32x16_t (&s)[NB], int step) {            // in NB * 4 steps
+        if (step == 0) top = s[0][0];
+#pragma unroll
+        for (int e = step * 4; e < step * 4 + 4; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+    };
+    // a query's reference moves only when a score lies 8 powers of two above it (see the absorbed form)
+    auto reference = [&] {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        const float mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * a.scale_log2e;
+        const float to = mx > m_run + 8.f ? mx : m_run;
+        base = to == -INFINITY ? 0.f : to;
+        alpha = __builtin_amdgcn_exp2f(m_run - base);
+        m_run = to;
+        l_run *= alpha;
+    };
+    f32x16_t sa[NB], sb[NB];
+    auto turn = [&](f32x16_t (&s)[NB], f32x16_t (&next)[NB], int blk) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (blk + 1 < blocks) load(blk + 1);
-        unsigned char* const stage = lds + (blk & 1) * STAGE;
-        const int k0 = blk * LX_BLOCK;
-        f32x16_t s[2];
+        load_k(blk + 2);
+        load_v(blk + 1);
+        unsigned char* const values = lds + 2 * KB + (blk & 1) * VB;
+        const unsigned char* const keys = lds + ((blk + 1) & 1) * KB;
+        if (a.causal && blk * LX_BLOCK + LX_BLOCK > limit_first) {     // uniform: what a key holds that a query does not see must not matter
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KD; ++ks) {
-                const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(stage + (kb * 32 + l32) * PITCH + ((ks * 2 + hl) ^ swizzle(l32)) * 16);
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[kb], 0, 0, 0);
+            for (int j = 0; j < DB; ++j) {
+                uint4* const at = reinterpret_cast<uint4*>(values + (j * 256 + tid) * 16);
+                *at = la_finite(*at);
             }
+            la_barrier();
         }
-        const bool partial = k0 + LX_BLOCK > limit_first;
-        if (partial) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (k0 + kb * 32 + (e >> 3) * 16 + hl * 8 + (e & 7) >= limit) s[kb][e] = -INFINITY;
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-        {
-            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-            mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-        }
-        mx = fmaxf(m_run, mx * a.scale_log2e);
-        const float base = mx == -INFINITY ? 0.f : mx;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - base);
-        float sum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][e], a.scale_log2e, -base));
-                s[kb][e] = p;
-                sum += p;
-            }
-        l_run = fmaf(l_run, alpha, sum);
-        m_run = mx;
         if (__any(alpha != 1.0f)) {
 #pragma unroll
             for (int i = 0; i < DB; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
         }
-        if (a.causal && partial) {                                     // uniform: what a key holds that a query does not see must not matter
-            la_barrier();
+        u32x4_t p[2 * NB];                                             // probabilities, the operands of the sums
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < DB; ++j) {
-                uint4* const at = reinterpret_cast<uint4*>(stage + KB + (j * 256 + tid) * 16);
-                *at = la_finite(*at);
+        for (int q = 0; q < AHEAD; ++q) fr[q] = read_k(keys, q);
+#pragma unroll
+        for (int q = 0; q < NK; ++q) {
+            if (q + AHEAD < NK) fr[(q + AHEAD) % RING] = read_k(keys, q + AHEAD);
+            else fr[(q + AHEAD) % RING] = read_v(values, q + AHEAD - NK);
+            __builtin_amdgcn_sched_barrier(0);
+            score(next, q);
+#pragma unroll
+            for (int e = NE * q / NK; e < NE * (q + 1) / NK; ++e) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale_log2e, -base));
+                s[e / 16][e % 16] = x;
+                l_run += x;
+                if (e & 1) p[e / 8][e / 2 % 4] = f2bf2(s[e / 16][e % 16 - 1], x);
             }
-            la_barrier();
+            __builtin_amdgcn_sched_barrier(0);
         }
+        mask(next, blk + 1);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {                                  // steps of 16 keys
-            const int kb = u >> 1, e0 = (u & 1) * 8;
-            uint4 pw = make_uint4(f2bf2(s[kb][e0], s[kb][e0 + 1]), f2bf2(s[kb][e0 + 2], s[kb][e0 + 3]), f2bf2(s[kb][e0 + 4], s[kb][e0 + 5]), f2bf2(s[kb][e0 + 6], s[kb][e0 + 7]));
-            const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(&pw);
+        for (int q = 0; q < NV; ++q) {
+            if (q + AHEAD < NV) fr[(NK + q + AHEAD) % RING] = read_v(values, q + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+            const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(&p[q / DB]);
+            o[q % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[(NK + q) % RING], pf, o[q % DB], 0, 0, 0);
+            // the score products' results are there once a few of these have gone out
 #pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(stage + KB + (i * 32 + l32) * 128 + ((u * 2 + hl) ^ ((l32 >> 1) & 7)) * 16);
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
-            }
+            for (int st = 0; st < 4 * NB; ++st)
+                if (st * (NV - 1) / (4 * NB) + 1 == q) maximum(next, st);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        reference();
+    };
+    if (blocks > 0) {
+#pragma unroll
+        for (int ks = 0; ks < KD; ++ks) asm volatile("" ::"v"(qf[ks]));
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < NK; ++q) { fr[q % RING] = read_k(lds, q); score(sa, q); }
+        mask(sa, 0);
+#pragma unroll
+        for (int st = 0; st < 4 * NB; ++st) maximum(sa, st);
+        reference();
+        for (int blk = 0;;) {
+            turn(sa, sb, blk);
+            if (++blk >= blocks) break;
+            turn(sb, sa, blk);
+            if (++blk >= blocks) break;
         }
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     {
         const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
         l_run = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (NB == 1) {
+        // the second half of the keys to the first's wave: [pair][register][lane]
+        __syncthreads();
+        float* const ex = reinterpret_cast<float*>(lds) + group * ((DB * 16 + 2) * 64) + lane;
+        if (kb0) {
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ex[(i * 16 + e) * 64] = o[i][e];
+            ex[DB * 16 * 64] = m_run;
+            ex[(DB * 16 + 1) * 64] = l_run;
+        }
+        __syncthreads();
+        if (kb0) return;
+        const float mo = ex[DB * 16 * 64], lo = ex[(DB * 16 + 1) * 64], mx = fmaxf(m_run, mo), ref = mx == -INFINITY ? 0.f : mx;
+        const float f = __builtin_amdgcn_exp2f(m_run - ref), fo = __builtin_amdgcn_exp2f(mo - ref);
+        l_run = l_run * f + lo * fo;
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * f + ex[(i * 16 + e) * 64] * fo;
     }
     if (!ok) return;
     const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;               // no key seen: zeros
@@ -275,10 +350,21 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const LatentArg
 #endif
 }
 
-template <int TILE> static int launch_tile(const LatentArgs& a, hipStream_t st) {
-    constexpr int KD = kExpandedTiles[TILE].KD, DB = kExpandedTiles[TILE].DB, lds = 2 * (LX_BLOCK * KD * 32 + DB * 32 * 128);
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_expanded_kernel<KD, DB>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+template <int KD, int DB, int NB> static int launch_attention(const LatentArgs& a, hipStream_t st) {
+    constexpr int stages = 2 * (LX_BLOCK * KD * 32 + DB * 32 * 128), halves = NB == 1 ? 2 * (DB * 16 + 2) * 256 : 0, lds = stages > halves ? stages : halves;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_expanded_kernel<KD, DB, NB>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_latent_attention: cannot raise the dynamic LDS limit");
+    const int nqt = ceil_div(a.M, 64 * NB);
+    {
+        ProfileScope prof(PROF_ATTENTION, 2.0 * a.B * a.M * a.heads * (double)a.n * (a.d + a.dr + a.dv), 2.0 * a.B * a.n * a.heads * (double)(a.d + a.dr + a.dv), st);
+        hipLaunchKernelGGL((latent_expanded_kernel<KD, DB, NB>), dim3((unsigned)(a.B * a.heads * nqt)), dim3(256), lds, st, a, nqt, a.B * a.heads % 8 ? 0 : a.B * a.heads / 8);
+    }
+    FISE_CHECK_LAUNCH("fise_latent_attention: expanded");
+    return FISE_OK;
+}
+
+template <int TILE> static int launch_tile(const LatentArgs& a, hipStream_t st) {
+    constexpr int KD = kExpandedTiles[TILE].KD, DB = kExpandedTiles[TILE].DB;
     const int key_tiles = (int)(a.n_pad / LX_KEYS), k_tiles = ceil_div(a.heads * a.d, 128), v_tiles = ceil_div(a.heads * a.dv, 128);
     if (key_tiles) {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * a.B * a.n * a.heads * (double)a.r * (a.d + a.dv), 2.0 * a.B * a.n * (a.r + a.heads * (double)(a.d + a.dv)), st);
@@ -286,13 +372,7 @@ template <int TILE> static int launch_tile(const LatentArgs& a, hipStream_t st) 
                            fast_div(key_tiles), fast_div(k_tiles + v_tiles));
     }
     FISE_CHECK_LAUNCH("fise_latent_attention: keys and values");
-    const int nqt = ceil_div(a.M, LX_QUERIES);
-    {
-        ProfileScope prof(PROF_ATTENTION, 2.0 * a.B * a.M * a.heads * (double)a.n * (a.d + a.dr + a.dv), 2.0 * a.B * a.n * a.heads * (double)(a.d + a.dr + a.dv), st);
-        hipLaunchKernelGGL((latent_expanded_kernel<KD, DB>), dim3((unsigned)(a.B * a.heads * nqt)), dim3(256), lds, st, a, nqt, a.B * a.heads % 8 ? 0 : a.B * a.heads / 8);
-    }
-    FISE_CHECK_LAUNCH("fise_latent_attention: expanded");
-    return FISE_OK;
+    return expanded_halves(a.B, a.heads, a.M) ? launch_attention<KD, DB, 1>(a, st) : launch_attention<KD, DB, 2>(a, st);
 }
 
 int launch_expanded(const LatentArgs& a, int tile, hipStream_t st) {
