@@ -10,10 +10,12 @@ struct LatentArgs {
     const bf16_t* q; const bf16_t* cache; const int* kv_len; const bf16_t* w_uk; const bf16_t* w_uv; bf16_t* out;
     int B, M, n, heads, d, dr, dv, r, causal; long long cache_tokens;
     float scale_log2e;
+    int tiles, groups, workgroups;                       // tiles of rows or queries; of all elements (and heads); workgroups that share the line of key blocks
+    int* table; float2* ml; float* part;                 // the line; of every part: reference and sum of a row, sums
     // absorbed
-    int tiles, groups, workgroups, tokens;               // tiles of rows, B * tiles, workgroups of the second launch, tokens of a workgroup of the third
-    int* table; bf16_t* qa; float2* ml; float* part;
+    int tokens; bf16_t* qa;                              // tokens of a workgroup of the third launch; queries behind W_uk
     // expanded
+    int whole;                                           // a workgroup for every tile
     long long n_pad; bf16_t* k; bf16_t* v;               // keys of a head [B, heads, n_pad, 16 KD], values [B, heads * dv, n_pad]
     FastDiv d_heads, d_tiles, d_M;
 };
@@ -21,6 +23,35 @@ struct LatentArgs {
 // Keys of a batch element, and how many of them query m sees: all, or (causal) the query is the key at len - M + m and sees those up to itself.
 __device__ __forceinline__ int la_len(const LatentArgs& a, int b) { return a.kv_len ? min(max(a.kv_len[b], 0), a.n) : a.n; }
 __device__ __forceinline__ int la_limit(const LatentArgs& a, int len, int m) { return a.causal ? min(max(len - a.M + m + 1, 0), len) : len; }
+
+// The line of key blocks: table[g] = blocks of all groups before g, by a workgroup of 256 lanes.  Workgroup w of G has blocks w T / G .. (w + 1) T / G of the T.
+template <typename F> __device__ __forceinline__ void la_line(int* table, int groups, int* lds, F&& blocks) {
+    const int tid = threadIdx.x, each = (groups + 255) / 256, g0 = min(tid * each, groups), g1 = min(g0 + each, groups);
+    int s = 0;
+    for (int g = g0; g < g1; ++g) s += blocks(g);
+    lds[tid] = s;
+    __syncthreads();
+    for (int o = 1; o < 256; o <<= 1) {
+        const int v = tid >= o ? lds[tid - o] : 0;
+        __syncthreads();
+        lds[tid] += v;
+        __syncthreads();
+    }
+    int at = lds[tid] - s;
+    for (int g = g0; g < g1; ++g) { table[g] = at; at += blocks(g); }
+    if (tid == 255) table[groups] = lds[255];
+}
+// the workgroup that has block x: the largest w with w total / workgroups <= x
+__device__ __forceinline__ int la_owner(int x, int workgroups, int total) { return (int)((((long long)x + 1) * workgroups - 1) / total); }
+// last group that starts at or before block x
+__device__ __forceinline__ int la_group(const int* table, int groups, int x) {
+    int lo = 0;
+    for (int hi = groups - 1; lo < hi;) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__builtin_amdgcn_readfirstlane(table[mid]) <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
 
 __device__ __forceinline__ void la_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 

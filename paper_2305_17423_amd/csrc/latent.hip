@@ -23,26 +23,11 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
     if (blockIdx.x == gridDim.x - 1) {
         if (blockIdx.y) return;
-        int* const sums = reinterpret_cast<int*>(lds);
-        const int each = (a.groups + 255) / 256, g0 = min(tid * each, a.groups), g1 = min(g0 + each, a.groups);
-        auto blocks = [&](int g) {
+        la_line(a.table, a.groups, reinterpret_cast<int*>(lds), [&](int g) {
             const int b = (int)fdiv((unsigned)g, a.d_tiles), t = g - b * a.tiles;
             const int last = min(a.M * a.heads, (t + 1) * LA_ROWS) - 1;
             return (la_limit(a, la_len(a, b), (int)fdiv((unsigned)last, a.d_heads)) + LA_KEYS - 1) / LA_KEYS;
-        };
-        int s = 0;
-        for (int g = g0; g < g1; ++g) s += blocks(g);
-        sums[tid] = s;
-        __syncthreads();
-        for (int o = 1; o < 256; o <<= 1) {
-            const int v = tid >= o ? sums[tid - o] : 0;
-            __syncthreads();
-            sums[tid] += v;
-            __syncthreads();
-        }
-        int at = sums[tid] - s;
-        for (int g = g0; g < g1; ++g) { a.table[g] = at; at += blocks(g); }
-        if (tid == 255) a.table[a.groups] = sums[255];
+        });
         return;
     }
     const int cols = R / LQ_COLS, h = blockIdx.x / cols, c0 = (blockIdx.x - h * cols) * LQ_COLS, tokens = a.B * a.M, width = R + DR;
@@ -141,12 +126,7 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
     if (w >= workgroups) return;
     { const int chunk = workgroups >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
     const int line0 = uniform((int)((long long)w * total / workgroups)), line1 = uniform((int)((long long)(w + 1) * total / workgroups));
-    int g = 0;
-    for (int lo = 0, hi = a.groups - 1;;) {                            // last group that starts at or before line0
-        if (lo >= hi) { g = lo; break; }
-        const int mid = (lo + hi + 1) >> 1;
-        if (uniform(a.table[mid]) <= line0) lo = mid; else hi = mid - 1;
-    }
+    int g = la_group(a.table, a.groups, line0);
     const int row_bytes = (a.r + a.dr) * 2, rows = a.M * a.heads;
 
     // ---- places that depend on the lane only: loads (offset of a piece in a block of the cache; pieces that do not exist past its end), operands
@@ -360,15 +340,14 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
     bf16x8_t wf[R / 32];
     if (wave < vt) weights(wf, wave);
 
-    // ---- what the parts of each token weigh: 32 lanes a token go over its parts (workgroups that had a part of its group's blocks; block x belongs to the largest w with
-    // w total / workgroups <= x), keeping a maximum and a sum, and meet.  l == 0: no key was seen, zeros.
+    // ---- what the parts of each token weigh: 32 lanes a token go over its parts (workgroups that had some of its group's blocks), keeping a maximum
+    // and a sum, and meet.  l == 0: no key was seen, zeros.
     if (tid < a.tokens * 32) {
         const int i = tid >> 5, t = t0 + i;
         if (i < tokens) {
             const int b = (int)fdiv((unsigned)t, a.d_M), row = (t - b * a.M) * a.heads + h, tile = row / LA_ROWS, g = b * a.tiles + tile;
             const int g0 = a.table[g], g1 = a.table[g + 1];
-            auto owner = [&](int x) { return (int)((((long long)x + 1) * workgroups - 1) / total); };
-            const int w0 = g1 > g0 ? owner(g0) : 0, n = g1 > g0 ? owner(g1 - 1) - w0 + 1 : 0;
+            const int w0 = g1 > g0 ? la_owner(g0, workgroups, total) : 0, n = g1 > g0 ? la_owner(g1 - 1, workgroups, total) - w0 + 1 : 0;
             const size_t at = ((size_t)g + w0) * LA_ROWS + (row - tile * LA_ROWS);
             float top = -INFINITY, l = 0.f;
             for (int p = tid & 31; p < n; p += 32) {
@@ -481,7 +460,9 @@ static int latent_check(const char* fn, const fise_latent_attention_args* g, Lat
     const long long rows = (long long)g->M * g->heads, tiles = (rows + LA_ROWS - 1) / LA_ROWS, blocks = ((long long)g->n_keys + LA_KEYS - 1) / LA_KEYS;
     if (g->n_keys > 1 << 26 || rows >= 1ll << 30 || (long long)g->B * tiles >= 1ll << 30 || (long long)g->B * tiles * (blocks + 1) >= 1ll << 31 || (long long)g->B * g->M > 1 << 20 || g->heads > 65535)
         return fail(FISE_ERR_SHAPE, "%s: B%d M%d heads%d keys%d: too many rows or key blocks", fn, g->B, g->M, g->heads, g->n_keys);
-    if ((long long)g->B * g->heads * (std::max(g->M, g->n_keys) / 64 + 2) * 10 >= 1ll << 31) return fail(FISE_ERR_SHAPE, "%s: B%d heads%d M%d keys%d: too many tiles", fn, g->B, g->heads, g->M, g->n_keys);
+    if ((long long)g->B * g->heads * (std::max(g->M, g->n_keys) / 64 + 2) * 10 >= 1ll << 31 ||
+        (long long)g->B * g->heads * (g->M / LX_QUERIES + 1) * ((long long)g->n_keys / LX_BLOCK + 2) >= 1ll << 31)
+        return fail(FISE_ERR_SHAPE, "%s: B%d heads%d M%d keys%d: too many tiles", fn, g->B, g->heads, g->M, g->n_keys);
     return FISE_OK;
 }
 
@@ -518,6 +499,8 @@ extern "C" int fise_latent_attention(const fise_latent_attention_args* g, void* 
     if (expanded) {
         const ExpandedLayout l = expanded_layout(s);
         a.n_pad = l.n_pad; a.k = (bf16_t*)(ws + l.k); a.v = (bf16_t*)(ws + l.v);
+        a.tiles = expanded_tiles(s); a.groups = (int)expanded_groups(s); a.whole = expanded_whole(s); a.workgroups = expanded_workgroups(s); a.d_tiles = fast_div(a.tiles);
+        a.table = (int*)(ws + l.table); a.ml = (float2*)(ws + l.ml); a.part = (float*)(ws + l.part);
         return launch_expanded(a, expanded_tile(s), st);
     }
     const AbsorbedLayout l = absorbed_layout(s);

@@ -44,23 +44,38 @@ inline int absorbed_tokens(const LatentShape& s) {
 
 // ---- expanded form.  Keys of a head are rows [W_uk c | k_pe | 0] of 16 KD channels, values are transposed, as everywhere in the library; both for whole tiles of
 // LX_KEYS keys.
-constexpr int LX_BLOCK = 64, LX_KEYS = 128;
-// 64 queries a workgroup, two waves sharing 32 of them, where 128 would leave CUs without one
-inline bool expanded_halves(int B, int heads, int M) { return (long long)B * heads * ((M + 127) / 128) < LA_CUS; }
+constexpr int LX_QUERIES = 128, LX_BLOCK = 64, LX_KEYS = 128;
 struct ExpandedTile { int KD, DB; };  // 16-channel steps of a key, 32-channel blocks of a value
 constexpr ExpandedTile kExpandedTiles[] = {{4, 2}, {6, 2}, {8, 2}, {8, 4}, {12, 2}, {12, 4}, {14, 5}};
 inline int expanded_tile(const LatentShape& s) {
     for (int i = 0;; ++i)
         if (16 * kExpandedTiles[i].KD >= s.d + s.dr && 32 * kExpandedTiles[i].DB >= s.dv) return i;      // (the last one holds the largest: 160 + 64, 160)
 }
-struct ExpandedLayout { long long n_pad; size_t k, v, total; };
+inline int expanded_tiles(const LatentShape& s) { return (s.M + LX_QUERIES - 1) / LX_QUERIES; }
+// Tiles of queries (of an element and head) enough for all workgroups that the CUs hold at once (two each; one of the widest heads): one for each tile.  Fewer: the blocks of
+// keys stand in one line too, and those workgroups share it evenly, three blocks each at least; a cut tile costs its parts written and read again.  us, tiles and line:
+// 512 causal tiles of 2 - 64 blocks 134, 154; 96 tiles of 64 blocks 80, 53; 32 of 64 blocks 108, 78 (the whole call).
+constexpr int expanded_per_cu(int KD) { return KD <= 12 ? 2 : 1; }
+inline long long expanded_groups(const LatentShape& s) { return (long long)s.B * s.heads * expanded_tiles(s); }
+inline bool expanded_whole(const LatentShape& s) { return expanded_groups(s) >= expanded_per_cu(kExpandedTiles[expanded_tile(s)].KD) * LA_CUS; }
+inline int expanded_workgroups(const LatentShape& s) {
+    if (expanded_whole(s)) return (int)expanded_groups(s);
+    const long long blocks = expanded_groups(s) * ((s.n + LX_BLOCK - 1) / LX_BLOCK);
+    return (int)std::max(1ll, std::min<long long>(expanded_per_cu(kExpandedTiles[expanded_tile(s)].KD) * LA_CUS, (blocks + 2) / 3));
+}
+struct ExpandedLayout { long long n_pad; size_t table, k, v, ml, part, total; };
 inline ExpandedLayout expanded_layout(const LatentShape& s) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    const ExpandedTile t = kExpandedTiles[expanded_tile(s)];
+    const size_t groups = (size_t)expanded_groups(s), slots = expanded_whole(s) ? 0 : groups + expanded_workgroups(s);
     ExpandedLayout l;
     l.n_pad = ((long long)s.n + LX_KEYS - 1) / LX_KEYS * LX_KEYS;
-    l.k = 0;
-    l.v = l.k + up((size_t)s.B * s.heads * l.n_pad * kExpandedTiles[expanded_tile(s)].KD * 32);
-    l.total = l.v + up((size_t)s.B * s.heads * s.dv * l.n_pad * 2) + 256;
+    l.table = 0;
+    l.k = l.table + up((groups + 1) * 4);
+    l.v = l.k + up((size_t)s.B * s.heads * l.n_pad * t.KD * 32);
+    l.ml = l.v + up((size_t)s.B * s.heads * s.dv * l.n_pad * 2);
+    l.part = l.ml + up(slots * LX_QUERIES * 8);
+    l.total = l.part + up(slots * LX_QUERIES * t.DB * 128);
     return l;
 }
 

@@ -10,15 +10,29 @@ namespace fise {
 // loaded directly to LDS, a step ahead.  Rows of 128 bytes, sixteen-byte pieces at piece ^ (row / 2 & 7): sixteen rows read at
 // once lie in different banks.  The first index of the product is the one that runs along the
 // result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.
+// Group g of the line: (element, head), and of its tiles of queries in turn the last and the first that are left, which together have as many keys as any other two
+// where rows are causal.
+struct LxGroup { int b, h, tile; };
+__device__ __forceinline__ LxGroup lx_group(const LatentArgs& a, int g) {
+    const int bh = (int)fdiv((unsigned)g, a.d_tiles), i = g - bh * a.tiles, b = (int)fdiv((unsigned)bh, a.d_heads);
+    return {b, bh - b * a.heads, i & 1 ? i >> 1 : a.tiles - 1 - (i >> 1)};
+}
 constexpr int LE_STEP = 64, LE_STAGE = 2 * 128 * LE_STEP * 2;
 __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs a, int KD, int key_tiles, int k_tiles, int v_tiles, FastDiv d_key_tiles, FastDiv d_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave >> 1, wc = wave & 1;
-    // weight tile slowest within an element: a key tile's workgroups follow one another in an XCD
     int w = blockIdx.x;
-    { const int chunk = gridDim.x >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
+    if (w == (int)gridDim.x - 1) {                                     // the line of key blocks
+        la_line(a.table, a.groups, reinterpret_cast<int*>(lds), [&](int g) {
+            const LxGroup p = lx_group(a, g);
+            return (la_limit(a, la_len(a, p.b), min(a.M, (p.tile + 1) * LX_QUERIES) - 1) + LX_BLOCK - 1) / LX_BLOCK;
+        });
+        return;
+    }
+    // weight tile slowest within an element: a key tile's workgroups follow one another in an XCD
+    { const int chunk = (gridDim.x - 1) >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
     const int kt_b = (int)fdiv((unsigned)w, d_tiles), wt = w - kt_b * (k_tiles + v_tiles), b = (int)fdiv((unsigned)kt_b, d_key_tiles), kt = kt_b - b * key_tiles;
     const int len = __builtin_amdgcn_readfirstlane(la_len(a, b)), key0 = kt * LX_KEYS;
     if (key0 >= len) return;                                           // nobody reads it
@@ -120,29 +134,48 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 // A turn is: scores of the next block, with the exponentials of this block between the products; sums of this block, with the maximum of the next between them.  So
 // neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
-// NB: blocks of 32 keys a wave takes of the 64.  2: 128 queries a workgroup.  1: 64, two waves share 32 queries, each has half of the keys, and meet at the end; where there
-// are fewer workgroups of 128 than CUs.
-template <int KD, int DB, int NB>
-__global__ __launch_bounds__(256, KD <= 12 ? 2 : 1) void latent_expanded_kernel(const LatentArgs a, int nqt, int heads_xcd) {
+// Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
+[[maybe_unused]] constexpr int LX_AHEAD = 4;
+template <int KD, int DB>
+__global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kernel(const LatentArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int PIECES = 2 * KD, PITCH = PIECES * 16, KB = LX_BLOCK * PITCH, VB = DB * 32 * 128, KL = KB / 4096, VL = VB / 4096, TQ = 64 * NB;
+    constexpr int PIECES = 2 * KD, PITCH = PIECES * 16, KB = LX_BLOCK * PITCH, VB = DB * 32 * 128, KL = KB / 4096, VL = VB / 4096;
     static_assert(KB % 4096 == 0 && KD % 2 == 0 && (PITCH % 256 || PIECES % 16 == 0), "whole loads of four waves");
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];                  // keys, keys, values, values
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     const unsigned lds0 = (unsigned)(size_t)(FISE_AS3 unsigned char*)(FISE_AS3 void*)lds;
-    const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = NB == 1 ? wave >> 1 : wave, kb0 = NB == 1 ? wave & 1 : 0;
-    // an XCD gets whole heads (where their number allows), the tiles of all of them with most keys first; where all are on the CUs at once, two a CU, the second half
-    // the other way round, so that the two that share a CU have as many keys as any other two
-    const int per_xcd = (gridDim.x & 7) == 0 && heads_xcd, i_xcd = per_xcd ? blockIdx.x >> 3 : blockIdx.x, heads_here = per_xcd ? heads_xcd : a.B * a.heads;
-    const int rank = i_xcd / heads_here, local = i_xcd - rank * heads_here, half = nqt >> 1;
-    const int bh = __builtin_amdgcn_readfirstlane((per_xcd ? (blockIdx.x & 7) * heads_xcd : 0) + local), b = (int)fdiv((unsigned)bh, a.d_heads), h = bh - b * a.heads;
-    const int qt = __builtin_amdgcn_readfirstlane(gridDim.x <= 2 * LA_CUS && rank >= nqt - half ? rank - (nqt - half) : nqt - 1 - rank);
-    const int len = __builtin_amdgcn_readfirstlane(la_len(a, b));
-    const int m = qt * TQ + group * 32 + l32;
-    const bool ok = m < a.M;
-    const int limit = la_limit(a, len, min(m, a.M - 1)), limit_first = la_limit(a, len, qt * TQ), limit_last = la_limit(a, len, min(qt * TQ + TQ, a.M) - 1);
-    const int blocks = (limit_last + LX_BLOCK - 1) / LX_BLOCK;
+    const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31, wave = uniform(tid >> 6);
+    // consecutive workgroups go to the eight XCDs in turn: give each XCD one run of the line, whole heads where their number allows
+    int w = blockIdx.x, g, line0, line1;
+    if (a.whole) {
+        // of an XCD's heads the tiles with most keys first; where all are on the CUs at once (workgroups i and i + 32 of an XCD on the same one) the second half the other
+        // way round, so that those two have as many keys as any other two
+        const int heads_all = a.B * a.heads, split = (heads_all & 7) == 0, heads_here = split ? heads_all >> 3 : heads_all, i = split ? w >> 3 : w;
+        const int rank = i / heads_here, bh = (split ? (w & 7) * heads_here : 0) + i - rank * heads_here, half = a.tiles >> 1;
+        const int back = a.tiles - 1 - rank;                           // the tile, last first; the second half of them in either order
+        const int tile = rank >= a.tiles - half && a.groups <= expanded_per_cu(KD) * LA_CUS ? rank - (a.tiles - half) : back;
+        g = bh * a.tiles + (tile >= half ? 2 * (a.tiles - 1 - tile) : 2 * tile + 1);
+        g = uniform(g);
+        line0 = uniform(a.table[g]); line1 = uniform(a.table[g + 1]);
+        if (line0 == line1) {                                          // no query of the tile sees a key: zeros
+            const LxGroup p = lx_group(a, g);
+            const int quads = a.dv / 4;
+            for (int e = tid; e < LX_QUERIES * quads; e += 256) {
+                const int m = p.tile * LX_QUERIES + e / quads;
+                if (m < a.M) *reinterpret_cast<uint2*>(a.out + (((size_t)p.b * a.M + m) * a.heads + p.h) * a.dv + e % quads * 4) = make_uint2(0, 0);
+            }
+            return;
+        }
+    } else {
+        const int total = uniform(a.table[a.groups]), workgroups = min(a.workgroups, total);
+        if (w >= workgroups) return;
+        const int chunk = workgroups >> 3;
+        if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3);
+        line0 = uniform((int)((long long)w * total / workgroups)); line1 = uniform((int)((long long)(w + 1) * total / workgroups));
+        g = la_group(a.table, a.groups, line0);
+    }
 
+    // ---- places that depend on the lane only
     auto swizzle = [](int row) { return PITCH % 128 ? (row >> 2) & 3 : PITCH % 256 ? (row >> 1) & 7 : row & 15; };
     unsigned k_off[KL], v_off[2];
 #pragma unroll
@@ -151,228 +184,274 @@ __global__ __launch_bounds__(256, KD <= 12 ? 2 : 1) void latent_expanded_kernel(
         const int key = (row & 32) + 16 * (row >> 4 & 1) + 8 * (row >> 2 & 1) + 4 * (row >> 3 & 1) + (row & 3);
         k_off[j] = (unsigned)(key * PITCH + piece * 16);
     }
-    const unsigned char* const k = (const unsigned char*)(a.k + (size_t)bh * a.n_pad * (KD * 16));
-    const unsigned char* const v = (const unsigned char*)(a.v + (size_t)bh * a.dv * a.n_pad);
     const unsigned v_pitch = (unsigned)(a.n_pad * 2);
 #pragma unroll
     for (int j = 0; j < 2; ++j) v_off[j] = (unsigned)(lane >> 3) * v_pitch + (unsigned)((lane & 7) ^ ((j * 8 + (lane >> 3)) >> 1)) * 16;
-    auto load_k = [&](int blk) {                                       // (behind the last block: nothing)
-        const u32x4_t from = la_buffer(k + (size_t)blk * KB, blk < blocks ? KB : 0);
-#pragma unroll
-        for (int j = 0; j < KL; ++j) la_to_lds(from, k_off[j], lds0 + (blk & 1) * KB + (wave * KL + j) * 1024);
-    };
-    auto load_v = [&](int blk) {                                       // eight rows a load, each with a base of its own: rows of a long cache lie far apart
-#pragma unroll
-        for (int j = 0; j < VL; ++j) {
-            const int row = (wave * VL + j) * 8;                       // rows past dv (a multiple of 8): zeros
-            const u32x4_t from = la_buffer(v + (size_t)row * v_pitch + (size_t)blk * (LX_BLOCK * 2), blk < blocks && row < a.dv ? 0x7fffffff : 0);
-            la_to_lds(from, v_off[(wave * VL + j) & 1], lds0 + 2 * KB + (blk & 1) * VB + (wave * VL + j) * 1024);
-        }
-    };
-    bf16x8_t qf[KD];
-    {
-        const bf16_t* const q = a.q + (((size_t)b * a.M + min(m, a.M - 1)) * a.heads + h) * (a.d + a.dr);
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            const int c = ks * 16 + hl * 8;
-            if (c < a.d + a.dr) x = *reinterpret_cast<const uint4*>(q + c);
-            qf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
-        }
-    }
-    load_k(0);
-    load_k(1);
-    load_v(0);
-    f32x16_t o[DB];
-#pragma unroll
-    for (int i = 0; i < DB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f, alpha = 1.f, base = 0.f;
-
-    constexpr int NK = NB * KD, NV = 2 * NB * DB, AHEAD = 4, RING = AHEAD + 1, NE = 16 * NB;      // products of the scores, of the sums; reads ahead of them; scores a lane
-    bf16x8_t fr[RING];
-    // where a lane's operands lie: key row l32 of a 32-key block (swizzle(l32 + 32) is that of l32), value row l32
+    // operands: key row l32 of a 32-key block (swizzle(l32 + 32) is that of l32), value row l32
     constexpr int KU = PITCH % 256 ? (PITCH % 128 ? 2 : 4) : 8;        // steps after which the places repeat
     unsigned k_at[KU], v_at[4];
 #pragma unroll
     for (int u = 0; u < KU; ++u) k_at[u] = (unsigned)(l32 * PITCH + ((u * 2 + hl) ^ swizzle(l32)) * 16);
 #pragma unroll
     for (int u = 0; u < 4; ++u) v_at[u] = (unsigned)(l32 * 128 + ((u * 2 + hl) ^ ((l32 >> 1) & 7)) * 16);
-    auto read_k = [&](const unsigned char* tile, int p) {              // product p: step p % KD of block p / KD
-        const int ks = p % KD;
-        return *reinterpret_cast<const bf16x8_t*>(tile + k_at[ks % KU] + (ks / KU) * (KU * 32) + (kb0 + p / KD) * (32 * PITCH));
-    };
-    // product p: value rows of block p % DB, keys of step p / DB (16 of them)
-    auto read_v = [&](const unsigned char* tile, int p) {
-        const int u = p / DB;
-        return *reinterpret_cast<const bf16x8_t*>(tile + (NB == 1 ? v_at[u] ^ (unsigned)(kb0 * 64) : v_at[u]) + p % DB * 4096);
-    };
-    auto score = [&](f32x16_t (&s)[NB], int p) {
-        if (p % KD == 0) {
+
+    constexpr int NK = 2 * KD, NV = 4 * DB, AHEAD = LX_AHEAD, RING = AHEAD + 1, NE = 32;      // products of the scores, of the sums; reads ahead of them; scores a lane
+    for (int at = line0; at < line1; ++g) {
+        const int g_at = uniform(a.table[g]), g_end = uniform(a.table[g + 1]), end = min(line1, g_end);
+        if (end <= at) continue;
+        const LxGroup place = lx_group(a, uniform(g));
+        const int b = uniform(place.b), h = uniform(place.h), m0 = uniform(place.tile) * LX_QUERIES, bh = b * a.heads + h;
+        const int blk0 = at - g_at, blk1 = end - g_at, len = uniform(la_len(a, b));
+        const bool whole = blk0 == 0 && end == g_end;
+        const int m = m0 + wave * 32 + l32;
+        const bool ok = m < a.M;
+        // (behind this part's last block: nothing)
+        const int limit = min(la_limit(a, len, min(m, a.M - 1)), blk1 * LX_BLOCK), seen_by_all = la_limit(a, len, m0), limit_first = min(seen_by_all, blk1 * LX_BLOCK);
+
+        const unsigned char* const k = (const unsigned char*)(a.k + (size_t)bh * a.n_pad * (KD * 16));
+        const unsigned char* const v = (const unsigned char*)(a.v + (size_t)bh * a.dv * a.n_pad);
+        auto load_k = [&](int blk) {                                   // (behind the last block: nothing)
+            const u32x4_t from = la_buffer(k + (size_t)blk * KB, blk < blk1 ? KB : 0);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[p / KD][e] = 0.f;
-        }
-        s[p / KD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[p % RING], qf[p % KD], s[p / KD], 0, 0, 0);
-    };
-    auto mask = [&](f32x16_t (&s)[NB], int blk) {
-        if (blk * LX_BLOCK + LX_BLOCK > limit_first) {                 // uniform: some query of the tile does not see all of the block
+            for (int j = 0; j < KL; ++j) la_to_lds(from, k_off[j], lds0 + (blk & 1) * KB + (wave * KL + j) * 1024);
+        };
+        auto load_v = [&](int blk) {                                   // eight rows a load, each with a base of its own: rows of a long cache lie far apart
 #pragma unroll
-            for (int e = 0; e < NE; ++e)
-                if (blk * LX_BLOCK + (kb0 + e / 16) * 32 + (e >> 3 & 1) * 16 + hl * 8 + (e & 7) >= limit) s[e / 16][e % 16] = -INFINITY;
-        }
-    };
-    float top;
-    auto maximum = [&](const f32x16_t (&s)[NB], int step) {            // in NB * 4 steps
-        if (step == 0) top = s[0][0];
-#pragma unroll
-        for (int e = step * 4; e < step * 4 + 4; ++e) top = fmaxf(top, s[e / 16][e % 16]);
-    };
-    // a query's reference moves only when a score lies 8 powers of two above it (see the absorbed form)
-    auto reference = [&] {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        const float mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * a.scale_log2e;
-        const float to = mx > m_run + 8.f ? mx : m_run;
-        base = to == -INFINITY ? 0.f : to;
-        alpha = __builtin_amdgcn_exp2f(m_run - base);
-        m_run = to;
-        l_run *= alpha;
-    };
-    f32x16_t sa[NB], sb[NB];
-    auto turn = [&](f32x16_t (&s)[NB], f32x16_t (&next)[NB], int blk) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        load_k(blk + 2);
-        load_v(blk + 1);
-        unsigned char* const values = lds + 2 * KB + (blk & 1) * VB;
-        const unsigned char* const keys = lds + ((blk + 1) & 1) * KB;
-        if (a.causal && blk * LX_BLOCK + LX_BLOCK > limit_first) {     // uniform: what a key holds that a query does not see must not matter
-#pragma unroll
-            for (int j = 0; j < DB; ++j) {
-                uint4* const at = reinterpret_cast<uint4*>(values + (j * 256 + tid) * 16);
-                *at = la_finite(*at);
+            for (int j = 0; j < VL; ++j) {
+                const int row = (wave * VL + j) * 8;                   // rows past dv (a multiple of 8): zeros
+                const u32x4_t from = la_buffer(v + (size_t)row * v_pitch + (size_t)blk * (LX_BLOCK * 2), blk < blk1 && row < a.dv ? 0x7fffffff : 0);
+                la_to_lds(from, v_off[(wave * VL + j) & 1], lds0 + 2 * KB + (blk & 1) * VB + (wave * VL + j) * 1024);
             }
-            la_barrier();
-        }
-        if (__any(alpha != 1.0f)) {
+        };
+        la_barrier();                                                  // the group before has been read to its end
+        load_k(blk0);
+        load_k(blk0 + 1);
+        load_v(blk0);
+        bf16x8_t qf[KD];
+        {
+            const bf16_t* const q = a.q + (((size_t)b * a.M + min(m, a.M - 1)) * a.heads + h) * (a.d + a.dr);
 #pragma unroll
-            for (int i = 0; i < DB; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-        }
-        u32x4_t p[2 * NB];                                             // probabilities, the operands of the sums
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int q = 0; q < AHEAD; ++q) fr[q] = read_k(keys, q);
-#pragma unroll
-        for (int q = 0; q < NK; ++q) {
-            if (q + AHEAD < NK) fr[(q + AHEAD) % RING] = read_k(keys, q + AHEAD);
-            else fr[(q + AHEAD) % RING] = read_v(values, q + AHEAD - NK);
-            __builtin_amdgcn_sched_barrier(0);
-            score(next, q);
-#pragma unroll
-            for (int e = NE * q / NK; e < NE * (q + 1) / NK; ++e) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], a.scale_log2e, -base));
-                s[e / 16][e % 16] = x;
-                l_run += x;
-                if (e & 1) p[e / 8][e / 2 % 4] = f2bf2(s[e / 16][e % 16 - 1], x);
+            for (int ks = 0; ks < KD; ++ks) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                const int c = ks * 16 + hl * 8;
+                if (c < a.d + a.dr) x = *reinterpret_cast<const uint4*>(q + c);
+                qf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
             }
-            __builtin_amdgcn_sched_barrier(0);
         }
-        mask(next, blk + 1);
-#pragma unroll
-        for (int q = 0; q < NV; ++q) {
-            if (q + AHEAD < NV) fr[(NK + q + AHEAD) % RING] = read_v(values, q + AHEAD);
-            __builtin_amdgcn_sched_barrier(0);
-            const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(&p[q / DB]);
-            o[q % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[(NK + q) % RING], pf, o[q % DB], 0, 0, 0);
-            // the score products' results are there once a few of these have gone out
-#pragma unroll
-            for (int st = 0; st < 4 * NB; ++st)
-                if (st * (NV - 1) / (4 * NB) + 1 == q) maximum(next, st);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        reference();
-    };
-    if (blocks > 0) {
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) asm volatile("" ::"v"(qf[ks]));
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll
-        for (int q = 0; q < NK; ++q) { fr[q % RING] = read_k(lds, q); score(sa, q); }
-        mask(sa, 0);
-#pragma unroll
-        for (int st = 0; st < 4 * NB; ++st) maximum(sa, st);
-        reference();
-        for (int blk = 0;;) {
-            turn(sa, sb, blk);
-            if (++blk >= blocks) break;
-            turn(sb, sa, blk);
-            if (++blk >= blocks) break;
-        }
-    }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
-        l_run = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    }
-    if constexpr (NB == 1) {
-        // the second half of the keys to the first's wave: [pair][register][lane]
-        __syncthreads();
-        float* const ex = reinterpret_cast<float*>(lds) + group * ((DB * 16 + 2) * 64) + lane;
-        if (kb0) {
-#pragma unroll
-            for (int i = 0; i < DB; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) ex[(i * 16 + e) * 64] = o[i][e];
-            ex[DB * 16 * 64] = m_run;
-            ex[(DB * 16 + 1) * 64] = l_run;
-        }
-        __syncthreads();
-        if (kb0) return;
-        const float mo = ex[DB * 16 * 64], lo = ex[(DB * 16 + 1) * 64], mx = fmaxf(m_run, mo), ref = mx == -INFINITY ? 0.f : mx;
-        const float f = __builtin_amdgcn_exp2f(m_run - ref), fo = __builtin_amdgcn_exp2f(mo - ref);
-        l_run = l_run * f + lo * fo;
+        f32x16_t o[DB];
 #pragma unroll
         for (int i = 0; i < DB; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[i][e] = o[i][e] * f + ex[(i * 16 + e) * 64] * fo;
-    }
-    if (!ok) return;
-    const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;               // no key seen: zeros
-    bf16_t* const out = a.out + (((size_t)b * a.M + m) * a.heads + h) * a.dv;
+            for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+        float m_run = -INFINITY, l_run = 0.f, alpha = 1.f, base = 0.f, top = 0.f;
+        bf16x8_t fr[RING];
+        auto read_k = [&](const unsigned char* tile, int p) {          // product p: step p % KD of the 32 keys p / KD
+            const int ks = p % KD;
+            return *reinterpret_cast<const bf16x8_t*>(tile + k_at[ks % KU] + (ks / KU) * (KU * 32) + p / KD * (32 * PITCH));
+        };
+        auto read_v = [&](const unsigned char* tile, int p) { return *reinterpret_cast<const bf16x8_t*>(tile + v_at[p / DB] + p % DB * 4096); };      // 16 keys p / DB, rows of block p % DB
+        auto score = [&](f32x16_t& s, int p) {
+            if (p % KD == 0) {
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+            }
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[p % RING], qf[p % KD], s, 0, 0, 0);
+        };
+        auto mask = [&](f32x16_t& s, f32x16_t& t, int blk) {
+            if (blk * LX_BLOCK + LX_BLOCK > limit_first) {             // uniform: some query of the tile does not see all of the block
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int c = i * 32 + q * 8 + hl * 4;
-            if (c < a.dv) *reinterpret_cast<uint2*>(out + c) = make_uint2(f2bf2(o[i][4 * q] * inv, o[i][4 * q + 1] * inv), f2bf2(o[i][4 * q + 2] * inv, o[i][4 * q + 3] * inv));
+                for (int e = 0; e < NE; ++e)
+                    if (blk * LX_BLOCK + (e >> 3) * 16 + hl * 8 + (e & 7) >= limit) (e < 16 ? s : t)[e % 16] = -INFINITY;
+            }
+        };
+        auto maximum = [&](const f32x16_t& s, const f32x16_t& t, int step) {      // in eight steps
+            if (step == 0) top = s[0];
+#pragma unroll
+            for (int e = step * 4; e < step * 4 + 4; ++e) top = fmaxf(top, (e < 16 ? s : t)[e % 16]);
+        };
+        // a query's reference moves only when a score lies 8 powers of two above it (see the absorbed form)
+        auto reference = [&] {
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            const float mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * a.scale_log2e;
+            const float to = mx > m_run + 8.f ? mx : m_run;
+            base = to == -INFINITY ? 0.f : to;
+            alpha = __builtin_amdgcn_exp2f(m_run - base);
+            m_run = to;
+            l_run *= alpha;
+        };
+        // c0, c1: scores of this block; n0: those of the next block's first 32 keys, the others' take c0, which has been used up by then
+        f32x16_t sa, sb, sc;
+        auto turn = [&](f32x16_t& c0, f32x16_t& c1, f32x16_t& n0, int blk) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            load_k(blk + 2);
+            load_v(blk + 1);
+            unsigned char* const values = lds + 2 * KB + (blk & 1) * VB;
+            const unsigned char* const keys = lds + ((blk + 1) & 1) * KB;
+            if (a.causal && blk * LX_BLOCK + LX_BLOCK > seen_by_all) { // uniform: what a key holds that a query does not see must not matter
+#pragma unroll
+                for (int j = 0; j < DB; ++j) {
+                    uint4* const at16 = reinterpret_cast<uint4*>(values + (j * 256 + tid) * 16);
+                    *at16 = la_finite(*at16);
+                }
+                la_barrier();
+            }
+            if (__any(alpha != 1.0f)) {
+#pragma unroll
+                for (int i = 0; i < DB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+            }
+            auto fetch = [&](int q) {                                  // the operand of product q of the turn
+                if (q < NK) fr[q % RING] = read_k(keys, q);
+                else if (q < NK + NV) fr[q % RING] = read_v(values, q - NK);
+            };
+            u32x4_t p[4];                                              // probabilities, the operands of the sums
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) fetch(q);
+#pragma unroll
+            for (int q = 0; q < NK; ++q) {
+                fetch(q + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                score(q < KD ? n0 : c0, q);
+#pragma unroll
+                for (int e = NE * q / NK; e < NE * (q + 1) / NK; ++e) {
+                    f32x16_t& c = e < 16 ? c0 : c1;
+                    const float x = __builtin_amdgcn_exp2f(fmaf(c[e % 16], a.scale_log2e, -base));
+                    c[e % 16] = x;
+                    l_run += x;
+                    if (e & 1) {
+                        unsigned pair = f2bf2(c[e % 16 - 1], x);
+                        asm volatile("" : "+v"(pair), "+v"(l_run));    // here, not behind the branch in front of their use
+                        p[e / 8][e / 2 % 4] = pair;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            mask(n0, c0, blk + 1);
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                fetch(NK + q + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(&p[q / DB]);
+                o[q % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[(NK + q) % RING], pf, o[q % DB], 0, 0, 0);
+                // the score products' results are there once a few of these have gone out
+#pragma unroll
+                for (int st = 0; st < 8; ++st)
+                    if (st * (NV - 1) / 8 + 1 == q) maximum(n0, c0, st);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            reference();
+        };
+#pragma unroll
+        for (int ks = 0; ks < KD; ++ks) asm volatile("" ::"v"(qf[ks]));
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        {
+            const unsigned char* const keys = lds + (blk0 & 1) * KB;
+#pragma unroll
+            for (int q = 0; q < NK; ++q) { fr[q % RING] = read_k(keys, q); score(q < KD ? sa : sb, q); }
         }
+        mask(sa, sb, blk0);
+#pragma unroll
+        for (int st = 0; st < 8; ++st) maximum(sa, sb, st);
+        reference();
+        for (int blk = blk0;;) {
+            turn(sa, sb, sc, blk);
+            if (++blk >= blk1) break;
+            turn(sc, sa, sb, blk);
+            if (++blk >= blk1) break;
+            turn(sb, sc, sa, blk);
+            if (++blk >= blk1) break;
+        }
+        at = end;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        {
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+            l_run = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        }
+        if (!ok) continue;
+        if (whole) {
+            const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;       // no key seen: zeros
+            bf16_t* const out = a.out + (((size_t)b * a.M + m) * a.heads + h) * a.dv;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = i * 32 + q * 8 + hl * 4;
+                    if (c < a.dv) *reinterpret_cast<uint2*>(out + c) = make_uint2(f2bf2(o[i][4 * q] * inv, o[i][4 * q + 1] * inv), f2bf2(o[i][4 * q + 2] * inv, o[i][4 * q + 3] * inv));
+                }
+        } else {
+            const size_t row = ((size_t)w + g) * LX_QUERIES + wave * 32 + l32;
+            if (hl == 0) a.ml[row] = make_float2(m_run, l_run);
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4*>(a.part + row * (DB * 32) + i * 32 + q * 8 + hl * 4) = make_float4(o[i][4 * q], o[i][4 * q + 1], o[i][4 * q + 2], o[i][4 * q + 3]);
+        }
+    }
 #endif
 }
 
-template <int KD, int DB, int NB> static int launch_attention(const LatentArgs& a, hipStream_t st) {
-    constexpr int stages = 2 * (LX_BLOCK * KD * 32 + DB * 32 * 128), halves = NB == 1 ? 2 * (DB * 16 + 2) * 256 : 0, lds = stages > halves ? stages : halves;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_expanded_kernel<KD, DB, NB>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_latent_attention: cannot raise the dynamic LDS limit");
-    const int nqt = ceil_div(a.M, 64 * NB);
-    {
-        ProfileScope prof(PROF_ATTENTION, 2.0 * a.B * a.M * a.heads * (double)a.n * (a.d + a.dr + a.dv), 2.0 * a.B * a.n * a.heads * (double)(a.d + a.dr + a.dv), st);
-        hipLaunchKernelGGL((latent_expanded_kernel<KD, DB, NB>), dim3((unsigned)(a.B * a.heads * nqt)), dim3(256), lds, st, a, nqt, a.B * a.heads % 8 ? 0 : a.B * a.heads / 8);
+// Tiles that several workgroups had blocks of: their parts, each with its weight exp2(m - max), divided by the sum.  Tiles without a key: zeros.  DB * 8 lanes a query, four
+// channels each.
+template <int DB>
+__global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int QUADS = DB * 8, QUERIES = 256 / QUADS;
+    const int g = blockIdx.x, total = a.table[a.groups], workgroups = min(a.workgroups, total), g0 = a.table[g], g1 = a.table[g + 1];
+    const int w0 = g1 > g0 ? la_owner(g0, workgroups, total) : 0, n = g1 > g0 ? la_owner(g1 - 1, workgroups, total) - w0 + 1 : 0;
+    if (n == 1) return;                                                // the workgroup that had it has written it
+    const LxGroup place = lx_group(a, g);
+    const int sub = threadIdx.x / QUADS, c = (threadIdx.x - sub * QUADS) * 4;
+    if (sub >= QUERIES || c >= a.dv) return;
+    for (int i = blockIdx.y * QUERIES + sub; i < LX_QUERIES; i += gridDim.y * QUERIES) {
+        const int m = place.tile * LX_QUERIES + i;
+        if (m >= a.M) return;
+        const size_t row = ((size_t)w0 + g) * LX_QUERIES + i;
+        float top = -INFINITY;
+#pragma unroll 4
+        for (int p = 0; p < n; ++p) top = fmaxf(top, a.ml[row + (size_t)p * LX_QUERIES].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        float l = 0.f;
+        float4 o = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+        for (int p = 0; p < n; ++p) {
+            const float2 ml = a.ml[row + (size_t)p * LX_QUERIES];
+            const float4 v = *reinterpret_cast<const float4*>(a.part + (row + (size_t)p * LX_QUERIES) * (DB * 32) + c);
+            const float f = __builtin_amdgcn_exp2f(ml.x - base);
+            l = fmaf(f, ml.y, l);
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        *reinterpret_cast<uint2*>(a.out + (((size_t)place.b * a.M + m) * a.heads + place.h) * a.dv + c) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
     }
-    FISE_CHECK_LAUNCH("fise_latent_attention: expanded");
-    return FISE_OK;
+#endif
 }
 
 template <int TILE> static int launch_tile(const LatentArgs& a, hipStream_t st) {
-    constexpr int KD = kExpandedTiles[TILE].KD, DB = kExpandedTiles[TILE].DB;
+    constexpr int KD = kExpandedTiles[TILE].KD, DB = kExpandedTiles[TILE].DB, lds = 2 * (LX_BLOCK * KD * 32 + DB * 32 * 128);
+    static_assert(expanded_per_cu(KD) * lds <= 160 * 1024, "LDS of a CU");
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_expanded_kernel<KD, DB>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_latent_attention: cannot raise the dynamic LDS limit");
     const int key_tiles = (int)(a.n_pad / LX_KEYS), k_tiles = ceil_div(a.heads * a.d, 128), v_tiles = ceil_div(a.heads * a.dv, 128);
-    if (key_tiles) {
+    {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * a.B * a.n * a.heads * (double)a.r * (a.d + a.dv), 2.0 * a.B * a.n * (a.r + a.heads * (double)(a.d + a.dv)), st);
-        hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)(a.B * key_tiles * (k_tiles + v_tiles))), dim3(256), 2 * LE_STAGE, st, a, KD, key_tiles, k_tiles, v_tiles,
-                           fast_div(key_tiles), fast_div(k_tiles + v_tiles));
+        hipLaunchKernelGGL(latent_expand_kernel, dim3((unsigned)(a.B * key_tiles * (k_tiles + v_tiles) + 1)), dim3(256), 2 * LE_STAGE, st, a, KD, key_tiles, k_tiles, v_tiles,
+                           fast_div(std::max(key_tiles, 1)), fast_div(k_tiles + v_tiles));
     }
     FISE_CHECK_LAUNCH("fise_latent_attention: keys and values");
-    return expanded_halves(a.B, a.heads, a.M) ? launch_attention<KD, DB, 1>(a, st) : launch_attention<KD, DB, 2>(a, st);
+    {
+        ProfileScope prof(PROF_ATTENTION, 2.0 * a.B * a.M * a.heads * (double)a.n * (a.d + a.dr + a.dv), 2.0 * a.B * a.n * a.heads * (double)(a.d + a.dr + a.dv), st);
+        hipLaunchKernelGGL((latent_expanded_kernel<KD, DB>), dim3((unsigned)a.workgroups), dim3(256), lds, st, a);
+    }
+    FISE_CHECK_LAUNCH("fise_latent_attention: expanded");
+    if (!a.whole) {
+        ProfileScope prof(PROF_ATTENTION_MERGE, 0, 0, st);
+        hipLaunchKernelGGL(latent_join_kernel<DB>, dim3((unsigned)a.groups, a.groups < 4 * LA_CUS ? 4u : 1u), dim3(256), 0, st, a);
+    }
+    FISE_CHECK_LAUNCH("fise_latent_attention: parts");
+    return FISE_OK;
 }
 
 int launch_expanded(const LatentArgs& a, int tile, hipStream_t st) {

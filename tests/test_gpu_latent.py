@@ -84,7 +84,9 @@ def check(got, want, rows=slice(None)):
 # for and widths between them, head dims that are no multiple of 16 or 32, more groups than workgroups and the other way round
 CASES = [(1, 1, 1, 1, 8, 0, 8, 8), (1, 1, 1000, 8, 64, 0, 64, 128), (2, 1, 33, 16, 128, 64, 128, 512), (3, 5, 31, 13, 40, 32, 40, 128), (2, 17, 64, 4, 80, 0, 80, 320),
          (1, 65, 65, 1, 160, 64, 160, 512), (2, 9, 200, 8, 64, 8, 96, 256), (5, 2, 127, 32, 32, 64, 64, 384), (1, 300, 300, 2, 40, 32, 40, 136), (1, 4, 4100, 8, 128, 64, 128, 512),
-         (2, 130, 257, 8, 160, 0, 64, 256), (1, 33, 95, 3, 24, 40, 56, 72), (4, 1, 2049, 64, 128, 64, 128, 512), (1, 200, 64, 16, 128, 64, 128, 512), (2, 768, 1024, 8, 40, 32, 40, 128)]
+         (2, 130, 257, 8, 160, 0, 64, 256), (1, 33, 95, 3, 24, 40, 56, 72), (4, 1, 2049, 64, 128, 64, 128, 512), (1, 200, 64, 16, 128, 64, 128, 512), (2, 768, 1024, 8, 40, 32, 40, 128),
+         # a workgroup for every tile of the expanded form: heads in eights and not, several tiles
+         (4, 3, 70, 128, 64, 32, 64, 128), (3, 2, 65, 171, 32, 0, 32, 64), (1, 1100, 130, 64, 128, 64, 128, 512), (1, 140, 200, 128, 160, 64, 160, 256)]
 
 
 @pytest.mark.parametrize("form", [ABSORBED, EXPANDED])
@@ -98,7 +100,8 @@ def test_all_keys(fb, B, M, n, H, d, dr, dv, r, form):
 
 # lengths of none, one, part and all of the keys, and outside of what there is; behind them NaN; with causal rows, more rows than keys leave rows empty
 LENGTHS = [(4, 1, 300, 8, 64, 32, 64, 128, [0, 1, 300, 129]), (3, 7, 96, 16, 128, 64, 128, 512, [96, 5, 0]), (2, 150, 200, 4, 40, 0, 40, 128, [200, 77]), (2, 70, 33, 2, 80, 64, 80, 320, [33, 32]),
-           (6, 3, 500, 30, 128, 64, 64, 256, [500, 0, 0, 64, 65, 3]), (1, 513, 700, 3, 64, 0, 64, 384, [640])]
+           (6, 3, 500, 30, 128, 64, 64, 256, [500, 0, 0, 64, 65, 3]), (1, 513, 700, 3, 64, 0, 64, 384, [640]), (4, 129, 300, 64, 32, 0, 32, 64, [300, 0, 64, 150]), (1, 1100, 1100, 64, 64, 32, 64, 128, [1100]),
+           (2, 300, 150, 90, 40, 8, 40, 64, [150, 2])]
 
 
 @pytest.mark.parametrize("form", [ABSORBED, EXPANDED])
