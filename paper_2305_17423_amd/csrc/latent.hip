@@ -32,31 +32,28 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
     }
     const int cols = R / LQ_COLS, h = blockIdx.x / cols, c0 = (blockIdx.x - h * cols) * LQ_COLS, tokens = a.B * a.M, width = R + DR;
     const int steps = (a.d + 31) / 32;
-    uint4 qv[LQ_TOKENS / 16][LQ_STEPS];
+    // (loads through buffers, which bring zeros for what does not exist: a condition would be a branch each)
+    u32x4_t qv[LQ_TOKENS / 16][LQ_STEPS];
+    const unsigned token_bytes = (unsigned)(a.heads * (a.d + a.dr) * 2);
     auto queries = [&](int t0) {
+        const auto from = buf(a.q + ((size_t)t0 * a.heads + h) * (a.d + a.dr), (unsigned)(min(tokens - t0, LQ_TOKENS) - 1) * token_bytes + (unsigned)a.d * 2);
 #pragma unroll
-        for (int tt = 0; tt < LQ_TOKENS / 16; ++tt) {
-            const int t = t0 + tt * 16 + l16;
+        for (int tt = 0; tt < LQ_TOKENS / 16; ++tt)
 #pragma unroll
             for (int ks = 0; ks < LQ_STEPS; ++ks) {
-                qv[tt][ks] = make_uint4(0, 0, 0, 0);
                 const int c = ks * 32 + lq * 8;
-                if (t < tokens && c < a.d) qv[tt][ks] = *reinterpret_cast<const uint4*>(a.q + ((size_t)t * a.heads + h) * (a.d + a.dr) + c);
+                qv[tt][ks] = __builtin_amdgcn_raw_buffer_load_b128(from, c < a.d ? (int)((unsigned)(tt * 16 + l16) * token_bytes + c * 2) : 0x7fffffff, 0, 0);
             }
-        }
     };
     {
-        uint4 w[LQ_STEPS * 2];
+        u32x4_t w[LQ_STEPS * 2];
         const int c = (tid & 15) * 8;
+        const auto from = buf(a.w_uk + (size_t)h * a.d * a.r, (unsigned)(a.d * a.r * 2));
 #pragma unroll
-        for (int i = 0; i < LQ_STEPS * 2; ++i) {
-            const int row = i * 16 + (tid >> 4);
-            w[i] = make_uint4(0, 0, 0, 0);
-            if (row < a.d && c0 + c < a.r) w[i] = *reinterpret_cast<const uint4*>(a.w_uk + ((size_t)h * a.d + row) * a.r + c0 + c);
-        }
+        for (int i = 0; i < LQ_STEPS * 2; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b128(from, c0 + c < a.r ? ((i * 16 + (tid >> 4)) * a.r + c0 + c) * 2 : 0x7fffffff, 0, 0);
         queries(blockIdx.y * LQ_TOKENS);
 #pragma unroll
-        for (int i = 0; i < LQ_STEPS * 2; ++i) *reinterpret_cast<uint4*>(lds + (i * 16 + (tid >> 4)) * LQ_PITCH + c * 2) = w[i];
+        for (int i = 0; i < LQ_STEPS * 2; ++i) *reinterpret_cast<u32x4_t*>(lds + (i * 16 + (tid >> 4)) * LQ_PITCH + c * 2) = w[i];
     }
     __syncthreads();
     const unsigned char* const from = lds + (lq * 8 + l16 / 4) * LQ_PITCH + (wave * 32 + (l16 % 4) * 4) * 2;
@@ -314,7 +311,7 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
 // exp2(m - max), divides, and leaves the sums in LDS as two bf16 numbers each (16 of the float's 24 bits, so that this product rounds only its result);
 // the waves take 16 value channels at a time.
 template <int R>
-__global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) {
+__global__ __launch_bounds__(512, 4) void latent_values_kernel(const LatentArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int QUADS = R / 4, PARTS = 512 / QUADS, PITCH = R + 8;   // parts: lanes that share the parts of a token, or have tokens of their own
     __shared__ __attribute__((aligned(16))) bf16_t hi[16][PITCH], lo[16][PITCH];
@@ -326,7 +323,6 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
     const int h = blockIdx.x, t0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.B * a.M - t0);
     const int part = tid / QUADS, quad = tid - part * QUADS;
     const int total = a.table[a.groups], workgroups = min(a.workgroups, total);
-    // the weights of the first 16 channels of this wave, on their way while the parts are added
     const int vt = (a.dv + 15) / 16;
     auto weights = [&](bf16x8_t (&wf)[R / 32], int v) {
         const bf16_t* const w = a.w_uv + ((size_t)h * a.dv + v * 16 + l16) * a.r;
@@ -337,9 +333,6 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
             wf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
         }
     };
-    bf16x8_t wf[R / 32];
-    if (wave < vt) weights(wf, wave);
-
     // ---- what the parts of each token weigh: 32 lanes a token go over its parts (workgroups that had some of its group's blocks), keeping a maximum
     // and a sum, and meet.  l == 0: no key was seen, zeros.
     if (tid < a.tokens * 32) {
@@ -373,11 +366,20 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
         const int n = count[i];
         const float2* const ml = a.ml + first[i];
         const float* const part_o = a.part + first[i] * R + quad * 4;
-#pragma unroll 4
-        for (int p = from; p < n; p += step) {
-            const float f = __builtin_amdgcn_exp2f(ml[(size_t)p * LA_ROWS].x - st.x) * st.y;
-            const float4 v = *reinterpret_cast<const float4*>(part_o + (size_t)p * (LA_ROWS * R));
-            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        for (int p0 = from; p0 < n; p0 += 4 * step) {                  // four parts requested at once (behind the last: that one again, without weight)
+            float4 v[4];
+            float f[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const size_t p = min(p0 + u * step, n - 1);
+                f[u] = ml[p * LA_ROWS].x;
+                v[u] = *reinterpret_cast<const float4*>(part_o + p * (LA_ROWS * R));
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float w = p0 + u * step < n ? __builtin_amdgcn_exp2f(f[u] - st.x) * st.y : 0.f;
+                o.x = fmaf(w, v[u].x, o.x); o.y = fmaf(w, v[u].y, o.y); o.z = fmaf(w, v[u].z, o.z); o.w = fmaf(w, v[u].w, o.w);
+            }
         }
         return o;
     };
@@ -403,6 +405,8 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
             put(i, o);
         }
     }
+    bf16x8_t wf[R / 32];
+    if (wave < vt) weights(wf, wave);
     __syncthreads();
     const int src = l16 < tokens ? l16 : 0;                            // (tokens that do not exist: the first one's sums, not stored)
     for (int v = wave; v < vt; v += 8) {
@@ -412,6 +416,7 @@ __global__ __launch_bounds__(512) void latent_values_kernel(const LatentArgs a) 
         for (int ks = 0; ks < R / 32; ++ks) {
             acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[ks], *reinterpret_cast<const bf16x8_t*>(&hi[src][ks * 32 + lq * 8]), acc[0], 0, 0, 0);
             acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[ks], *reinterpret_cast<const bf16x8_t*>(&lo[src][ks * 32 + lq * 8]), acc[1], 0, 0, 0);
+            if (ks % 4 == 3) __builtin_amdgcn_sched_barrier(0);        // (all sums read at once would not leave room for a second workgroup on the CU)
         }
         const int c = v * 16 + lq * 4;
         if (l16 < tokens && c < a.dv)
