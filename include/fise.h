@@ -483,7 +483,7 @@ int fise_w4_unpack(const void* packed, int N, int K, int group, void* w, int dty
  * single tokens, the tokens a mask leaves at the deep levels); more rows are taken 64
  * at a time, the weights read again for each.  x, y and bias have a type of their own
  * (residual has y's); all sums are float: the products of a group first, then those
- * sums times their scale.  x rows: K and x_stride multiples of 8, 16-byte aligned; y and
+ * sums times their scale.  x rows: K and x_stride multiples of 8, 16-byte aligned, x_stride at most 2^23; y and
  * residual rows: any alignment of their type.  residual may be y itself; y must not
  * otherwise overlap an input.  M == 0 touches nothing. */
 typedef struct {

@@ -6,7 +6,8 @@
 // four 16x16x32 instructions.  A weight goes to float as q / 16 (v_cvt_off_f32_i4) and two of those to a bf16 pair; both are exact, and so are the
 // products; they are added in float, a group at a time, and the group's scale is applied to that sum, in float too.  Nothing is added to the
 // weights that would have to be taken off again, so an infinite x gives what the definition gives.
-// x is staged in LDS as bf16.  Float x, and x behind SiLU, is split into three bf16 numbers that add up to it exactly: three rows of the
+// x of a wave's columns stays in registers as operands, and the wave streams the weights of one tile of outputs after the other past it; nothing else is read again.
+// Float x, and x behind SiLU, is split into three bf16 numbers that add up to it exactly: three rows of the
 // instruction, of which a few rows of x leave most idle, added in the epilogue.
 #include "igemm.h"
 #include "profile.h"
@@ -77,15 +78,23 @@ struct W4Args {
     W4Choice c;
 };
 
-__device__ __forceinline__ unsigned w4_pair(unsigned w) {              // two weights / 16 from the lowest eight bits, as a bf16 pair: exact
 #if defined(__HIP_DEVICE_COMPILE__)
-    return f2bf2(__builtin_amdgcn_cvt_off_f32_i4(w), __builtin_amdgcn_cvt_off_f32_i4(w >> 4));
-#else
-    return w;
-#endif
+// Eight weights / 16 of a word as the operand's four bf16 pairs: exact.  A conversion takes the lowest four bits of a byte that it picks itself.
+__device__ __forceinline__ bf16x8_t w4_operand(unsigned w) {
+    const unsigned odd = w >> 4;
+    u32x4_t r;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        float lo, hi;
+        if (b == 0) asm("v_cvt_off_f32_i4_sdwa %0, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0\n\tv_cvt_off_f32_i4_sdwa %1, %3 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=&v"(lo), "=v"(hi) : "v"(w), "v"(odd));
+        if (b == 1) asm("v_cvt_off_f32_i4_sdwa %0, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1\n\tv_cvt_off_f32_i4_sdwa %1, %3 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=&v"(lo), "=v"(hi) : "v"(w), "v"(odd));
+        if (b == 2) asm("v_cvt_off_f32_i4_sdwa %0, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2\n\tv_cvt_off_f32_i4_sdwa %1, %3 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=&v"(lo), "=v"(hi) : "v"(w), "v"(odd));
+        if (b == 3) asm("v_cvt_off_f32_i4_sdwa %0, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3\n\tv_cvt_off_f32_i4_sdwa %1, %3 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=&v"(lo), "=v"(hi) : "v"(w), "v"(odd));
+        r[b] = f2bf2(lo, hi);
+    }
+    return *reinterpret_cast<const bf16x8_t*>(&r);
 }
-
-__device__ __forceinline__ void w4_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }      // (weights that are on their way stay there)
+#endif
 
 // a value of x as three bf16 numbers that add up to it
 __device__ __forceinline__ void w4_split(float v, bf16_t (&p)[3]) {    // truncated, not rounded: no piece of a finite number overflows, and what is left has 8 bits in the end
@@ -99,120 +108,149 @@ __device__ __forceinline__ void w4_split(float v, bf16_t (&p)[3]) {    // trunca
     if (v != v) p[0] |= 0x40;                                          // a NaN whose bits are all in the lower half stays one
 }
 
-// MT: tiles of 16 rows of x; GS: matrix instructions a scale covers (1, 2, 4: groups of 32, 64, 128 and more).
-template <int MT, int GS>
-__global__ __launch_bounds__(1024) void w4_linear_kernel(const W4Args a) {
+// MT: tiles of 16 rows of x; KT: tile columns of a wave; GS: matrix instructions a scale covers (1, 2, 4: groups of 32, 64, 128 and more); SPLIT: three pieces a value.
+template <int MT, int KT, int GS, bool SPLIT>
+__global__ __launch_bounds__(MT == 4 ? 512 : 1024) void w4_linear_kernel(const W4Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    bf16_t* const xs = reinterpret_cast<bf16_t*>(lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), threads = blockDim.x;
     const W4Choice& c = a.c;
-    const int kw = wave % c.waves_k, nw = wave / c.waves_k;
-    const int tn = blockIdx.x * c.waves_n + nw, tiles_n = (a.N + W4_ROWS - 1) / W4_ROWS;
-    const bool live = tn < tiles_n;
-    const int m0 = blockIdx.y * c.slab, rows = min(c.slab, a.M - m0), rows_x = rows * c.pieces;
     const int l16 = lane & 15, lq = lane >> 4;
+    const int m0 = blockIdx.y * c.slab, rows = min(c.slab, a.M - m0);
+    const int all_n = (a.N + W4_ROWS - 1) / W4_ROWS, n0 = blockIdx.x * c.tiles_n, n_n = min(c.tiles_n, all_n - n0);
+    float* const red = reinterpret_cast<float*>(lds);                  // [tile of outputs][wave][row of x][16]
 
-    constexpr int PF = 4, NS = 4 / GS;                                 // tiles in flight; scales of a tile
-    const unsigned char* const wt = a.tiles + (size_t)(live ? tn : 0) * a.tiles_k * W4_TILE_BYTES + lane * 16;
-    const bf16_t* const st = a.scales + (size_t)(live ? tn : 0) * (GS < 4 ? a.tiles_k * NS : a.groups) * W4_ROWS;
-    u32x4_t w[PF];
-    unsigned s[PF][(NS + 1) / 2];
-    auto fetch = [&](int slot, int t) {
-        w[slot] = *reinterpret_cast<const u32x4_t*>(wt + (size_t)t * W4_TILE_BYTES);
-        if constexpr (GS == 4) s[slot][0] = st[(size_t)(t >> a.group_shift) * W4_ROWS + l16];
-        else if constexpr (GS == 2) s[slot][0] = *reinterpret_cast<const unsigned*>(st + ((size_t)t * W4_ROWS + l16) * 2);
-        else { const uint2 v = *reinterpret_cast<const uint2*>(st + ((size_t)t * W4_ROWS + l16) * 4); s[slot][0] = v.x; s[slot][1] = v.y; }
-    };
-    f32x4_t acc[MT];
+    constexpr int NS = 4 / GS, SW = (NS + 1) / 2, U = 4 / KT;          // scales of a tile, words of them; tiles of outputs in flight
+    u32x4_t w[U][KT];
+    unsigned s[U][KT][SW];
+    bf16x8_t xf[KT][4][MT];
+    for (int chunk = 0; chunk < c.chunks; ++chunk) {
+        const int t0 = (chunk * c.waves_k + wave) * KT, n_t = min(max(a.tiles_k - t0, 0), KT);      // this wave's tile columns
+        auto fetch = [&](int slot, int n) {
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = f32x4_t{0, 0, 0, 0};
-    // rows of LDS that do not exist: the lane reads the first one instead, and its results are not stored
-    const bf16_t* xr[MT];
+            for (int t = 0; t < KT; ++t)
+                if (t < n_t) {
+                    w[slot][t] = *reinterpret_cast<const u32x4_t*>(a.tiles + ((size_t)(n0 + n) * a.tiles_k + t0 + t) * W4_TILE_BYTES + lane * 16);
+                    const bf16_t* const st = a.scales + (size_t)(n0 + n) * (GS < 4 ? a.tiles_k * NS : a.groups) * W4_ROWS;
+                    if constexpr (GS == 4) s[slot][t][0] = st[(size_t)((t0 + t) >> a.group_shift) * W4_ROWS + l16];
+                    else if constexpr (GS == 2) s[slot][t][0] = *reinterpret_cast<const unsigned*>(st + ((size_t)(t0 + t) * W4_ROWS + l16) * 2);
+                    else { const uint2 v = *reinterpret_cast<const uint2*>(st + ((size_t)(t0 + t) * W4_ROWS + l16) * 4); s[slot][t][0] = v.x; s[slot][t][SW - 1] = v.y; }
+                }
+        };
 #pragma unroll
-    for (int t = 0; t < MT; ++t) xr[t] = xs + (size_t)(t * 16 + l16 < rows_x ? t * 16 + l16 : 0) * c.pitch + lq * 8;
+        for (int u = 0; u < U; ++u)
+            if (u < n_n) fetch(u, u);
 
-    for (int t0 = 0; t0 < a.tiles_k; t0 += c.chunk) {
-        const int t1 = min(a.tiles_k, t0 + c.chunk);
-        const int first = t0 + kw, n_t = live && first < t1 ? (t1 - first + c.waves_k - 1) / c.waves_k : 0;
+        // ---- x of this wave's columns
+        if constexpr (!SPLIT) {
+            const auto from = buf((const bf16_t*)a.x + (size_t)m0 * a.x_stride, (unsigned)((rows - 1) * a.x_stride + a.K) * 2);
 #pragma unroll
-        for (int p = 0; p < PF; ++p)
-            if (p < n_t) fetch(p, first + p * c.waves_k);
-        // ---- x of this chunk: pieces of eight columns; columns past K are zeros
-        const int cols8 = (t1 - t0) * (W4_COLS / 8);
-        if (t0) w4_barrier();
-        for (int i = tid; i < rows * cols8; i += threads) {
-            const int m = i / cols8, k = t0 * W4_COLS + (i - m * cols8) * 8;
-            float v[8];
-            uint4 raw = make_uint4(0, 0, 0, 0);
-            if (a.x_f32) {
-                float4 lo = make_float4(0, 0, 0, 0), hi = lo;
-                if (k < a.K) { const float* p = (const float*)a.x + (size_t)(m0 + m) * a.x_stride + k; lo = *reinterpret_cast<const float4*>(p); hi = *reinterpret_cast<const float4*>(p + 4); }
-                v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
-            } else {
-                if (k < a.K) raw = *reinterpret_cast<const uint4*>((const bf16_t*)a.x + (size_t)(m0 + m) * a.x_stride + k);
-                v[0] = lo16(raw.x); v[1] = hi16(raw.x); v[2] = lo16(raw.y); v[3] = hi16(raw.y);
-                v[4] = lo16(raw.z); v[5] = hi16(raw.z); v[6] = lo16(raw.w); v[7] = hi16(raw.w);
-            }
-            bf16_t* const to = xs + (size_t)m * c.pieces * c.pitch + (k - t0 * W4_COLS);
-            if (c.pieces == 1) { *reinterpret_cast<uint4*>(to) = raw; continue; }
-            unsigned out[3][4];
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                bf16_t p[3];
-                w4_split(a.silu ? silu_f(v[e]) : v[e], p);
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int q = 0; q < 3; ++q) out[q][e >> 1] = e & 1 ? out[q][e >> 1] | (unsigned)p[q] << 16 : p[q];
-            }
+                    for (int r = 0; r < MT; ++r) {                     // (rows and columns that do not exist: zeros)
+                        const int k = (t0 + t) * W4_COLS + j * 32 + lq * 8, m = r * 16 + l16;
+                        const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(from, k < a.K && m < rows ? (m * (int)a.x_stride + k) * 2 : 0x7fffffff, 0, 0);
+                        xf[t][j][r] = *reinterpret_cast<const bf16x8_t*>(&v);
+                    }
+        } else {
+            // a tile column of every wave and 16 rows (pieces) at a time through LDS, so that a value is worked out once
+            bf16_t* const xs = reinterpret_cast<bf16_t*>(lds + c.x_at);
+            const int cols = c.waves_k * W4_COLS, pitch = cols + 8;
 #pragma unroll
-            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + (size_t)q * c.pitch) = make_uint4(out[q][0], out[q][1], out[q][2], out[q][3]);
-        }
-        w4_barrier();
-        for (int i0 = 0; i0 < n_t; i0 += PF) {
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int p = 0; p < PF; ++p) {
-                const int i = i0 + p;
-                if (i < n_t) {
-                    const int kx = (first + i * c.waves_k - t0) * W4_COLS;
-                    f32x4_t part[MT];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const unsigned q = w[p][j];
-                        const u32x4_t bw = {w4_pair(q), w4_pair(q >> 8), w4_pair(q >> 16), w4_pair(q >> 24)};
-                        const bf16x8_t b = *reinterpret_cast<const bf16x8_t*>(&bw);
-#pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(xr[t] + kx + j * 32);
-                            part[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b, j % GS ? part[t] : f32x4_t{0, 0, 0, 0}, 0, 0, 0);
+                for (int r = 0; r < MT; ++r) {
+                    __syncthreads();
+                    const int mlo = r * 16 / 3, mhi = min(rows, (r * 16 + 15) / 3 + 1);      // rows of x with a piece among these
+                    for (int i = tid; i < (mhi - mlo) * (cols / 8); i += threads) {
+                        const int m = mlo + i / (cols / 8), col = (i - (m - mlo) * (cols / 8)) * 8;
+                        const int k = ((chunk * c.waves_k + col / W4_COLS) * KT + t) * W4_COLS + col % W4_COLS;
+                        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                        if (k < a.K) {
+                            if (a.x_f32) {
+                                const float* const p = (const float*)a.x + (size_t)(m0 + m) * a.x_stride + k;
+                                const float4 lo = *reinterpret_cast<const float4*>(p), hi = *reinterpret_cast<const float4*>(p + 4);
+                                v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+                            } else {
+                                const uint4 raw = *reinterpret_cast<const uint4*>((const bf16_t*)a.x + (size_t)(m0 + m) * a.x_stride + k);
+                                v[0] = lo16(raw.x); v[1] = hi16(raw.x); v[2] = lo16(raw.y); v[3] = hi16(raw.y);
+                                v[4] = lo16(raw.z); v[5] = hi16(raw.z); v[6] = lo16(raw.w); v[7] = hi16(raw.w);
+                            }
                         }
-                        if (j % GS == GS - 1) {
-                            const unsigned sw = s[p][j / GS / 2];
-                            const float sc = GS < 4 && (j / GS) % 2 ? hi16(sw) : lo16(sw);
+                        unsigned out[3][4];
 #pragma unroll
-                            for (int t = 0; t < MT; ++t)
+                        for (int e = 0; e < 8; ++e) {
+                            bf16_t p[3];
+                            w4_split(a.silu ? silu_f(v[e]) : v[e], p);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(part[t][e], sc, acc[t][e]);
+                            for (int q = 0; q < 3; ++q) out[q][e >> 1] = e & 1 ? out[q][e >> 1] | (unsigned)p[q] << 16 : p[q];
+                        }
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) {
+                            const int row = m * 3 + q - r * 16;
+                            if (row >= 0 && row < 16) *reinterpret_cast<uint4*>(xs + (size_t)row * pitch + col) = make_uint4(out[q][0], out[q][1], out[q][2], out[q][3]);
                         }
                     }
-                    if (i + PF < n_t) fetch(p, first + (i + PF) * c.waves_k);
+                    __syncthreads();
+                    const int row = r * 16 + l16 < rows * 3 ? l16 : 0; // (pieces that do not exist: the first one's, not stored in the end)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) xf[t][j][r] = *reinterpret_cast<const bf16x8_t*>(xs + (size_t)row * pitch + wave * W4_COLS + j * 32 + lq * 8);
+                }
+            __syncthreads();                                           // the parts may take the same room
+        }
+
+        for (int i0 = 0; i0 < n_n; i0 += U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int n = i0 + u;
+                if (n < n_n) {
+                    f32x4_t acc[MT];
+#pragma unroll
+                    for (int r = 0; r < MT; ++r) acc[r] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+                        if (t < n_t) {
+                            f32x4_t part[MT];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const bf16x8_t b = w4_operand(w[u][t][j]);
+#pragma unroll
+                                for (int r = 0; r < MT; ++r) part[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[t][j][r], b, j % GS ? part[r] : f32x4_t{0, 0, 0, 0}, 0, 0, 0);
+                                if (j % GS == GS - 1) {
+                                    const unsigned sw = s[u][t][j / GS / 2];
+                                    const float sc = GS < 4 && (j / GS) % 2 ? hi16(sw) : lo16(sw);
+#pragma unroll
+                                    for (int r = 0; r < MT; ++r)
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(part[r][e], sc, acc[r][e]);
+                                }
+                            }
+                        }
+                    if (n + U < n_n) fetch(u, n + U);
+                    float* const to = red + ((size_t)n * c.waves_k + wave) * (MT * 256) + lane * 4;      // [row tile][lane][4]: rows lq * 4 + (0..3), output l16
+#pragma unroll
+                    for (int r = 0; r < MT; ++r) {
+                        f32x4_t* const at = reinterpret_cast<f32x4_t*>(to + r * 256);
+                        *at = chunk ? *at + acc[r] : acc[r];
+                    }
                 }
             }
         }
     }
-    // ---- the waves of an output tile and the pieces of a row meet in LDS, in order
+    // ---- the waves of an output tile and the pieces of a row, in order
     __syncthreads();
-    float* const red = reinterpret_cast<float*>(lds);                  // [wave][row of x][16]
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) red[((wave * MT + t) * 16 + lq * 4 + e) * 16 + l16] = acc[t][e];
-    __syncthreads();
-    for (int i = tid; i < c.waves_n * rows * 16; i += threads) {
-        const int col = i & 15, rest = i >> 4, g = rest / rows, m = rest - g * rows, n = (blockIdx.x * c.waves_n + g) * W4_ROWS + col;
+    for (int i = tid; i < n_n * rows * 16; i += threads) {
+        const int col = i & 15, rest = i >> 4, g = rest / rows, m = rest - g * rows, n = (n0 + g) * W4_ROWS + col;
         if (n >= a.N) continue;
         float v = 0.f;
         for (int k = 0; k < c.waves_k; ++k)
-            for (int q = c.pieces - 1; q >= 0; --q) v += red[((g * c.waves_k + k) * MT * 16 + m * c.pieces + q) * 16 + col];
+#pragma unroll
+            for (int q = SPLIT ? 2 : 0; q >= 0; --q) {
+                const int row = SPLIT ? m * 3 + q : m;
+                v += red[((size_t)g * c.waves_k + k) * (MT * 256) + (row >> 4) * 256 + ((row >> 2 & 3) * 16 + col) * 4 + (row & 3)];
+            }
         v *= 16.f;
         if (a.bias) v += a.bias_f32 ? ((const float*)a.bias)[n] : bf2f(((const bf16_t*)a.bias)[n]);
         const size_t at = (size_t)(m0 + m) * a.y_stride + n;
@@ -225,20 +263,21 @@ __global__ __launch_bounds__(1024) void w4_linear_kernel(const W4Args a) {
 #endif
 }
 
-template <int MT, int GS> static int launch_w4(const W4Args& a, hipStream_t st) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&w4_linear_kernel<MT, GS>), hipFuncAttributeMaxDynamicSharedMemorySize, W4_LDS);
+template <int MT, int KT, int GS, bool SPLIT> static int launch_w4(const W4Args& a, hipStream_t st) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&w4_linear_kernel<MT, KT, GS, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, W4_LDS);
     if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_w4_linear: cannot raise the dynamic LDS limit");
     const W4Choice& c = a.c;
     {
         const double bytes = (double)a.N * a.K / 2 + 2.0 * a.N * a.groups + (double)a.M * a.K * (a.x_f32 ? 4 : 2) + (double)a.M * a.N * (a.y_f32 ? 4 : 2);
         ProfileScope prof(PROF_ROWS_GEMM, 2.0 * a.M * a.N * a.K, bytes, st);
-        hipLaunchKernelGGL((w4_linear_kernel<MT, GS>), dim3((unsigned)ceil_div(ceil_div(a.N, W4_ROWS), c.waves_n), (unsigned)c.slabs), dim3(64u * c.waves_n * c.waves_k), (size_t)c.lds, st, a);
+        hipLaunchKernelGGL((w4_linear_kernel<MT, KT, GS, SPLIT>), dim3((unsigned)c.groups_n, (unsigned)c.slabs), dim3(64u * c.waves_k), (size_t)c.lds, st, a);
     }
     FISE_CHECK_LAUNCH("fise_w4_linear");
     return FISE_OK;
 }
-template <int MT> static int launch_w4(const W4Args& a, int group, hipStream_t st) {
-    return group == 32 ? launch_w4<MT, 1>(a, st) : group == 64 ? launch_w4<MT, 2>(a, st) : launch_w4<MT, 4>(a, st);
+template <int MT, int KT> static int launch_w4(const W4Args& a, int group, hipStream_t st) {
+    if (a.c.pieces == 3) return group == 32 ? launch_w4<MT, KT, 1, true>(a, st) : group == 64 ? launch_w4<MT, KT, 2, true>(a, st) : launch_w4<MT, KT, 4, true>(a, st);
+    return group == 32 ? launch_w4<MT, KT, 1, false>(a, st) : group == 64 ? launch_w4<MT, KT, 2, false>(a, st) : launch_w4<MT, KT, 4, false>(a, st);
 }
 
 // sizes that pack, unpack and product share; numbers of tiles have 31 bits
@@ -313,6 +352,7 @@ extern "C" int fise_w4_linear(const fise_w4_linear_args* g, void* stream) {
     if (int e = w4_check(fn, g->N, g->K, g->group)) return e;
     if (g->M < 0 || g->M > 1 << 20 || g->x_stride < g->K || g->y_stride < g->N || (g->residual && g->residual_stride < g->N))
         return fail(FISE_ERR_SHAPE, "%s: M=%d, strides x %lld, y %lld, residual %lld", fn, g->M, (long long)g->x_stride, (long long)g->y_stride, (long long)g->residual_stride);
+    if (g->x_stride > 1 << 23) return fail(FISE_ERR_SHAPE, "%s: rows of x %lld apart (at most 2^23)", fn, (long long)g->x_stride);      // a slab's offsets have 31 bits
     if (g->K % 8 || g->x_stride % 8 || !aligned16(g->x) || !aligned16(g->packed))
         return fail(FISE_ERR_ALIGN, "%s: K and the row stride of x must be multiples of 8, x and the weights 16-byte aligned", fn);
     const size_t ye = g->y_dtype == FISE_F32 ? 4 : 2, be = g->bias_dtype == FISE_F32 ? 4 : 2;
@@ -329,5 +369,7 @@ extern "C" int fise_w4_linear(const fise_w4_linear_args* g, void* stream) {
     a.c = w4_choose(g->M, g->N, g->K, a.x_f32 || a.silu);
     if (a.c.slabs > 65535) return fail(FISE_ERR_SHAPE, "%s: M=%d rows", fn, g->M);
     const hipStream_t st = as_stream(stream);
-    return a.c.mt == 1 ? launch_w4<1>(a, g->group, st) : a.c.mt == 2 ? launch_w4<2>(a, g->group, st) : launch_w4<4>(a, g->group, st);
+    if (a.c.mt == 1) return a.c.kt == 1 ? launch_w4<1, 1>(a, g->group, st) : a.c.kt == 2 ? launch_w4<1, 2>(a, g->group, st) : launch_w4<1, 4>(a, g->group, st);
+    if (a.c.mt == 2) return a.c.kt == 1 ? launch_w4<2, 1>(a, g->group, st) : launch_w4<2, 2>(a, g->group, st);
+    return launch_w4<4, 1>(a, g->group, st);
 }

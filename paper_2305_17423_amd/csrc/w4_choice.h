@@ -22,27 +22,38 @@ inline W4Layout w4_layout(int N, int K, int group) {
 }
 
 // ---- the launch.  A row of x is one row of the matrix instruction, or three where x is float or goes through SiLU (its value as the sum of three bf16
-// numbers, which is exact); a workgroup takes up to 64 of those (one `slab`) and waves_n tiles of 16 outputs, each of them by waves_k waves that share its
-// columns.  x passes through LDS in chunks of `chunk` tile columns.
-struct W4Choice { int pieces, slab, slabs, mt, waves_n, waves_k, chunk, pitch, lds; };
+// numbers, which is exact); a workgroup takes up to 64 of those (a `slab`): mt tiles of 16.  Its waves_k waves split the columns, kt tile columns each (x of those stays
+// in registers, 64 of them at most, so kt * mt is at most 4), in `chunks` rounds where that does not cover all; every wave goes through the workgroup's tiles_n tiles of
+// outputs, and what the waves have of an output meets in LDS.
+struct W4Choice { int pieces, slab, slabs, mt, kt, waves_k, chunks, tiles_n, groups_n, x_at, lds; };
 constexpr int W4_LDS = 152 * 1024;
 inline W4Choice w4_choose(int M, int N, int K, bool split) {
     W4Choice c;
     c.pieces = split ? 3 : 1;
-    c.slab = std::min(M, 64 / c.pieces); c.slabs = (M + c.slab - 1) / c.slab;
-    const int rows = c.slab * c.pieces;
-    c.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const W4Layout l = w4_layout(N, K, 128);
     const int tk = (int)l.tiles_k;
-    const long long tiles = l.tiles_n * c.slabs;
-    c.waves_k = tiles < 512 ? 16 : tiles < 1024 ? 8 : 4;
-    while (c.waves_k > 1 && c.waves_k / 2 >= tk) c.waves_k /= 2;
-    c.waves_n = std::max(1, 8 / c.waves_k);
-    const int waves = c.waves_n * c.waves_k;
-    const int room = (waves > 8 ? W4_LDS : W4_LDS / 2);
-    c.chunk = std::min<long long>(tk, (room / (2 * rows) - 8) / W4_COLS);
-    c.pitch = c.chunk * W4_COLS + 8;
-    c.lds = std::max(rows * c.pitch * 2, waves * c.mt * 1024);
+    // slabs of the fewest row tiles that still leave at most one workgroup for every CU: fewer rows are less x to read for every one of them (27 rows, 1283 outputs, 5120
+    // columns: two of 16 rows 8.6 us, one of 27 11.7); else, and with many outputs, as many rows as fit, so that weights are read once
+    for (c.mt = 1;; c.mt *= 2) {
+        c.slab = std::min(M, 16 * c.mt / c.pieces);
+        c.slabs = (M + c.slab - 1) / c.slab;
+        if (c.mt == 4 || c.slabs == 1 || l.tiles_n * c.slabs <= 256) break;
+    }
+    const int kt_max = 4 / c.mt, most = c.mt == 4 ? 8 : 16;                      // tile columns and waves
+    c.kt = 1;
+    while (c.kt < kt_max && (tk + c.kt - 1) / c.kt > most) c.kt *= 2;
+    const int units = (tk + c.kt - 1) / c.kt;
+    c.chunks = (units + most - 1) / most;
+    c.waves_k = (units + c.chunks - 1) / c.chunks;
+    // as many workgroups as the CUs hold at once, but no more outputs a workgroup than LDS holds the parts of
+    const long long at_once = 256 * ((c.mt * c.kt == 1 ? 24 : 16) / c.waves_k);
+    const int x_bytes = split ? 16 * (c.waves_k * W4_COLS + 8) * 2 : 0;          // x of a tile column of every wave, 16 rows at a time, on its way to registers
+    const long long room = (W4_LDS - (c.chunks > 1 ? x_bytes : 0)) / (1024 * c.mt * c.waves_k);
+    c.tiles_n = (int)std::max(1ll, std::min(room, (l.tiles_n * c.slabs + at_once - 1) / at_once));
+    c.groups_n = (int)((l.tiles_n + c.tiles_n - 1) / c.tiles_n);
+    const int parts = c.tiles_n * c.waves_k * c.mt * 1024;
+    c.x_at = c.chunks > 1 ? parts : 0;                                           // one round: before there are parts
+    c.lds = std::max(parts, c.x_at + x_bytes);
     return c;
 }
 
