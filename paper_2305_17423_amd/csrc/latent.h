@@ -43,14 +43,16 @@ template <typename F> __device__ __forceinline__ void la_line(int* table, int gr
 }
 // the workgroup that has block x: the largest w with w total / workgroups <= x
 __device__ __forceinline__ int la_owner(int x, int workgroups, int total) { return (int)((((long long)x + 1) * workgroups - 1) / total); }
-// last group that starts at or before block x
+// last group that starts at or before block x: 64 entries at a time, one trip to memory for up to 64 groups, two for 4096
 __device__ __forceinline__ int la_group(const int* table, int groups, int x) {
     int lo = 0;
-    for (int hi = groups - 1; lo < hi;) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__builtin_amdgcn_readfirstlane(table[mid]) <= x) lo = mid; else hi = mid - 1;
+    for (int n = groups; n > 1;) {
+        const int step = (n + 63) >> 6, i = (int)(threadIdx.x & 63) * step;
+        const int below = __popcll(__ballot(i < n && table[lo + min(i, n - 1)] <= x)) - 1;      // (the first is always)
+        lo += below * step;
+        n = min(step, n - below * step);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 __device__ __forceinline__ void la_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }

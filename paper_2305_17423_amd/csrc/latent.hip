@@ -149,11 +149,11 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
     const unsigned lds0 = (unsigned)(size_t)(FISE_AS3 unsigned char*)(FISE_AS3 void*)lds;
 
     for (int at = line0; at < line1; ++g) {
-        const int g_at = uniform(a.table[g]), g_end = uniform(a.table[g + 1]);
-        const int end = min(line1, g_end);
-        if (end <= at) continue;
         const int b = uniform((int)fdiv((unsigned)g, a.d_tiles)), row0 = (g - b * a.tiles) * LA_ROWS;
-        const int blk0 = at - g_at, blk1 = end - g_at, len = uniform(la_len(a, b));
+        const int2 of_g = make_int2(a.table[g], a.table[g + 1]);       // (with the length: one trip)
+        const int len = uniform(la_len(a, b)), g_at = uniform(of_g.x), end = min(line1, uniform(of_g.y));
+        if (end <= at) continue;
+        const int blk0 = at - g_at, blk1 = end - g_at;
         const int row = row0 + wave * 16 + l16;
         const int sees = row < rows ? la_limit(a, len, (int)fdiv((unsigned)row, a.d_heads)) : len;
         const int limit = min(sees, blk1 * LA_KEYS);                   // (behind this part's last block: nothing)

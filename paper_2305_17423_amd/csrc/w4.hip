@@ -96,6 +96,8 @@ __device__ __forceinline__ bf16x8_t w4_operand(unsigned w) {
 }
 #endif
 
+__device__ __forceinline__ void w4_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }      // (loads to registers that are on their way stay there)
+
 // a value of x as three bf16 numbers that add up to it
 __device__ __forceinline__ void w4_split(float v, bf16_t (&p)[3]) {    // truncated, not rounded: no piece of a finite number overflows, and what is left has 8 bits in the end
     const unsigned a = __float_as_uint(v) & 0xffff0000u;
@@ -106,6 +108,39 @@ __device__ __forceinline__ void w4_split(float v, bf16_t (&p)[3]) {    // trunca
     p[1] = (bf16_t)(b >> 16);
     p[2] = (bf16_t)(__float_as_uint(r1 - __uint_as_float(b)) >> 16);
     if (v != v) p[0] |= 0x40;                                          // a NaN whose bits are all in the lower half stays one
+}
+
+struct W4Eight { uint4 a, b; };                                        // eight values of x as they lie in memory (bf16: the first half)
+__device__ __forceinline__ W4Eight w4_load(const W4Args& g, int m, int k) {
+    W4Eight r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (k >= g.K || m >= g.M) return r;
+    if (g.x_f32) {
+        const uint4* const p = reinterpret_cast<const uint4*>((const float*)g.x + (size_t)m * g.x_stride + k);
+        r.a = p[0]; r.b = p[1];
+    } else r.a = *reinterpret_cast<const uint4*>((const bf16_t*)g.x + (size_t)m * g.x_stride + k);
+    return r;
+}
+__device__ __forceinline__ void w4_pieces(const W4Args& g, const W4Eight& x, unsigned (&out)[3][4]) {
+    const unsigned f[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float v = g.x_f32 ? __uint_as_float(f[e]) : e & 1 ? hi16(f[e >> 1]) : lo16(f[e >> 1]);
+        bf16_t p[3];
+        w4_split(g.silu ? silu_f(v) : v, p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) out[q][e >> 1] = e & 1 ? out[q][e >> 1] | (unsigned)p[q] << 16 : p[q];
+    }
+}
+// What is left when the sums of an output are there (times 1/16, as the weights were): bias, residual, store
+__device__ __forceinline__ void w4_store(const W4Args& a, int m, int n, float v) {
+    v *= 16.f;
+    if (a.bias) v += a.bias_f32 ? ((const float*)a.bias)[n] : bf2f(((const bf16_t*)a.bias)[n]);
+    const size_t at = (size_t)m * a.y_stride + n;
+    if (a.residual) {
+        const size_t ar = (size_t)m * a.residual_stride + n;
+        v += a.y_f32 ? ((const float*)a.residual)[ar] : bf2f(((const bf16_t*)a.residual)[ar]);
+    }
+    if (a.y_f32) ((float*)a.y)[at] = v; else ((bf16_t*)a.y)[at] = f2bf(v);
 }
 
 // MT: tiles of 16 rows of x; KT: tile columns of a wave; GS: matrix instructions a scale covers (1, 2, 4: groups of 32, 64, 128 and more); SPLIT: three pieces a value.
@@ -167,26 +202,8 @@ __global__ __launch_bounds__(MT == 4 ? 512 : 1024) void w4_linear_kernel(const W
                     for (int i = tid; i < (mhi - mlo) * (cols / 8); i += threads) {
                         const int m = mlo + i / (cols / 8), col = (i - (m - mlo) * (cols / 8)) * 8;
                         const int k = ((chunk * c.waves_k + col / W4_COLS) * KT + t) * W4_COLS + col % W4_COLS;
-                        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                        if (k < a.K) {
-                            if (a.x_f32) {
-                                const float* const p = (const float*)a.x + (size_t)(m0 + m) * a.x_stride + k;
-                                const float4 lo = *reinterpret_cast<const float4*>(p), hi = *reinterpret_cast<const float4*>(p + 4);
-                                v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
-                            } else {
-                                const uint4 raw = *reinterpret_cast<const uint4*>((const bf16_t*)a.x + (size_t)(m0 + m) * a.x_stride + k);
-                                v[0] = lo16(raw.x); v[1] = hi16(raw.x); v[2] = lo16(raw.y); v[3] = hi16(raw.y);
-                                v[4] = lo16(raw.z); v[5] = hi16(raw.z); v[6] = lo16(raw.w); v[7] = hi16(raw.w);
-                            }
-                        }
                         unsigned out[3][4];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            bf16_t p[3];
-                            w4_split(a.silu ? silu_f(v[e]) : v[e], p);
-#pragma unroll
-                            for (int q = 0; q < 3; ++q) out[q][e >> 1] = e & 1 ? out[q][e >> 1] | (unsigned)p[q] << 16 : p[q];
-                        }
+                        w4_pieces(a, w4_load(a, m0 + m, k), out);
 #pragma unroll
                         for (int q = 0; q < 3; ++q) {
                             const int row = m * 3 + q - r * 16;
@@ -251,14 +268,124 @@ __global__ __launch_bounds__(MT == 4 ? 512 : 1024) void w4_linear_kernel(const W
                 const int row = SPLIT ? m * 3 + q : m;
                 v += red[((size_t)g * c.waves_k + k) * (MT * 256) + (row >> 4) * 256 + ((row >> 2 & 3) * 16 + col) * 4 + (row & 3)];
             }
-        v *= 16.f;
-        if (a.bias) v += a.bias_f32 ? ((const float*)a.bias)[n] : bf2f(((const bf16_t*)a.bias)[n]);
-        const size_t at = (size_t)(m0 + m) * a.y_stride + n;
-        if (a.residual) {
-            const size_t ar = (size_t)(m0 + m) * a.residual_stride + n;
-            v += a.y_f32 ? ((const float*)a.residual)[ar] : bf2f(((const bf16_t*)a.residual)[ar]);
+        w4_store(a, m0 + m, n, v);
+    }
+#endif
+}
+
+// The staged form.  Every wave has a tile of outputs (or waves_k waves share one and take turns with its tile columns) and all rows; x of the next four tile columns is on its
+// way to registers while these are multiplied, and goes to the other half of LDS behind them.
+template <int MT, int GS, bool SPLIT>
+__global__ __launch_bounds__(512) void w4_staged_kernel(const W4Args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    constexpr int ROWS = MT * 16, PITCH = W4_STAGE_PITCH, PIECES = W4_STAGE_COLS / 8, NS = 4 / GS, SW = (NS + 1) / 2;
+    constexpr int SRC_ROWS = SPLIT ? (ROWS - 1) / 3 : ROWS, LOADS = (SRC_ROWS * PIECES + 511) / 512;      // rows of x of a slab, pieces of eight columns a lane
+    bf16_t* const xs = reinterpret_cast<bf16_t*>(lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, lq = lane >> 4;
+    const W4Choice& c = a.c;
+    const int kw = wave % c.waves_k, nw = wave / c.waves_k, m0 = blockIdx.y * c.slab, rows = min(c.slab, a.M - m0);
+    const int all_n = (a.N + W4_ROWS - 1) / W4_ROWS, n0 = blockIdx.x * c.tiles_n, tn = min(n0 + nw, all_n - 1);      // (behind the last tile: that one again, not stored)
+
+    W4Eight raw[LOADS];
+    auto load_x = [&](int chunk) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int p = tid + i * 512, m = p / PIECES, k = chunk * W4_STAGE_COLS + p % PIECES * 8;
+            raw[i] = m < rows ? w4_load(a, m0 + m, k) : W4Eight{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
         }
-        if (a.y_f32) ((float*)a.y)[at] = v; else ((bf16_t*)a.y)[at] = f2bf(v);
+    };
+    auto put_x = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int p = tid + i * 512, m = p / PIECES;
+            if (m >= SRC_ROWS) continue;
+            bf16_t* const to = xs + (size_t)(half * ROWS + (SPLIT ? m * 3 : m)) * PITCH + p % PIECES * 8;
+            if constexpr (SPLIT) {
+                unsigned out[3][4];
+                w4_pieces(a, raw[i], out);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + q * PITCH) = make_uint4(out[q][0], out[q][1], out[q][2], out[q][3]);
+            } else *reinterpret_cast<uint4*>(to) = raw[i].a;
+        }
+    };
+    // four tile columns of a chunk, of which this wave has every waves_k-th
+    u32x4_t w[2][4];
+    unsigned s[2][4][SW];
+    auto load_w = [&](int set, int chunk) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = min(chunk * 4 + i, a.tiles_k - 1);           // (behind the last column: that one again; x is zeros there)
+            if (i % c.waves_k == kw) {
+                w[set][i] = *reinterpret_cast<const u32x4_t*>(a.tiles + ((size_t)tn * a.tiles_k + t) * W4_TILE_BYTES + lane * 16);
+                const bf16_t* const st = a.scales + (size_t)tn * (GS < 4 ? a.tiles_k * NS : a.groups) * W4_ROWS;
+                if constexpr (GS == 4) s[set][i][0] = st[(size_t)(t >> a.group_shift) * W4_ROWS + l16];
+                else if constexpr (GS == 2) s[set][i][0] = *reinterpret_cast<const unsigned*>(st + ((size_t)t * W4_ROWS + l16) * 2);
+                else { const uint2 v = *reinterpret_cast<const uint2*>(st + ((size_t)t * W4_ROWS + l16) * 4); s[set][i][0] = v.x; s[set][i][SW - 1] = v.y; }
+            }
+        }
+    };
+    f32x4_t acc[MT];
+#pragma unroll
+    for (int r = 0; r < MT; ++r) acc[r] = f32x4_t{0, 0, 0, 0};
+    const bf16_t* const from = xs + (size_t)l16 * PITCH + lq * 8;
+    auto multiply = [&](int set, int chunk) {
+        const int half = chunk & 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i % c.waves_k == kw && chunk * 4 + i < a.tiles_k) {
+                f32x4_t part[MT];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8_t b = w4_operand(w[set][i][j]);
+#pragma unroll
+                    for (int r = 0; r < MT; ++r) {
+                        const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(from + (size_t)(half * ROWS + r * 16) * PITCH + i * W4_COLS + j * 32);
+                        part[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b, j % GS ? part[r] : f32x4_t{0, 0, 0, 0}, 0, 0, 0);
+                    }
+                    if (j % GS == GS - 1) {
+                        const unsigned sw = s[set][i][j / GS / 2];
+                        const float sc = GS < 4 && (j / GS) % 2 ? hi16(sw) : lo16(sw);
+#pragma unroll
+                        for (int r = 0; r < MT; ++r)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(part[r][e], sc, acc[r][e]);
+                    }
+                }
+            }
+    };
+    if constexpr (SPLIT)                                               // the row that three pieces leave over
+        for (int i = tid; i < 2 * PITCH / 8; i += 512) *reinterpret_cast<uint4*>(xs + (size_t)((i / (PITCH / 8)) * ROWS + ROWS - 1) * PITCH + i % (PITCH / 8) * 8) = make_uint4(0, 0, 0, 0);
+    load_x(0);
+    load_w(0, 0);
+    put_x(0);
+    for (int chunk = 0; chunk < c.chunks; chunk += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int at = chunk + u;
+            if (at >= c.chunks) break;
+            w4_barrier();                                              // x of this chunk is there, that of the chunk before has been read
+            if (at + 1 < c.chunks) { load_w(u ^ 1, at + 1); load_x(at + 1); }
+            multiply(u, at);
+            if (at + 1 < c.chunks) put_x((at + 1) & 1);
+        }
+    }
+    __syncthreads();
+    float* const red = reinterpret_cast<float*>(lds);                  // [wave][row tile][lane][4]
+#pragma unroll
+    for (int r = 0; r < MT; ++r) *reinterpret_cast<f32x4_t*>(red + (wave * MT + r) * 256 + lane * 4) = acc[r];
+    __syncthreads();
+    for (int i = tid; i < c.tiles_n * rows * 16; i += 512) {
+        const int col = i & 15, rest = i >> 4, g = rest / rows, m = rest - g * rows, n = (n0 + g) * W4_ROWS + col;
+        if (n >= a.N) continue;
+        float v = 0.f;
+        for (int k = 0; k < c.waves_k; ++k)
+#pragma unroll
+            for (int q = SPLIT ? 2 : 0; q >= 0; --q) {
+                const int row = SPLIT ? m * 3 + q : m;
+                v += red[((g * c.waves_k + k) * MT + (row >> 4)) * 256 + ((row >> 2 & 3) * 16 + col) * 4 + (row & 3)];
+            }
+        w4_store(a, m0 + m, n, v);
     }
 #endif
 }
@@ -274,6 +401,22 @@ template <int MT, int KT, int GS, bool SPLIT> static int launch_w4(const W4Args&
     }
     FISE_CHECK_LAUNCH("fise_w4_linear");
     return FISE_OK;
+}
+template <int MT, int GS, bool SPLIT> static int launch_staged(const W4Args& a, hipStream_t st) {
+    constexpr int lds = 2 * MT * 16 * W4_STAGE_PITCH * 2;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&w4_staged_kernel<MT, GS, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_w4_linear: cannot raise the dynamic LDS limit");
+    {
+        const double bytes = (double)a.N * a.K / 2 + 2.0 * a.N * a.groups + (double)a.M * a.K * (a.x_f32 ? 4 : 2) + (double)a.M * a.N * (a.y_f32 ? 4 : 2);
+        ProfileScope prof(PROF_ROWS_GEMM, 2.0 * a.M * a.N * a.K, bytes, st);
+        hipLaunchKernelGGL((w4_staged_kernel<MT, GS, SPLIT>), dim3((unsigned)a.c.groups_n, (unsigned)a.c.slabs), dim3(512), lds, st, a);
+    }
+    FISE_CHECK_LAUNCH("fise_w4_linear");
+    return FISE_OK;
+}
+template <int MT> static int launch_staged(const W4Args& a, int group, hipStream_t st) {
+    if (a.c.pieces == 3) return group == 32 ? launch_staged<MT, 1, true>(a, st) : group == 64 ? launch_staged<MT, 2, true>(a, st) : launch_staged<MT, 4, true>(a, st);
+    return group == 32 ? launch_staged<MT, 1, false>(a, st) : group == 64 ? launch_staged<MT, 2, false>(a, st) : launch_staged<MT, 4, false>(a, st);
 }
 template <int MT, int KT> static int launch_w4(const W4Args& a, int group, hipStream_t st) {
     if (a.c.pieces == 3) return group == 32 ? launch_w4<MT, KT, 1, true>(a, st) : group == 64 ? launch_w4<MT, KT, 2, true>(a, st) : launch_w4<MT, KT, 4, true>(a, st);
@@ -369,6 +512,7 @@ extern "C" int fise_w4_linear(const fise_w4_linear_args* g, void* stream) {
     a.c = w4_choose(g->M, g->N, g->K, a.x_f32 || a.silu);
     if (a.c.slabs > 65535) return fail(FISE_ERR_SHAPE, "%s: M=%d rows", fn, g->M);
     const hipStream_t st = as_stream(stream);
+    if (a.c.staged) return a.c.mt == 2 ? launch_staged<2>(a, g->group, st) : launch_staged<4>(a, g->group, st);
     if (a.c.mt == 1) return a.c.kt == 1 ? launch_w4<1, 1>(a, g->group, st) : a.c.kt == 2 ? launch_w4<1, 2>(a, g->group, st) : launch_w4<1, 4>(a, g->group, st);
     if (a.c.mt == 2) return a.c.kt == 1 ? launch_w4<2, 1>(a, g->group, st) : launch_w4<2, 2>(a, g->group, st);
     return launch_w4<4, 1>(a, g->group, st);

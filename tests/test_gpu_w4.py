@@ -61,7 +61,10 @@ CASES = [(1, 1280, 320, 32, "f32", "f32", False, False), (2, 513, 1280, 64, "f32
          (27, 129, 5120, 128, "bf16", "bf16", False, True), (64, 96, 1288, 32, "bf16", "bf16", False, False), (65, 33, 256, 64, "bf16", "f32", False, True),
          (130, 64, 520, 256, "bf16", "bf16", True, False), (5, 50, 384, 32, "f32", "bf16", True, True), (21, 40, 128, 128, "f32", "f32", False, False),
          (22, 40, 264, 64, "f32", "f32", True, False), (16, 9000, 8192, 128, "bf16", "bf16", False, False), (64, 17000, 512, 64, "bf16", "bf16", False, False),
-         (48, 300, 8200, 256, "bf16", "bf16", False, False), (1, 20160, 1280, 32, "f32", "f32", True, False), (11, 31, 4104, 32, "f32", "f32", False, False)]
+         (48, 300, 8200, 256, "bf16", "bf16", False, False), (1, 20160, 1280, 32, "f32", "f32", True, False), (11, 31, 4104, 32, "f32", "f32", False, False),
+         # more than 16 rows and many columns and outputs: x through LDS, one to four waves an output, 33 to 64 rows, pieces
+         (64, 8200, 2200, 64, "bf16", "bf16", False, True), (40, 4100, 3200, 32, "bf16", "bf16", False, False), (20, 4200, 4104, 256, "bf16", "f32", False, False),
+         (21, 4097, 1160, 128, "f32", "f32", True, False), (70, 2100, 1032, 64, "f32", "bf16", False, True), (25, 30000, 2056, 128, "bf16", "bf16", True, False)]
 
 
 @pytest.mark.parametrize("M,N,K,group,xt,yt,silu,res", CASES)
