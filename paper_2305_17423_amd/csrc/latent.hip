@@ -93,13 +93,15 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
 // the key, and a lane reads the key rows in the order that makes its eight scores those of eight consecutive keys: its probabilities are
 // then, as they stand, its part of the second product's operand.  Sums: the waves exchange probabilities and a wave has all 64 rows x a quarter
 // of the latent channels, whose operand is the same block read turned, so nothing is read twice from memory and no transposed copy exists.
+// Probabilities go in as two bf16 numbers, the second what rounding leaves of the first, for half as many products again: one number's rounding (2^-9 of each term, root mean
+// square) would show as much as that of the result itself.  A long cache still waits for its bytes (32 tokens on 32768 keys: 189 -> 194 us for the whole call).
 // A turn is the scores of one block and the sums of the block before, so that one barrier serves both and neither product waits for the softmax of its own block.
 // A row's reference moves only when a score lies 8 powers of two above it: any reference gives the same quotient, probabilities stay below 256 (a bf16 and a float have
 // the same relative steps there) and the factor for the sums before is 1 almost always.
 template <int R_, int DR_> struct LaTile {
     static constexpr int R = R_, DR = DR_, PIECES = (R + DR) / 8, PITCH = PIECES * 16, TILE = LA_KEYS * PITCH, PER_CU = latent_per_cu(R);
-    static constexpr int RING = R == 128 || (R == 256 && DR) ? 3 : 4, AHEAD = RING - 1, LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32;
-    static constexpr int P = RING * TILE, PB = LA_ROWS * LA_KEYS * 2, ALPHA = P + 2 * PB, AB = LA_ROWS * 4, LDS = ALPHA + 2 * AB;      // probabilities and factors: two of each
+    static constexpr int RING = R <= 256 || (R == 512 && DR) ? 3 : 4, AHEAD = RING - 1, LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32;
+    static constexpr int P = RING * TILE, PB = LA_ROWS * LA_KEYS * 4, ALPHA = P + 2 * PB, AB = LA_ROWS * 4, LDS = ALPHA + 2 * AB;      // probabilities and factors: two of each
     // Place of a row's pieces.  A sixteen-byte read takes lanes 0-3, 12-15, 20-23, 24-27 at once (then the other sixteen of a half wave), which are sixteen keys of the
     // score product's operand, two neighbouring pieces alternating with key / 8; half a turned read takes two pieces of keys k .. k + 3 and k + 8 .. k + 11.  Both
     // meet every bank once.  (Where rows are 128 bytes off a multiple of 256, odd keys are in the other half of the banks anyway.)
@@ -224,7 +226,14 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
                 for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(p[e]); sum += p[e]; }
                 l_run = fmaf(l_run, alpha, sum);
             } else {
-                *reinterpret_cast<uint4*>(lds + T::P + which * T::PB + tid * 16) = make_uint4(f2bf2(p[0], p[1]), f2bf2(p[2], p[3]), f2bf2(p[4], p[5]), f2bf2(p[6], p[7]));
+                unsigned high[4], low[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    high[e] = f2bf2(p[2 * e], p[2 * e + 1]);
+                    low[e] = f2bf2(p[2 * e] - lo16(high[e]), p[2 * e + 1] - hi16(high[e]));
+                }
+                *reinterpret_cast<uint4*>(lds + T::P + which * T::PB + tid * 16) = make_uint4(high[0], high[1], high[2], high[3]);
+                *reinterpret_cast<uint4*>(lds + T::P + which * T::PB + T::PB / 2 + tid * 16) = make_uint4(low[0], low[1], low[2], low[3]);
                 if (lq == 0) *reinterpret_cast<float*>(lds + T::ALPHA + which * T::AB + (wave * 16 + l16) * 4) = alpha;
             }
         };
@@ -263,7 +272,7 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
             }
             // ---- scores of the next block, then sums of this one (a quarter of the latent channels for all 64 rows) with the softmax of the next between them; in this
             // order, which the compiler's own would give up for fewer registers: every product would wait for its operand
-            bf16x8_t pf[4], vf[2];
+            bf16x8_t pf[4], pl[4], vf[2];
             auto read_v = [&](int j) { return la_turned(tile + vat[j % VB] + j / VB * (T::PERIOD * 16), 4 * PITCH); };
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -277,11 +286,15 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
             }
             static_assert(LA_AHEAD > 4, "probabilities and the first values are read with the last scores");
 #pragma unroll
+            for (int t = 0; t < 4; ++t) pl[t] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + which * T::PB + T::PB / 2 + (t * 64 + lane) * 16);
+#pragma unroll
             for (int j = 0; j < RT; ++j) {
                 if (j + 1 < RT) vf[(j + 1) & 1] = read_v(j + 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pf[t], acc[j][t], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pl[t], acc[j][t], 0, 0, 0);
                 if (j * 5 / RT != (j + 1) * 5 / RT || RT < 5)          // five pieces over the RT steps (fewer steps than pieces: what is left at the end)
                     softmax(RT < 5 ? j : j * 5 / RT, (blk + 1) * LA_KEYS, which ^ 1);
                 __builtin_amdgcn_sched_barrier(0);

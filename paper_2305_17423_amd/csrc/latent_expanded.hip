@@ -134,6 +134,8 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 // A turn is: scores of the next block, with the exponentials of this block between the products; sums of this block, with the maximum of the next between them.  So
 // neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
+// Probabilities are two bf16 numbers, as in the absorbed form: 16 heads of 4096 causal queries go from 148 to 174 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
+// the result's own rounding, the rest that of keys and values).
 // Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
 [[maybe_unused]] constexpr int LX_AHEAD = 4;
 template <int KD, int DB>
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                 if (q < NK) fr[q % RING] = read_k(keys, q);
                 else if (q < NK + NV) fr[q % RING] = read_v(values, q - NK);
             };
-            u32x4_t p[4];                                              // probabilities, the operands of the sums
+            u32x4_t p[4], rest[4];                                     // probabilities, the operands of the sums, and what their rounding left
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q) fetch(q);
@@ -324,6 +326,9 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                         unsigned pair = f2bf2(c[e % 16 - 1], x);
                         asm volatile("" : "+v"(pair), "+v"(l_run));    // here, not behind the branch in front of their use
                         p[e / 8][e / 2 % 4] = pair;
+                        unsigned less = f2bf2(c[e % 16 - 1] - lo16(pair), x - hi16(pair));
+                        asm volatile("" : "+v"(less));
+                        rest[e / 8][e / 2 % 4] = less;
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -334,7 +339,9 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                 fetch(NK + q + AHEAD);
                 __builtin_amdgcn_sched_barrier(0);
                 const bf16x8_t pf = *reinterpret_cast<const bf16x8_t*>(&p[q / DB]);
+                const bf16x8_t rf = *reinterpret_cast<const bf16x8_t*>(&rest[q / DB]);
                 o[q % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[(NK + q) % RING], pf, o[q % DB], 0, 0, 0);
+                o[q % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[(NK + q) % RING], rf, o[q % DB], 0, 0, 0);
                 // the score products' results are there once a few of these have gone out
 #pragma unroll
                 for (int st = 0; st < 8; ++st)
