@@ -86,7 +86,8 @@ CASES = [(1, 1, 1, 1, 8, 0, 8, 8), (1, 1, 1000, 8, 64, 0, 64, 128), (2, 1, 33, 1
          (1, 65, 65, 1, 160, 64, 160, 512), (2, 9, 200, 8, 64, 8, 96, 256), (5, 2, 127, 32, 32, 64, 64, 384), (1, 300, 300, 2, 40, 32, 40, 136), (1, 4, 4100, 8, 128, 64, 128, 512),
          (2, 130, 257, 8, 160, 0, 64, 256), (1, 33, 95, 3, 24, 40, 56, 72), (4, 1, 2049, 64, 128, 64, 128, 512), (1, 200, 64, 16, 128, 64, 128, 512), (2, 768, 1024, 8, 40, 32, 40, 128),
          # a workgroup for every tile of the expanded form: heads in eights and not, several tiles
-         (4, 3, 70, 128, 64, 32, 64, 128), (3, 2, 65, 171, 32, 0, 32, 64), (1, 1100, 130, 64, 128, 64, 128, 512), (1, 140, 200, 128, 160, 64, 160, 256)]
+         (4, 3, 70, 128, 64, 32, 64, 128), (3, 2, 65, 171, 32, 0, 32, 64), (1, 1100, 130, 64, 128, 64, 128, 512), (1, 140, 200, 128, 160, 64, 160, 256),
+         (2, 20, 300, 8, 64, 0, 64, 512), (1, 3, 1500, 24, 64, 0, 64, 440), (2, 130, 140, 6, 64, 64, 64, 128), (1, 150, 300, 5, 64, 40, 56, 264)]
 
 
 @pytest.mark.parametrize("form", [ABSORBED, EXPANDED])

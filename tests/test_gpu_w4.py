@@ -64,7 +64,12 @@ CASES = [(1, 1280, 320, 32, "f32", "f32", False, False), (2, 513, 1280, 64, "f32
          (48, 300, 8200, 256, "bf16", "bf16", False, False), (1, 20160, 1280, 32, "f32", "f32", True, False), (11, 31, 4104, 32, "f32", "f32", False, False),
          # more than 16 rows and many columns and outputs: x through LDS, one to four waves an output, 33 to 64 rows, pieces
          (64, 8200, 2200, 64, "bf16", "bf16", False, True), (40, 4100, 3200, 32, "bf16", "bf16", False, False), (20, 4200, 4104, 256, "bf16", "f32", False, False),
-         (21, 4097, 1160, 128, "f32", "f32", True, False), (70, 2100, 1032, 64, "f32", "bf16", False, True), (25, 30000, 2056, 128, "bf16", "bf16", True, False)]
+         (21, 4097, 1160, 128, "f32", "f32", True, False), (70, 2100, 1032, 64, "f32", "bf16", False, True), (25, 30000, 2056, 128, "bf16", "bf16", True, False),
+         # x of two tiles of rows or of columns, or both, in a wave's registers
+         (1, 40, 2200, 64, "bf16", "bf16", False, False), (7, 700, 3000, 32, "f32", "f32", True, False), (30, 2100, 640, 64, "bf16", "bf16", False, True),
+         (20, 2304, 2200, 128, "bf16", "f32", False, False), (10, 4500, 1160, 256, "f32", "f32", False, False),
+         # and in several rounds, x's parts behind the sums of several tiles of outputs
+         (5, 300, 8328, 64, "f32", "f32", True, False), (2, 4200, 8328, 128, "f32", "f32", False, True), (9, 4200, 4200, 64, "f32", "bf16", True, False)]
 
 
 @pytest.mark.parametrize("M,N,K,group,xt,yt,silu,res", CASES)
