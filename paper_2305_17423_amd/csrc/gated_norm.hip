@@ -15,7 +15,7 @@ struct GatedNorm {
     const void* x; const void* h; void* r; void* y;
     const void* post_w; const void* post_b; const void* pre_w; const void* pre_b;
     const float* gate; const float* scale; const float* shift; long long mod_stride;
-    const int* tile_idx; int tile, tiles_w, HW, W, M, rows, C, pieces;        // M: rows of a batch element; pieces: of eight channels
+    const int* tile_idx; int tile, tiles_w, HW, W, M, rows, row0, C, pieces;  // M: rows of a batch element; row0: of this launch; pieces: of eight channels
     int post, pre, h_is_map, y_is_map;
     float res_scale, eps, channels;
     FastDiv d_M, d_tt, d_tile, d_tiles_w;
@@ -64,9 +64,9 @@ __global__ __launch_bounds__(256) void gated_norm_kernel(const GatedNorm a) {
     int slot = 0;
     constexpr int LANES = 64 * WAVES;
     const int tid = threadIdx.x, lane = WAVES > 1 ? tid : tid & 63;
-    const int row = WAVES > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + (tid >> 6);
-    if (row >= a.rows) return;                                         // (whole waves, and with WAVES > 1 none)
-    const int b = (int)fdiv((unsigned)row, a.d_M), m = row - b * a.M;
+    const unsigned row = a.row0 + (WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + (tid >> 6));
+    if (row >= (unsigned)a.rows) return;                                         // (whole waves, and with WAVES > 1 none)
+    const int b = (int)fdiv(row, a.d_M), m = (int)row - b * a.M;
     int token = m;
     if (a.tile) {
         const int ti = (int)fdiv((unsigned)m, a.d_tt), p = m - ti * a.tile * a.tile, t = a.tile_idx[ti];
@@ -166,9 +166,13 @@ __global__ __launch_bounds__(256) void gated_norm_kernel(const GatedNorm a) {
         }
 }
 
-template <typename T, int WAVES, int J> static int launch_gated(const GatedNorm& a, hipStream_t st) {
-    hipLaunchKernelGGL((gated_norm_kernel<T, WAVES, J>), dim3((unsigned)(WAVES > 1 ? a.rows : ceil_div(a.rows, 4))), dim3(256), 0, st, a);
-    FISE_CHECK_LAUNCH("fise_masked_gated_norm");
+template <typename T, int WAVES, int J> static int launch_gated(GatedNorm a, hipStream_t st) {
+    constexpr int per = WAVES > 1 ? 1 : 4, most = 1 << 23;             // rows of a workgroup; workgroups of a launch, whose lanes are counted in 32 bits
+    for (long long row0 = 0; row0 < a.rows; row0 += (long long)most * per) {
+        a.row0 = (int)row0;
+        hipLaunchKernelGGL((gated_norm_kernel<T, WAVES, J>), dim3((unsigned)std::min<long long>((a.rows - row0 + per - 1) / per, most)), dim3(256), 0, st, a);
+        FISE_CHECK_LAUNCH("fise_masked_gated_norm");
+    }
     return FISE_OK;
 }
 // A wave for rows of up to 512 channels, else the four of a workgroup, with as many pieces a lane as the row has.

@@ -169,3 +169,20 @@ def test_captured_and_replayed(fb):
         gr.replay()
         torch.cuda.synchronize()
         assert torch.equal(r, want[0]) and torch.equal(y, want[1]), rep
+
+
+@pytest.mark.parametrize("H,W,C", [(8192, 4097, 8), (4096, 2049, 520)])
+def test_more_rows_than_a_launch_has(fb, H, W, C):
+    x = torch.zeros((1, H, W, C), dtype=torch.bfloat16, device=DEV)
+    y = torch.full_like(x, float("nan"))
+    g = torch.Generator().manual_seed(8)
+    at = torch.tensor([0, 1, 2 ** 23 - 1, 2 ** 23, 2 ** 23 + 5, H * W // 2, 2 ** 25 - 1, 2 ** 25, H * W - 1])
+    at = at[at < H * W]
+    rows = torch.randn((at.numel(), C), generator=g).to(torch.bfloat16)
+    x.view(-1, C)[at.to(DEV)] = rows.to(DEV)
+    fb.fise_masked_gated_norm(fb.gated_norm_args(x, pre="layer", y=y))
+    want, mag, wy, my = reference(rows[None], None, None, None, None, "none", None, None, "layer", None, None, 1.0, 1e-5)
+    close(y.view(-1, C)[at.to(DEV)][None], wy, my)
+    hit = torch.ones(H * W, dtype=torch.bool, device=DEV)
+    hit[at.to(DEV)] = False
+    assert bool((y.view(-1, C)[hit] == 0).all())
