@@ -484,7 +484,7 @@ int fise_w4_unpack(const void* packed, int N, int K, int group, void* w, int dty
  * at a time, the weights read again for each.  x, y and bias have a type of their own
  * (residual has y's); all sums are float: the products of a group first, then those
  * sums times their scale.  x rows: K and x_stride multiples of 8, 16-byte aligned, x_stride at most 2^23; y and
- * residual rows: any alignment of their type.  residual may be y itself; y must not
+ * residual rows: any alignment of their type.  M at most 2^20.  residual may be y itself; y must not
  * otherwise overlap an input.  M == 0 touches nothing. */
 typedef struct {
     const void* x; int x_dtype; int64_t x_stride;           /* [M, K], rows x_stride elements apart */
@@ -536,7 +536,7 @@ int fise_masked_gated_norm(const fise_gated_norm_args* a /* host */, void* strea
  * gives zeros; a key that it does not see has no effect on it, whatever it holds.
  * q [B, M, heads, d + dr], w_uk [heads, d, r], w_uv [heads, dv, r] (out, in), out
  * [B, M, heads * dv].  bf16 only; d, dv, r multiples of 8 up to 160, 160, 512, dr a multiple
- * of 8 up to 64 (0: no shared key); scale > 0.
+ * of 8 up to 64 (0: no shared key); scale > 0; B * M < 2^20, n_keys up to 2^26, heads up to 65535.
  * Forms: ABSORBED brings W_uk to the queries and W_uv to the sums, and every head meets the
  * latent vectors themselves: the cache is read once for 64 (query, head) rows.  EXPANDED
  * makes keys and values of all heads first.  AUTO takes the one that is expected to be faster

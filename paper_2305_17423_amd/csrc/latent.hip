@@ -463,6 +463,7 @@ template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStre
 }
 template <int R> static int launch_absorbed(const LatentArgs& a, hipStream_t st) { return a.dr ? launch_absorbed<R, 64>(a, st) : launch_absorbed<R, 0>(a, st); }
 
+static bool expands(const fise_latent_attention_args* g, const LatentShape& s) { return g->form == FISE_LATENT_AUTO ? latent_expands(s) : g->form == FISE_LATENT_EXPANDED; }
 static int latent_check(const char* fn, const fise_latent_attention_args* g, LatentShape& s) {
     if (!g || !g->q || !g->cache || !g->w_uk || !g->w_uv || !g->out) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
     if (g->dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d (bf16 only)", fn, g->dtype);
@@ -474,17 +475,15 @@ static int latent_check(const char* fn, const fise_latent_attention_args* g, Lat
         if (!aligned16(p)) return fail(FISE_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
     if (!(g->scale > 0) || g->scale > 1e30f) return fail(FISE_ERR_SHAPE, "%s: scale %g", fn, g->scale);
     s = LatentShape{g->B, g->M, g->n_keys, g->heads, g->d, g->dr, g->dv, g->r, g->causal != 0};
-    // row numbers and key blocks are counted in 31 bits, heads and tokens are grid dimensions
+    // rows, blocks of keys and tiles are counted in 31 bits, the lanes of a launch in 32, tokens of the absorbed form are a grid's second dimension
     const long long rows = (long long)g->M * g->heads, tiles = (rows + LA_ROWS - 1) / LA_ROWS, blocks = ((long long)g->n_keys + LA_KEYS - 1) / LA_KEYS;
-    if (g->n_keys > 1 << 26 || rows >= 1ll << 30 || (long long)g->B * tiles >= 1ll << 30 || (long long)g->B * tiles * (blocks + 1) >= 1ll << 31 || (long long)g->B * g->M > 1 << 20 || g->heads > 65535)
+    if (g->n_keys > 1 << 26 || rows >= 1ll << 30 || (long long)g->B * tiles >= 1ll << 30 || (long long)g->B * tiles * (blocks + 1) >= 1ll << 31 || (long long)g->B * g->M >= 1 << 20 || g->heads > 65535)
         return fail(FISE_ERR_SHAPE, "%s: B%d M%d heads%d keys%d: too many rows or key blocks", fn, g->B, g->M, g->heads, g->n_keys);
-    if ((long long)g->B * g->heads * (std::max(g->M, g->n_keys) / 64 + 2) * 10 >= 1ll << 31 ||
-        (long long)g->B * g->heads * (g->M / LX_QUERIES + 1) * ((long long)g->n_keys / LX_BLOCK + 2) >= 1ll << 31)
+    const double groups = (double)g->B * g->heads * expanded_tiles(s), makes = (double)g->B * (g->n_keys / LX_KEYS + 1) * ((double)g->heads * (g->d + g->dv) / 128 + 2);
+    if (expands(g, s) && (groups >= 1 << 24 || makes >= 1 << 24 || groups * (g->n_keys / LX_BLOCK + 1) >= 0x7fffffff))
         return fail(FISE_ERR_SHAPE, "%s: B%d heads%d M%d keys%d: too many tiles", fn, g->B, g->heads, g->M, g->n_keys);
     return FISE_OK;
 }
-
-static bool expands(const fise_latent_attention_args* g, const LatentShape& s) { return g->form == FISE_LATENT_AUTO ? latent_expands(s) : g->form == FISE_LATENT_EXPANDED; }
 
 }  // namespace fise
 

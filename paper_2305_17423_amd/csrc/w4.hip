@@ -510,7 +510,6 @@ extern "C" int fise_w4_linear(const fise_w4_linear_args* g, void* stream) {
     a.residual = g->residual; a.residual_stride = g->residual_stride; a.y = g->y; a.y_stride = g->y_stride; a.y_f32 = g->y_dtype == FISE_F32;
     a.M = g->M;
     a.c = w4_choose(g->M, g->N, g->K, a.x_f32 || a.silu);
-    if (a.c.slabs > 65535) return fail(FISE_ERR_SHAPE, "%s: M=%d rows", fn, g->M);
     const hipStream_t st = as_stream(stream);
     if (a.c.staged) return a.c.mt == 2 ? launch_staged<2>(a, g->group, st) : launch_staged<4>(a, g->group, st);
     if (a.c.mt == 1) return a.c.kt == 1 ? launch_w4<1, 1>(a, g->group, st) : a.c.kt == 2 ? launch_w4<1, 2>(a, g->group, st) : launch_w4<1, 4>(a, g->group, st);

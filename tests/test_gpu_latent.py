@@ -201,3 +201,35 @@ def test_two_captured_graphs_and_eager_calls(fb):
         torch.cuda.synchronize()
         for (a, lens, out, *_), w in zip(calls, want):
             assert torch.equal(out, w), rep
+
+
+@pytest.mark.parametrize("form", [ABSORBED, EXPANDED])
+@pytest.mark.parametrize("M", [1, 200])
+def test_no_keys_at_all(fb, form, M):
+    q, c, wk, wv = inputs(torch.Generator().manual_seed(16), 2, M, 9, 3, 64, 32, 64, 128)
+    assert bool((run(fb, q, c * math.nan, wk, wv, form, 0.1, n_keys=0) == 0).all())
+
+
+@pytest.mark.parametrize("form", [ABSORBED, EXPANDED])
+def test_offsets_past_32_bits(fb, form):
+    """Caches of 4.8 GB an element, keys of 7 GB and values of 5 GB: all keys zeros but a few, the last ones among them, whose shared keys give them scores near ln(n), so
+    that they and the zeros (score 0) each have a part.  Scores are exact; values and output are rounded as ever, and a lane's sum of n / 512 probabilities by 2^-24 each, 5e-4
+    at most, which the tolerance for rounded keys that there are not has room for."""
+    g = torch.Generator().manual_seed(17)
+    B, M, n, H, d, dr, dv, r = 2, 3, 4200000, 2, 160, 64, 160, 512
+    q, few, wk, wv = inputs(g, B, M, 8, H, d, dr, dv, r)
+    at = torch.tensor([0, 77777, n // 2, 3728300, n - 130, n - 64, n - 2, n - 1], device=DEV)
+    q.zero_()
+    q[..., d] = 1
+    few[..., r:] = torch.tensor([15, 15.5, 16, 14, 15.25, 14.5, 15.75, 16.5], device=DEV).to(BF)[None, :, None]
+    cache = torch.zeros((B, n, r + dr), dtype=BF, device=DEV)
+    cache[:, at] = few
+    out = torch.full((B, M, H * dv), float("nan"), dtype=BF, device=DEV)
+    a = fb.latent_attention_args(q, cache, wk, wv, out, 1.0, form=form)
+    fb.fise_latent_attention(a, torch.empty((fb.fise_latent_attention_workspace_bytes(a),), dtype=torch.uint8, device=DEV))
+    e = torch.exp(few[..., r].double().cpu())
+    p = e / (e.sum(-1, keepdim=True) + n - at.numel())
+    assert 0.5 < float(p.sum(-1).min()) and float(p.sum(-1).max()) < 0.95
+    v = torch.einsum("bjr,hdr->bhjd", few[..., :r].double().cpu(), wv.double().cpu())
+    want, spread = torch.einsum("bj,bhjd->bhd", p, v), torch.einsum("bj,bhjd->bhd", p ** 2, v ** 2).sqrt()
+    check(out, tuple(t.reshape(B, 1, -1).expand(B, M, -1) for t in (want, spread)))

@@ -129,3 +129,12 @@ def test_latent_attention_binding_checks_its_tensors():
                 dict(cache=c.transpose(1, 2)), dict(w_uk=wk.transpose(1, 2))):
         with pytest.raises(ValueError):
             fb.latent_attention_args(**{**dict(q=q, cache=c, w_uk=wk, w_uv=wv, out=out, scale=0.2), **bad})
+
+
+@pytest.mark.parametrize("change,code", [({"B": 1 << 10, "M": 1 << 10}, -2), ({"B": 1 << 10, "M": (1 << 10) - 1, "form": 1}, -1), ({"form": 2, "n_keys": 1 << 26, "cache_tokens": 1 << 26}, -2),
+                                         ({"form": 1, "n_keys": 1 << 26, "cache_tokens": 1 << 26, "M": 1}, -1), ({"form": 2, "B": 300, "heads": 65535}, -2), ({"form": 1, "B": 300, "heads": 65535}, -1),
+                                         ({"form": 2, "M": 1 << 10, "heads": 1024}, -1)])
+def test_latent_attention_grids(change, code):
+    """What a launch's grid holds is taken (and ends at the missing workspace), more refused."""
+    assert call("fise_latent_attention", latent, {"M": 1, **change}, None, 0, None) == code
+    assert (fb.fise_latent_attention_workspace_bytes(set_all(latent(), M=change.get("M", 1), **{k: v for k, v in change.items() if k != "M"})) > 0 if code == -1 else True)
