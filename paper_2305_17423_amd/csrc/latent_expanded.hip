@@ -116,13 +116,23 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
         }
     }
     if (!values) {
-        // the shared key (and zeros) behind the channels of the heads that begin in this tile
+        // the shared key (and zeros) behind the channels of the heads that begin in this tile: four pieces on their way at once, each stored for every head
         const int h0 = (w0 + a.d - 1) / a.d, h1 = min((w0 + 127) / a.d + 1, a.heads), tail = (width - a.d) / 8;
-        for (int i = tid; i < (h1 - h0) * 128 * tail; i += 256) {
-            const int c = (i % tail) * 8, key = i / tail % 128, h = h0 + i / (tail * 128);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (c < a.dr && key0 + key < len) v = *reinterpret_cast<const uint4*>(a.cache + ((size_t)b * a.cache_tokens + key0 + key) * (a.r + a.dr) + a.r + c);
-            *reinterpret_cast<uint4*>(a.k + (((size_t)b * a.heads + h) * a.n_pad + key0 + key) * width + a.d + c) = v;
+        for (int i0 = tid; i0 < 128 * tail; i0 += 1024) {
+            u32x4_t v[4];
+            bf16_t* to[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * 256, key = i / tail, c = (i - key * tail) * 8;
+                v[u] = __builtin_amdgcn_raw_buffer_load_b128(keys, c < a.dr ? key * row_bytes + (a.r + c) * 2 : 0x7fffffff, 0, 0);      // (zeros behind the last key)
+                to[u] = a.k + (((size_t)b * a.heads + h0) * a.n_pad + key0 + key) * width + a.d + c;
+            }
+            for (int h = h0; h < h1; ++h)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (i0 + u * 256 < 128 * tail) *reinterpret_cast<u32x4_t*>(to[u]) = v[u];
+                    to[u] += a.n_pad * width;
+                }
         }
     }
 #endif
