@@ -563,13 +563,17 @@ int fise_latent_attention(const fise_latent_attention_args* a /* host */, void* 
  * and the number of launches recorded for `kind`:
  *   0 gathered GEMM over maps (and over 2048 - 4095 compact rows of one output)
  *   1 gathered GEMM with the GEGLU epilogue
- *   2 attention (main kernels)          3 gathered GEMM, 64x128 tiles (>= 4096 compact rows)
+ *   2 attention (main kernels), of latent vectors too
+ *   3 gathered GEMM, 64x128 tiles (>= 4096 compact rows); keys and values made of latent vectors
  *   4 split-K reduce launches           5 gathered GEMM, 32x128 tiles (<= 32 rows of odd widths)
  *   6 gathered GEMM with the GroupNorm prologue / 32-wide K steps, and four columns under a 3x3
  *     kernel behind a GroupNorm
- *   7 attention merge launches          8 empty brackets (fise_profile_calibrate)
- *   9 gathered GEMM over compact rows (fewer than 2048, or several outputs), and cross-attention
- *     that is one launch with the products beside it
+ *   7 attention merge launches, with the latent vectors' values weights where they are one launch
+ *   8 empty brackets (fise_profile_calibrate)
+ *   9 gathered GEMM over compact rows (fewer than 2048, or several outputs), cross-attention
+ *     that is one launch with the products beside it, and products with 4-bit weights
+ * (masked norms, the packing of 4-bit weights and the queries' launch of attention over latent
+ * vectors are not recorded)
  * kind = -1 clears the log.  fise_profile_calibrate records n brackets with no
  * launch inside on `stream`: their average is what a bracket itself adds to every
  * figure above.  All pointers host.  Not thread safe.
