@@ -19,10 +19,13 @@ inline int latent_shared(int dr) { return dr ? 64 : 0; }
 // ---- absorbed form.  Blocks of keys of all (batch element, tile of rows) groups stand in one line, which the workgroups share evenly: workgroup w has
 // blocks w T / G .. (w + 1) T / G of T.  A workgroup's part of a group is a partial result in slot w + group, which no other pair has.
 inline int absorbed_tiles(const LatentShape& s) { return (int)(((long long)s.M * s.heads + LA_ROWS - 1) / LA_ROWS); }
-// As many workgroups as find room on the CUs at once, and two blocks each at least: a partial result costs as much to write and read as a block of keys.
+// As many workgroups as find room on the CUs at once, and two blocks each at least, as a partial result costs as much to write and read as a block of keys; one where its rows
+// are few and short, 8 KB.  us, one and two blocks: 1000 keys, 8 rows of 128 (4 KB) 12.6, 13.4; 4096 keys, 16 rows of 512 (32 KB) 25.3, 23.7; 64 rows of 512 34.4, 30.4.  Four
+// blocks: 14.5, 24.8, 30.1, but 37 instead of 27 where 128 rows have 300 keys.
 inline int absorbed_workgroups(const LatentShape& s) {
     const long long blocks = (long long)s.B * absorbed_tiles(s) * ((s.n + LA_KEYS - 1) / LA_KEYS);
-    return (int)std::max(1ll, std::min<long long>(latent_per_cu(latent_width(s.r)) * LA_CUS, (blocks + 1) / 2));
+    const long long part = std::min<long long>(LA_ROWS, (long long)s.M * s.heads) * latent_width(s.r) * 4, each = part <= 8192 ? 1 : 2;
+    return (int)std::max(1ll, std::min<long long>(latent_per_cu(latent_width(s.r)) * LA_CUS, (blocks + each - 1) / each));
 }
 struct AbsorbedLayout { size_t table, q, ml, part, total; };
 inline AbsorbedLayout absorbed_layout(const LatentShape& s) {
@@ -36,7 +39,8 @@ inline AbsorbedLayout absorbed_layout(const LatentShape& s) {
     l.total = l.part + up(slots * LA_ROWS * R * 4);
     return l;
 }
-// Tokens a workgroup of the last launch (merge, then the values' weights) takes
+// Tokens a workgroup of the last launch (merge, then the values' weights) takes: more read W_uv less often, as long as that leaves workgroups enough.  us of the whole call with
+// 1, 4, 16: 128 rows 40.6, 47.7, 47.7; 1024 rows 77, 65, 68; 2048 rows 246, 224, 228; 16384 rows 410, 200, 158.
 inline int absorbed_tokens(const LatentShape& s) {
     const long long tokens = (long long)s.B * s.M;
     return tokens * s.heads >= 16 * 2 * LA_CUS ? 16 : tokens * s.heads >= 4 * LA_CUS ? 4 : 1;
@@ -53,7 +57,7 @@ inline int expanded_tile(const LatentShape& s) {
 }
 inline int expanded_tiles(const LatentShape& s) { return (s.M + LX_QUERIES - 1) / LX_QUERIES; }
 // Tiles of queries (of an element and head) enough for all workgroups that the CUs hold at once (two each; one of the widest heads): one for each tile.  Fewer: the blocks of
-// keys stand in one line too, and those workgroups share it evenly, three blocks each at least; a cut tile costs its parts written and read again.  us, tiles and line:
+// keys stand in one line too, and those workgroups share it evenly, three blocks each at least (192 queries on 1024 keys: with three 33 us, one and six 39); a cut tile costs its parts written and read again.  us, tiles and line:
 // 512 causal tiles of 2 - 64 blocks 134, 154; 96 tiles of 64 blocks 80, 53; 32 of 64 blocks 108, 78 (the whole call).
 constexpr int expanded_per_cu(int KD) { return KD <= 12 ? 2 : 1; }
 inline long long expanded_groups(const LatentShape& s) { return (long long)s.B * s.heads * expanded_tiles(s); }
@@ -82,7 +86,8 @@ inline ExpandedLayout expanded_layout(const LatentShape& s) {
     return l;
 }
 
-// ---- which form.  Operations of each at the rate that its kernels reach.
+// ---- which form: the one with fewer operations; both reach about the same rate.  us, absorbed and expanded, 4096 keys: 16 heads of 128 + 64, r 512: 64 queries 64, 87;
+// 256 queries 149, 104; 4096 causal queries 1074, 171.  8 heads of 40 + 32, r 128: 16 queries 21, 32; 64 queries 33, 34; 768 79, 57.
 inline bool latent_expands(const LatentShape& s) {
     const double keys = (double)s.n, pairs = (double)s.M * s.heads * (s.causal && s.M > 1 ? keys - 0.5 * std::min<double>(s.M, keys) : keys);
     const double absorbed = pairs * (2.0 * latent_width(s.r) + latent_shared(s.dr)) + (double)s.M * s.heads * s.r * (s.d + s.dv);

@@ -9,7 +9,8 @@ namespace fise {
 // Tiles of 128 keys x 128 weight rows of one batch element on 32x32x16 products, four waves of 64 x 64; both operands run along the latent channels, 64 a step,
 // loaded directly to LDS, a step ahead.  Rows of 128 bytes, sixteen-byte pieces at piece ^ (row / 2 & 7): sixteen rows read at
 // once lie in different banks.  The first index of the product is the one that runs along the
-// result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.
+// result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.  16 heads of 4096 keys, r 512: 27 us, bound by
+// what it reads from the L2 caches again (268 MB); 8 heads of 2 x 4096 keys, r 128: 10 us.
 // Group g of the line: (element, head), and of its tiles of queries in turn the last and the first that are left, which together have as many keys as any other two
 // where rows are causal.
 struct LxGroup { int b, h, tile; };
@@ -144,8 +145,10 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 // A turn is: scores of the next block, with the exponentials of this block between the products; sums of this block, with the maximum of the next between them.  So
 // neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
-// Probabilities are two bf16 numbers, as in the absorbed form: 16 heads of 4096 causal queries go from 148 to 174 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
+// Probabilities are two bf16 numbers, as in the absorbed form: 16 heads of 4096 causal queries go from 148 to 165 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
 // the result's own rounding, the rest that of keys and values).
+// 135 of those 165 us are this kernel's: 16 x 1056 pairs of a tile and a block at 0.66 PFLOP/s, bound by instructions (56 products, 32 exponentials, 40 reads of LDS a turn, which two
+// workgroups on a CU overlap in part).  768 queries on 4096 keys, twice, 8 heads of 40: 30 us.
 // Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
 [[maybe_unused]] constexpr int LX_AHEAD = 4;
 template <int KD, int DB>
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
 }
 
 // Tiles that several workgroups had blocks of: their parts, each with its weight exp2(m - max), divided by the sum.  Tiles without a key: zeros.  DB * 8 lanes a query, four
-// channels each.
+// channels each.  480 parts of 128 queries x 64 channels: 7 us, bound by their 16 MB and one launch.
 template <int DB>
 __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
