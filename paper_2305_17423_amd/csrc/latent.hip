@@ -100,10 +100,10 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
 // bytes do.
 // A row's reference moves only when a score lies 8 powers of two above it: any reference gives the same quotient, probabilities stay below 256 (a bf16 and a float have
 // the same relative steps there) and the factor for the sums before is 1 almost always.
-template <int R_, int DR_> struct LaTile {
+template <int R_, int DR_, int NT> struct LaTile {
     static constexpr int R = R_, DR = DR_, PIECES = (R + DR) / 8, PITCH = PIECES * 16, TILE = LA_KEYS * PITCH, PER_CU = latent_per_cu(R);
-    static constexpr int RING = R <= 256 || (R == 512 && DR) ? 3 : 4, AHEAD = RING - 1, LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32;
-    static constexpr int P = RING * TILE, PB = LA_ROWS * LA_KEYS * 4, ALPHA = P + 2 * PB, AB = LA_ROWS * 4, LDS = ALPHA + 2 * AB;      // probabilities and factors: two of each
+    static constexpr int RING = R <= 256 || (R == 512 && DR && NT == 4) ? 3 : 4, AHEAD = RING - 1, LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32;
+    static constexpr int P = RING * TILE, PB = NT * 16 * LA_KEYS * 4, ALPHA = P + 2 * PB, AB = NT * 16 * 4, LDS = ALPHA + 2 * AB;      // probabilities and factors: two of each
     // Place of a row's pieces.  A sixteen-byte read takes lanes 0-3, 12-15, 20-23, 24-27 at once (then the other sixteen of a half wave), which are sixteen keys of the
     // score product's operand, two neighbouring pieces alternating with key / 8; half a turned read takes two pieces of keys k .. k + 3 and k + 8 .. k + 11.  Both
     // meet every bank once.  (Where rows are 128 bytes off a multiple of 256, odd keys are in the other half of the banks anyway.)
@@ -112,10 +112,12 @@ template <int R_, int DR_> struct LaTile {
     static_assert(TILE % 4096 == 0 && PIECES % PERIOD == 0 && PER_CU * LDS <= 160 * 1024, "whole loads of four waves; LDS of a CU");
 };
 
-template <int R, int DR>
+// NT: tiles of 16 rows that there are (4 but where a token's heads are few): the waves past them have no scores, and the sums are over those only.  16 elements of 16 rows, 8192 keys,
+// whole call: 40 us, with four tiles 45; 32 rows and 1000 keys, r 256: 26, 27.5.
+template <int R, int DR, int NT>
 __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(const LatentArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using T = LaTile<R, DR>;
+    using T = LaTile<R, DR, NT>;
     constexpr int RT = T::RT, KS = T::KS, PITCH = T::PITCH, LPW = T::LPW, AHEAD = T::AHEAD;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4;
@@ -187,11 +189,12 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" ::"v"(qf[ks]));
 
-        f32x4_t acc[RT][4];
+        const bool has_rows = NT == 4 || wave < NT;
+        f32x4_t acc[RT][NT];
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[j][t] = f32x4_t{0, 0, 0, 0};
+            for (int t = 0; t < NT; ++t) acc[j][t] = f32x4_t{0, 0, 0, 0};
         float m_run = -INFINITY, l_run = 0.f;                          // l: of this lane's keys until the end
 
         // Product m of the scores takes key rows of half m & 1, step m >> 1; reads go out LA_AHEAD products before theirs.
@@ -240,10 +243,12 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
             }
         };
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPW) : "memory");
+        if (has_rows) {
 #pragma unroll
-        for (int m = 0; m < NK; ++m) { kf[m % RK] = read_k(lds, m); score(m); }
+            for (int m = 0; m < NK; ++m) { kf[m % RK] = read_k(lds, m); score(m); }
 #pragma unroll
-        for (int i = 0; i < 5; ++i) softmax(i, blk0 * LA_KEYS, 0);
+            for (int i = 0; i < 5; ++i) softmax(i, blk0 * LA_KEYS, 0);
+        }
         int which = 0;
         for (int blk = blk0; blk < blk1; ++blk, which ^= 1) {
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 2) * LPW) : "memory");
@@ -259,58 +264,71 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
                 }
                 la_barrier();
             }
+            if (has_rows) {
 #pragma unroll
-            for (int m = 0; m < LA_AHEAD; ++m) kf[m] = read_k(lds + get, m);
-            float al[4];
+                for (int m = 0; m < LA_AHEAD; ++m) kf[m] = read_k(lds + get, m);
+            }
+            float al[NT];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) al[t] = *reinterpret_cast<const float*>(lds + T::ALPHA + which * T::AB + (t * 16 + l16) * 4);
-            if (__any(al[0] != 1.0f || al[1] != 1.0f || al[2] != 1.0f || al[3] != 1.0f)) {      // a reference has moved, which becomes rare
+            for (int t = 0; t < NT; ++t) al[t] = *reinterpret_cast<const float*>(lds + T::ALPHA + which * T::AB + (t * 16 + l16) * 4);
+            bool moved = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) moved |= al[t] != 1.0f;
+            if (__any(moved)) {                                        // a reference has moved, which becomes rare
 #pragma unroll
                 for (int j = 0; j < RT; ++j)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[j][t][e] *= al[t];
             }
             // ---- scores of the next block, then sums of this one (a quarter of the latent channels for all 64 rows) with the softmax of the next between them; in this
             // order, which the compiler's own would give up for fewer registers: every product would wait for its operand
-            bf16x8_t pf[4], pl[4], vf[2];
+            bf16x8_t pf[NT], pl[NT], vf[2];
             auto read_v = [&](int j) { return la_turned(tile + vat[j % VB] + j / VB * (T::PERIOD * 16), 4 * PITCH); };
+            auto read_p = [&](int t) { return *reinterpret_cast<const bf16x8_t*>(lds + T::P + which * T::PB + (t * 64 + lane) * 16); };
             __builtin_amdgcn_sched_barrier(0);
+            if (has_rows) {
 #pragma unroll
-            for (int m = 0; m < NK; ++m) {
-                if (m + LA_AHEAD < NK) kf[(m + LA_AHEAD) % RK] = read_k(lds + get, m + LA_AHEAD);
-                else if (m + LA_AHEAD < NK + 4) pf[m + LA_AHEAD - NK] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + which * T::PB + ((m + LA_AHEAD - NK) * 64 + lane) * 16);
-                else if (m + LA_AHEAD == NK + 4) vf[0] = read_v(0);
-                __builtin_amdgcn_sched_barrier(0);
-                score(m);
-                __builtin_amdgcn_sched_barrier(0);
+                for (int m = 0; m < NK; ++m) {
+                    if (m + LA_AHEAD < NK) kf[(m + LA_AHEAD) % RK] = read_k(lds + get, m + LA_AHEAD);
+                    else if (m + LA_AHEAD < NK + NT) pf[m + LA_AHEAD - NK] = read_p(m + LA_AHEAD - NK);
+                    else if (m + LA_AHEAD == NK + NT) vf[0] = read_v(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    score(m);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) pf[t] = read_p(t);
+                vf[0] = read_v(0);
             }
             static_assert(LA_AHEAD > 4, "probabilities and the first values are read with the last scores");
 #pragma unroll
-            for (int t = 0; t < 4; ++t) pl[t] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + which * T::PB + T::PB / 2 + (t * 64 + lane) * 16);
+            for (int t = 0; t < NT; ++t) pl[t] = *reinterpret_cast<const bf16x8_t*>(lds + T::P + which * T::PB + T::PB / 2 + (t * 64 + lane) * 16);
 #pragma unroll
             for (int j = 0; j < RT; ++j) {
                 if (j + 1 < RT) vf[(j + 1) & 1] = read_v(j + 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pf[t], acc[j][t], 0, 0, 0);
+                for (int t = 0; t < NT; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pf[t], acc[j][t], 0, 0, 0);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pl[t], acc[j][t], 0, 0, 0);
-                if (j * 5 / RT != (j + 1) * 5 / RT || RT < 5)          // five pieces over the RT steps (fewer steps than pieces: what is left at the end)
+                for (int t = 0; t < NT; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j & 1], pl[t], acc[j][t], 0, 0, 0);
+                if (has_rows && (j * 5 / RT != (j + 1) * 5 / RT || RT < 5))        // five pieces over the RT steps (fewer steps than pieces: what is left at the end)
                     softmax(RT < 5 ? j : j * 5 / RT, (blk + 1) * LA_KEYS, which ^ 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (has_rows)
 #pragma unroll
-            for (int i = RT; i < 5; ++i) softmax(i, (blk + 1) * LA_KEYS, which ^ 1);
+                for (int i = RT; i < 5; ++i) softmax(i, (blk + 1) * LA_KEYS, which ^ 1);
         }
         at = end;
         // ---- partial result of this part of the group
         const size_t slot = (size_t)w + g;
         l_run = la_sum4(l_run);
-        if (lq == 0) a.ml[slot * LA_ROWS + wave * 16 + l16] = make_float2(m_run, l_run);
+        if (has_rows && lq == 0) a.ml[slot * LA_ROWS + wave * 16 + l16] = make_float2(m_run, l_run);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < NT; ++t) {
             if (row0 + t * 16 + l16 >= rows) continue;
             float* const o = a.part + (slot * LA_ROWS + t * 16 + l16) * R + wave * (RT * 16) + lq * 4;
 #pragma unroll
@@ -441,9 +459,9 @@ __global__ __launch_bounds__(512, 4) void latent_values_kernel(const LatentArgs 
 #endif
 }
 
-template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStream_t st) {
-    using T = LaTile<R, DR>;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_absorbed_kernel<R, DR>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+template <int R, int DR, int NT> static int launch_absorbed(const LatentArgs& a, hipStream_t st) {
+    using T = LaTile<R, DR, NT>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&latent_absorbed_kernel<R, DR, NT>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
     if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_latent_attention: cannot raise the dynamic LDS limit");
     const int tokens = a.B * a.M;
     // up to three workgroups a CU, which take several rounds of tokens where there are more
@@ -453,7 +471,7 @@ template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStre
     {
         const double pairs = (double)tokens * a.heads * a.n;
         ProfileScope prof(PROF_ATTENTION, 2.0 * pairs * (2 * a.r + a.dr), 2.0 * a.B * a.n * (a.r + a.dr), st);
-        hipLaunchKernelGGL((latent_absorbed_kernel<R, DR>), dim3((unsigned)a.workgroups), dim3(256), T::LDS, st, a);
+        hipLaunchKernelGGL((latent_absorbed_kernel<R, DR, NT>), dim3((unsigned)a.workgroups), dim3(256), T::LDS, st, a);
     }
     FISE_CHECK_LAUNCH("fise_latent_attention: absorbed");
     {
@@ -462,6 +480,9 @@ template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStre
     }
     FISE_CHECK_LAUNCH("fise_latent_attention: values");
     return FISE_OK;
+}
+template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStream_t st) {
+    return a.M * a.heads <= 16 ? launch_absorbed<R, DR, 1>(a, st) : a.M * a.heads <= 32 ? launch_absorbed<R, DR, 2>(a, st) : launch_absorbed<R, DR, 4>(a, st);
 }
 template <int R> static int launch_absorbed(const LatentArgs& a, hipStream_t st) { return a.dr ? launch_absorbed<R, 64>(a, st) : launch_absorbed<R, 0>(a, st); }
 

@@ -105,6 +105,18 @@ def test_all_keys(fb, B, M, n, H, d, dr, dv, r, form):
     check(run(fb, q, c, wk, wv, form, scale), reference(q, c, wk, wv, [n] * B, scale, False))
 
 
+@pytest.mark.parametrize("M,H", [(1, 5), (2, 8), (1, 17), (4, 8), (3, 11)])
+@pytest.mark.parametrize("r", [128, 256, 384, 512])
+@pytest.mark.parametrize("dr", [0, 64])
+def test_few_rows(fb, M, H, r, dr):
+    """16 rows or fewer, 32 or fewer, more, at every width; causal, lengths that differ."""
+    g = torch.Generator().manual_seed(M * H + r + dr)
+    B, n, lens = 3, 333, [333, 40, 1]
+    q, c, wk, wv = inputs(g, B, M, n, H, 64, dr, 64, r, poison=lens)
+    want = reference(q, c, wk, wv, lens, 0.1, True, ABSORBED)
+    check(run(fb, q, c, wk, wv, ABSORBED, 0.1, kv_len=torch.tensor(lens, dtype=torch.int32, device=DEV), causal=True), want)
+
+
 # lengths of none, one, part and all of the keys, and outside of what there is; behind them NaN; with causal rows, more rows than keys leave rows empty
 LENGTHS = [(4, 1, 300, 8, 64, 32, 64, 128, [0, 1, 300, 129]), (3, 7, 96, 16, 128, 64, 128, 512, [96, 5, 0]), (2, 150, 200, 4, 40, 0, 40, 128, [200, 77]), (2, 70, 33, 2, 80, 64, 80, 320, [33, 32]),
            (6, 3, 500, 30, 128, 64, 64, 256, [500, 0, 0, 64, 65, 3]), (1, 513, 700, 3, 64, 0, 64, 384, [640]), (4, 129, 300, 64, 32, 0, 32, 64, [300, 0, 64, 150]), (1, 1100, 1100, 64, 64, 32, 64, 128, [1100]),
