@@ -145,9 +145,9 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 // A turn is: scores of the next block, with the exponentials of this block between the products; sums of this block, with the maximum of the next between them.  So
 // neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
-// Probabilities are two bf16 numbers, as in the absorbed form: 16 heads of 4096 causal queries go from 148 to 165 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
+// Probabilities are two bf16 numbers, as in the absorbed form: 16 heads of 4096 causal queries go from 148 to 169 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
 // the result's own rounding, the rest that of keys and values).
-// 135 of those 165 us are this kernel's: 16 x 1056 pairs of a tile and a block at 0.66 PFLOP/s, bound by instructions (56 products, 32 exponentials, 40 reads of LDS a turn, which two
+// 135 of those 169 us are this kernel's: 16 x 1056 pairs of a tile and a block at 0.66 PFLOP/s, bound by instructions (56 products, 32 exponentials, 40 reads of LDS a turn, which two
 // workgroups on a CU overlap in part).  768 queries on 4096 keys, twice, 8 heads of 40: 30 us.
 // Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
 [[maybe_unused]] constexpr int LX_AHEAD = 4;
