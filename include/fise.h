@@ -460,6 +460,9 @@ int fise_masked_attention_restricted(const void* x, const void* ln_gamma, const 
  * around a block with its gate and modulation, attention over a cache of latent
  * vectors.  Together they are a block whose weights, cache and conditioning are
  * small; the masked 1x1 convolution writes the latent cache at the active tokens.
+ * An empty selection (M == 0, n_active == 0) or an empty cache (n_keys == 0) leaves
+ * buffers without elements: their pointers are not followed but must not be NULL,
+ * which means a buffer that is missing.
  * ------------------------------------------------------------------------ */
 
 /* 4-bit weights W[N, K] (out, in): W[n, k] = s[n, k / group] * q[n, k], q a whole

@@ -406,6 +406,15 @@ def fise_masked_transformer_block(args, workspace, stream=None):
 
 
 # --------------------------------------------------------------------------- transformer denoisers
+_NOTHING = 256
+
+
+def _pn(t):
+    """Address of a tensor that an empty selection leaves without elements, and so without an address of its own: one that is not NULL, which the library takes for a
+    missing buffer, and which nothing is read from or written to."""
+    return _NOTHING if t is not None and t.numel() == 0 else _p(t)
+
+
 def _like(name, t, shape, dtype):
     """A tensor of that shape and one of those types, contiguous in memory."""
     if tuple(t.shape) != tuple(shape) or t.dtype not in dtype or not t.is_contiguous():
@@ -453,18 +462,18 @@ def w4_linear_args(x, packed, group, y, bias=None, residual=None, silu_in=False)
     N = y.shape[1]
     _packed_size(packed, N, K, group)
     a = fise_w4_linear_args()
-    a.x, a.x_dtype, a.x_stride = _p(x), _dt(x), _rows_of("x", x, (M, K))
+    a.x, a.x_dtype, a.x_stride = _pn(x), _dt(x), _rows_of("x", x, (M, K))
     if M == 1:
         a.x_stride = (K + 7) // 8 * 8
     a.packed, a.N, a.K, a.group = _p(packed), N, K, group
     if bias is not None:
         _like("bias", bias, (N,), (torch.float32, torch.bfloat16))
         a.bias, a.bias_dtype = _p(bias), _dt(bias)
-    a.y, a.y_dtype, a.y_stride = _p(y), _dt(y), _rows_of("y", y, (M, N))
+    a.y, a.y_dtype, a.y_stride = _pn(y), _dt(y), _rows_of("y", y, (M, N))
     if residual is not None:
         if residual.dtype != y.dtype:
             raise ValueError(f"residual is {residual.dtype}, y {y.dtype}")
-        a.residual, a.residual_stride = _p(residual), _rows_of("residual", residual, (M, N))
+        a.residual, a.residual_stride = _pn(residual), _rows_of("residual", residual, (M, N))
     a.M, a.silu_in = M, int(bool(silu_in))
     a.keep = (x, packed, bias, residual, y)
     return a
@@ -491,7 +500,7 @@ def gated_norm_args(x, h=None, post="none", post_w=None, post_b=None, gate=None,
     for name, t in (("h", h), ("y", y)):
         if t is not None:
             _like(name, t, (B, H, W, Cc) if t.dim() == 4 else (B, M, Cc), types)
-            setattr(a, name, _p(t))
+            setattr(a, name, _pn(t))
             setattr(a, name + "_is_map", int(t.dim() == 4))
     if r is not None:
         _like("r", r, (B, H, W, Cc), types)
@@ -538,7 +547,7 @@ def latent_attention_args(q, cache, w_uk, w_uv, out, scale, kv_len=None, n_keys=
     if kv_len is not None:
         _like("kv_len", kv_len, (B,), (torch.int32,))
     a = fise_latent_attention_args()
-    a.q, a.cache, a.kv_len, a.w_uk, a.w_uv, a.out = _p(q), _p(cache), _p(kv_len), _p(w_uk), _p(w_uv), _p(out)
+    a.q, a.cache, a.kv_len, a.w_uk, a.w_uv, a.out = _pn(q), _pn(cache), _p(kv_len), _p(w_uk), _p(w_uv), _pn(out)
     a.B, a.M, a.n_keys, a.cache_tokens = B, M, tokens if n_keys is None else n_keys, tokens
     a.heads, a.d, a.dr, a.dv, a.r = heads, d, dr, dv, r
     a.scale, a.causal, a.form, a.dtype = scale, int(bool(causal)), form, FISE_BF16
