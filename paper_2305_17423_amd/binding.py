@@ -514,7 +514,8 @@ def gated_norm_args(x, h=None, post="none", post_w=None, post_b=None, gate=None,
         if t is not None:
             if t.dtype != torch.float32:
                 raise ValueError(f"{name}: float is what modulations are, got {t.dtype}")
-            strides.add(_rows_of(name, t, (B, Cc)) if B > 1 else 0)
+            apart = _rows_of(name, t, (B, Cc))
+            strides.add(apart if B > 1 else 0)
             setattr(a, name, _p(t))
     if len(strides) > 1:
         raise ValueError(f"gate, mod_scale and mod_shift: rows {sorted(strides)} apart, they share one distance")
