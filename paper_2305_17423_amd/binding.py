@@ -436,8 +436,8 @@ def fise_w4_bytes(N, K, group):
 
 
 def _packed_size(packed, N, K, group):
-    if packed.numel() * packed.element_size() < fise_w4_bytes(N, K, group):
-        raise ValueError(f"packed weights of {N} x {K} in groups of {group} take {fise_w4_bytes(N, K, group)} bytes")
+    if not packed.is_contiguous() or packed.numel() * packed.element_size() < fise_w4_bytes(N, K, group):
+        raise ValueError(f"packed weights of {N} x {K} in groups of {group} take {fise_w4_bytes(N, K, group)} bytes side by side")
 
 
 def fise_w4_pack(w, packed, group, scale=None, stream=None):
@@ -561,6 +561,8 @@ def fise_latent_attention_workspace_bytes(args):
 
 
 def fise_latent_attention(args, workspace, stream=None):
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace: its bytes must lie side by side")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _ck(lib().fise_latent_attention(C.byref(args), _p(workspace), nbytes, _stream(stream)))
 

@@ -28,3 +28,31 @@ def test_modulations_that_fit():
         x, y, mod = torch.zeros((B, 4, 4, 64)), torch.zeros((B, 16, 64)), torch.zeros((B, 192))
         assert fb.gated_norm_args(x, y=y, mod_scale=mod[:, :64], mod_shift=mod[:, 64:128]).mod_stride == (192 if B > 1 else 0)
         assert fb.gated_norm_args(x, y=y, mod_scale=mod[:1, :64].expand(B, 64), mod_shift=mod[:1, 64:128].expand(B, 64)).mod_stride == 0
+
+
+def test_packed_weights_with_gaps():
+    """Bytes that are counted but do not lie side by side: the packed weights are one block of memory."""
+    need = fb.fise_w4_bytes(64, 256, 64)
+    for packed in (torch.zeros(2 * need, dtype=torch.uint8)[::2], torch.zeros((16, need // 8), dtype=torch.uint8)[:, :need // 16]):
+        assert packed.numel() >= need
+        with pytest.raises(ValueError):
+            fb.w4_linear_args(torch.zeros((3, 256)), packed, 64, torch.zeros((3, 64)))
+        with pytest.raises(ValueError):
+            fb.fise_w4_pack(torch.zeros((64, 256)), packed, 64, stream=0)
+        with pytest.raises(ValueError):
+            fb.fise_w4_unpack(packed, torch.zeros((64, 256)), 64, stream=0)
+
+
+def test_workspaces_with_gaps():
+    bf = dict(dtype=torch.bfloat16)
+    q, c, wk, wv, out = (torch.zeros(s, **bf) for s in ((2, 3, 4, 48), (2, 5, 6, 80), (4, 32, 64), (4, 24, 64), (2, 3, 96)))
+    a = fb.latent_attention_args(q, c, wk, wv, out, 0.2)
+    with pytest.raises(ValueError):
+        fb.fise_latent_attention(a, torch.zeros(2 * fb.fise_latent_attention_workspace_bytes(a), dtype=torch.uint8)[::2], stream=0)
+
+
+@pytest.mark.parametrize("kw", [dict(tile_idx=torch.zeros(4, dtype=torch.int32)[::2])])
+def test_lists_with_gaps(kw):
+    x = torch.zeros((2, 8, 8, 64))
+    with pytest.raises(ValueError):
+        fb.gated_norm_args(x, r=x, n_active=2, tile=4, **kw)
