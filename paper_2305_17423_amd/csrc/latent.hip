@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
 template <int R_, int DR_, int NT> struct LaTile {
     static constexpr int R = R_, DR = DR_, PIECES = (R + DR) / 8, PITCH = PIECES * 16, TILE = LA_KEYS * PITCH, PER_CU = latent_per_cu(R);
     static constexpr int RING = R <= 256 || (R == 512 && DR && NT == 4) ? 3 : 4, AHEAD = RING - 1, LPW = TILE / 4096, RT = R / 64, KS = (R + DR) / 32;
-    static constexpr int P = RING * TILE, PB = NT * 16 * LA_KEYS * 4, ALPHA = P + 2 * PB, AB = NT * 16 * 4, LDS = ALPHA + 2 * AB;      // probabilities and factors: two of each
+    static constexpr int P = RING * TILE, PB = NT * 16 * LA_KEYS * 4, ALPHA = P + 2 * PB, AB = NT * 16 * 4, BAD = ALPHA + 2 * AB, LDS = BAD + 16;      // probabilities and factors: two of each; first key that is not finite
     // Place of a row's pieces.  A sixteen-byte read takes lanes 0-3, 12-15, 20-23, 24-27 at once (then the other sixteen of a half wave), which are sixteen keys of the
     // score product's operand, two neighbouring pieces alternating with key / 8; half a turned read takes two pieces of keys k .. k + 3 and k + 8 .. k + 11.  Both
     // meet every bank once.  (Where rows are 128 bytes off a multiple of 256, odd keys are in the other half of the banks anyway.)
@@ -183,6 +183,8 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
             for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(q + ks * 32);
         }
         la_barrier();                                                  // the group before has been read to its end
+        int* const bad = reinterpret_cast<int*>(lds + T::BAD);
+        if (tid == 0) *bad = 0x7fffffff;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) load(blk0 + i);
         // the queries have arrived before the loop (the compiler's count would otherwise wait for every load in flight)
@@ -256,13 +258,18 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
             const unsigned char* const tile = lds + get;
             get = next(get);
             if (a.causal && blk * LA_KEYS + LA_KEYS > limit_first) {
-                // a key that a row does not see takes part with probability 0: what is not finite in it must not
+                // a key that a row does not see takes part with probability 0: what is not finite in it must not.  A row that does see it is NaN (its score is NaN or
+                // infinite, and the probability 0 of a score of -inf meets a value that is not finite)
+                int first = 0x7fffffff;
                 for (int i = tid; i < LA_KEYS * (R / 8); i += 256) {
                     const int key = i / (R / 8), piece = (i - key * (R / 8)) ^ T::swizzle(key);
                     uint4* const at16 = reinterpret_cast<uint4*>(const_cast<unsigned char*>(tile) + key * PITCH + piece * 16);
-                    *at16 = la_finite(*at16);
+                    const uint4 v = *at16, finite = la_finite(v);
+                    if ((v.x ^ finite.x) | (v.y ^ finite.y) | (v.z ^ finite.z) | (v.w ^ finite.w)) { *at16 = finite; first = min(first, blk * LA_KEYS + key); }
                 }
+                if (first != 0x7fffffff) atomicMin(bad, first);
                 la_barrier();
+                if (*bad < limit) l_run = NAN;
             }
             if (has_rows) {
 #pragma unroll
