@@ -544,7 +544,7 @@ int fise_masked_gated_norm(const fise_gated_norm_args* a /* host */, void* strea
  * latent vectors themselves: the cache is read once for 64 (query, head) rows.  EXPANDED
  * makes keys and values of all heads first.  AUTO takes the one that is expected to be faster
  * (few queries: absorbed).  They round at different places (absorbed: the queries behind W_uk,
- * bf16; expanded: keys and values, bf16); probabilities are two bf16 numbers in both (the
+ * bf16; expanded: keys and values, bf16, a value beyond its range infinite); probabilities are two bf16 numbers in both (the
  * second what rounding leaves of the first), sums and softmax statistics float.  Results of a form depend on the arguments only, not on the run.
  * workspace: fise_latent_attention_workspace_bytes(a), which reads sizes, form and pointers but
  * not what they point to.  M == 0 touches nothing; nothing may overlap out. */

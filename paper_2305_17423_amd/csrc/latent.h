@@ -17,6 +17,7 @@ struct LatentArgs {
     // expanded
     int whole;                                           // a workgroup for every tile
     long long n_pad; bf16_t* k; bf16_t* v;               // keys of a head [B, heads, n_pad, 16 KD], values [B, heads * dv, n_pad]
+    unsigned* flags;                                     // [B, value tiles, key tiles]: a byte for each wave that made the tile, not 0 if it holds a value that is not finite
     FastDiv d_heads, d_tiles, d_M;
 };
 
@@ -86,6 +87,11 @@ __device__ __forceinline__ uint4 la_finite(uint4 v) {
         return x;
     };
     return make_uint4(clean(v.x), clean(v.y), clean(v.z), clean(v.w));
+}
+// whether one of those values is not finite
+__device__ __forceinline__ bool la_odd(uint4 v) {
+    const uint4 f = la_finite(v);
+    return ((v.x ^ f.x) | (v.y ^ f.y) | (v.z ^ f.z) | (v.w ^ f.w)) != 0;
 }
 // over the four lanes l, l + 16, l + 32, l + 48
 __device__ __forceinline__ float la_max4(float x) {

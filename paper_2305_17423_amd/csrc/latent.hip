@@ -264,8 +264,8 @@ __global__ __launch_bounds__(256, latent_per_cu(R)) void latent_absorbed_kernel(
                 for (int i = tid; i < LA_KEYS * (R / 8); i += 256) {
                     const int key = i / (R / 8), piece = (i - key * (R / 8)) ^ T::swizzle(key);
                     uint4* const at16 = reinterpret_cast<uint4*>(const_cast<unsigned char*>(tile) + key * PITCH + piece * 16);
-                    const uint4 v = *at16, finite = la_finite(v);
-                    if ((v.x ^ finite.x) | (v.y ^ finite.y) | (v.z ^ finite.z) | (v.w ^ finite.w)) { *at16 = finite; first = min(first, blk * LA_KEYS + key); }
+                    const uint4 v = *at16;
+                    if (la_odd(v)) { *at16 = la_finite(v); first = min(first, blk * LA_KEYS + key); }
                 }
                 if (first != 0x7fffffff) atomicMin(bad, first);
                 la_barrier();
@@ -545,7 +545,7 @@ extern "C" int fise_latent_attention(const fise_latent_attention_args* g, void* 
     const hipStream_t st = as_stream(stream);
     if (expanded) {
         const ExpandedLayout l = expanded_layout(s);
-        a.n_pad = l.n_pad; a.k = (bf16_t*)(ws + l.k); a.v = (bf16_t*)(ws + l.v);
+        a.n_pad = l.n_pad; a.k = (bf16_t*)(ws + l.k); a.v = (bf16_t*)(ws + l.v); a.flags = (unsigned*)(ws + l.flags);
         a.tiles = expanded_tiles(s); a.groups = (int)expanded_groups(s); a.whole = expanded_whole(s); a.workgroups = expanded_workgroups(s); a.d_tiles = fast_div(a.tiles);
         a.table = (int*)(ws + l.table); a.ml = (float2*)(ws + l.ml); a.part = (float*)(ws + l.part);
         return launch_expanded(a, expanded_tile(s), st);

@@ -70,7 +70,8 @@ inline int expanded_workgroups(const LatentShape& s) {
     // (96 tiles of 64 blocks on 480 workgroups 54 us, on 512 57; of 16 blocks 41, 48)
     return (int)(groups <= most && most / groups * groups * 8 >= most * 7 ? most / groups * groups : most);
 }
-struct ExpandedLayout { long long n_pad; size_t table, k, v, ml, part, total; };
+inline long long latent_value_tiles(const LatentShape& s) { return ((long long)s.heads * s.dv + 127) / 128; }
+struct ExpandedLayout { long long n_pad; size_t table, k, v, flags, ml, part, total; };
 inline ExpandedLayout expanded_layout(const LatentShape& s) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     const ExpandedTile t = kExpandedTiles[expanded_tile(s)];
@@ -80,7 +81,8 @@ inline ExpandedLayout expanded_layout(const LatentShape& s) {
     l.table = 0;
     l.k = l.table + up((groups + 1) * 4);
     l.v = l.k + up((size_t)s.B * s.heads * l.n_pad * t.KD * 32);
-    l.ml = l.v + up((size_t)s.B * s.heads * s.dv * l.n_pad * 2);
+    l.flags = l.v + up((size_t)s.B * s.heads * s.dv * l.n_pad * 2);
+    l.ml = l.flags + up((size_t)s.B * latent_value_tiles(s) * (l.n_pad / LX_KEYS) * 4);
     l.part = l.ml + up(slots * LX_QUERIES * 8);
     l.total = l.part + up(slots * LX_QUERIES * t.DB * 128);
     return l;

@@ -18,6 +18,7 @@ __device__ __forceinline__ LxGroup lx_group(const LatentArgs& a, int g) {
     const int bh = (int)fdiv((unsigned)g, a.d_tiles), i = g - bh * a.tiles, b = (int)fdiv((unsigned)bh, a.d_heads);
     return {b, bh - b * a.heads, i & 1 ? i >> 1 : a.tiles - 1 - (i >> 1)};
 }
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 constexpr int LE_STEP = 64, LE_STAGE = 2 * 128 * LE_STEP * 2;
 __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs a, int KD, int key_tiles, int k_tiles, int v_tiles, FastDiv d_key_tiles, FastDiv d_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -105,18 +106,48 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
                     make_uint2(f2bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f2bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
             }
     la_barrier();
+    u16x2_t largest = {0, 0};                                          // bits of the largest magnitude: infinity and NaN are at least 0x7f80
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int col = i * 16 + (tid >> 4), row = (tid & 15) * 8;
         const uint4 v = *reinterpret_cast<const uint4*>(lds + col * 256 + ((tid & 15) ^ (col & 15)) * 16);
         if (values) {
+            for (const unsigned x : {v.x, v.y, v.z, v.w}) {
+                const unsigned bits = x & 0x7fff7fffu;
+                largest = __builtin_elementwise_max(largest, *reinterpret_cast<const u16x2_t*>(&bits));
+            }
             if (w0 + col < n_w) *reinterpret_cast<uint4*>(a.v + ((size_t)b * n_w + w0 + col) * a.n_pad + key0 + row) = v;
         } else if (w0 + row < n_w) {
             const int c = w0 + row, h = c / a.d;
             *reinterpret_cast<uint4*>(a.k + (((size_t)b * a.heads + h) * a.n_pad + key0 + col) * width + (c - h * a.d)) = v;
         }
     }
-    if (!values) {
+    if (values) {
+        const bool odd = __any(largest[0] >= 0x7f80 || largest[1] >= 0x7f80);
+        if (odd) {
+            // Where the latent vector itself is not finite, every channel is NaN: the score of its key is NaN or infinite, and the probability 0 of a score of -inf meets
+            // an infinite value.  (What is infinite without that has overflown, and stays.)
+            unsigned long long bad[2];
+            for (int half = 0; half < 2; ++half) {
+                bool is = false;
+                for (int c = 0; c < a.r; c += 8) {
+                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(keys, (half * 64 + lane) * row_bytes + c * 2, 0, 0);
+                    is |= la_odd(make_uint4(x[0], x[1], x[2], x[3]));
+                }
+                bad[half] = __ballot(is);
+            }
+            asm volatile("" ::: "memory");                             // behind the stores above, of other types
+            const int row = (tid & 15) * 8;
+            const unsigned mine = (unsigned)((row & 64 ? bad[1] : bad[0]) >> (row & 63)) & 255;
+            for (int i = 0; i < 8; ++i) {
+                const int col = i * 16 + (tid >> 4);
+                if (w0 + col < n_w)
+                    for (int e = 0; e < 8; ++e)
+                        if (mine >> e & 1) a.v[((size_t)b * n_w + w0 + col) * a.n_pad + key0 + row + e] = 0x7fc0;
+            }
+        }
+        if (lane == 0) reinterpret_cast<unsigned char*>(a.flags + ((size_t)b * v_tiles + wt - k_tiles) * key_tiles + kt)[wave] = odd;
+    } else {
         // the shared key (and zeros) behind the channels of the heads that begin in this tile: four pieces on their way at once, each stored for every head
         const int h0 = (w0 + a.d - 1) / a.d, h1 = min((w0 + 127) / a.d + 1, a.heads), tail = (width - a.d) / 8;
         for (int i0 = tid; i0 < 128 * tail; i0 += 1024) {
@@ -151,6 +182,43 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // workgroups on a CU overlap in part).  768 queries on 4096 keys, twice, 8 heads of 40: 30 us.
 // Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
 [[maybe_unused]] constexpr int LX_AHEAD = 4;
+
+// Values that are not finite, added to what a wave's queries have (a query sees the keys below `limit`, none that does not exist; part: its partial result, else `out` holds it): the first key
+// of +inf, of -inf and of NaN in each channel tells what a query gets, and parts that find the same ones add the same.  Lanes share the keys; rare, so it is
+// made to be short, not fast.
+__device__ __forceinline__ void lx_add_odd(const LatentArgs& a, int bh, int lane, int limit, float* part, bf16_t* out) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                   // the finite sums are where they belong
+    const int none = 0x7fffffff;
+    auto first = [&](int key) {                                        // over the wave (addresses of shuffles would stay in registers through all blocks)
+        int least = none;
+#pragma unroll 1
+        for (int l = 0; l < 64; ++l) least = min(least, __builtin_amdgcn_readlane(key, l));
+        return least;
+    };
+    const int end = -first(-limit);                                    // the first key that none of them sees
+    for (int c = 0; c < a.dv; ++c) {
+        const bf16_t* const v = a.v + ((size_t)bh * a.dv + c) * a.n_pad;
+        int plus = none, minus = none, nan = none;
+        for (int at = lane * 8; at < end; at += 512) {
+            const uint4 x = *reinterpret_cast<const uint4*>(v + at);
+            if (!la_odd(x)) continue;
+            const unsigned words[4] = {x.x, x.y, x.z, x.w};
+            for (int e = 0; e < 8; ++e) {
+                const unsigned bits = words[e >> 1] >> (e & 1) * 16 & 0xffff;
+                int& to = (bits & 0x7fff) > 0x7f80 ? nan : bits == 0x7f80 ? plus : minus;
+                if ((bits & 0x7f80) == 0x7f80) to = min(to, at + e);
+            }
+        }
+        plus = first(plus); minus = first(minus); nan = first(nan);
+        if ((c >> 2 & 1) != lane >> 5 || limit <= min(min(plus, minus), nan)) continue;
+        const float add = limit > nan || (limit > plus && limit > minus) ? NAN : limit > plus ? INFINITY : -INFINITY;
+        if (part) part[c] += add;
+        else out[c] = f2bf(bf2f(out[c]) + add);
+    }
+#endif
+}
+
 template <int KD, int DB>
 __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kernel(const LatentArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -219,9 +287,8 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
         const int blk0 = at - g_at, blk1 = end - g_at, len = uniform(la_len(a, b));
         const bool whole = blk0 == 0 && end == g_end;
         const int m = m0 + wave * 32 + l32;
-        const bool ok = m < a.M;
         // (behind this part's last block: nothing)
-        const int limit = min(la_limit(a, len, min(m, a.M - 1)), blk1 * LX_BLOCK), seen_by_all = la_limit(a, len, m0), limit_first = min(seen_by_all, blk1 * LX_BLOCK);
+        const int limit = min(la_limit(a, len, min(m, a.M - 1)), blk1 * LX_BLOCK), limit_first = min(la_limit(a, len, m0), blk1 * LX_BLOCK);
 
         const unsigned char* const k = (const unsigned char*)(a.k + (size_t)bh * a.n_pad * (KD * 16));
         const unsigned char* const v = (const unsigned char*)(a.v + (size_t)bh * a.dv * a.n_pad);
@@ -253,6 +320,14 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                 qf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
             }
         }
+        // Values that are not finite are in none of the sums (times what rounding left of a probability, or 0 of a key that a query does not see, they would be NaN), but added
+        // behind them: a part with such a tile of values knows it before its first block.
+        const int row_v = h * a.dv, tile_v = row_v >> 7, tiles_v = ((row_v + a.dv - 1) >> 7) - tile_v + 1, key_tiles = (int)(a.n_pad / LX_KEYS);
+        const unsigned* const flags = a.flags + ((size_t)b * ((a.heads * a.dv + 127) >> 7) + tile_v) * key_tiles;
+        bool odd = false;
+        for (int t = (blk0 >> 1) + lane; t <= (blk1 - 1) >> 1; t += 64)
+            for (int i = 0; i < tiles_v; ++i) odd |= flags[(size_t)i * key_tiles + t] != 0;
+        odd = __any(odd);
         f32x16_t o[DB];
 #pragma unroll
         for (int i = 0; i < DB; ++i)
@@ -302,7 +377,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
             load_v(blk + 1);
             unsigned char* const values = lds + 2 * KB + (blk & 1) * VB;
             const unsigned char* const keys = lds + ((blk + 1) & 1) * KB;
-            if (a.causal && blk * LX_BLOCK + LX_BLOCK > seen_by_all) { // uniform: what a key holds that a query does not see must not matter
+            if (odd) {
 #pragma unroll
                 for (int j = 0; j < DB; ++j) {
                     uint4* const at16 = reinterpret_cast<uint4*>(values + (j * 256 + tid) * 16);
@@ -389,26 +464,32 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
             const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
             l_run = __uint_as_float(p[0]) + __uint_as_float(p[1]);
         }
-        if (!ok) continue;
-        if (whole) {
+        // (places anew: kept through the blocks they would not leave room for these)
+        int again = threadIdx.x & 63;
+        asm volatile("" : "+v"(again));
+        const int half = again >> 5, query = m0 + wave * 32 + (again & 31);
+        if (query >= a.M && !odd) continue;
+        bf16_t* const out = a.out + (((size_t)b * a.M + query) * a.heads + h) * a.dv;
+        const size_t row = ((size_t)w + g) * LX_QUERIES + wave * 32 + (again & 31);
+        float* const part = a.part + row * (DB * 32);
+        if (query < a.M && whole) {
             const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;       // no key seen: zeros
-            bf16_t* const out = a.out + (((size_t)b * a.M + m) * a.heads + h) * a.dv;
 #pragma unroll
             for (int i = 0; i < DB; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int c = i * 32 + q * 8 + hl * 4;
+                    const int c = i * 32 + q * 8 + half * 4;
                     if (c < a.dv) *reinterpret_cast<uint2*>(out + c) = make_uint2(f2bf2(o[i][4 * q] * inv, o[i][4 * q + 1] * inv), f2bf2(o[i][4 * q + 2] * inv, o[i][4 * q + 3] * inv));
                 }
-        } else {
-            const size_t row = ((size_t)w + g) * LX_QUERIES + wave * 32 + l32;
-            if (hl == 0) a.ml[row] = make_float2(m_run, l_run);
+        } else if (query < a.M) {
+            if (half == 0) a.ml[row] = make_float2(m_run, l_run);
 #pragma unroll
             for (int i = 0; i < DB; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<float4*>(a.part + row * (DB * 32) + i * 32 + q * 8 + hl * 4) = make_float4(o[i][4 * q], o[i][4 * q + 1], o[i][4 * q + 2], o[i][4 * q + 3]);
+                    *reinterpret_cast<float4*>(part + i * 32 + q * 8 + half * 4) = make_float4(o[i][4 * q], o[i][4 * q + 1], o[i][4 * q + 2], o[i][4 * q + 3]);
         }
+        if (odd) lx_add_odd(a, bh, again, query < a.M ? limit : 0, whole ? nullptr : part, out);
     }
 #endif
 }
@@ -441,7 +522,8 @@ __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs a) {
             const float4 v = *reinterpret_cast<const float4*>(a.part + (row + (size_t)p * LX_QUERIES) * (DB * 32) + c);
             const float f = __builtin_amdgcn_exp2f(ml.x - base);
             l = fmaf(f, ml.y, l);
-            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+            auto add = [&](float& to, float x) { to = fabsf(x) < INFINITY ? fmaf(f, x, to) : to + x; };      // (what is infinite stays so however little its part weighs)
+            add(o.x, v.x); add(o.y, v.y); add(o.z, v.z); add(o.w, v.w);
         }
         const float inv = l == 0.f ? 0.f : 1.0f / l;
         *reinterpret_cast<uint2*>(a.out + (((size_t)place.b * a.M + m) * a.heads + place.h) * a.dv + c) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));

@@ -1,7 +1,9 @@
 """GPU checks of latent attention where a key or a value is not finite: what a query sees of it comes out as the formula says, what it does not see has no effect.
 
 A latent vector that is not finite makes the score of its key infinite or NaN and every channel of its value infinite or NaN: with a score of +inf the softmax is NaN, with one of
--inf the probability 0 meets an infinite value.  So a query that sees it gets NaN in every channel."""
+-inf the probability 0 meets an infinite value.  So a query that sees it gets NaN in every channel.
+A value beyond the range of bf16 (or float) from a latent vector that is finite is infinite in the expanded form, which rounds values: each query that sees it gets that infinity in its
+channel, NaN where it sees both signs, and the other channels as ever (tolerances as in the tests of finite values)."""
 import math
 
 import pytest
@@ -25,7 +27,37 @@ def places(M, n):
     return sorted({0, n // 3, n - M, n - M + M // 2, n - 2, n - 1} & set(range(n)))
 
 
-@pytest.mark.parametrize("form", [ABSORBED])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_values_that_overflow(fb, shape, causal):  # noqa: F811
+    B, M, n, H, d, dr, dv, r = shape
+    g = torch.Generator().manual_seed(21)
+    q, c, wk, wv = inputs(g, B, M, n, H, d, dr, dv, r)
+    x, h, up, down = r - 3, H - 1, dv - 1, 1
+    c[..., x], wk[..., x], wv[..., x] = 0, 0, 0
+    want = reference(q, c, wk, wv, [n] * B, 0.1, causal)
+    wv[h, up, x], wv[h, down, x] = 4, -4
+    seen = sees(M, n, causal)
+    for first in places(M, n):
+        for second in (None, n - 1):                                            # one key with 8e38 in a channel and -8e38 in another, or a later one the other way round besides
+            if second == first:
+                continue
+            bad = c.clone()
+            bad[:, first, x] = 2e38
+            if second is not None:
+                bad[:, second, x] = -2e38
+            got = run(fb, q, bad, wk, wv, EXPANDED, 0.1, causal=causal).cpu().view(B, M, H, dv)
+            one, other = seen[:, first], seen[:, second] if second is not None else torch.zeros(M, dtype=torch.bool)
+            for channel, sign in ((up, 1.0), (down, -1.0)):
+                is_ = got[:, :, h, channel].float()
+                assert bool(is_[:, one & ~other].eq(sign * math.inf).all()), (first, second, channel)
+                assert bool(is_[:, other & ~one].eq(-sign * math.inf).all()) and bool(is_[:, one & other].isnan().all()), (first, second, channel)
+                keep = got[:, :, h, channel]
+                keep[:, one | other] = want[0].view(B, M, H, dv)[:, one | other][:, :, h, channel].to(keep)
+            check(got.reshape(B, M, -1), want)
+
+
+@pytest.mark.parametrize("form", [ABSORBED, EXPANDED])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("shape", SHAPES)
