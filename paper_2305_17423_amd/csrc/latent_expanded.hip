@@ -333,7 +333,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
         for (int i = 0; i < DB; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-        float m_run = -INFINITY, l_run = 0.f, alpha = 1.f, base = 0.f, top = 0.f;
+        float m_run = -INFINITY, l_run = 0.f, alpha = 1.f, scale = a.scale_log2e, base = 0.f, top = 0.f;
         bf16x8_t fr[RING];
         auto read_k = [&](const unsigned char* tile, int p) {          // product p: step p % KD of the 32 keys p / KD
             const int ks = p % KD;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
             for (int e = step * 4; e < step * 4 + 4; ++e) top = fmaxf(top, (e < 16 ? s : t)[e % 16]);
         };
         // a query's reference moves only when a score lies 8 powers of two above it (see the absorbed form)
-        auto reference = [&] {
+        auto reference = [&](f32x16_t& s, f32x16_t& t) {
             const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             const float mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * a.scale_log2e;
             const float to = mx > m_run + 8.f ? mx : m_run;
@@ -368,6 +368,19 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
             alpha = __builtin_amdgcn_exp2f(m_run - base);
             m_run = to;
             l_run *= alpha;
+            // The exponentials' fma has the scores' products unrounded, the reference is a rounded one: from 2^31 on they are more than 127 apart.  There the scores are
+            // rounded too before the reference is taken off.
+            scale = a.scale_log2e;
+            if (__builtin_expect(__any(fabsf(base) > 0x1p29f), 0)) {
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    float x = (e < 16 ? s : t)[e % 16] * a.scale_log2e;
+                    asm volatile("" : "+v"(x));                        // (not one fma again)
+                    (e < 16 ? s : t)[e % 16] = x - base;
+                }
+                scale = 1.f;
+                base = 0.f;
+            }
         };
         // c0, c1: scores of this block; n0: those of the next block's first 32 keys, the others' take c0, which has been used up by then
         f32x16_t sa, sb, sc;
@@ -407,7 +420,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
 #pragma unroll
                 for (int e = NE * q / NK; e < NE * (q + 1) / NK; ++e) {
                     f32x16_t& c = e < 16 ? c0 : c1;
-                    const float x = __builtin_amdgcn_exp2f(fmaf(c[e % 16], a.scale_log2e, -base));
+                    const float x = __builtin_amdgcn_exp2f(fmaf(c[e % 16], scale, -base));
                     c[e % 16] = x;
                     l_run += x;
                     if (e & 1) {
@@ -436,7 +449,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                     if (st * (NV - 1) / 8 + 1 == q) maximum(n0, c0, st);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            reference();
+            reference(n0, c0);
         };
 #pragma unroll
         for (int ks = 0; ks < KD; ++ks) asm volatile("" ::"v"(qf[ks]));
@@ -449,7 +462,7 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
         mask(sa, sb, blk0);
 #pragma unroll
         for (int st = 0; st < 8; ++st) maximum(sa, sb, st);
-        reference();
+        reference(sa, sb);
         for (int blk = blk0;;) {
             turn(sa, sb, sc, blk);
             if (++blk >= blk1) break;
