@@ -71,6 +71,20 @@ inline int expanded_workgroups(const LatentShape& s) {
     return (int)(groups <= most && most / groups * groups * 8 >= most * 7 ? most / groups * groups : most);
 }
 inline long long latent_value_tiles(const LatentShape& s) { return ((long long)s.heads * s.dv + 127) / 128; }
+// The line has of a head's tiles in turn the last and the first that are left, which together have as many keys as any other two where rows are causal: place i, and the place of a tile.
+constexpr int expanded_line_tile(int i, int tiles) { return i & 1 ? i >> 1 : tiles - 1 - (i >> 1); }
+constexpr int expanded_line_place(int tile, int tiles) { return tile >= tiles >> 1 ? 2 * (tiles - 1 - tile) : 2 * tile + 1; }
+// A workgroup for every tile: which one workgroup w has, of `heads` heads (of all elements) with `tiles` tiles of queries each.  Consecutive workgroups go to the eight XCDs in turn;
+// each XCD has whole heads where their number allows, and takes their tiles with most keys (causal rows: the last ones) first.  Where a CU holds two workgroups, the
+// second ones of all CUs go the other way round, so that the two of a CU have about as many keys as any other two; what follows fills the room that comes free.  us, the other
+// way round and not: 16 heads of 32 causal tiles 165, 170; of 33 170, 174; of 64 480, 500; 40 heads of 16 126, 125; 64 of 8 (d 40) 41, 41.
+struct ExpandedPlace { int head, tile; };
+constexpr ExpandedPlace expanded_place(int w, int heads, int tiles, int per_cu) {
+    const bool split = heads % 8 == 0;
+    const int here = split ? heads / 8 : heads, cus = split ? LA_CUS / 8 : LA_CUS, at = split ? w >> 3 : w;
+    const int i = per_cu == 2 && at >= cus && at < 2 * cus ? 3 * cus - 1 - at : at, rank = i / here;
+    return {(split ? (w & 7) * here : 0) + i - rank * here, tiles - 1 - rank};
+}
 struct ExpandedLayout { long long n_pad; size_t table, k, v, flags, ml, part, total; };
 inline ExpandedLayout expanded_layout(const LatentShape& s) {
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };

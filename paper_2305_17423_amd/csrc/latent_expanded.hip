@@ -11,12 +11,11 @@ namespace fise {
 // once lie in different banks.  The first index of the product is the one that runs along the
 // result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.  16 heads of 4096 keys, r 512: 27 us, bound by
 // what it reads from the L2 caches again (268 MB); 8 heads of 2 x 4096 keys, r 128: 10 us.
-// Group g of the line: (element, head), and of its tiles of queries in turn the last and the first that are left, which together have as many keys as any other two
-// where rows are causal.
+// Group g of the line: (element, head) and one of its tiles of queries.
 struct LxGroup { int b, h, tile; };
 __device__ __forceinline__ LxGroup lx_group(const LatentArgs& a, int g) {
     const int bh = (int)fdiv((unsigned)g, a.d_tiles), i = g - bh * a.tiles, b = (int)fdiv((unsigned)bh, a.d_heads);
-    return {b, bh - b * a.heads, i & 1 ? i >> 1 : a.tiles - 1 - (i >> 1)};
+    return {b, bh - b * a.heads, expanded_line_tile(i, a.tiles)};
 }
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 constexpr int LE_STEP = 64, LE_STAGE = 2 * 128 * LE_STEP * 2;
@@ -228,17 +227,11 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
     auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     const unsigned lds0 = (unsigned)(size_t)(FISE_AS3 unsigned char*)(FISE_AS3 void*)lds;
     const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5, l32 = lane & 31, wave = uniform(tid >> 6);
-    // consecutive workgroups go to the eight XCDs in turn: give each XCD one run of the line, whole heads where their number allows
+    // consecutive workgroups go to the eight XCDs in turn: give each XCD one run of the line
     int w = blockIdx.x, g, line0, line1;
     if (a.whole) {
-        // of an XCD's heads the tiles with most keys first; where all are on the CUs at once (workgroups i and i + 32 of an XCD on the same one) the second half the other
-        // way round, so that those two have as many keys as any other two
-        const int heads_all = a.B * a.heads, split = (heads_all & 7) == 0, heads_here = split ? heads_all >> 3 : heads_all, i = split ? w >> 3 : w;
-        const int rank = i / heads_here, bh = (split ? (w & 7) * heads_here : 0) + i - rank * heads_here, half = a.tiles >> 1;
-        const int back = a.tiles - 1 - rank;                           // the tile, last first; the second half of them in either order
-        const int tile = rank >= a.tiles - half && a.groups <= expanded_per_cu(KD) * LA_CUS ? rank - (a.tiles - half) : back;
-        g = bh * a.tiles + (tile >= half ? 2 * (a.tiles - 1 - tile) : 2 * tile + 1);
-        g = uniform(g);
+        const ExpandedPlace p = expanded_place(w, a.B * a.heads, a.tiles, expanded_per_cu(KD));
+        g = uniform(p.head * a.tiles + expanded_line_place(p.tile, a.tiles));
         line0 = uniform(a.table[g]); line1 = uniform(a.table[g + 1]);
         if (line0 == line1) {                                          // no query of the tile sees a key: zeros
             const LxGroup p = lx_group(a, g);
