@@ -556,7 +556,7 @@ template <int TILE> static int launch_tile(const LatentArgs& a, hipStream_t st) 
     FISE_CHECK_LAUNCH("fise_latent_attention: expanded");
     if (!a.whole) {
         ProfileScope prof(PROF_ATTENTION_MERGE, 0, 0, st);
-        hipLaunchKernelGGL(latent_join_kernel<DB>, dim3((unsigned)a.groups, a.groups < 4 * LA_CUS ? 4u : 1u), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(latent_join_kernel<DB>, dim3((unsigned)a.groups, 4), dim3(256), 0, st, a);      // (fewer tiles than workgroups on the CUs: four for each)
     }
     FISE_CHECK_LAUNCH("fise_latent_attention: parts");
     return FISE_OK;
