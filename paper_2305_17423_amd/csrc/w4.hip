@@ -275,7 +275,8 @@ __global__ __launch_bounds__(MT == 4 ? 512 : 1024) void w4_linear_kernel(const W
 }
 
 // The staged form.  Every wave has a tile of outputs (or waves_k waves share one and take turns with its tile columns) and all rows; x of the next four tile columns is on its
-// way to registers while these are multiplied, and goes to the other half of LDS behind them.
+// way to registers while these are multiplied, and goes to the other half of LDS behind them.  Rows of the last tiles that three pieces a value leave over hold whatever LDS
+// held: the matrix unit keeps rows apart, and theirs are not stored.
 template <int MT, int GS, bool SPLIT>
 __global__ __launch_bounds__(512) void w4_staged_kernel(const W4Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -355,8 +356,6 @@ __global__ __launch_bounds__(512) void w4_staged_kernel(const W4Args a) {
                 }
             }
     };
-    if constexpr (SPLIT)                                               // the row that three pieces leave over
-        for (int i = tid; i < 2 * PITCH / 8; i += 512) *reinterpret_cast<uint4*>(xs + (size_t)((i / (PITCH / 8)) * ROWS + ROWS - 1) * PITCH + i % (PITCH / 8) * 8) = make_uint4(0, 0, 0, 0);
     load_x(0);
     load_w(0, 0);
     put_x(0);
