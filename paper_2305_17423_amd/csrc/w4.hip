@@ -26,7 +26,8 @@ __device__ __forceinline__ size_t w4_scale_at(int n, int k, int group, int tiles
 }
 
 // A lane packs eight columns of an output; the lanes of a group find its largest magnitude among them.  The scale is that / 7 in bf16, a weight the
-// nearest multiple of it: at most half a scale off (7 scales are at least 7 / (7 (1 + 2^-8)) of the largest).  Magnitudes are compared as
+// nearest multiple of it: at most half a scale off (7 scales are at least 7 / (7 (1 + 2^-8)) of the largest; below bf16's normal range, where its steps are a larger part,
+// one step more if they are not).  Magnitudes are compared as
 // whole numbers, so that a NaN wins: a group with a value that is not finite has a scale that is not, and comes back as NaN.
 template <typename T>
 __global__ __launch_bounds__(256) void w4_pack_kernel(const T* __restrict__ w, const bf16_t* __restrict__ given, int N, int K, int group, int tiles_k, int groups,
@@ -42,7 +43,10 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const T* __restrict__ w, c
     for (int o = 1; o < group / 8; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
     if (k >= cols) return;
     bf16_t s = 0;
-    if (n < N && k < K) s = given ? given[(size_t)n * groups + k / group] : f2bf(__uint_as_float(top) / 7.f);
+    if (n < N && k < K) {
+        s = given ? given[(size_t)n * groups + k / group] : f2bf(__uint_as_float(top) / 7.f);
+        if (!given && 7.5f * bf2f(s) < __uint_as_float(top)) ++s;
+    }
     const float sf = bf2f(s);
     unsigned word = 0;
 #pragma unroll
