@@ -543,7 +543,10 @@ int fise_masked_gated_norm(const fise_gated_norm_args* a /* host */, void* strea
  * Forms: ABSORBED brings W_uk to the queries and W_uv to the sums, and every head meets the
  * latent vectors themselves: the cache is read once for 64 (query, head) rows.  EXPANDED
  * makes keys and values of all heads first.  AUTO takes the one that is expected to be faster
- * (few queries: absorbed).  They round at different places (absorbed: the queries behind W_uk,
+ * (few queries: absorbed), or the other where only that one holds the call: absorbed, fewer than
+ * 2^31 blocks of 32 keys over all tiles of 64 (query, head) rows; expanded, fewer than 2^31 blocks
+ * of 64 keys over all tiles of 128 queries, and fewer than 2^24 of those tiles and of tiles of 128
+ * keys x 128 channels of all heads' keys and values.  They round at different places (absorbed: the queries behind W_uk,
  * bf16; expanded: keys and values, bf16, a value beyond its range infinite); probabilities are two bf16 numbers in both (the
  * second what rounding leaves of the first), sums and softmax statistics float.  Results of a form depend on the arguments only, not on the run.
  * workspace: fise_latent_attention_workspace_bytes(a), which reads sizes, form and pointers but

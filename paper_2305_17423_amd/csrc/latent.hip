@@ -493,7 +493,19 @@ template <int R, int DR> static int launch_absorbed(const LatentArgs& a, hipStre
 }
 template <int R> static int launch_absorbed(const LatentArgs& a, hipStream_t st) { return a.dr ? launch_absorbed<R, 64>(a, st) : launch_absorbed<R, 0>(a, st); }
 
-static bool expands(const fise_latent_attention_args* g, const LatentShape& s) { return g->form == FISE_LATENT_AUTO ? latent_expands(s) : g->form == FISE_LATENT_EXPANDED; }
+// What a launch's grid and 31 bits hold: blocks of keys of all tiles; of the expanded form tiles of queries and of keys x weights, too, 256 lanes each.
+static bool absorbed_holds(const LatentShape& s) {
+    const long long tiles = (long long)s.B * absorbed_tiles(s);
+    return tiles < 1ll << 30 && tiles * ((s.n + LA_KEYS - 1) / LA_KEYS + 1) < 1ll << 31;
+}
+static bool expanded_holds(const LatentShape& s) {
+    const double groups = (double)s.B * s.heads * expanded_tiles(s), makes = (double)s.B * (s.n / LX_KEYS + 1) * ((double)s.heads * (s.d + s.dv) / 128 + 2);
+    return groups < 1 << 24 && makes < 1 << 24 && groups * (s.n / LX_BLOCK + 1) < 0x7fffffff;
+}
+// AUTO: the faster one of those that hold the call
+static bool expands(int form, const LatentShape& s) {
+    return form == FISE_LATENT_AUTO ? (latent_expands(s) ? expanded_holds(s) || !absorbed_holds(s) : !absorbed_holds(s)) : form == FISE_LATENT_EXPANDED;
+}
 static int latent_check(const char* fn, const fise_latent_attention_args* g, LatentShape& s) {
     if (!g || !g->q || !g->cache || !g->w_uk || !g->w_uv || !g->out) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
     if (g->dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d (bf16 only)", fn, g->dtype);
@@ -505,13 +517,9 @@ static int latent_check(const char* fn, const fise_latent_attention_args* g, Lat
         if (!aligned16(p)) return fail(FISE_ERR_ALIGN, "%s: pointers must be 16-byte aligned", fn);
     if (!(g->scale > 0) || g->scale > 1e30f) return fail(FISE_ERR_SHAPE, "%s: scale %g", fn, g->scale);
     s = LatentShape{g->B, g->M, g->n_keys, g->heads, g->d, g->dr, g->dv, g->r, g->causal != 0};
-    // rows, blocks of keys and tiles are counted in 31 bits, the lanes of a launch in 32, tokens of the absorbed form are a grid's second dimension
-    const long long rows = (long long)g->M * g->heads, tiles = (rows + LA_ROWS - 1) / LA_ROWS, blocks = ((long long)g->n_keys + LA_KEYS - 1) / LA_KEYS;
-    if (g->n_keys > 1 << 26 || rows >= 1ll << 30 || (long long)g->B * tiles >= 1ll << 30 || (long long)g->B * tiles * (blocks + 1) >= 1ll << 31 || (long long)g->B * g->M >= 1 << 20 || g->heads > 65535)
-        return fail(FISE_ERR_SHAPE, "%s: B%d M%d heads%d keys%d: too many rows or key blocks", fn, g->B, g->M, g->heads, g->n_keys);
-    const double groups = (double)g->B * g->heads * expanded_tiles(s), makes = (double)g->B * (g->n_keys / LX_KEYS + 1) * ((double)g->heads * (g->d + g->dv) / 128 + 2);
-    if (expands(g, s) && (groups >= 1 << 24 || makes >= 1 << 24 || groups * (g->n_keys / LX_BLOCK + 1) >= 0x7fffffff))
-        return fail(FISE_ERR_SHAPE, "%s: B%d heads%d M%d keys%d: too many tiles", fn, g->B, g->heads, g->M, g->n_keys);
+    // limits of either form (tokens: the absorbed one's, a grid's second dimension, but what AUTO refuses should not depend on what it would choose); then of the one that runs
+    if (g->n_keys > 1 << 26 || (long long)g->M * g->heads >= 1ll << 30 || (long long)g->B * g->M >= 1 << 20 || g->heads > 65535 || !(expands(g->form, s) ? expanded_holds(s) : absorbed_holds(s)))
+        return fail(FISE_ERR_SHAPE, "%s: B%d M%d heads%d keys%d: too many rows, tiles or key blocks", fn, g->B, g->M, g->heads, g->n_keys);
     return FISE_OK;
 }
 
@@ -523,7 +531,7 @@ extern "C" size_t fise_latent_attention_workspace_bytes(const fise_latent_attent
     LatentShape s;
     if (latent_check("fise_latent_attention_workspace_bytes", g, s)) return 0;
     if (s.M == 0) return 256;
-    return expands(g, s) ? expanded_layout(s).total : absorbed_layout(s).total;
+    return expands(g->form, s) ? expanded_layout(s).total : absorbed_layout(s).total;
 }
 
 extern "C" int fise_latent_attention(const fise_latent_attention_args* g, void* workspace, size_t workspace_bytes, void* stream) {
@@ -533,7 +541,7 @@ extern "C" int fise_latent_attention(const fise_latent_attention_args* g, void* 
     if (s.M == 0) return FISE_OK;
     if (!workspace) return fail(FISE_ERR_NULL, "%s: null workspace", fn);
     if ((uintptr_t)workspace & 255) return fail(FISE_ERR_ALIGN, "%s: the workspace must be 256-byte aligned", fn);
-    const bool expanded = expands(g, s);
+    const bool expanded = expands(g->form, s);
     const size_t need = expanded ? expanded_layout(s).total : absorbed_layout(s).total;
     if (workspace_bytes < need) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, workspace_bytes, need);
     unsigned char* const ws = (unsigned char*)workspace;
