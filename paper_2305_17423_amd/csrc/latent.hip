@@ -11,7 +11,9 @@ namespace fise {
 
 // ---------------------------------------------------------------------------------------------------------------- queries
 // qa[b, m, h] = [W_uk[h]^T q_c | q_pe | 0]: a workgroup has 128 latent channels of a head (a wave 32 of them) and takes 64 tokens at a time; W_uk's rows run along the
-// result, so they are turned on the way out of LDS.  The result is rounded to bf16, as any operand of the matrix unit.  All loads of a round go out together: few
+// result, so they are turned on the way out of LDS.  The result is rounded to bf16, which is what makes a result of this form 2.3e-3 off in the root mean square instead of the
+// 1.66e-3 of its own rounding.  Two bf16 numbers would end that, and cost as many score products again: 16 elements of 16 rows on 8192 keys 40 -> 43 us, 32 of 64 rows on
+// 20480 keys 205 -> 240.  All loads of a round go out together: few
 // tokens wait for one trip to memory, not for one a step.  64 tokens of 32 heads, r 512: 9 us, bound by that trip; 128 tokens of 128 heads 24 us (41 MB).
 // The last workgroup writes the line of key blocks instead: table[g] = blocks of all groups before g.
 constexpr int LQ_COLS = 128, LQ_TOKENS = 64;
@@ -96,8 +98,8 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
 // Probabilities go in as two bf16 numbers, the second what rounding leaves of the first, for half as many products again: one number's rounding (2^-9 of each term, root mean
 // square) would show as much as that of the result itself.  A long cache still waits for its bytes (32 tokens on 32768 keys: 189 -> 194 us for the whole call).
 // A turn is the scores of one block and the sums of the block before, so that one barrier serves both and neither product waits for the softmax of its own block.
-// 32 elements of 20480 keys on average, 64 rows, r 512: 162 us, 4.7 TB/s, bound by the cache's bytes; a block of 32 keys for 64 rows takes 1.9 us a CU, a little more than its
-// bytes do.
+// 32 elements of 20480 keys on average, 64 rows, r 512: 162 - 192 us, 3.9 - 4.7 TB/s (the clock under load differs from card to card); the cache's bytes alone take 147, the matrix
+// units are busy 39 % of the time, and a block of 32 keys for 64 rows takes 1.9 us a CU, a little more than its bytes do.
 // A row's reference moves only when a score lies 8 powers of two above it: any reference gives the same quotient, probabilities stay below 256 (a bf16 and a float have
 // the same relative steps there) and the factor for the sums before is 1 almost always.
 template <int R_, int DR_, int NT> struct LaTile {

@@ -9,8 +9,9 @@ namespace fise {
 // Tiles of 128 keys x 128 weight rows of one batch element on 32x32x16 products, four waves of 64 x 64; both operands run along the latent channels, 64 a step,
 // loaded directly to LDS, a step ahead.  Rows of 128 bytes, sixteen-byte pieces at piece ^ (row / 2 & 7): sixteen rows read at
 // once lie in different banks.  The first index of the product is the one that runs along the
-// result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.  16 heads of 4096 keys, r 512: 27 us, bound by
-// what it reads from the L2 caches again (268 MB); 8 heads of 2 x 4096 keys, r 128: 10 us.
+// result's memory (a key's channels; a value channel's keys), so that a lane has four neighbours.  Keys that do not exist are zeros.  Keys and values are rounded to bf16, as the
+// library's caches of them are; in two numbers each their products would double and LDS would not hold two workgroups' blocks.  16 heads of 4096 keys, r 512: 30 us, bound by
+// what it reads from the L2 caches again (268 MB); 8 heads of 2 x 4096 keys, r 128: 11 us.
 // Group g of the line: (element, head) and one of its tiles of queries.
 struct LxGroup { int b, h, tile; };
 __device__ __forceinline__ LxGroup lx_group(const LatentArgs& a, int g) {
@@ -175,10 +176,11 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // they stand.  A row's pieces are placed so that sixteen rows read at once lie in different banks, by what 256 leaves of the row's bytes.
 // A turn is: scores of the next block, with the exponentials of this block between the products; sums of this block, with the maximum of the next between them.  So
 // neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
-// Probabilities are two bf16 numbers, as in the absorbed form: 16 heads of 4096 causal queries go from 148 to 169 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
+// Probabilities are two bf16 numbers, as in the absorbed form: that took 16 heads of 4096 causal queries from 148 to 169 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
 // the result's own rounding, the rest that of keys and values).
-// 135 of those 169 us are this kernel's: 16 x 1056 pairs of a tile and a block at 0.66 PFLOP/s, bound by instructions (56 products, 32 exponentials, 40 reads of LDS a turn, which two
-// workgroups on a CU overlap in part).  768 queries on 4096 keys, twice, 8 heads of 40: 30 us.
+// The prompt's 16 x 1056 pairs of a tile and a block take this kernel 142 us with a pause between calls and 160 without, as the clock falls; at 0.6 PFLOP/s it is bound by what a SIMD
+// issues: while it has waves its matrix unit is busy 52 % of the time (56 products a turn) and vector instructions take 45 % (32 exponentials and what turns scores into operands),
+// so two waves a SIMD overlap little; LDS is busy a third of it.  768 queries on 4096 keys, twice, 8 heads of 40: 36 us, 12 or 13 turns a workgroup.
 // Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
 [[maybe_unused]] constexpr int LX_AHEAD = 4;
 

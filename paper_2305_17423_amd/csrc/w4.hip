@@ -9,7 +9,8 @@
 // x of a wave's columns stays in registers as operands, and the wave streams the weights of one tile of outputs after the other past it; nothing else is read again.
 // Float x, and x behind SiLU, is split into three bf16 numbers that add up to it exactly: three rows of the
 // instruction, of which a few rows of x leave most idle, added in the epilogue.
-// 16 rows, 28672 outputs of 8192 columns: 31 us, 3.9 TB/s; 2 float rows behind SiLU, 20160 outputs of 1280 columns: 8.1 us, of which the launch is the larger part.
+// 16 rows, 28672 outputs of 8192 columns: 31 us, 3.9 TB/s, with six sets of weights in turn, which no cache holds, and 28 us, 4.4 TB/s, with the same ones again and again (a sum over
+// arrays of that size reads 3.2 and 4.5, over 1 GB 3.9); 2 float rows behind SiLU, 20160 outputs of 1280 columns: 10 and 8 us, of which the launch is the larger part.
 #include "igemm.h"
 #include "profile.h"
 #include "w4_choice.h"
@@ -281,6 +282,9 @@ __global__ __launch_bounds__(MT == 4 ? 512 : 1024) void w4_linear_kernel(const W
 // The staged form.  Every wave has a tile of outputs (or waves_k waves share one and take turns with its tile columns) and all rows; x of the next four tile columns is on its
 // way to registers while these are multiplied, and goes to the other half of LDS behind them.  Rows of the last tiles that three pieces a value leave over hold whatever LDS
 // held: the matrix unit keeps rows apart, and theirs are not stored.
+// 64 rows, 8192 outputs of 8192 columns: 35 us, five times what the bytes take.  No unit is full (of a CU's cycles the matrix units are busy 11 %, the vector units 40 %, LDS about
+// half, a fifth of it bank conflicts): with one workgroup a CU, loads, the writes of x to LDS and the products of a chunk wait for one another at its barrier, and a CU moves 64 KB
+// of x for every 8 KB of weights.
 template <int MT, int GS, bool SPLIT>
 __global__ __launch_bounds__(512) void w4_staged_kernel(const W4Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -37,7 +37,7 @@ inline W4Choice w4_choose(int M, int N, int K, bool split) {
     const W4Layout l = w4_layout(N, K, 128);
     const int tk = (int)l.tiles_k;
     // slabs of the fewest row tiles that still leave at most one workgroup for every CU: fewer rows are less x to read for every one of them (27 rows, 1283 outputs, 5120
-    // columns: two of 16 rows 8.1 us, one of 27 11.7); else, and with many outputs, as many rows as fit, so that weights are read once
+    // columns: two of 16 rows 8.4 us, one of 27 11.7); else, and with many outputs, as many rows as fit, so that weights are read once
     for (c.mt = 1;; c.mt *= 2) {
         c.slab = std::min(M, 16 * c.mt / c.pieces);
         c.slabs = (M + c.slab - 1) / c.slab;
