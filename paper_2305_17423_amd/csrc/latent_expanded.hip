@@ -94,6 +94,7 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
     }
     // through LDS, column by column of the product (its pieces of eight rows at piece ^ (column & 15)), so that sixteen lanes store 256 bytes side by side
     const int width = KD * 16;
+    u16x2_t largest = {0, 0};                                          // bits of the largest magnitude: infinity and NaN are at least 0x7f80
     la_barrier();
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -102,52 +103,43 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int piece = wr * 8 + i * 4 + q, col = wc * 64 + j * 32 + l32;
-                *reinterpret_cast<uint2*>(lds + col * 256 + (piece ^ (col & 15)) * 16 + hl * 8) =
-                    make_uint2(f2bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f2bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+                const uint2 v = make_uint2(f2bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]), f2bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+                const uint2 bits = make_uint2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu);
+                largest = __builtin_elementwise_max(largest, __builtin_elementwise_max(*reinterpret_cast<const u16x2_t*>(&bits.x), *reinterpret_cast<const u16x2_t*>(&bits.y)));
+                *reinterpret_cast<uint2*>(lds + col * 256 + (piece ^ (col & 15)) * 16 + hl * 8) = v;
             }
+    if (values) {
+        const bool odd = __any(largest[0] >= 0x7f80 || largest[1] >= 0x7f80);
+        if (lane == 0) reinterpret_cast<unsigned char*>(a.flags + ((size_t)b * v_tiles + wt - k_tiles) * key_tiles + kt)[wave] = odd;
+        if (odd) {
+            // Where the latent vector itself is not finite, every channel is NaN: the score of its key is NaN or infinite, and the probability 0 of a score of -inf meets
+            // an infinite value.  (What is infinite without that has overflown, and stays.)
+            bool bad = false;
+            for (int c = 0; c < a.r; c += 8) {
+                const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(keys, (wr * 64 + lane) * row_bytes + c * 2, 0, 0);
+                bad |= la_odd(make_uint4(x[0], x[1], x[2], x[3]));
+            }
+            const int col = wc * 64 + lane;
+            asm volatile("" ::: "memory");                             // behind the writes above, of other types
+            for (unsigned long long left = __ballot(bad); left; left &= left - 1) {
+                const int key = wr * 64 + __ffsll(left) - 1;
+                *reinterpret_cast<unsigned short*>(lds + col * 256 + ((key >> 3) ^ (col & 15)) * 16 + (key & 7) * 2) = 0x7fc0;
+            }
+        }
+    }
     la_barrier();
-    u16x2_t largest = {0, 0};                                          // bits of the largest magnitude: infinity and NaN are at least 0x7f80
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int col = i * 16 + (tid >> 4), row = (tid & 15) * 8;
         const uint4 v = *reinterpret_cast<const uint4*>(lds + col * 256 + ((tid & 15) ^ (col & 15)) * 16);
         if (values) {
-            for (const unsigned x : {v.x, v.y, v.z, v.w}) {
-                const unsigned bits = x & 0x7fff7fffu;
-                largest = __builtin_elementwise_max(largest, *reinterpret_cast<const u16x2_t*>(&bits));
-            }
             if (w0 + col < n_w) *reinterpret_cast<uint4*>(a.v + ((size_t)b * n_w + w0 + col) * a.n_pad + key0 + row) = v;
         } else if (w0 + row < n_w) {
             const int c = w0 + row, h = c / a.d;
             *reinterpret_cast<uint4*>(a.k + (((size_t)b * a.heads + h) * a.n_pad + key0 + col) * width + (c - h * a.d)) = v;
         }
     }
-    if (values) {
-        const bool odd = __any(largest[0] >= 0x7f80 || largest[1] >= 0x7f80);
-        if (odd) {
-            // Where the latent vector itself is not finite, every channel is NaN: the score of its key is NaN or infinite, and the probability 0 of a score of -inf meets
-            // an infinite value.  (What is infinite without that has overflown, and stays.)
-            unsigned long long bad[2];
-            for (int half = 0; half < 2; ++half) {
-                bool is = false;
-                for (int c = 0; c < a.r; c += 8) {
-                    const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(keys, (half * 64 + lane) * row_bytes + c * 2, 0, 0);
-                    is |= la_odd(make_uint4(x[0], x[1], x[2], x[3]));
-                }
-                bad[half] = __ballot(is);
-            }
-            asm volatile("" ::: "memory");                             // behind the stores above, of other types
-            const int row = (tid & 15) * 8;
-            const unsigned mine = (unsigned)((row & 64 ? bad[1] : bad[0]) >> (row & 63)) & 255;
-            for (int i = 0; i < 8; ++i) {
-                const int col = i * 16 + (tid >> 4);
-                if (w0 + col < n_w)
-                    for (int e = 0; e < 8; ++e)
-                        if (mine >> e & 1) a.v[((size_t)b * n_w + w0 + col) * a.n_pad + key0 + row + e] = 0x7fc0;
-            }
-        }
-        if (lane == 0) reinterpret_cast<unsigned char*>(a.flags + ((size_t)b * v_tiles + wt - k_tiles) * key_tiles + kt)[wave] = odd;
-    } else {
+    if (!values) {
         // the shared key (and zeros) behind the channels of the heads that begin in this tile: four pieces on their way at once, each stored for every head
         const int h0 = (w0 + a.d - 1) / a.d, h1 = min((w0 + 127) / a.d + 1, a.heads), tail = (width - a.d) / 8;
         for (int i0 = tid; i0 < 128 * tail; i0 += 1024) {
@@ -300,6 +292,16 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                 la_to_lds(from, v_off[(wave * VL + j) & 1], lds0 + 2 * KB + (blk & 1) * VB + (wave * VL + j) * 1024);
             }
         };
+        // Values that are not finite are in none of the sums (times what rounding left of a probability, or 0 of a key that a query does not see, they would be NaN), but added
+        // behind them: a part with such a tile of values knows it before its first block.
+        const int row_v = h * a.dv, tile_v = row_v >> 7, tiles_v = ((row_v + a.dv - 1) >> 7) - tile_v + 1, key_tiles = (int)(a.n_pad / LX_KEYS);
+        const unsigned* const flags = a.flags + ((size_t)b * ((a.heads * a.dv + 127) >> 7) + tile_v) * key_tiles;
+        auto odd_of = [&](int t0) {                                    // 64 tiles of keys from t0 on, the last one again behind it
+            const int t = min(t0 + lane, (blk1 - 1) >> 1);
+            return flags[t] | flags[(size_t)min(1, tiles_v - 1) * key_tiles + t] | flags[(size_t)(tiles_v - 1) * key_tiles + t];
+        };
+        unsigned odd_bits = odd_of(blk0 >> 1);                         // (on its way with the first blocks)
+        bool odd;
         la_barrier();                                                  // the group before has been read to its end
         load_k(blk0);
         load_k(blk0 + 1);
@@ -315,14 +317,6 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
                 qf[ks] = *reinterpret_cast<const bf16x8_t*>(&x);
             }
         }
-        // Values that are not finite are in none of the sums (times what rounding left of a probability, or 0 of a key that a query does not see, they would be NaN), but added
-        // behind them: a part with such a tile of values knows it before its first block.
-        const int row_v = h * a.dv, tile_v = row_v >> 7, tiles_v = ((row_v + a.dv - 1) >> 7) - tile_v + 1, key_tiles = (int)(a.n_pad / LX_KEYS);
-        const unsigned* const flags = a.flags + ((size_t)b * ((a.heads * a.dv + 127) >> 7) + tile_v) * key_tiles;
-        bool odd = false;
-        for (int t = (blk0 >> 1) + lane; t <= (blk1 - 1) >> 1; t += 64)
-            for (int i = 0; i < tiles_v; ++i) odd |= flags[(size_t)i * key_tiles + t] != 0;
-        odd = __any(odd);
         f32x16_t o[DB];
 #pragma unroll
         for (int i = 0; i < DB; ++i)
@@ -448,6 +442,8 @@ __global__ __launch_bounds__(256, expanded_per_cu(KD)) void latent_expanded_kern
         };
 #pragma unroll
         for (int ks = 0; ks < KD; ++ks) asm volatile("" ::"v"(qf[ks]));
+        for (int t0 = (blk0 >> 1) + 64; t0 <= (blk1 - 1) >> 1; t0 += 64) odd_bits |= odd_of(t0);
+        odd = __any(odd_bits != 0);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         {
             const unsigned char* const keys = lds + (blk0 & 1) * KB;
@@ -530,8 +526,16 @@ __global__ __launch_bounds__(256) void latent_join_kernel(const LatentArgs a) {
             const float4 v = *reinterpret_cast<const float4*>(a.part + (row + (size_t)p * LX_QUERIES) * (DB * 32) + c);
             const float f = __builtin_amdgcn_exp2f(ml.x - base);
             l = fmaf(f, ml.y, l);
-            auto add = [&](float& to, float x) { to = fabsf(x) < INFINITY ? fmaf(f, x, to) : to + x; };      // (what is infinite stays so however little its part weighs)
-            add(o.x, v.x); add(o.y, v.y); add(o.z, v.z); add(o.w, v.w);
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        }
+        if (!(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY)) {      // what is infinite stays so however little its part weighs
+            o = make_float4(0, 0, 0, 0);
+            for (int p = 0; p < n; ++p) {
+                const float f = __builtin_amdgcn_exp2f(a.ml[row + (size_t)p * LX_QUERIES].x - base);
+                const float4 v = *reinterpret_cast<const float4*>(a.part + (row + (size_t)p * LX_QUERIES) * (DB * 32) + c);
+                auto add = [&](float& to, float x) { to = fabsf(x) < INFINITY ? fmaf(f, x, to) : to + x; };
+                add(o.x, v.x); add(o.y, v.y); add(o.z, v.z); add(o.w, v.w);
+            }
         }
         const float inv = l == 0.f ? 0.f : 1.0f / l;
         *reinterpret_cast<uint2*>(a.out + (((size_t)place.b * a.M + m) * a.heads + place.h) * a.dv + c) = make_uint2(f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv));
