@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(const LatentArgs a, i
 // Probabilities go in as two bf16 numbers, the second what rounding leaves of the first, for half as many products again: one number's rounding (2^-9 of each term, root mean
 // square) would show as much as that of the result itself.  A long cache still waits for its bytes (32 tokens on 32768 keys: 189 -> 194 us for the whole call).
 // A turn is the scores of one block and the sums of the block before, so that one barrier serves both and neither product waits for the softmax of its own block.
-// 32 elements of 20480 keys on average, 64 rows, r 512: 162 - 192 us, 3.9 - 4.7 TB/s (the clock under load differs from card to card); the cache's bytes alone take 147, the matrix
+// 32 elements of 20480 keys on average, 64 rows, r 512: 162 - 197 us, 3.8 - 4.7 TB/s (the clock under load differs from card to card); the cache's bytes alone take 147, the matrix
 // units are busy 39 % of the time, and a block of 32 keys for 64 rows takes 1.9 us a CU, a little more than its bytes do.
 // A row's reference moves only when a score lies 8 powers of two above it: any reference gives the same quotient, probabilities stay below 256 (a bf16 and a float have
 // the same relative steps there) and the factor for the sums before is 1 almost always.

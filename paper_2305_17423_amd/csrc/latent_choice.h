@@ -103,8 +103,8 @@ inline ExpandedLayout expanded_layout(const LatentShape& s) {
 }
 
 // ---- which form: the one with fewer operations (sums counted once; launches and joining are left out, so that near the border the other one can be a few percent faster).  us,
-// absorbed and expanded, 4096 keys, 2 elements: 16 heads of 128 + 64, r 512: 64 queries 64, 93; 256 queries 149, 107; 4096 causal queries of one element 1107, 167.  8 heads of 40 + 32,
-// r 128: 16 queries 21, 33; 64 queries 34, 35 (the rule takes the latter); 192 41, 41; 768 87, 54.
+// absorbed and expanded, 4096 keys, 2 elements: 16 heads of 128 + 64, r 512: 64 queries 62, 80; 256 queries 135, 97; 4096 causal queries of one element 1102, 157.  8 heads of 40 + 32,
+// r 128: 16 queries 20, 31; 64 queries 33, 33 - 35 (the rule takes the latter); 192 40, 39; 768 88, 54.
 inline bool latent_expands(const LatentShape& s) {
     const double keys = (double)s.n, pairs = (double)s.M * s.heads * (s.causal && s.M > 1 ? keys - 0.5 * std::min<double>(s.M, keys) : keys);
     const double absorbed = pairs * (2.0 * latent_width(s.r) + latent_shared(s.dr)) + (double)s.M * s.heads * s.r * (s.d + s.dv);

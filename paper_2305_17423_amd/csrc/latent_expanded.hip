@@ -170,9 +170,9 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(const LatentArgs 
 // neither product waits for a softmax, nor the vector unit for a product; the order is written down, as the compiler's own keeps them apart.
 // Probabilities are two bf16 numbers, as in the absorbed form: that took 16 heads of 4096 causal queries from 148 to 169 us, their root mean square error from 2.7e-3 to 2.4e-3 (1.7e-3 is
 // the result's own rounding, the rest that of keys and values).
-// The prompt's 16 x 1056 pairs of a tile and a block take this kernel 142 us with a pause between calls and 160 without, as the clock falls; at 0.6 PFLOP/s it is bound by what a SIMD
-// issues: while it has waves its matrix unit is busy 52 % of the time (56 products a turn) and vector instructions take 45 % (32 exponentials and what turns scores into operands),
-// so two waves a SIMD overlap little; LDS is busy a third of it.  768 queries on 4096 keys, twice, 8 heads of 40: 36 us, 12 or 13 turns a workgroup.
+// The prompt's 16 x 1056 pairs of a tile and a block take this kernel 137 us with a pause between calls and 154 without, as the clock falls; at 0.6 PFLOP/s it is bound by what a SIMD
+// issues: while it has waves its matrix unit is busy 53 % of the time (56 products a turn) and vector instructions take 44 % (32 exponentials and what turns scores into operands),
+// so two waves a SIMD overlap little; LDS is busy a third of it.  768 queries on 4096 keys, twice, 8 heads of 40: 35 us, 12 or 13 turns a workgroup, matrix units 34 %, vector instructions 52 %.
 // Few tiles: the workgroups share the line of key blocks evenly (latent.h), and latent_join_kernel adds up what a cut tile's parts came to.
 [[maybe_unused]] constexpr int LX_AHEAD = 4;
 

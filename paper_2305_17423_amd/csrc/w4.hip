@@ -282,7 +282,7 @@ __global__ __launch_bounds__(MT == 4 ? 512 : 1024) void w4_linear_kernel(const W
 // The staged form.  Every wave has a tile of outputs (or waves_k waves share one and take turns with its tile columns) and all rows; x of the next four tile columns is on its
 // way to registers while these are multiplied, and goes to the other half of LDS behind them.  Rows of the last tiles that three pieces a value leave over hold whatever LDS
 // held: the matrix unit keeps rows apart, and theirs are not stored.
-// 64 rows, 8192 outputs of 8192 columns: 35 us, five times what the bytes take.  No unit is full (of a CU's cycles the matrix units are busy 11 %, the vector units 40 %, LDS about
+// 64 rows, 8192 outputs of 8192 columns: 35 us, five times what the bytes take.  No unit is full (of a CU's cycles the matrix units are busy 10 %, the vector units 38 %, LDS about
 // half, a fifth of it bank conflicts): with one workgroup a CU, loads, the writes of x to LDS and the products of a chunk wait for one another at its barrier, and a CU moves 64 KB
 // of x for every 8 KB of weights.
 template <int MT, int GS, bool SPLIT>
