@@ -45,7 +45,7 @@
 extern "C" {
 #endif
 
-typedef enum { FISE_F32 = 0, FISE_BF16 = 1 } fise_dtype;
+typedef enum { FISE_F32 = 0, FISE_BF16 = 1, FISE_E4M3 = 2 /* codes, where an entry point says so */ } fise_dtype;
 
 typedef enum {
     FISE_OK = 0,
@@ -560,6 +560,127 @@ typedef struct {
 } fise_latent_attention_args;
 size_t fise_latent_attention_workspace_bytes(const fise_latent_attention_args* a /* host */);
 int fise_latent_attention(const fise_latent_attention_args* a /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Transformer denoisers with experts: rotary positions, products in 8-bit floating
+ * point, routing of tokens to experts and the experts' feed-forward.  Rows of an empty
+ * selection (M == 0, T == 0) touch nothing; their pointers must not be NULL.
+ * ------------------------------------------------------------------------ */
+
+/* Rotary positions on several axes, of one tensor or two (queries and keys) in one launch: in each
+ * head the channels [start, start + rot) are rot / 2 pairs (u, v), and
+ *   (u, v) -> (u cos a - v sin a, u sin a + v cos a),   a = (pos[axis] + offset[axis]) * theta[axis]^(-2 j / n)
+ * for pair j of an axis that has n = axis_dim[axis] channels, n even, rot = their sum (at most 1024).
+ * The axes' pairs follow one another.  shared_freq: one sequence of frequencies over all
+ * pairs, theta[0]^(-2 i / rot) for pair i of all.  inverse: the angle's sign changed (takes a
+ * rotation back; the gradient of a rotation).  Pairs: ADJACENT channels 2i, 2i + 1; HALVES i and
+ * i + rot / 2; AXIS_HALVES i and i + n / 2 among an axis' own channels.  Angles are taken in 64
+ * bits, so far positions lose nothing; the rotation is float, rounded once.
+ * Positions: pos [pos_B, M, n_axes] (float or int32; pos_B 1 or B), or with pos NULL the place of a
+ * token on the grid T x H x W: its number (one axis), y, x (two) or t, y, x (three).
+ * Rows: with tile == 0 all T H W tokens in order (with pos: M rows); with tile > 0 those of the active
+ * tiles of tile x tile, ids on the T x (H / tile) x (W / tile) grid, tile by tile, row-major inside a tile
+ * (ids outside the grid: rows left out).  M is the number of rows.
+ * x is [B, rows, heads, d] with neighbouring channels and any strides (in elements, at least 0; of y
+ * without overlap); x_is_map / y_is_map: its rows are tokens of the whole map, else 0..M-1.  The other
+ * channels of a head are copied.  y may be x with the same strides and form (in place); nothing else may overlap. */
+enum { FISE_ROTARY_ADJACENT = 0, FISE_ROTARY_HALVES = 1, FISE_ROTARY_AXIS_HALVES = 2 };
+typedef struct {
+    const void* x; void* y;
+    int heads, d, start;
+    int64_t x_batch, x_row, x_head, y_batch, y_row, y_head;
+    int x_is_map, y_is_map;
+} fise_rotary_tensor;
+typedef struct {
+    fise_rotary_tensor t[2]; int n_tensors; int dtype;
+    int B, M;
+    int n_axes; int axis_dim[4]; double theta[4]; double offset[4];
+    int pairing, shared_freq, inverse;
+    const void* pos; int pos_is_float; int pos_B;
+    int T, H, W; const int32_t* tile_idx; int n_active; int tile;
+} fise_rotary_args;
+int fise_rotary(const fise_rotary_args* a /* host */, void* stream);
+
+/* 8-bit floating point: e4m3 codes (four bits of exponent, three of mantissa, largest value 448, no
+ * infinity, NaN 0x7f / 0xff) with one float scale for a block of 128 columns and of 1 row
+ * (activations) or 128 rows (weights): a value is code * scale.
+ * fise_fp8_quantize chooses the scales: the smallest power of two, 2^-126 at least, that leaves no
+ * finite value of the block above 448, which makes dividing by it exact; codes are the nearest, ties to the
+ * even one, of values that are not finite NaN.  x [M, K] float or bf16, rows x_stride apart (K, x_stride
+ * multiples of 8, 16-byte aligned); codes [M, K], rows code_stride apart (a multiple of 8, 8-byte aligned).  scale: block_rows
+ * 1: [ceil(K / 128), M], the rows of one block of columns side by side, blocks scale_stride apart;
+ * block_rows 128: [ceil(M / 128), ceil(K / 128)], rows of blocks scale_stride apart. */
+int fise_fp8_quantize(const void* x, int dtype, int64_t x_stride, int M, int K, int block_rows,
+                      uint8_t* codes, int64_t code_stride, float* scale, int64_t scale_stride, void* stream);
+
+/* y[m, n] = sum_b x_scale[b, m] w_scale[n / 128, b] sum_k x[m, k] w[n, k] + bias[n] (+ residual[m, n]),
+ * the inner sum over the 128 columns of block b, of codes; all sums float, but for y in bf16 the matrix unit adds products of codes eight at a
+ * time and drops of each what is below 2^-13 of the largest of them (up to 2^-10 of the magnitudes' sum).  w [N, K] codes, rows w_stride apart.
+ * x: codes (FISE_E4M3) with x_scale [ceil(K / 128), M], blocks x_scale_stride apart, or float / bf16 rows, which
+ * the call puts in 8 bits as fise_fp8_quantize does (x_scale NULL).  y float or bf16, bias a type of its own, residual y's.
+ * K and the strides of codes multiples of 16, of other x of 8, x and w 16-byte aligned, strides at most
+ * 2^22; y and residual any alignment of their type; M, N, K at most 2^20.  Scales must be finite; a product of two
+ * of them beyond float's range is infinite, below its normal range it loses bits.  residual may be y; nothing else may overlap y. */
+typedef struct {
+    const void* x; int x_dtype; int64_t x_stride;           /* [M, K] */
+    const float* x_scale; int64_t x_scale_stride;
+    const uint8_t* w; int64_t w_stride; const float* w_scale;   /* [N, K], [ceil(N / 128), ceil(K / 128)] */
+    int M, N, K;
+    const void* bias; int bias_dtype;                       /* [N] or NULL */
+    const void* residual; int64_t residual_stride;          /* [M, N] or NULL */
+    void* y; int y_dtype; int64_t y_stride;                 /* [M, N] */
+} fise_fp8_linear_args;
+size_t fise_fp8_linear_workspace_bytes(const fise_fp8_linear_args* a /* host; sizes and types only */);
+int fise_fp8_linear(const fise_fp8_linear_args* a /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Routing: for each of T tokens the k of E experts with the largest keys, largest first, the lower index
+ * first among equal ones.  score = softmax of the token's logits, or the sigmoid of each; key = score + bias[e]
+ * (bias float [E] or NULL: for the choice only).  With groups > 1 the experts are groups of E / groups
+ * neighbours, of which the top_groups with the largest sums of their group_top (1 or 2) largest keys take part.
+ *   weights[t, j] = scale * score (/ the sum of the token's k scores, with renormalize; 0 where that sum is 0)
+ * An expert whose logit (or key) is minus infinity is not chosen, and a group without others neither; places that are left
+ * over get id -1 and weight 0.  A token with a NaN among its logits or keys, or with an infinite
+ * logit under softmax, has ids -1 and weights NaN.  Keys, and the weights' sums, are as in 64 bits.
+ * offsets [E + 1], slots [T * k]: the pairs t * k + j in the order of their experts, within an expert
+ * ascending; expert e has slots[offsets[e] .. offsets[e + 1]).  slots behind offsets[E] are not written.  Both
+ * may be NULL (ids and weights only).  logits float or bf16 [T, E], rows stride apart, any alignment of
+ * their type.  E 1..1024, k 1..min(E, 64), T * k < 2^31.
+ * workspace: fise_route_experts_workspace_bytes (may be 0). */
+enum { FISE_SCORE_SOFTMAX = 0, FISE_SCORE_SIGMOID = 1 };
+typedef struct {
+    const void* logits; int dtype; int64_t stride;
+    int T, E, k;
+    int score; const float* bias;
+    int groups, top_groups, group_top;
+    int renormalize; float scale;
+    int32_t* ids; float* weights;                           /* [T, k] */
+    int32_t* offsets; int32_t* slots;
+} fise_route_args;
+size_t fise_route_experts_workspace_bytes(const fise_route_args* a /* host; sizes only */);
+int fise_route_experts(const fise_route_args* a /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The feed-forward of the chosen experts and its weighted sum:
+ *   h = silu(Wg[e] x_t) * (Wu[e] x_t),   y[t] = sum_j weights[t, j] * Wo[e] h (+ residual[t]),   e = ids[t, j]
+ * Products as in fise_fp8_linear for y in bf16: x and h are put in 8 bits with a power of two for 128 channels; sums float,
+ * and for y in bf16 an expert's result is rounded to bf16 before its weight (y float: not rounded).  A
+ * pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots as fise_route_experts leaves them (pairs
+ * in offsets / slots decide which expert's product a pair gets; places out of range are skipped).
+ * w_in codes [E, 2, I, K] (gate, up), w_in_scale [E, 2, ceil(I / 128), ceil(K / 128)]; w_out codes [E, N, I],
+ * w_out_scale [E, ceil(N / 128), ceil(I / 128)]; 16-byte aligned.  x float or bf16 [T, K], rows x_stride apart; y,
+ * residual [T, N], 16-byte aligned, strides multiples of 8.  K, I multiples of 16, N of 8, each at most 2^16; E 1..1024; T * k < 2^24;
+ * T * K below 2^30 (K rounded up to 128).
+ * residual may be y; nothing else may overlap y. */
+typedef struct {
+    const void* x; int x_dtype; int64_t x_stride; int T, K;
+    const int32_t* ids; const float* weights; const int32_t* offsets; const int32_t* slots; int k;
+    int E, I, N;
+    const uint8_t* w_in; const float* w_in_scale;
+    const uint8_t* w_out; const float* w_out_scale;
+    const void* residual; int64_t residual_stride;
+    void* y; int y_dtype; int64_t y_stride;
+} fise_expert_mlp_args;
+size_t fise_expert_mlp_workspace_bytes(const fise_expert_mlp_args* a /* host; sizes and types only */);
+int fise_expert_mlp(const fise_expert_mlp_args* a /* host */, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Tracing.  With profiling enabled every launch of the gathered-GEMM and

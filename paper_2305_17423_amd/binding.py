@@ -14,7 +14,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("FISE_LIB", os.path.join(_HERE, "libfise.so"))
 
-FISE_F32, FISE_BF16 = 0, 1
+FISE_F32, FISE_BF16, FISE_E4M3 = 0, 1, 2
 FISE_STATS_CACHED, FISE_STATS_FRESH = 0, 1
 FISE_MAX_LEVELS = 8
 _lib = None
@@ -76,6 +76,36 @@ class fise_latent_attention_args(C.Structure):
                 ("B", i32), ("M", i32), ("n_keys", i32), ("cache_tokens", i64),
                 ("heads", i32), ("d", i32), ("dr", i32), ("dv", i32), ("r", i32),
                 ("scale", f32), ("causal", i32), ("form", i32), ("dtype", i32)]
+
+
+class fise_rotary_tensor(C.Structure):
+    _fields_ = [("x", vp), ("y", vp), ("heads", i32), ("d", i32), ("start", i32), ("x_batch", i64), ("x_row", i64), ("x_head", i64),
+                ("y_batch", i64), ("y_row", i64), ("y_head", i64), ("x_is_map", i32), ("y_is_map", i32)]
+
+
+class fise_rotary_args(C.Structure):
+    _fields_ = [("t", fise_rotary_tensor * 2), ("n_tensors", i32), ("dtype", i32), ("B", i32), ("M", i32),
+                ("n_axes", i32), ("axis_dim", i32 * 4), ("theta", C.c_double * 4), ("offset", C.c_double * 4),
+                ("pairing", i32), ("shared_freq", i32), ("inverse", i32), ("pos", vp), ("pos_is_float", i32), ("pos_B", i32),
+                ("T", i32), ("H", i32), ("W", i32), ("tile_idx", vp), ("n_active", i32), ("tile", i32)]
+
+
+class fise_fp8_linear_args(C.Structure):
+    _fields_ = [("x", vp), ("x_dtype", i32), ("x_stride", i64), ("x_scale", vp), ("x_scale_stride", i64),
+                ("w", vp), ("w_stride", i64), ("w_scale", vp), ("M", i32), ("N", i32), ("K", i32),
+                ("bias", vp), ("bias_dtype", i32), ("residual", vp), ("residual_stride", i64), ("y", vp), ("y_dtype", i32), ("y_stride", i64)]
+
+
+class fise_route_args(C.Structure):
+    _fields_ = [("logits", vp), ("dtype", i32), ("stride", i64), ("T", i32), ("E", i32), ("k", i32), ("score", i32), ("bias", vp),
+                ("groups", i32), ("top_groups", i32), ("group_top", i32), ("renormalize", i32), ("scale", f32),
+                ("ids", vp), ("weights", vp), ("offsets", vp), ("slots", vp)]
+
+
+class fise_expert_mlp_args(C.Structure):
+    _fields_ = [("x", vp), ("x_dtype", i32), ("x_stride", i64), ("T", i32), ("K", i32), ("ids", vp), ("weights", vp), ("offsets", vp), ("slots", vp),
+                ("k", i32), ("E", i32), ("I", i32), ("N", i32), ("w_in", vp), ("w_in_scale", vp), ("w_out", vp), ("w_out_scale", vp),
+                ("residual", vp), ("residual_stride", i64), ("y", vp), ("y_dtype", i32), ("y_stride", i64)]
 
 
 class fise_unet_desc(C.Structure):
@@ -143,6 +173,14 @@ _SIGS = {
     "fise_masked_gated_norm": (i32, [C.POINTER(fise_gated_norm_args), vp]),
     "fise_latent_attention_workspace_bytes": (sz, [C.POINTER(fise_latent_attention_args)]),
     "fise_latent_attention": (i32, [C.POINTER(fise_latent_attention_args), vp, sz, vp]),
+    "fise_rotary": (i32, [C.POINTER(fise_rotary_args), vp]),
+    "fise_fp8_quantize": (i32, [vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
+    "fise_fp8_linear_workspace_bytes": (sz, [C.POINTER(fise_fp8_linear_args)]),
+    "fise_fp8_linear": (i32, [C.POINTER(fise_fp8_linear_args), vp, sz, vp]),
+    "fise_route_experts_workspace_bytes": (sz, [C.POINTER(fise_route_args)]),
+    "fise_route_experts": (i32, [C.POINTER(fise_route_args), vp, sz, vp]),
+    "fise_expert_mlp_workspace_bytes": (sz, [C.POINTER(fise_expert_mlp_args)]),
+    "fise_expert_mlp": (i32, [C.POINTER(fise_expert_mlp_args), vp, sz, vp]),
     "fise_profile_enable": (i32, [i32]),
     "fise_profile_calibrate": (i32, [i32, vp]),
     "fise_calibrate_peaks": (i32, [vp, sz, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
@@ -565,6 +603,229 @@ def fise_latent_attention(args, workspace, stream=None):
         raise ValueError("workspace: its bytes must lie side by side")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _ck(lib().fise_latent_attention(C.byref(args), _p(workspace), nbytes, _stream(stream)))
+
+
+# --------------------------------------------------------------------------- transformer denoisers with experts
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _one_device(args, *tensors):
+    """The call's tensors, kept alive; all on one device, which is the current one when the call is made."""
+    args.keep = tensors
+    where = {t.device for t in tensors if t is not None}
+    if len(where) > 1:
+        raise ValueError(f"tensors of one call on {sorted(map(str, where))}")
+    args.device = where.pop()
+
+
+def _here(args, workspace=None):
+    """Address and size of the workspace, once the call's tensors are known to be where it is made."""
+    d = args.device
+    if d.type != "cuda" or (workspace is not None and workspace.device != d):
+        raise ValueError(f"tensors on {d}, workspace on {None if workspace is None else workspace.device}: a call works on one GPU")
+    if d.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {d}, which is not the current device")
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace: its bytes must lie side by side")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+FISE_ROTARY_ADJACENT, FISE_ROTARY_HALVES, FISE_ROTARY_AXIS_HALVES = 0, 1, 2
+_PAIRINGS = {"adjacent": FISE_ROTARY_ADJACENT, "halves": FISE_ROTARY_HALVES, "axis_halves": FISE_ROTARY_AXIS_HALVES}
+
+
+def rotary_tensor(x, y=None, start=0, x_is_map=False, y_is_map=False):
+    """One tensor of a fise_rotary call: x and y [B, rows, heads, d], neighbouring channels, any other strides; y None: in place.  The pairs begin at channel `start`."""
+    return (x, x if y is None else y, start, bool(x_is_map), bool(x_is_map if y is None else y_is_map))
+
+
+def rotary_args(tensors, axes, theta, pos=None, offset=None, grid=(0, 0, 0), tile_idx=None, n_active=0, tile=0, pairing="adjacent", shared_frequencies=False, inverse=False):
+    """Arguments of fise_rotary for one or two rotary_tensor()s; they keep the tensors alive.  axes: channels of each; theta: one number or one an axis;
+    pos: int32 or float [B or 1, M, axes], or None for the places on grid (T, H, W)."""
+    if not 1 <= len(tensors) <= 2 or not 1 <= len(axes) <= 4:
+        raise ValueError(f"{len(tensors)} tensors of {len(axes)} axes: 1 or 2 of 1 to 4")
+    theta = [float(theta)] * len(axes) if isinstance(theta, (int, float)) else [float(v) for v in theta]
+    offset = [0.0] * len(axes) if offset is None else [float(v) for v in offset]
+    if len(theta) != len(axes) or len(offset) != len(axes):
+        raise ValueError(f"{len(axes)} axes, theta for {len(theta)}, offsets for {len(offset)}")
+    T, H, W = grid
+    tokens = T * H * W
+    B = tensors[0][0].shape[0]
+    M = n_active * tile * tile if tile else tokens if pos is None else pos.shape[1]
+    a = fise_rotary_args()
+    for i, (x, y, start, x_map, y_map) in enumerate(tensors):
+        if x.dim() != 4 or x.shape != (B, tokens if x_map else M, *x.shape[2:]) or y.shape != (B, tokens if y_map else M, *x.shape[2:]) or x.dtype != y.dtype or x.dtype != tensors[0][0].dtype:
+            raise ValueError(f"tensor {i}: {tuple(x.shape)} of {x.dtype} to {tuple(y.shape)} of {y.dtype}, {B} elements of {M} rows (a map's: {tokens}) expected")
+        t = a.t[i]
+        for v in (x, y):
+            if v.shape[3] > 1 and v.stride(3) != 1:
+                raise ValueError(f"tensor {i}: channels must be neighbours, strides {v.stride()}")
+        if any(y.shape[j] > 1 and y.stride(j) == 0 for j in range(3)):
+            raise ValueError(f"tensor {i}: an output that repeats itself, strides {y.stride()}")
+        t.x, t.y, t.heads, t.d, t.start, t.x_is_map, t.y_is_map = _pn(x), _pn(y), x.shape[2], x.shape[3], start, int(x_map), int(y_map)
+        for side, v in (("x", x), ("y", y)):
+            for n, name in enumerate(("_batch", "_row", "_head")):
+                setattr(t, side + name, v.stride(n) if v.shape[n] > 1 else 0)      # (a stride that nothing steps by may be any number)
+    if pos is not None:
+        if pos.dtype not in (torch.int32, torch.float32) or pos.dim() != 3 or pos.shape[0] not in (1, B) or pos.shape[1:] != (M, len(axes)) or not pos.is_contiguous():
+            raise ValueError(f"pos: expected contiguous int32 or float [{B} or 1, {M}, {len(axes)}], got {tuple(pos.shape)} of {pos.dtype} with strides {pos.stride()}")
+        a.pos, a.pos_is_float, a.pos_B = _pn(pos), int(pos.dtype == torch.float32), pos.shape[0]
+    if tile_idx is not None and (tile_idx.dtype != torch.int32 or not tile_idx.is_contiguous() or tile_idx.numel() < n_active):
+        raise ValueError(f"tile_idx: expected {n_active} int32 numbers")
+    a.n_tensors, a.dtype, a.B, a.M, a.n_axes = len(tensors), _dt(tensors[0][0]), B, M, len(axes)
+    for j in range(len(axes)):
+        a.axis_dim[j], a.theta[j], a.offset[j] = axes[j], theta[j], offset[j]
+    a.pairing, a.shared_freq, a.inverse = _PAIRINGS[pairing], int(bool(shared_frequencies)), int(bool(inverse))
+    a.T, a.H, a.W, a.tile_idx, a.n_active, a.tile = T, H, W, _p(tile_idx), n_active, tile
+    _one_device(a, pos, tile_idx, *(v for t in tensors for v in t[:2]))
+    return a
+
+
+def fise_rotary(args, stream=None):
+    _here(args)
+    _ck(lib().fise_rotary(C.byref(args), _stream(stream)))
+
+
+def fise_fp8_quantize(x, codes, scale, block_rows=1, stream=None):
+    """x [M, K] -> codes [M, K] (uint8 or float8_e4m3fn) and scale [ceil(K / 128), M] (block_rows 1) or [ceil(M / 128), ceil(K / 128)] (block_rows 128)."""
+    M, K = x.shape
+    blocks = -(-K // 128)
+    if codes.dtype not in _CODES:
+        raise ValueError(f"codes: {codes.dtype}, expected one of {_CODES}")
+    if scale.dtype != torch.float32:
+        raise ValueError(f"scale: {scale.dtype}, expected float")
+    a = fise_fp8_linear_args()
+    _one_device(a, x, codes, scale)
+    x_stride, code_stride = _rows_of("x", x, (M, K)), _rows_of("codes", codes, (M, K))
+    scale_stride = _rows_of("scale", scale, (blocks, M) if block_rows == 1 else (-(-M // 128), blocks))
+    if M == 1:
+        x_stride = code_stride = -(-K // 16) * 16
+    _here(a)
+    _ck(lib().fise_fp8_quantize(_pn(x), _dt(x), x_stride, M, K, block_rows, _pn(codes), code_stride, _pn(scale), max(scale_stride, M if block_rows == 1 else blocks), _stream(stream)))
+
+
+def fp8_linear_args(x, w, w_scale, y, x_scale=None, bias=None, residual=None):
+    """Arguments of fise_fp8_linear for x [M, K] (float, bf16, or codes with x_scale [ceil(K / 128), M]), w [N, K] codes with w_scale [ceil(N / 128), ceil(K / 128)] and
+    y [M, N]; they keep the tensors alive."""
+    M, K = x.shape
+    N = w.shape[0]
+    a = fise_fp8_linear_args()
+    if w.dtype not in _CODES or (x_scale is not None and x.dtype not in _CODES):
+        raise ValueError(f"codes: w {w.dtype}, x {x.dtype}, expected one of {_CODES}")
+    a.x, a.x_dtype, a.x_stride = _pn(x), FISE_E4M3 if x_scale is not None else _dt(x), _rows_of("x", x, (M, K))
+    if M == 1:
+        a.x_stride = -(-K // 16) * 16
+    if x_scale is not None:
+        if x_scale.dtype != torch.float32:
+            raise ValueError(f"x_scale: {x_scale.dtype}, expected float")
+        a.x_scale, a.x_scale_stride = _pn(x_scale), max(_rows_of("x_scale", x_scale, (-(-K // 128), M)), M)
+    a.w, a.w_stride = _p(w), _rows_of("w", w, (N, K))
+    if N == 1:
+        a.w_stride = -(-K // 16) * 16
+    _like("w_scale", w_scale, (-(-N // 128), -(-K // 128)), (torch.float32,))
+    a.w_scale, a.M, a.N, a.K = _p(w_scale), M, N, K
+    if bias is not None:
+        _like("bias", bias, (N,), (torch.float32, torch.bfloat16))
+        a.bias, a.bias_dtype = _p(bias), _dt(bias)
+    a.y, a.y_dtype, a.y_stride = _pn(y), _dt(y), _rows_of("y", y, (M, N))
+    if residual is not None:
+        if residual.dtype != y.dtype:
+            raise ValueError(f"residual is {residual.dtype}, y {y.dtype}")
+        a.residual, a.residual_stride = _pn(residual), _rows_of("residual", residual, (M, N))
+    _one_device(a, x, x_scale, w, w_scale, bias, residual, y)
+    return a
+
+
+def fise_fp8_linear_workspace_bytes(args):
+    return lib().fise_fp8_linear_workspace_bytes(C.byref(args))
+
+
+def fise_fp8_linear(args, workspace=None, stream=None):
+    ws, nbytes = _here(args, workspace)
+    _ck(lib().fise_fp8_linear(C.byref(args), ws, nbytes, _stream(stream)))
+
+
+FISE_SCORE_SOFTMAX, FISE_SCORE_SIGMOID = 0, 1
+_SCORES = {"softmax": FISE_SCORE_SOFTMAX, "sigmoid": FISE_SCORE_SIGMOID}
+
+
+def route_args(logits, ids, weights, offsets=None, slots=None, score="softmax", bias=None, groups=1, top_groups=1, group_top=1, renormalize=True, scale=1.0):
+    """Arguments of fise_route_experts for logits [T, E], ids int32 and weights float [T, k], offsets int32 [E + 1] and slots int32 [T * k]; they keep the tensors alive."""
+    T, E = logits.shape
+    k = ids.shape[1]
+    a = fise_route_args()
+    a.logits, a.dtype, a.stride = _pn(logits), _dt(logits), max(_rows_of("logits", logits, (T, E)), E)
+    _like("ids", ids, (T, k), (torch.int32,))
+    _like("weights", weights, (T, k), (torch.float32,))
+    if (offsets is None) != (slots is None):
+        raise ValueError("offsets and slots are given together")
+    if offsets is not None:
+        _like("offsets", offsets, (E + 1,), (torch.int32,))
+        _like("slots", slots, (T * k,), (torch.int32,))
+        a.offsets, a.slots = _p(offsets), _pn(slots)
+    if bias is not None:
+        _like("bias", bias, (E,), (torch.float32,))
+        a.bias = _p(bias)
+    a.ids, a.weights = _pn(ids), _pn(weights)
+    a.T, a.E, a.k, a.score, a.groups, a.top_groups, a.group_top = T, E, k, _SCORES[score], groups, top_groups, group_top
+    a.renormalize, a.scale = int(bool(renormalize)), scale
+    _one_device(a, logits, bias, ids, weights, offsets, slots)
+    return a
+
+
+def fise_route_experts_workspace_bytes(args):
+    return lib().fise_route_experts_workspace_bytes(C.byref(args))
+
+
+def fise_route_experts(args, workspace=None, stream=None):
+    ws, nbytes = _here(args, workspace)
+    _ck(lib().fise_route_experts(C.byref(args), ws, nbytes, _stream(stream)))
+
+
+def expert_mlp_args(x, ids, weights, offsets, slots, w_in, w_in_scale, w_out, w_out_scale, y, residual=None):
+    """Arguments of fise_expert_mlp for x [T, K], what fise_route_experts left, codes w_in [E, 2, I, K] and w_out [E, N, I] with their scales, y [T, N]; they keep the
+    tensors alive."""
+    T, K = x.shape
+    E, _, I, _ = w_in.shape
+    N, k = w_out.shape[1], ids.shape[1]
+    blocks = lambda n: -(-n // 128)
+    a = fise_expert_mlp_args()
+    a.x, a.x_dtype, a.x_stride = _pn(x), _dt(x), max(_rows_of("x", x, (T, K)), K)
+    if T == 1:
+        a.x_stride = -(-K // 8) * 8
+    _like("ids", ids, (T, k), (torch.int32,))
+    _like("weights", weights, (T, k), (torch.float32,))
+    _like("offsets", offsets, (E + 1,), (torch.int32,))
+    _like("slots", slots, (T * k,), (torch.int32,))
+    _like("w_in", w_in, (E, 2, I, K), _CODES)
+    _like("w_in_scale", w_in_scale, (E, 2, blocks(I), blocks(K)), (torch.float32,))
+    _like("w_out", w_out, (E, N, I), _CODES)
+    _like("w_out_scale", w_out_scale, (E, blocks(N), blocks(I)), (torch.float32,))
+    a.ids, a.weights, a.offsets, a.slots = _pn(ids), _pn(weights), _p(offsets), _pn(slots)
+    a.T, a.K, a.k, a.E, a.I, a.N = T, K, k, E, I, N
+    a.w_in, a.w_in_scale, a.w_out, a.w_out_scale = _p(w_in), _p(w_in_scale), _p(w_out), _p(w_out_scale)
+    a.y, a.y_dtype, a.y_stride = _pn(y), _dt(y), max(_rows_of("y", y, (T, N)), N)
+    if T == 1:
+        a.y_stride = -(-N // 8) * 8
+    if residual is not None:
+        if residual.dtype != y.dtype:
+            raise ValueError(f"residual is {residual.dtype}, y {y.dtype}")
+        a.residual, a.residual_stride = _pn(residual), max(_rows_of("residual", residual, (T, N)), N)
+        if T == 1:
+            a.residual_stride = a.y_stride
+    _one_device(a, x, ids, weights, offsets, slots, w_in, w_in_scale, w_out, w_out_scale, residual, y)
+    return a
+
+
+def fise_expert_mlp_workspace_bytes(args):
+    return lib().fise_expert_mlp_workspace_bytes(C.byref(args))
+
+
+def fise_expert_mlp(args, workspace, stream=None):
+    ws, nbytes = _here(args, workspace)
+    _ck(lib().fise_expert_mlp(C.byref(args), ws, nbytes, _stream(stream)))
 
 
 # --------------------------------------------------------------------------- UNet

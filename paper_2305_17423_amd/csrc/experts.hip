@@ -1,0 +1,156 @@
+// The feed-forward of the chosen experts: h = silu(Wg x) * (Wu x) and Wo h for every pair (token, expert) in the experts' order, then a token's weighted sum.
+//
+// Four launches: rows of x into 8 bits, with the table of tiles (a tile has rows of one expert); gate and up of a tile side by side in a wave, so that h leaves the
+// accumulators in 8 bits with the scale of its 128 channels; Wo; and the sum, which reads a pair's row where its token's list says it is.  No atomics: a result depends on its arguments only.
+#include "fp8.h"
+#include "fp8_choice.h"
+
+namespace fise {
+
+struct ExpertsArgs {
+    const void* x; long long x_stride; int T, K, units;
+    unsigned char* codes; long long code_stride; float* scale;
+    const int* offsets; int E, pairs, bm, m_tiles; int* table;
+};
+
+// table[2 t] = first row of tile t in the experts' order, table[2 t + 1] = expert << 16 | rows (0: no such tile).  Offsets that do not ascend or leave 0..pairs count as the nearest that do not.
+__device__ void experts_table(const ExpertsArgs& a) {
+    __shared__ int sums[2][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (a.E + 255) / 256, e0 = min(tid * each, a.E), e1 = min(e0 + each, a.E);
+    // the offsets' running maximum
+    int top = 0;
+    for (int e = e0; e < e1; ++e) top = max(top, min(max(a.offsets[e], 0), a.pairs));
+    int before = top;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int n = __shfl_up(before, o); if (lane >= o) before = max(before, n); }
+    if (lane == 63) sums[0][wave] = before;
+    __syncthreads();
+    before = __shfl_up(before, 1);
+    if (lane == 0) before = 0;
+    for (int w = 0; w < wave; ++w) before = max(before, sums[0][w]);
+    auto tiles_from = [&](int at, bool write) {
+        int start = before;
+        for (int e = e0; e < e1; ++e) {
+            start = max(start, min(max(a.offsets[e], 0), a.pairs));
+            const int end = max(start, min(max(a.offsets[e + 1], 0), a.pairs));
+            for (int r = start; r < end; r += a.bm, ++at)
+                if (write && at < a.m_tiles) { a.table[2 * at] = r; a.table[2 * at + 1] = e << 16 | min(a.bm, end - r); }
+        }
+        return at;
+    };
+    int n = tiles_from(0, false), upto = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int m = __shfl_up(upto, o); if (lane >= o) upto += m; }
+    if (lane == 63) sums[1][wave] = upto;
+    __syncthreads();
+    int at = upto - n, all = 0;
+    for (int w = 0; w < 4; ++w) { if (w < wave) at += sums[1][w]; all += sums[1][w]; }
+    tiles_from(at, true);
+    for (int t = all + tid; t < a.m_tiles; t += 256) { a.table[2 * t] = 0; a.table[2 * t + 1] = 0; }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void experts_rows_kernel(ExpertsArgs a) {
+    if (blockIdx.x == 0) { experts_table(a); return; }
+    fp8_quantize_unit((const T*)a.x, a.x_stride, a.T, a.K, a.units, a.units * 8, a.codes, a.code_stride, a.scale, (long long)a.T, (long long)(blockIdx.x - 1) * 256 + threadIdx.x);
+}
+
+struct ExpertsSum {
+    const void* rows; const int* ids; const float* weights; const void* residual; long long residual_stride; void* y; long long y_stride;
+    int T, k, N, units;
+};
+template <typename T> __global__ __launch_bounds__(256) void experts_sum_kernel(ExpertsSum a) {
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x, t = id / a.units;
+    const int n = (int)(id - t * a.units) * 8;
+    if (t >= a.T) return;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.residual) fp8_load8((const T*)a.residual + t * a.residual_stride + n, v);
+    for (int j = 0; j < a.k; ++j) {
+        const long long p = t * a.k + j;
+        const float w = a.weights[p];
+        float r[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (a.ids[p] >= 0) fp8_load8((const T*)a.rows + p * a.N + n, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(w, r[i], v[i]);
+    }
+    T* const y = (T*)a.y + t * a.y_stride + n;
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4_t*>(y) = f32x4_t{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4_t*>(y + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+    } else *reinterpret_cast<u32x4_t*>(y) = u32x4_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])};
+}
+
+static int expert_sizes(const char* fn, const fise_expert_mlp_args* g) {
+    if ((g->x_dtype != FISE_F32 && g->x_dtype != FISE_BF16) || (g->y_dtype != FISE_F32 && g->y_dtype != FISE_BF16)) return fail(FISE_ERR_DTYPE, "%s: dtypes x %d, y %d", fn, g->x_dtype, g->y_dtype);
+    if (g->T < 0 || g->K < 1 || g->I < 1 || g->N < 1 || g->K > 1 << 16 || g->I > 1 << 16 || g->N > 1 << 16 || g->E < 1 || g->E > 1024 || g->k < 1 || g->k > 64)
+        return fail(FISE_ERR_SHAPE, "%s: T=%d K=%d I=%d N=%d E=%d k=%d", fn, g->T, g->K, g->I, g->N, g->E, g->k);
+    if ((long long)g->T * g->k >= 1 << 24 || (long long)g->T * ((g->K + 127) / 128 * 128) >= 1 << 30)
+        return fail(FISE_ERR_SHAPE, "%s: T=%d k=%d K=%d: T k below 2^24, T K below 2^30", fn, g->T, g->k, g->K);
+    if (g->K % 16 || g->I % 16 || g->N % 8) return fail(FISE_ERR_ALIGN, "%s: K=%d, I=%d must be multiples of 16, N=%d of 8", fn, g->K, g->I, g->N);
+    return FISE_OK;
+}
+
+}  // namespace fise
+
+using namespace fise;
+
+extern "C" size_t fise_expert_mlp_workspace_bytes(const fise_expert_mlp_args* g) {
+    const char* fn = "fise_expert_mlp";
+    if (!g) { fail(FISE_ERR_NULL, "%s: null pointer", fn); return 0; }
+    if (expert_sizes(fn, g)) return 0;
+    return (size_t)expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, g->y_dtype == FISE_F32 ? 4 : 2).bytes;
+}
+
+extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fise_expert_mlp";
+    if (!g || !g->x || !g->ids || !g->weights || !g->offsets || !g->slots || !g->w_in || !g->w_in_scale || !g->w_out || !g->w_out_scale || !g->y) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (int e = expert_sizes(fn, g)) return e;
+    if (g->x_stride < g->K || g->y_stride < g->N || (g->residual && g->residual_stride < g->N))
+        return fail(FISE_ERR_SHAPE, "%s: strides x %lld, y %lld, residual %lld", fn, (long long)g->x_stride, (long long)g->y_stride, (long long)g->residual_stride);
+    if (g->x_stride % 8 || g->y_stride % 8 || (g->residual && g->residual_stride % 8) || !aligned16(g->x) || !aligned16(g->y) || !aligned16(g->residual) || !aligned16(g->w_in) || !aligned16(g->w_out) ||
+        ((uintptr_t)g->ids | (uintptr_t)g->weights | (uintptr_t)g->offsets | (uintptr_t)g->slots | (uintptr_t)g->w_in_scale | (uintptr_t)g->w_out_scale) & 3)
+        return fail(FISE_ERR_ALIGN, "%s: rows and codes must be 16-byte aligned, strides multiples of 8, lists and scales aligned to their type", fn);
+    const int es = g->y_dtype == FISE_F32 ? 4 : 2;
+    const ExpertChoice c = expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, es);
+    if (g->T && (!workspace || workspace_bytes < (size_t)c.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)c.bytes);
+    if ((uintptr_t)workspace & 255) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
+    if (g->T == 0) return FISE_OK;
+    const int blocks_i = (g->I + FP8_BLOCK - 1) / FP8_BLOCK, blocks_k = (g->K + FP8_BLOCK - 1) / FP8_BLOCK, blocks_n = (g->N + FP8_BLOCK - 1) / FP8_BLOCK, n_tiles = (g->N + 255) / 256;
+    if (c.m_tiles * std::max(blocks_i, n_tiles) > 0x7fffffff) return fail(FISE_ERR_SHAPE, "%s: more tiles than a launch holds", fn);
+    const hipStream_t st = as_stream(stream);
+    unsigned char* const ws = (unsigned char*)workspace;
+    const int pairs = g->T * g->k;
+    ExpertsArgs r{};
+    r.x = g->x; r.x_stride = g->x_stride; r.T = g->T; r.K = g->K; r.units = blocks_k * 16; r.codes = ws; r.code_stride = c.x_stride; r.scale = (float*)(ws + c.x_scale_off);
+    r.offsets = g->offsets; r.E = g->E; r.pairs = pairs; r.bm = c.bm; r.m_tiles = (int)c.m_tiles; r.table = (int*)(ws + c.table_off);
+    const dim3 rows_grid((unsigned)(1 + ((long long)g->T * r.units + 255) / 256));
+    if (g->x_dtype == FISE_F32) hipLaunchKernelGGL(experts_rows_kernel<float>, rows_grid, dim3(256), 0, st, r);
+    else hipLaunchKernelGGL(experts_rows_kernel<bf16_t>, rows_grid, dim3(256), 0, st, r);
+    FISE_CHECK_LAUNCH(fn);
+    Fp8TileArgs a{};
+    a.table = r.table; a.pairs = pairs; a.k = g->k; a.slots = g->slots; a.M = pairs; a.m_tiles = (int)c.m_tiles;
+    a.x = ws; a.x_stride = c.x_stride; a.x_bytes = (long long)g->T * c.x_stride; a.x_scale = r.scale; a.x_scale_stride = g->T;
+    a.w = g->w_in; a.w_stride = g->K; a.w_expert = 2LL * g->I * g->K; a.w_scale = g->w_in_scale; a.w_scale_expert = 2 * blocks_i * blocks_k;
+    a.N = g->I; a.K = g->K; a.n_tiles = blocks_i;
+    a.h = ws + c.h_off; a.h_stride = c.h_stride; a.h_scale = (float*)(ws + c.h_scale_off); a.h_scale_stride = pairs;
+    {
+        ProfileScope prof(PROF_IGEMM_GEGLU, 4.0 * pairs * g->I * g->K, 2.0 * std::min(g->E, pairs) * g->I * g->K + (double)pairs * (g->K + g->I), st);
+        if (int e = c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED>(a, fn, st)) return e;
+    }
+    a.x = a.h; a.x_stride = c.h_stride; a.x_scale = a.h_scale; a.x_scale_stride = pairs;
+    a.w = g->w_out; a.w_stride = g->I; a.w_expert = (long long)g->N * g->I; a.w_scale = g->w_out_scale; a.w_scale_expert = blocks_n * blocks_i;
+    a.N = g->N; a.K = g->I; a.n_tiles = n_tiles;
+    a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4;
+    {
+        ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * pairs * g->I * g->N, (double)std::min(g->E, pairs) * g->I * g->N + (double)pairs * (g->I + g->N * es), st);
+        if (int e = c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS>(a, fn, st)) return e;
+    }
+    ExpertsSum s{};
+    s.rows = a.y; s.ids = g->ids; s.weights = g->weights; s.residual = g->residual; s.residual_stride = g->residual_stride; s.y = g->y; s.y_stride = g->y_stride;
+    s.T = g->T; s.k = g->k; s.N = g->N; s.units = g->N / 8;
+    const dim3 sum_grid((unsigned)(((long long)g->T * s.units + 255) / 256));
+    if (es == 4) hipLaunchKernelGGL(experts_sum_kernel<float>, sum_grid, dim3(256), 0, st, s);
+    else hipLaunchKernelGGL(experts_sum_kernel<bf16_t>, sum_grid, dim3(256), 0, st, s);
+    FISE_CHECK_LAUNCH(fn);
+    return FISE_OK;
+}

@@ -1,0 +1,139 @@
+// 8-bit floating point (e4m3) with a scale for each block of 128 columns: rows and weights into codes, and the product of the two.
+//
+// Scales that the library makes are powers of two: dividing by one is exact, so a code is the value rounded once, and the largest of a block uses the format's range to
+// within a factor of two, which costs none of the three bits of mantissa.
+#include "fp8.h"
+#include "fp8_choice.h"
+
+namespace fise {
+
+template <typename T>
+__global__ __launch_bounds__(256) void fp8_rows_kernel(const T* x, long long x_stride, int M, int K, int units, int written, unsigned char* codes, long long code_stride,
+                                                       float* scale, long long scale_stride) {
+    fp8_quantize_unit(x, x_stride, M, K, units, written, codes, code_stride, scale, scale_stride, (long long)blockIdx.x * 256 + threadIdx.x);
+}
+
+// A workgroup has 128 x 128 values: a lane eight columns of every sixteenth row.
+template <typename T>
+__global__ __launch_bounds__(256) void fp8_block_kernel(const T* x, long long x_stride, int M, int K, int blocks, unsigned char* codes, long long code_stride,
+                                                        float* scale, long long scale_stride) {
+    __shared__ unsigned largest[4];
+    const int tid = threadIdx.x, bk = blockIdx.x % blocks, bm = blockIdx.x / blocks, col = bk * FP8_BLOCK + (tid & 15) * 8;
+    const long long row0 = (long long)bm * FP8_BLOCK + (tid >> 4);
+    float v[8][8];
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const long long row = row0 + 16 * j;
+        if (row < M && col < K) fp8_load8(x + row * x_stride + col, v[j]);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, fp8_magnitude(v[j][i]));
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
+    if ((tid & 63) == 0) largest[tid >> 6] = top;
+    __syncthreads();
+    const int e = fp8_exponent(max(max(largest[0], largest[1]), max(largest[2], largest[3])));
+    const float inv = fp8_inverse(e);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const long long row = row0 + 16 * j;
+        if (row < M && col < K)
+            *reinterpret_cast<u32x2_t*>(codes + row * code_stride + col) =
+                u32x2_t{fp8_codes(v[j][0], v[j][1], v[j][2], v[j][3], inv), fp8_codes(v[j][4], v[j][5], v[j][6], v[j][7], inv)};
+    }
+    if (tid == 0) scale[bm * scale_stride + bk] = fp8_power(e);
+}
+
+static int fp8_rows(const char* fn, const void* x, int dtype, long long x_stride, int M, int K, int written, unsigned char* codes, long long code_stride, float* scale,
+                    long long scale_stride, hipStream_t st) {
+    const int units = (K + FP8_BLOCK - 1) / FP8_BLOCK * 16;
+    const dim3 grid((unsigned)(((long long)M * units + 255) / 256));
+    if (dtype == FISE_F32) hipLaunchKernelGGL(fp8_rows_kernel<float>, grid, dim3(256), 0, st, (const float*)x, x_stride, M, K, units, written, codes, code_stride, scale, scale_stride);
+    else hipLaunchKernelGGL(fp8_rows_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)x, x_stride, M, K, units, written, codes, code_stride, scale, scale_stride);
+    FISE_CHECK_LAUNCH(fn);
+    return FISE_OK;
+}
+
+}  // namespace fise
+
+using namespace fise;
+
+extern "C" int fise_fp8_quantize(const void* x, int dtype, int64_t x_stride, int M, int K, int block_rows, uint8_t* codes, int64_t code_stride, float* scale, int64_t scale_stride,
+                                 void* stream) {
+    const char* fn = "fise_fp8_quantize";
+    if (!x || !codes || !scale) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (dtype != FISE_F32 && dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d", fn, dtype);
+    if (M < 0 || K < 1 || M > 1 << 30 || K > 1 << 20 || (block_rows != 1 && block_rows != 128)) return fail(FISE_ERR_SHAPE, "%s: M=%d K=%d, blocks of %d rows (1 or 128)", fn, M, K, block_rows);
+    const long long blocks = (K + FP8_BLOCK - 1) / FP8_BLOCK;
+    if (x_stride < K || code_stride < K || scale_stride < (block_rows == 1 ? M : blocks))
+        return fail(FISE_ERR_SHAPE, "%s: strides x %lld, codes %lld, scales %lld", fn, (long long)x_stride, (long long)code_stride, (long long)scale_stride);
+    if (K % 8 || x_stride % 8 || code_stride % 8 || !aligned16(x) || ((uintptr_t)codes & 7) || ((uintptr_t)scale & 3))
+        return fail(FISE_ERR_ALIGN, "%s: K and the strides of x and of the codes must be multiples of 8, x 16-byte, codes 8-byte aligned", fn);
+    if (M == 0) return FISE_OK;
+    if (block_rows == 1) return fp8_rows(fn, x, dtype, x_stride, M, K, K, codes, code_stride, scale, scale_stride, as_stream(stream));
+    const dim3 grid((unsigned)(((long long)M + 127) / 128 * blocks));
+    if (dtype == FISE_F32) hipLaunchKernelGGL(fp8_block_kernel<float>, grid, dim3(256), 0, as_stream(stream), (const float*)x, (long long)x_stride, M, K, (int)blocks, codes, (long long)code_stride, scale, (long long)scale_stride);
+    else hipLaunchKernelGGL(fp8_block_kernel<bf16_t>, grid, dim3(256), 0, as_stream(stream), (const bf16_t*)x, (long long)x_stride, M, K, (int)blocks, codes, (long long)code_stride, scale, (long long)scale_stride);
+    FISE_CHECK_LAUNCH(fn);
+    return FISE_OK;
+}
+
+static int fp8_linear_sizes(const char* fn, const fise_fp8_linear_args* g) {
+    if (g->x_dtype != FISE_F32 && g->x_dtype != FISE_BF16 && g->x_dtype != FISE_E4M3) return fail(FISE_ERR_DTYPE, "%s: dtype of x %d", fn, g->x_dtype);
+    if (g->M < 0 || g->N < 1 || g->K < 1 || g->M > 1 << 20 || g->N > 1 << 20 || g->K > 1 << 20) return fail(FISE_ERR_SHAPE, "%s: M=%d N=%d K=%d", fn, g->M, g->N, g->K);
+    return FISE_OK;
+}
+
+extern "C" size_t fise_fp8_linear_workspace_bytes(const fise_fp8_linear_args* g) {
+    const char* fn = "fise_fp8_linear";
+    if (!g) { fail(FISE_ERR_NULL, "%s: null pointer", fn); return 0; }
+    if (fp8_linear_sizes(fn, g) || g->x_dtype == FISE_E4M3) return 0;
+    return (size_t)fp8_space(g->M, g->K).bytes;
+}
+
+extern "C" int fise_fp8_linear(const fise_fp8_linear_args* g, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fise_fp8_linear";
+    if (!g || !g->x || !g->w || !g->w_scale || !g->y) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (int e = fp8_linear_sizes(fn, g)) return e;
+    auto known = [](int d) { return d == FISE_F32 || d == FISE_BF16; };
+    if (!known(g->y_dtype) || (g->bias && !known(g->bias_dtype))) return fail(FISE_ERR_DTYPE, "%s: dtypes y %d, bias %d", fn, g->y_dtype, g->bias_dtype);
+    const bool codes = g->x_dtype == FISE_E4M3;
+    if (codes != (g->x_scale != nullptr)) return fail(FISE_ERR_NULL, "%s: codes have scales, other rows have none", fn);
+    if (g->x_stride < g->K || g->w_stride < g->K || g->y_stride < g->N || (g->residual && g->residual_stride < g->N) || (codes && g->x_scale_stride < g->M) || g->x_stride > 1 << 22 || g->w_stride > 1 << 22)
+        return fail(FISE_ERR_SHAPE, "%s: M=%d N=%d K=%d, strides x %lld, its scales %lld, w %lld, y %lld, residual %lld", fn, g->M, g->N, g->K, (long long)g->x_stride, (long long)g->x_scale_stride,
+                    (long long)g->w_stride, (long long)g->y_stride, (long long)g->residual_stride);
+    if (g->K % 16 || g->w_stride % 16 || g->x_stride % (codes ? 16 : 8) || !aligned16(g->x) || !aligned16(g->w))
+        return fail(FISE_ERR_ALIGN, "%s: K and the strides of codes must be multiples of 16, that of other x of 8, x and w 16-byte aligned", fn);
+    const size_t ye = g->y_dtype == FISE_F32 ? 4 : 2, be = g->bias_dtype == FISE_F32 ? 4 : 2;
+    if ((uintptr_t)g->y % ye || (uintptr_t)g->residual % ye || (g->bias && (uintptr_t)g->bias % be) || ((uintptr_t)g->x_scale | (uintptr_t)g->w_scale) & 3)
+        return fail(FISE_ERR_ALIGN, "%s: y, residual, bias and scales must be aligned to their type", fn);
+    const Fp8Space space = codes ? Fp8Space{} : fp8_space(g->M, g->K);
+    if (space.bytes && (!workspace || workspace_bytes < (size_t)space.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)space.bytes);
+    if (space.bytes && ((uintptr_t)workspace & 255)) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
+    if (g->M == 0) return FISE_OK;
+    const hipStream_t st = as_stream(stream);
+    Fp8TileArgs a{};
+    const Fp8Choice c = fp8_choose(g->M, g->N, g->y_dtype == FISE_F32);
+    if (c.m_tiles * c.n_tiles > 0x7fffffff) return fail(FISE_ERR_SHAPE, "%s: M=%d N=%d: more tiles than a launch holds", fn, g->M, g->N);
+    if (codes) {
+        a.x = (const unsigned char*)g->x; a.x_stride = g->x_stride; a.x_scale = g->x_scale; a.x_scale_stride = g->x_scale_stride;
+    } else {
+        float* const scale = (float*)((unsigned char*)workspace + space.scale_off);
+        if (int e = fp8_rows(fn, g->x, g->x_dtype, g->x_stride, g->M, g->K, (int)space.stride, (unsigned char*)workspace, space.stride, scale, g->M, st)) return e;
+        a.x = (const unsigned char*)workspace; a.x_stride = space.stride; a.x_scale = scale; a.x_scale_stride = g->M;
+    }
+    a.w = g->w; a.w_stride = g->w_stride; a.w_scale = g->w_scale;
+    a.M = g->M; a.N = g->N; a.K = g->K; a.m_tiles = (int)c.m_tiles; a.n_tiles = (int)c.n_tiles;
+    a.bias = g->bias; a.bias_f32 = g->bias_dtype == FISE_F32; a.residual = g->residual; a.residual_stride = g->residual_stride;
+    a.y = g->y; a.y_stride = g->y_stride; a.y_f32 = g->y_dtype == FISE_F32;
+    ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * g->M * g->N * g->K, (double)g->N * g->K + (double)g->M * g->K + (double)g->M * g->N * ye, st);
+    switch (c.form) {
+        case FP8_FORM_256: return launch_fp8_tile<8, 4, 2, 4, FP8_LINEAR>(a, fn, st);
+        case FP8_FORM_128: return a.y_f32 ? launch_fp8_tile<4, 4, 2, 2, FP8_LINEAR, true>(a, fn, st) : launch_fp8_tile<4, 4, 2, 2, FP8_LINEAR>(a, fn, st);
+        default: return a.y_f32 ? launch_fp8_tile<2, 2, 4, 1, FP8_LINEAR, true>(a, fn, st) : launch_fp8_tile<2, 2, 4, 1, FP8_LINEAR>(a, fn, st);
+    }
+}

@@ -1,0 +1,53 @@
+// Products in 8-bit floating point: which tile a call takes and what its workspace holds.  Plain C++: the CPU tests compile it too.
+#pragma once
+#include <algorithm>
+#include <cstdint>
+
+namespace fise {
+
+enum { FP8_FORM_256 = 0, FP8_FORM_128 = 1, FP8_FORM_32 = 2 };          // 256 x 256, 128 x 128, 32 tokens x 128 outputs
+
+struct Fp8Choice { int form, bm, bn; int64_t m_tiles, n_tiles; };
+
+// exact: products in bf16 (float results), whose operands leave no room for the largest tile
+inline Fp8Choice fp8_choose(int64_t M, int64_t N, bool exact) {
+    Fp8Choice c{};
+    auto set = [&](int form, int bm, int bn) { c.form = form; c.bm = bm; c.bn = bn; c.m_tiles = (M + bm - 1) / bm; c.n_tiles = (N + bn - 1) / bn; };
+    set(FP8_FORM_256, 256, 256);
+    if (exact || c.m_tiles * c.n_tiles < 200) set(FP8_FORM_128, 128, 128);
+    if (M <= 32) set(FP8_FORM_32, 32, 128);
+    return c;
+}
+
+// rows that the call puts in 8 bits: codes of whole blocks, then the scales of each block
+struct Fp8Space { int64_t stride, scale_off, bytes; };
+inline Fp8Space fp8_space(int64_t M, int64_t K) {
+    Fp8Space s{};
+    const int64_t blocks = (K + 127) / 128;
+    s.stride = blocks * 128;
+    s.scale_off = (M * s.stride + 255) / 256 * 256;
+    s.bytes = s.scale_off + (M * blocks * 4 + 255) / 256 * 256;
+    return s;
+}
+
+// The experts' feed-forward: tokens of a tile, an upper bound of the tiles, and the workspace.
+struct ExpertChoice {
+    int bm; int64_t m_tiles;
+    int64_t x_stride, x_scale_off, h_off, h_stride, h_scale_off, out_off, table_off, bytes;
+};
+inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, int64_t E, int64_t k, int y_bytes) {
+    ExpertChoice c{};
+    const int64_t P = T * k;
+    auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
+    c.bm = P >= 64 * E ? 128 : 32;
+    c.m_tiles = P / c.bm + std::min(E, P);
+    const Fp8Space x = fp8_space(T, K), h = fp8_space(P, I);
+    c.x_stride = x.stride; c.x_scale_off = x.scale_off;
+    c.h_off = x.bytes; c.h_stride = h.stride; c.h_scale_off = c.h_off + h.scale_off;
+    c.out_off = c.h_off + h.bytes;
+    c.table_off = c.out_off + up(P * N * y_bytes);
+    c.bytes = c.table_off + up(c.m_tiles * 8);
+    return c;
+}
+
+}  // namespace fise

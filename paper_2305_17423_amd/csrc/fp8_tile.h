@@ -1,0 +1,325 @@
+// Products of 8-bit rows with 8-bit weights on tiles: what fp8.hip and experts.hip share.  Internal.
+//
+// A block of 128 columns is one 16x16x128 matrix instruction, so the sum of a block's products comes out of it by itself and goes to the float accumulators times its two
+// scales: one multiply-add for each value of a result, beside the matrix unit.  The weights' rows are the first index of the product: a lane has one token (its scale is
+// the lane's) and four neighbouring outputs.
+// The 8-bit instruction adds its products eight at a time and drops of each what is below 2^-13 of the largest of the eight (measured: eight of 2^14 and 2^1 add up exactly, those of 2^0
+// are gone); 16x16x32, of half its rate, does the same.  That is up to 2^-10 of the magnitudes' sum, next to 2^-8 of a bf16 result, so bf16 results and the experts take it; float results
+// (EXACT) are made of the same codes as bf16, whose instruction keeps all of a product, at half the rate.
+#pragma once
+#include "common.h"
+#include "latent.h"
+
+namespace fise {
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 fp8_bf16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int FP8_BLOCK = 128;                      // columns of a scale, bytes of a row in a tile
+
+// exponent of the smallest power of two, 2^-126 at least, that leaves a magnitude (its bits; finite) at most 448 = 1.75 * 2^8
+__device__ __forceinline__ int fp8_exponent(unsigned bits) {
+    return max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -126);
+}
+__device__ __forceinline__ float fp8_power(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+// magnitude for the scale: what is not finite does not count
+__device__ __forceinline__ unsigned fp8_magnitude(float v) {
+    const unsigned b = __float_as_uint(v) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+// four values times `inverse`, a power of two that brings them to 448 at most, as codes; what is not finite is NaN (there is no infinity)
+__device__ __forceinline__ unsigned fp8_codes(float a, float b, float c, float d, float inverse) {
+    const float v[4] = {a * inverse, b * inverse, c * inverse, d * inverse};
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(fabsf(v[i]) <= 448.f)) w |= 0x7f << (8 * i);
+    return (unsigned)w;
+}
+__device__ __forceinline__ float fp8_inverse(int e) { return fp8_power(-e); }      // (e is between -126 and 119)
+
+// What a tile kernel works on.  Rows of x are codes padded with zeros to whole blocks where the library made them.
+enum { FP8_LINEAR = 0,      // y[m, n] of rows 0..M-1
+       FP8_GATED = 1,       // rows of pairs, gate and up: silu(gate) * up in 8 bits again
+       FP8_PAIRS = 2 };     // rows of those, to the pair's row of a scratch
+struct Fp8TileArgs {
+    const unsigned char* x; long long x_stride; long long x_bytes;     // rows of codes (GATED: of tokens, in one buffer of x_bytes)
+    const float* x_scale; long long x_scale_stride;                    // [block][row]
+    const unsigned char* w; long long w_stride, w_expert;              // an expert's weights apart
+    const float* w_scale; int w_scale_expert;
+    int M, N, K;                                                       // N: rows of the weights (GATED: of the gate)
+    int m_tiles, n_tiles;
+    const void* bias; int bias_f32; const void* residual; long long residual_stride;
+    void* y; long long y_stride; int y_f32;
+    // experts
+    const int* table; int pairs, k;                                    // table[tile] = expert << 24 ..., see experts.hip
+    const int* slots;
+    unsigned char* h; long long h_stride; float* h_scale; long long h_scale_stride;
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ f32x4_t fp8_mfma(i32x8_t a, i32x8_t b) {
+    const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, z, 0, 0, 0, 0, 0, 0);      // (no scales: the plain instruction)
+}
+// A lane's 32 codes of a row; EXACT: as bf16, which holds every code.
+template <bool EXACT> struct Fp8Operand;
+template <> struct Fp8Operand<false> {
+    i32x8_t v;
+    __device__ __forceinline__ void ld(const unsigned char* row, int at0, int at1) {
+        const i32x4_t lo = *reinterpret_cast<const i32x4_t*>(row + at0), hi = *reinterpret_cast<const i32x4_t*>(row + at1);
+        v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+template <> struct Fp8Operand<true> {
+    bf16x8_t v[4];
+    __device__ __forceinline__ void ld(const unsigned char* row, int at0, int at1) {
+        const i32x4_t c[2] = {*reinterpret_cast<const i32x4_t*>(row + at0), *reinterpret_cast<const i32x4_t*>(row + at1)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4_t w;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int four = c[j >> 1][(j & 1) * 2 + i];
+                w[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, 1.f, false));
+                w[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, 1.f, true));
+            }
+            v[j] = __builtin_bit_cast(bf16x8_t, w);
+        }
+    }
+};
+__device__ __forceinline__ f32x4_t fp8_product(const Fp8Operand<false>& a, const Fp8Operand<false>& b) { return fp8_mfma(a.v, b.v); }
+__device__ __forceinline__ f32x4_t fp8_product(const Fp8Operand<true>& a, const Fp8Operand<true>& b) {
+    f32x4_t p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(fp8_bf16x8_t, a.v[j]), __builtin_bit_cast(fp8_bf16x8_t, b.v[j]), p, 0, 0, 0);
+    return p;
+}
+__device__ __forceinline__ void fp8_store4(void* y, int f32, long long at, const float* v, int n, bool wide) {
+    if (f32) {
+        float* p = reinterpret_cast<float*>(y) + at;
+        if (wide) *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
+    } else {
+        bf16_t* p = reinterpret_cast<bf16_t*>(y) + at;
+        if (wide) *reinterpret_cast<u32x2_t*>(p) = u32x2_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (i < n) p[i] = f2bf(v[i]);
+    }
+}
+__device__ __forceinline__ float fp8_value(const void* p, int f32, long long at) {
+    return f32 ? reinterpret_cast<const float*>(p)[at] : bf2f(reinterpret_cast<const bf16_t*>(p)[at]);
+}
+#endif
+
+// WN x WM waves, each with NF x MF pieces of 16 outputs x 16 tokens.  Two stages of LDS: the loads of the next block of columns run under the products of this one.  Rows of 128
+// bytes lie with their pieces of 16 bytes at piece ^ (row / 2 & 7): sixteen rows read at once meet no bank twice.
+template <int NF, int MF, int WN, int WM, int KIND, bool EXACT>
+__global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int WAVES = WN * WM, BN = NF * WN * 16, BM = MF * WM * 16, STAGE = (BN + BM) * FP8_BLOCK, LN = BN / 8 / WAVES, LM = BM / 8 / WAVES;
+    static_assert(BN / 8 % WAVES == 0 && BM / 8 % WAVES == 0, "whole loads a wave");
+    static_assert(KIND != FP8_GATED || (BN == 256 && NF % 2 == 0), "gate and up of one block of 128");
+    extern __shared__ __align__(16) unsigned char fp8_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave / WM, wm = wave % WM;
+    // neighbouring tiles of an XCD share weights: workgroup w runs on XCD w mod 8, which gets a run of tiles, weights slowest
+    int w = blockIdx.x;
+    { const int chunk = gridDim.x >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
+    const int nt = w / a.m_tiles, mt = w - nt * a.m_tiles;
+    int m0 = mt * BM, rows = min(BM, a.M - m0), expert = 0;
+    if constexpr (KIND != FP8_LINEAR) {
+        const int first = a.table[2 * mt], info = a.table[2 * mt + 1];
+        m0 = __builtin_amdgcn_readfirstlane(first);
+        rows = __builtin_amdgcn_readfirstlane(info) & 0xffff;
+        expert = __builtin_amdgcn_readfirstlane(info) >> 16;
+        if (rows == 0) return;
+    }
+    constexpr int TILE_N = KIND == FP8_GATED ? BN / 2 : BN;            // outputs, of gate and of up
+    const int n0 = nt * TILE_N, n_rows = min(TILE_N, a.N - n0);
+    const unsigned char* const wt = a.w + expert * a.w_expert;
+    const auto w_bytes = (int)((n_rows - 1) * a.w_stride + a.K);
+    const u32x4_t from_w = la_buffer(wt + n0 * a.w_stride, w_bytes);
+    const u32x4_t from_up = la_buffer(wt + (KIND == FP8_GATED ? (long long)a.N + n0 : (long long)n0) * a.w_stride, w_bytes);
+    const u32x4_t from_x = KIND == FP8_GATED ? la_buffer(a.x, (int)a.x_bytes) : la_buffer(a.x + m0 * a.x_stride, (int)((rows - 1) * a.x_stride + (KIND == FP8_LINEAR ? a.K : a.x_stride)));
+    constexpr unsigned OOB = 0x80000000u;
+    unsigned off_w[LN], off_x[LM];
+    static_assert(WAVES % 2 == 0, "loads of a wave start at rows that are alike modulo 16");
+    const int piece = (lane & 7) ^ (((wave & 1) * 4 + (lane >> 4)) & 7);      // of its row that a lane loads
+#pragma unroll
+    for (int j = 0; j < LN; ++j) {
+        const int instr = j * WAVES + wave, row = instr * 8 + (lane >> 3), r = KIND == FP8_GATED ? row % TILE_N : row;
+        off_w[j] = r < n_rows ? (unsigned)(r * (int)a.w_stride + piece * 16) : OOB;
+    }
+#pragma unroll
+    for (int j = 0; j < LM; ++j) {
+        const int instr = j * WAVES + wave, row = instr * 8 + (lane >> 3);
+        unsigned off = OOB;
+        if (row < rows) {
+            if constexpr (KIND == FP8_GATED) {
+                const unsigned p = (unsigned)a.slots[m0 + row];
+                if (p < (unsigned)a.pairs) off = (p / (unsigned)a.k) * (unsigned)a.x_stride + piece * 16;
+            } else off = (unsigned)(row * (int)a.x_stride + piece * 16);
+        }
+        off_x[j] = off;
+    }
+    const int blocks = (a.K + FP8_BLOCK - 1) / FP8_BLOCK;
+    auto load = [&](int s) {
+        const unsigned stage = (unsigned)((s & 1) * STAGE);
+        const bool part = (s + 1) * FP8_BLOCK > a.K;                   // columns past K: zeros on both sides (there is no telling what lies behind a row)
+#pragma unroll
+        for (int j = 0; j < LN; ++j) {
+            const int instr = j * WAVES + wave;
+            const unsigned off = part && s * FP8_BLOCK + piece * 16 >= a.K ? OOB : off_w[j] + (unsigned)(s * FP8_BLOCK);
+            la_to_lds(KIND == FP8_GATED && j >= LN / 2 ? from_up : from_w, off, stage + (unsigned)instr * 1024u);
+        }
+#pragma unroll
+        for (int j = 0; j < LM; ++j) {
+            const int instr = j * WAVES + wave;
+            const unsigned off = part && s * FP8_BLOCK + piece * 16 >= a.K ? OOB : off_x[j] + (unsigned)(s * FP8_BLOCK);
+            la_to_lds(from_x, off, stage + (unsigned)(BN * FP8_BLOCK + instr * 1024));
+        }
+    };
+    // a lane's token of each piece, and where its scales are
+    const int l16 = lane & 15, lq = lane >> 4;
+    long long scale_at[MF];
+#pragma unroll
+    for (int b = 0; b < MF; ++b) {
+        const int row = wm * MF * 16 + b * 16 + l16;
+        long long at = 0;
+        if (row < rows) {
+            at = m0 + row;
+            if constexpr (KIND == FP8_GATED) {
+                const unsigned p = (unsigned)a.slots[m0 + row];
+                at = p < (unsigned)a.pairs ? p / (unsigned)a.k : 0;
+            }
+        }
+        scale_at[b] = at;                                              // (of rows that are not there: a scale that is, times zeros)
+    }
+    // a wave's outputs lie in one block of the weights' scales (gate and up in one each)
+    const int n_block = KIND == FP8_GATED ? n0 / FP8_BLOCK : min((n0 + wn * NF * 16) / FP8_BLOCK, (a.N - 1) / FP8_BLOCK);
+    const float* const ws = a.w_scale + (long long)expert * a.w_scale_expert + (long long)n_block * blocks;
+    const int up_scale = (a.N + FP8_BLOCK - 1) / FP8_BLOCK * blocks;   // (GATED: from the gate's scales to the up's)
+    f32x4_t acc[NF][MF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int b = 0; b < MF; ++b) acc[f][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float xs[MF];
+    load(0);
+#pragma unroll
+    for (int b = 0; b < MF; ++b) xs[b] = a.x_scale[scale_at[b]];
+    const int at0 = ((2 * lq) ^ ((l16 >> 1) & 7)) * 16, at1 = ((2 * lq + 1) ^ ((l16 >> 1) & 7)) * 16;
+    for (int s = 0; s < blocks; ++s) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const unsigned char* const stage = fp8_lds + (s & 1) * STAGE;
+        float sc[MF], su[MF];
+        const float wg = ws[s], wu = KIND == FP8_GATED ? ws[up_scale + s] : 0.f;
+#pragma unroll
+        for (int b = 0; b < MF; ++b) { sc[b] = xs[b] * wg; su[b] = KIND == FP8_GATED ? xs[b] * wu : 0.f; }
+        if (s + 1 < blocks) {
+            load(s + 1);
+#pragma unroll
+            for (int b = 0; b < MF; ++b) xs[b] = a.x_scale[(s + 1) * a.x_scale_stride + scale_at[b]];
+        }
+        Fp8Operand<EXACT> x[MF];
+#pragma unroll
+        for (int b = 0; b < MF; ++b) x[b].ld(stage + (BN + (wm * MF + b) * 16 + l16) * FP8_BLOCK, at0, at1);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            // GATED: the first half of a wave's pieces are gate rows, the second the same rows of up
+            const int row = KIND == FP8_GATED ? (f < NF / 2 ? (wn * (NF / 2) + f) * 16 : BN / 2 + (wn * (NF / 2) + f - NF / 2) * 16) : (wn * NF + f) * 16;
+            Fp8Operand<EXACT> v;
+            v.ld(stage + (row + l16) * FP8_BLOCK, at0, at1);
+#pragma unroll
+            for (int b = 0; b < MF; ++b) {
+                const f32x4_t p = fp8_product(v, x[b]);
+                const float k = KIND == FP8_GATED && f >= NF / 2 ? su[b] : sc[b];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[f][b][i] = fmaf(p[i], k, acc[f][b][i]);
+            }
+        }
+    }
+    if constexpr (KIND == FP8_GATED) {
+        // silu(gate) * up, the largest magnitude of a token's 128 channels over pieces, lanes and waves, codes
+        unsigned* const largest = reinterpret_cast<unsigned*>(fp8_lds);      // [WN][BM]
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < MF; ++b) {
+            unsigned top = 0;
+#pragma unroll
+            for (int f = 0; f < NF / 2; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float g = acc[f][b][i];
+                    acc[f][b][i] = g / (1.f + __expf(-g)) * acc[f + NF / 2][b][i];
+                    top = max(top, fp8_magnitude(acc[f][b][i]));
+                }
+            top = max(top, (unsigned)__shfl_xor((int)top, 16));
+            top = max(top, (unsigned)__shfl_xor((int)top, 32));
+            if (lq == 0) largest[wn * BM + (wm * MF + b) * 16 + l16] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < MF; ++b) {
+            const int row = (wm * MF + b) * 16 + l16;
+            unsigned top = 0;
+#pragma unroll
+            for (int v = 0; v < WN; ++v) top = max(top, largest[v * BM + row]);
+            const int e = fp8_exponent(top);
+            if (row >= rows) continue;
+            if (wn == 0 && lq == 0) a.h_scale[nt * a.h_scale_stride + m0 + row] = fp8_power(e);
+            const float inv = fp8_inverse(e);
+#pragma unroll
+            for (int f = 0; f < NF / 2; ++f)
+                *reinterpret_cast<unsigned*>(a.h + (m0 + row) * a.h_stride + n0 + (wn * (NF / 2) + f) * 16 + lq * 4) =
+                    fp8_codes(acc[f][b][0], acc[f][b][1], acc[f][b][2], acc[f][b][3], inv);
+        }
+    } else {
+        const int es = a.y_f32 ? 4 : 2;
+        const bool wide = ((uintptr_t)a.y % (4 * es)) == 0 && a.y_stride % 4 == 0;
+#pragma unroll
+        for (int b = 0; b < MF; ++b) {
+            const int row = (wm * MF + b) * 16 + l16;
+            if (row >= rows) continue;
+            long long to = m0 + row;
+            if constexpr (KIND == FP8_PAIRS) {
+                const unsigned p = (unsigned)a.slots[m0 + row];
+                if (p >= (unsigned)a.pairs) continue;
+                to = p;
+            }
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const int n = n0 + (wn * NF + f) * 16 + lq * 4, left = min(4, a.N - n);
+                if (left <= 0) continue;
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = acc[f][b][i];
+                    if constexpr (KIND == FP8_LINEAR) {
+                        if (i < left && a.bias) v[i] += fp8_value(a.bias, a.bias_f32, n + i);
+                        if (i < left && a.residual) v[i] += fp8_value(a.residual, a.y_f32, to * a.residual_stride + n + i);
+                    }
+                }
+                fp8_store4(a.y, a.y_f32, to * a.y_stride + n, v, left, wide && left == 4);
+            }
+        }
+    }
+#endif
+}
+
+template <int NF, int MF, int WN, int WM, int KIND, bool EXACT = false> inline int launch_fp8_tile(const Fp8TileArgs& a, const char* fn, hipStream_t st) {
+    constexpr int lds = 2 * (NF * WN + MF * WM) * 16 * FP8_BLOCK;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_tile_kernel<NF, MF, WN, WM, KIND, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (attr != hipSuccess) return fail(FISE_ERR_HIP, "%s: cannot raise the dynamic LDS limit", fn);
+    hipLaunchKernelGGL((fp8_tile_kernel<NF, MF, WN, WM, KIND, EXACT>), dim3((unsigned)(a.m_tiles * a.n_tiles)), dim3(64 * WN * WM), lds, st, a);
+    FISE_CHECK_LAUNCH(fn);
+    return FISE_OK;
+}
+
+}  // namespace fise

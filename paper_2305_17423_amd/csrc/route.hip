@@ -1,0 +1,318 @@
+// Routing of tokens to experts: keys (a score by softmax or sigmoid, and a bias), groups, the k largest, their weights, and the pairs (token, place) in the
+// experts' order.
+//
+// Reading the logits once bounds it for many tokens, a launch for few.  Sixteen lanes (64 for more than 256 experts) share a token, each with neighbouring experts in
+// registers; k rounds take the largest key, the lowest expert among equal ones.  Which expert is chosen is a whole number, so keys are compared as they are in 64 bits.
+// The order of the pairs is that of a counting sort: a wave gives each of its pairs its rank among those of the same expert (ballots of the expert's bits find the lanes that
+// share it), the workgroup adds up its waves, and further launches add the workgroups, all in order, so that nothing depends on the run.  Few tokens are one workgroup and one launch.
+#include <algorithm>
+#include <cmath>
+#include "common.h"
+#include "route_choice.h"
+
+namespace fise {
+
+struct RouteArgs {
+    const void* logits; long long stride; int f32;
+    int T, E, k, sigmoid, groups, top_groups, group_top, renorm, lists;
+    const float* bias; float scale;
+    int* ids; float* weights; int* offsets; int* slots;
+    unsigned* pairs; int* hist; int* total;
+    int wave_tokens, chunks, bits;
+};
+
+__device__ __forceinline__ double route_shfl(double v, int lane) { return __shfl(v, lane); }
+
+// The largest key of a token's lanes, the lowest lane among equal ones: all its lanes get both.
+template <int L> __device__ __forceinline__ void route_first(double& key, int& lane) {
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) {
+        const double k2 = __shfl_xor(key, o);
+        const int l2 = __shfl_xor(lane, o);
+        if (k2 > key || (k2 == key && l2 < lane)) { key = k2; lane = l2; }
+    }
+}
+
+template <int L, int V, bool SINGLE>
+__global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a) {
+    extern __shared__ int route_lds[];                                 // [wave][E] counts, then (single) the pairs
+    constexpr int WAVES = SINGLE ? ROUTE_SINGLE_WAVES : ROUTE_WAVES, AT_ONCE = 64 / L;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane % L, part = lane / L;
+    int* const count = route_lds + wave * a.E;
+    unsigned* const held = reinterpret_cast<unsigned*>(route_lds + WAVES * a.E);
+    const long long first = ((long long)blockIdx.x * WAVES + wave) * a.wave_tokens;
+    const double none = -INFINITY;
+    if (a.lists)
+        for (int e = lane; e < a.E; e += 64) count[e] = 0;
+    for (int r0 = 0; r0 < a.wave_tokens; r0 += AT_ONCE) {
+        const long long t = first + r0 + part;
+        const bool there = t < a.T;
+        float l[V];
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = sub * V + i;
+            l[i] = -INFINITY;
+            if (there && e < a.E) l[i] = a.f32 ? reinterpret_cast<const float*>(a.logits)[t * a.stride + e] : bf2f(reinterpret_cast<const bf16_t*>(a.logits)[t * a.stride + e]);
+            bad = bad || l[i] != l[i] || (!a.sigmoid && l[i] == INFINITY);
+        }
+        double score[V], key[V];
+        if (a.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) score[i] = 1.0 / (1.0 + exp(-(double)l[i]));
+        } else {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = fmaxf(top, l[i]);
+#pragma unroll
+            for (int o = 1; o < L; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { score[i] = l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)top); sum += score[i]; }
+#pragma unroll
+            for (int o = 1; o < L; o <<= 1) sum += __shfl_xor(sum, o);
+#pragma unroll
+            for (int i = 0; i < V; ++i) score[i] = sum > 0.0 ? score[i] / sum : 0.0;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = sub * V + i;
+            key[i] = l[i] == -INFINITY || e >= a.E ? none : a.bias ? score[i] + (double)a.bias[e] : (a.groups > 1 && a.group_top > 1) ? score[i] : (double)l[i];
+            bad = bad || key[i] != key[i];
+        }
+        const unsigned long long mask = L == 64 ? ~0ull : ((1ull << L) - 1) << (part * L);
+        bad = (__ballot(bad) & mask) != 0;
+        if (a.groups > 1) {
+            const int size = a.E / a.groups;
+            double mine = none;                                        // of group `sub`
+            for (int g = 0; g < a.groups; ++g) {
+                double m1 = none, m2 = none;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int e = sub * V + i;
+                    if (e < g * size || e >= (g + 1) * size) continue;
+                    if (key[i] > m1) { m2 = m1; m1 = key[i]; }
+                    else if (key[i] > m2) m2 = key[i];
+                }
+#pragma unroll
+                for (int o = 1; o < L; o <<= 1) {
+                    const double n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o);
+                    m2 = fmax(fmin(m1, n1), fmax(m2, n2));
+                    m1 = fmax(m1, n1);
+                }
+                if (a.group_top > 1 && m2 > none) m1 += m2;
+                if (sub == g) mine = m1;
+            }
+            unsigned long long kept = 0;
+            for (int j = 0; j < a.top_groups; ++j) {
+                double best = mine;
+                int g = sub;
+                route_first<L>(best, g);
+                if (best > none) kept |= 1ull << g;
+                if (sub == g) mine = none;
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (!(kept >> ((sub * V + i) / size) & 1)) key[i] = none;
+        }
+        int id = -1;                                                   // of place `sub`
+        double w = 0.0;
+        for (int j = 0; j < a.k; ++j) {
+            double best = none, s = 0.0;
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (key[i] > best) { best = key[i]; s = score[i]; at = i; }
+            int from = sub;
+            route_first<L>(best, from);
+            const int e = from * V + __shfl(at, part * L + from);
+            s = route_shfl(s, part * L + from);
+            if (best > none && sub == j) { id = e; w = s; }
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (sub == from && i == at) key[i] = none;
+        }
+        if (bad) id = -1;
+        if (a.renorm) {
+            double sum = w;
+#pragma unroll
+            for (int o = 1; o < L; o <<= 1) sum += __shfl_xor(sum, o);
+            w = sum > 0.0 ? w / sum : 0.0;
+        }
+        const bool out = there && sub < a.k;
+        if (out) {
+            a.ids[t * a.k + sub] = id;
+            a.weights[t * a.k + sub] = bad ? NAN : (float)(w * (double)a.scale);
+        }
+        if (!a.lists) continue;
+        // rank among the pairs of this wave with the same expert: pairs ascend with the lanes
+        unsigned long long same = __ballot(out && id >= 0);
+        for (int b = 0; b < a.bits; ++b) {
+            const unsigned long long set = __ballot(id >> b & 1);
+            same &= (id >> b & 1) ? set : ~set;
+        }
+        const bool counted = out && id >= 0;
+        const unsigned long long before = same & ((1ull << lane) - 1);
+        const int rank = counted ? count[id] + __popcll(before) : 0;
+        if (counted && before == 0) count[id] += __popcll(same);       // (LDS is read and written in order within a wave)
+        if (out) {
+            const unsigned packed = counted ? (unsigned)id << 16 | (unsigned)rank : 0xffffffffu;
+            if (SINGLE) held[t * a.k + sub] = packed;
+            else a.pairs[t * a.k + sub] = packed;
+        }
+    }
+    if (!a.lists) return;
+    __syncthreads();
+    // counts become starts: of a wave within the workgroup, and (single) of an expert among all
+    if constexpr (SINGLE) {
+        int* const sums = reinterpret_cast<int*>(held + a.T * a.k);    // of the 16 waves
+        int mine = 0;
+        if (tid < a.E)
+            for (int w = 0; w < WAVES; ++w) { const int n = route_lds[w * a.E + tid]; route_lds[w * a.E + tid] = mine; mine += n; }
+        int up = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int n = __shfl_up(up, o); if (lane >= o) up += n; }
+        if (lane == 63) sums[wave] = up;
+        __syncthreads();
+        int base = up - mine;
+        for (int w = 0; w < wave; ++w) base += sums[w];
+        if (tid < a.E) {
+            for (int w = 0; w < WAVES; ++w) route_lds[w * a.E + tid] += base;
+            a.offsets[tid] = base;
+            if (tid == a.E - 1) a.offsets[a.E] = base + mine;
+        }
+        __syncthreads();
+        for (int p = tid; p < a.T * a.k; p += 1024) {
+            const unsigned v = held[p];
+            if (v == 0xffffffffu) continue;
+            const int w = p / a.k / a.wave_tokens;
+            a.slots[route_lds[w * a.E + (int)(v >> 16)] + (int)(v & 0xffffu)] = p;
+        }
+    } else {
+        for (int e = tid; e < a.E; e += 256) {
+            int sum = 0;
+            for (int w = 0; w < WAVES; ++w) { const int n = route_lds[w * a.E + e]; route_lds[w * a.E + e] = sum; sum += n; }
+            a.hist[(long long)e * a.chunks + blockIdx.x] = sum;
+        }
+        __syncthreads();
+        const long long t0 = (long long)blockIdx.x * WAVES * a.wave_tokens, p0 = t0 * a.k;
+        const int n = (int)min((long long)WAVES * a.wave_tokens, a.T - t0) * a.k;
+        for (int i = tid; i < n; i += 256) {                           // (what this workgroup wrote)
+            const unsigned v = a.pairs[p0 + i];
+            if (v != 0xffffffffu) a.pairs[p0 + i] = v + (unsigned)route_lds[(i / a.k / a.wave_tokens) * a.E + (int)(v >> 16)];
+        }
+    }
+}
+
+// Counts of an expert in all chunks become starts among its pairs: a wave an expert.
+__global__ __launch_bounds__(64) void route_scan_kernel(int* hist, int* total, int chunks) {
+    int* const h = hist + (long long)blockIdx.x * chunks;
+    const int lane = threadIdx.x;
+    int sum = 0;
+    for (int c0 = 0; c0 < chunks; c0 += 64) {
+        const int n = c0 + lane < chunks ? h[c0 + lane] : 0;
+        int up = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int m = __shfl_up(up, o); if (lane >= o) up += m; }
+        if (c0 + lane < chunks) h[c0 + lane] = sum + up - n;
+        sum += __shfl(up, 63);
+    }
+    if (lane == 0) total[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a) {
+    __shared__ int base[ROUTE_MAX_EXPERTS];
+    __shared__ int sums[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int v[4], mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const int e = tid * 4 + i; v[i] = e < a.E ? a.total[e] : 0; mine += v[i]; }
+    int up = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int n = __shfl_up(up, o); if (lane >= o) up += n; }
+    if (lane == 63) sums[wave] = up;
+    __syncthreads();
+    int at = up - mine;
+    for (int w = 0; w < wave; ++w) at += sums[w];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = tid * 4 + i;
+        if (e < a.E) {
+            base[e] = at;
+            if (blockIdx.x == 0) { a.offsets[e] = at; if (e == a.E - 1) a.offsets[a.E] = at + v[i]; }
+        }
+        at += v[i];
+    }
+    __syncthreads();
+    const int per_chunk = ROUTE_WAVES * a.wave_tokens * a.k;
+    const long long pairs = (long long)a.T * a.k, p1 = min(pairs, (long long)(blockIdx.x + 1) * 1024);
+    for (long long p = (long long)blockIdx.x * 1024 + tid; p < p1; p += 256) {
+        const unsigned w = a.pairs[p];
+        if (w == 0xffffffffu) continue;
+        const int e = (int)(w >> 16);
+        a.slots[base[e] + a.hist[(long long)e * a.chunks + p / per_chunk] + (int)(w & 0xffffu)] = (int)p;
+    }
+}
+
+template <int L, int V> static int launch_route(const RouteArgs& a, const RouteChoice& c, hipStream_t st) {
+    const int lds = (c.waves * a.E + (c.single ? a.T * a.k + 16 : 0)) * 4;
+    if (c.single) {
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&route_kernel<L, V, true>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                           (ROUTE_SINGLE_WAVES * L * V + ROUTE_SINGLE_PAIRS + 16) * 4);
+        if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_route_experts: cannot raise the dynamic LDS limit");
+        hipLaunchKernelGGL((route_kernel<L, V, true>), dim3(1), dim3(1024), (size_t)lds, st, a);
+    } else hipLaunchKernelGGL((route_kernel<L, V, false>), dim3((unsigned)c.chunks), dim3(256), (size_t)lds, st, a);
+    FISE_CHECK_LAUNCH("fise_route_experts");
+    return FISE_OK;
+}
+
+static int route_check(const char* fn, const fise_route_args* g) {
+    if (g->E < 1 || g->E > ROUTE_MAX_EXPERTS || g->k < 1 || g->k > g->E || g->k > ROUTE_MAX_K || g->T < 0 || (long long)g->T * g->k > 0x7fffffffLL)
+        return fail(FISE_ERR_SHAPE, "%s: T=%d E=%d k=%d", fn, g->T, g->E, g->k);
+    if (g->groups < 1 || g->groups > 64 || g->E % g->groups || g->top_groups < 1 || g->top_groups > g->groups || (g->groups > 1 && g->group_top != 1 && g->group_top != 2))
+        return fail(FISE_ERR_SHAPE, "%s: %d groups of %d experts, %d of them, by %d", fn, g->groups, g->E, g->top_groups, g->group_top);
+    return FISE_OK;
+}
+
+}  // namespace fise
+
+using namespace fise;
+
+extern "C" size_t fise_route_experts_workspace_bytes(const fise_route_args* g) {
+    if (!g) { fail(FISE_ERR_NULL, "fise_route_experts: null pointer"); return 0; }
+    if (route_check("fise_route_experts", g)) return 0;
+    return (size_t)route_choose(g->T, g->E, g->k, g->groups, g->offsets || g->slots).bytes;
+}
+
+extern "C" int fise_route_experts(const fise_route_args* g, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* fn = "fise_route_experts";
+    if (!g || !g->logits || !g->ids || !g->weights) return fail(FISE_ERR_NULL, "%s: null pointer", fn);
+    if (!g->offsets != !g->slots) return fail(FISE_ERR_NULL, "%s: offsets and slots are given together", fn);
+    if (g->dtype != FISE_F32 && g->dtype != FISE_BF16) return fail(FISE_ERR_DTYPE, "%s: dtype %d", fn, g->dtype);
+    if (int e = route_check(fn, g)) return e;
+    if (g->score != FISE_SCORE_SOFTMAX && g->score != FISE_SCORE_SIGMOID) return fail(FISE_ERR_SHAPE, "%s: score %d", fn, g->score);
+    if (g->stride < g->E) return fail(FISE_ERR_SHAPE, "%s: rows of %d logits %lld apart", fn, g->E, (long long)g->stride);
+    if ((uintptr_t)g->logits % (g->dtype == FISE_F32 ? 4 : 2) || ((uintptr_t)g->ids | (uintptr_t)g->weights | (uintptr_t)g->offsets | (uintptr_t)g->slots | (uintptr_t)g->bias) & 3)
+        return fail(FISE_ERR_ALIGN, "%s: pointers must be aligned to their type", fn);
+    const bool lists = g->offsets != nullptr;
+    const RouteChoice c = route_choose(g->T, g->E, g->k, g->groups, lists);
+    if (c.bytes && (!workspace || workspace_bytes < (size_t)c.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)c.bytes);
+    if (c.bytes && ((uintptr_t)workspace & 255)) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
+    if (g->T == 0) return FISE_OK;
+    RouteArgs a{};
+    a.logits = g->logits; a.stride = g->stride; a.f32 = g->dtype == FISE_F32;
+    a.T = g->T; a.E = g->E; a.k = g->k; a.sigmoid = g->score == FISE_SCORE_SIGMOID; a.groups = g->groups; a.top_groups = g->top_groups; a.group_top = g->group_top;
+    a.renorm = g->renormalize != 0; a.lists = lists; a.bias = g->bias; a.scale = g->scale;
+    a.ids = g->ids; a.weights = g->weights; a.offsets = g->offsets; a.slots = g->slots;
+    a.pairs = (unsigned*)workspace; a.hist = (int*)((unsigned char*)workspace + c.hist_off); a.total = (int*)((unsigned char*)workspace + c.total_off);
+    a.wave_tokens = c.wave_tokens; a.chunks = c.chunks;
+    while ((1 << a.bits) < a.E) ++a.bits;
+    const hipStream_t st = as_stream(stream);
+    if (int e = c.lanes == 64 ? launch_route<64, 16>(a, c, st) : c.values == 4 ? launch_route<16, 4>(a, c, st) : launch_route<16, 16>(a, c, st)) return e;
+    if (!lists || c.single) return FISE_OK;
+    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)a.E), dim3(64), 0, st, a.hist, a.total, a.chunks);
+    FISE_CHECK_LAUNCH(fn);
+    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)(((long long)a.T * a.k + 1023) / 1024)), dim3(256), 0, st, a);
+    FISE_CHECK_LAUNCH(fn);
+    return FISE_OK;
+}
