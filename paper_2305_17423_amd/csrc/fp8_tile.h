@@ -65,6 +65,10 @@ __device__ __forceinline__ f32x4_t fp8_mfma(i32x8_t a, i32x8_t b) {
     const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, z, 0, 0, 0, 0, 0, 0);      // (no scales: the plain instruction)
 }
+// Sixteen bytes a lane to LDS as la_to_lds, `at` bytes (the same for all lanes) behind `off`.  `off` alone is held against the buffer's size: it is that of a row that is there, in which `at` stays.
+__device__ __forceinline__ void fp8_to_lds(u32x4_t from, unsigned off, unsigned at, unsigned to) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(off), "s"(from), "s"(at), "s"(to) : "memory");
+}
 // A lane's 32 codes of a row; EXACT: as bf16, which holds every code.
 template <bool EXACT> struct Fp8Operand;
 template <> struct Fp8Operand<false> {
@@ -119,7 +123,8 @@ __device__ __forceinline__ float fp8_value(const void* p, int f32, long long at)
 #endif
 
 // WN x WM waves, each with NF x MF pieces of 16 outputs x 16 tokens.  Two stages of LDS: the loads of the next block of columns run under the products of this one.  Rows of 128
-// bytes lie with their pieces of 16 bytes at piece ^ (row / 2 & 7): sixteen rows read at once meet no bank twice.
+// bytes lie with their pieces of 16 bytes at piece ^ (row / 2 & 7), and a lane reads the pieces lane / 16 and lane / 16 + 4: no bank is met twice (pieces 2 (lane / 16) and the next: a third of
+// the LDS' time was conflicts).
 template <int NF, int MF, int WN, int WM, int KIND, bool EXACT>
 __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -128,10 +133,11 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
     static_assert(KIND != FP8_GATED || (BN == 256 && NF % 2 == 0), "gate and up of one block of 128");
     extern __shared__ __align__(16) unsigned char fp8_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave / WM, wm = wave % WM;
-    // neighbouring tiles of an XCD share weights: workgroup w runs on XCD w mod 8, which gets a run of tiles, weights slowest
+    // workgroup w runs on XCD w mod 8, which gets a run of tiles: bands of eight tiles of tokens, all outputs of a band before the next, so that the tiles at work in an XCD
+    // share rows of both sides in its L2
     int w = blockIdx.x;
     { const int chunk = gridDim.x >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
-    const int nt = w / a.m_tiles, mt = w - nt * a.m_tiles;
+    const int band = w / (8 * a.n_tiles), in = w - band * 8 * a.n_tiles, high = min(8, a.m_tiles - band * 8), nt = in / high, mt = band * 8 + in - nt * high;
     int m0 = mt * BM, rows = min(BM, a.M - m0), expert = 0;
     if constexpr (KIND != FP8_LINEAR) {
         const int first = a.table[2 * mt], info = a.table[2 * mt + 1];
@@ -169,22 +175,18 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
         off_x[j] = off;
     }
     const int blocks = (a.K + FP8_BLOCK - 1) / FP8_BLOCK;
-    auto load = [&](int s) {
-        const unsigned stage = (unsigned)((s & 1) * STAGE);
-        const bool part = (s + 1) * FP8_BLOCK > a.K;                   // columns past K: zeros on both sides (there is no telling what lies behind a row)
-#pragma unroll
-        for (int j = 0; j < LN; ++j) {
-            const int instr = j * WAVES + wave;
-            const unsigned off = part && s * FP8_BLOCK + piece * 16 >= a.K ? OOB : off_w[j] + (unsigned)(s * FP8_BLOCK);
-            la_to_lds(KIND == FP8_GATED && j >= LN / 2 ? from_up : from_w, off, stage + (unsigned)instr * 1024u);
-        }
-#pragma unroll
-        for (int j = 0; j < LM; ++j) {
-            const int instr = j * WAVES + wave;
-            const unsigned off = part && s * FP8_BLOCK + piece * 16 >= a.K ? OOB : off_x[j] + (unsigned)(s * FP8_BLOCK);
-            la_to_lds(from_x, off, stage + (unsigned)(BN * FP8_BLOCK + instr * 1024));
+    // load i of block s (a wave has LN of weights, then LM of tokens); columns past K are zeros on both sides (there is no telling what lies behind a row), and so are blocks past the last
+    auto load = [&](int s, bool in, int i) {
+        const unsigned to = (unsigned)((s & 1) * STAGE), at = (unsigned)(s * FP8_BLOCK);
+        if (i < LN) {
+            const int instr = i * WAVES + wave;
+            fp8_to_lds(KIND == FP8_GATED && i >= LN / 2 ? from_up : from_w, in ? off_w[i] : OOB, at, to + (unsigned)instr * 1024u);
+        } else {
+            const int instr = (i - LN) * WAVES + wave;
+            fp8_to_lds(from_x, in ? off_x[i - LN] : OOB, at, to + (unsigned)(BN * FP8_BLOCK + instr * 1024));
         }
     };
+    auto inside = [&](int s) { return s * FP8_BLOCK + piece * 16 < a.K; };
     // a lane's token of each piece, and where its scales are
     const int l16 = lane & 15, lq = lane >> 4;
     long long scale_at[MF];
@@ -210,40 +212,61 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
     for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int b = 0; b < MF; ++b) acc[f][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float xs[MF];
-    load(0);
+    float xs[MF], wg, wu = 0.f;
+    auto scales = [&](int s) {
 #pragma unroll
-    for (int b = 0; b < MF; ++b) xs[b] = a.x_scale[scale_at[b]];
-    const int at0 = ((2 * lq) ^ ((l16 >> 1) & 7)) * 16, at1 = ((2 * lq + 1) ^ ((l16 >> 1) & 7)) * 16;
+        for (int b = 0; b < MF; ++b) xs[b] = a.x_scale[s * a.x_scale_stride + scale_at[b]];
+        wg = ws[s];
+        if (KIND == FP8_GATED) wu = ws[up_scale + s];
+    };
+#pragma unroll
+    for (int i = 0; i < LN + LM; ++i) load(0, inside(0), i);
+    scales(0);
+    const int at0 = (lq ^ ((l16 >> 1) & 7)) * 16, at1 = at0 ^ 64;      // (which codes of the block a lane has is the same on both sides)
+    constexpr int EVERY = NF * MF >= 2 * (LN + LM) ? 2 : 1;            // products from a load to the next
     for (int s = 0; s < blocks; ++s) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         const unsigned char* const stage = fp8_lds + (s & 1) * STAGE;
+        const bool in = inside(s + 1);
         float sc[MF], su[MF];
-        const float wg = ws[s], wu = KIND == FP8_GATED ? ws[up_scale + s] : 0.f;
 #pragma unroll
-        for (int b = 0; b < MF; ++b) { sc[b] = xs[b] * wg; su[b] = KIND == FP8_GATED ? xs[b] * wu : 0.f; }
-        if (s + 1 < blocks) {
-            load(s + 1);
-#pragma unroll
-            for (int b = 0; b < MF; ++b) xs[b] = a.x_scale[(s + 1) * a.x_scale_stride + scale_at[b]];
+        for (int b = 0; b < MF; ++b) {
+            sc[b] = xs[b] * wg;
+            asm volatile("" : "+v"(sc[b]));                            // here, in front of the next loads: behind them it would wait for those
+            if (KIND == FP8_GATED) { su[b] = xs[b] * wu; asm volatile("" : "+v"(su[b])); }
         }
         Fp8Operand<EXACT> x[MF];
 #pragma unroll
         for (int b = 0; b < MF; ++b) x[b].ld(stage + (BN + (wm * MF + b) * 16 + l16) * FP8_BLOCK, at0, at1);
+        // a product is added up two products later, when it is there
+        Fp8Operand<EXACT> v[2];
+        f32x4_t p[3];
+        auto row_of = [&](int f) {                                     // GATED: the first half of a wave's pieces are gate rows, the second the same rows of up
+            return KIND == FP8_GATED ? (f < NF / 2 ? (wn * (NF / 2) + f) * 16 : BN / 2 + (wn * (NF / 2) + f - NF / 2) * 16) : (wn * NF + f) * 16;
+        };
+        auto add = [&](int j) {
+            const int f = j / MF, b = j % MF;
+            const float k = KIND == FP8_GATED && f >= NF / 2 ? su[b] : sc[b];
 #pragma unroll
-        for (int f = 0; f < NF; ++f) {
-            // GATED: the first half of a wave's pieces are gate rows, the second the same rows of up
-            const int row = KIND == FP8_GATED ? (f < NF / 2 ? (wn * (NF / 2) + f) * 16 : BN / 2 + (wn * (NF / 2) + f - NF / 2) * 16) : (wn * NF + f) * 16;
-            Fp8Operand<EXACT> v;
-            v.ld(stage + (row + l16) * FP8_BLOCK, at0, at1);
+            for (int i = 0; i < 4; ++i) acc[f][b][i] = fmaf(p[j % 3][i], k, acc[f][b][i]);
+        };
+        v[0].ld(stage + (row_of(0) + l16) * FP8_BLOCK, at0, at1);
 #pragma unroll
-            for (int b = 0; b < MF; ++b) {
-                const f32x4_t p = fp8_product(v, x[b]);
-                const float k = KIND == FP8_GATED && f >= NF / 2 ? su[b] : sc[b];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[f][b][i] = fmaf(p[i], k, acc[f][b][i]);
-            }
+        for (int j = 0; j < NF * MF; ++j) {
+            const int f = j / MF, b = j % MF;
+            if (b == 0 && f + 1 < NF) v[(f + 1) & 1].ld(stage + (row_of(f + 1) + l16) * FP8_BLOCK, at0, at1);
+            // the next block's loads between the products: issued together they keep the waves from their products until the last is taken
+            if (j % EVERY == 0 && j / EVERY < LN + LM) load(s + 1, in, j / EVERY);
+            p[j % 3] = fp8_product(v[f & 1], x[b]);
+            if constexpr (!EXACT) __builtin_amdgcn_sched_barrier(0);   // (left alone, the compiler waits for each product where it is made)
+            if (j >= 2) add(j - 2);
+            if constexpr (!EXACT) __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = (NF * MF - 1) / EVERY + 1; i < LN + LM; ++i) load(s + 1, in, i);
+        scales(min(s + 1, blocks - 1));                                // (no branch: behind one the compiler would gather all sums, and spill)
+        if (NF * MF >= 2) add(NF * MF - 2);
+        add(NF * MF - 1);
     }
     if constexpr (KIND == FP8_GATED) {
         // silu(gate) * up, the largest magnitude of a token's 128 channels over pieces, lanes and waves, codes
