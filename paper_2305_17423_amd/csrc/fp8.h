@@ -4,17 +4,6 @@
 
 namespace fise {
 
-__device__ __forceinline__ void fp8_load8(const float* p, float* v) {
-    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p), b = *reinterpret_cast<const f32x4_t*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-}
-__device__ __forceinline__ void fp8_load8(const bf16_t* p, float* v) {
-    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = lo16(a[i]); v[2 * i + 1] = hi16(a[i]); }
-}
-
 // Unit `id` of a row-major line of units of 8 columns, `units` (a multiple of 16) a row: sixteen lanes have a block of 128 columns.  Columns from K on are zeros, written up to
 // `written` columns of a row.
 template <typename T>

@@ -39,7 +39,7 @@ inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, in
     ExpertChoice c{};
     const int64_t P = T * k;
     auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
-    c.bm = P >= 64 * E ? 128 : 32;
+    c.bm = P >= 512 * E ? 256 : P >= 64 * E ? 128 : 32;
     c.m_tiles = P / c.bm + std::min(E, P);
     const Fp8Space x = fp8_space(T, K), h = fp8_space(P, I);
     c.x_stride = x.stride; c.x_scale_off = x.scale_off;

@@ -41,6 +41,17 @@ __device__ __forceinline__ unsigned fp8_codes(float a, float b, float c, float d
 }
 __device__ __forceinline__ float fp8_inverse(int e) { return fp8_power(-e); }      // (e is between -126 and 119)
 
+__device__ __forceinline__ void fp8_load8(const float* p, float* v) {
+    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p), b = *reinterpret_cast<const f32x4_t*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
+__device__ __forceinline__ void fp8_load8(const bf16_t* p, float* v) {
+    const u32x4_t a = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = lo16(a[i]); v[2 * i + 1] = hi16(a[i]); }
+}
+
 // What a tile kernel works on.  Rows of x are codes padded with zeros to whole blocks where the library made them.
 enum { FP8_LINEAR = 0,      // y[m, n] of rows 0..M-1
        FP8_GATED = 1,       // rows of pairs, gate and up: silu(gate) * up in 8 bits again
@@ -102,21 +113,6 @@ __device__ __forceinline__ f32x4_t fp8_product(const Fp8Operand<true>& a, const 
     for (int j = 0; j < 4; ++j) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(fp8_bf16x8_t, a.v[j]), __builtin_bit_cast(fp8_bf16x8_t, b.v[j]), p, 0, 0, 0);
     return p;
 }
-__device__ __forceinline__ void fp8_store4(void* y, int f32, long long at, const float* v, int n, bool wide) {
-    if (f32) {
-        float* p = reinterpret_cast<float*>(y) + at;
-        if (wide) *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-        else
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
-    } else {
-        bf16_t* p = reinterpret_cast<bf16_t*>(y) + at;
-        if (wide) *reinterpret_cast<u32x2_t*>(p) = u32x2_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
-        else
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (i < n) p[i] = f2bf(v[i]);
-    }
-}
 __device__ __forceinline__ float fp8_value(const void* p, int f32, long long at) {
     return f32 ? reinterpret_cast<const float*>(p)[at] : bf2f(reinterpret_cast<const bf16_t*>(p)[at]);
 }
@@ -133,11 +129,11 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
     static_assert(KIND != FP8_GATED || (BN == 256 && NF % 2 == 0), "gate and up of one block of 128");
     extern __shared__ __align__(16) unsigned char fp8_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave / WM, wm = wave % WM;
-    // workgroup w runs on XCD w mod 8, which gets a run of tiles: bands of eight tiles of tokens, all outputs of a band before the next, so that the tiles at work in an XCD
+    // workgroup w runs on XCD w mod 8, which gets a run of tiles: bands of six tiles of tokens, all outputs of a band before the next, so that the tiles at work in an XCD
     // share rows of both sides in its L2
     int w = blockIdx.x;
     { const int chunk = gridDim.x >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
-    const int band = w / (8 * a.n_tiles), in = w - band * 8 * a.n_tiles, high = min(8, a.m_tiles - band * 8), nt = in / high, mt = band * 8 + in - nt * high;
+    const int band = w / (6 * a.n_tiles), in = w - band * 6 * a.n_tiles, high = min(6, a.m_tiles - band * 6), nt = in / high, mt = band * 6 + in - nt * high;
     int m0 = mt * BM, rows = min(BM, a.M - m0), expert = 0;
     if constexpr (KIND != FP8_LINEAR) {
         const int first = a.table[2 * mt], info = a.table[2 * mt + 1];
@@ -270,7 +266,10 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
     }
     if constexpr (KIND == FP8_GATED) {
         // silu(gate) * up, the largest magnitude of a token's 128 channels over pieces, lanes and waves, codes
+        constexpr int PITCH = FP8_BLOCK + 16;
+        static_assert(WN * BM * 4 + BM * PITCH <= 2 * STAGE, "magnitudes and codes in LDS");
         unsigned* const largest = reinterpret_cast<unsigned*>(fp8_lds);      // [WN][BM]
+        unsigned char* const codes = fp8_lds + WN * BM * 4;            // [BM], rows 16 bytes off the banks' round
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < MF; ++b) {
@@ -300,37 +299,88 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
             const float inv = fp8_inverse(e);
 #pragma unroll
             for (int f = 0; f < NF / 2; ++f)
-                *reinterpret_cast<unsigned*>(a.h + (m0 + row) * a.h_stride + n0 + (wn * (NF / 2) + f) * 16 + lq * 4) =
-                    fp8_codes(acc[f][b][0], acc[f][b][1], acc[f][b][2], acc[f][b][3], inv);
+                *reinterpret_cast<unsigned*>(codes + row * PITCH + (wn * (NF / 2) + f) * 16 + lq * 4) = fp8_codes(acc[f][b][0], acc[f][b][1], acc[f][b][2], acc[f][b][3], inv);
         }
+        __syncthreads();
+        for (int i = tid; i < rows * 8; i += 64 * WAVES)               // a line of 128 bytes by eight lanes
+            *reinterpret_cast<u32x4_t*>(a.h + (m0 + (i >> 3)) * a.h_stride + n0 + (i & 7) * 16) = *reinterpret_cast<const u32x4_t*>(codes + (i >> 3) * PITCH + (i & 7) * 16);
     } else {
-        const int es = a.y_f32 ? 4 : 2;
-        const bool wide = ((uintptr_t)a.y % (4 * es)) == 0 && a.y_stride % 4 == 0;
+        // sixteen tokens at a time through LDS, a part of it for each wave, so that a wave's outputs of a token are stored side by side; its rows are 16 bytes off the banks' round
+        constexpr int W = NF * 16, PITCH = W * 4 + 16;
+        static_assert(WAVES * 16 * PITCH <= 2 * STAGE, "the results of sixteen tokens in LDS");
+        unsigned char* const mine = fp8_lds + wave * 16 * PITCH;
+        const int es = a.y_f32 ? 4 : 2, nw = n0 + wn * W, n_left = min(W, a.N - nw);      // (n_left may be negative)
+        bool wide = (((uintptr_t)a.y | (uintptr_t)(a.y_stride * es)) & 15) == 0;
+        float bias[NF][4];
+        if constexpr (KIND == FP8_LINEAR) {
+            if (a.residual) wide = wide && (((uintptr_t)a.residual | (uintptr_t)(a.residual_stride * es)) & 15) == 0;
 #pragma unroll
-        for (int b = 0; b < MF; ++b) {
-            const int row = (wm * MF + b) * 16 + l16;
-            if (row >= rows) continue;
-            long long to = m0 + row;
-            if constexpr (KIND == FP8_PAIRS) {
-                const unsigned p = (unsigned)a.slots[m0 + row];
-                if (p >= (unsigned)a.pairs) continue;
-                to = p;
-            }
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                const int n = n0 + (wn * NF + f) * 16 + lq * 4, left = min(4, a.N - n);
-                if (left <= 0) continue;
-                float v[4];
+            for (int f = 0; f < NF; ++f)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = acc[f][b][i];
-                    if constexpr (KIND == FP8_LINEAR) {
-                        if (i < left && a.bias) v[i] += fp8_value(a.bias, a.bias_f32, n + i);
-                        if (i < left && a.residual) v[i] += fp8_value(a.residual, a.y_f32, to * a.residual_stride + n + i);
-                    }
+                    const int n = f * 16 + lq * 4 + i;
+                    bias[f][i] = a.bias && n < n_left ? fp8_value(a.bias, a.bias_f32, nw + n) : 0.f;
                 }
-                fp8_store4(a.y, a.y_f32, to * a.y_stride + n, v, left, wide && left == 4);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < MF; ++b) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                f32x4_t v = acc[f][b];
+                if constexpr (KIND == FP8_LINEAR)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += bias[f][i];
+                *reinterpret_cast<f32x4_t*>(mine + l16 * PITCH + (f * 16 + lq * 4) * 4) = v;
             }
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            auto row_to = [&](int r, long long& to) {                  // where the wave's row r goes
+                const int row = (wm * MF + b) * 16 + r;
+                to = m0 + row;
+                if (row >= rows) return false;
+                if constexpr (KIND == FP8_PAIRS) {
+                    const unsigned p = (unsigned)a.slots[m0 + row];
+                    if (p >= (unsigned)a.pairs) return false;
+                    to = p;
+                }
+                return true;
+            };
+            constexpr int LANES = W / 8, AT_ONCE = 64 / LANES;         // eight outputs a lane
+            const int n = lane % LANES * 8;
+#pragma unroll
+            for (int r0 = 0; r0 < 16; r0 += AT_ONCE) {
+                const int r = r0 + lane / LANES;
+                long long to;
+                if (!row_to(r, to) || n >= n_left) continue;
+                const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(mine + r * PITCH + n * 4), hi = *reinterpret_cast<const f32x4_t*>(mine + r * PITCH + n * 4 + 16);
+                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                if (wide && n + 8 <= n_left) {
+                    if constexpr (KIND == FP8_LINEAR)
+                        if (a.residual) {
+                            float res[8];
+                            if (a.y_f32) fp8_load8(reinterpret_cast<const float*>(a.residual) + to * a.residual_stride + nw + n, res);
+                            else fp8_load8(reinterpret_cast<const bf16_t*>(a.residual) + to * a.residual_stride + nw + n, res);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] += res[i];
+                        }
+                    if (a.y_f32) {
+                        float* const p = reinterpret_cast<float*>(a.y) + to * a.y_stride + nw + n;
+                        *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+                        *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+                    } else *reinterpret_cast<u32x4_t*>(reinterpret_cast<bf16_t*>(a.y) + to * a.y_stride + nw + n) = u32x4_t{f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (n + i < n_left) {
+                            if constexpr (KIND == FP8_LINEAR)
+                                if (a.residual) v[i] += fp8_value(a.residual, a.y_f32, to * a.residual_stride + nw + n + i);
+                            if (a.y_f32) reinterpret_cast<float*>(a.y)[to * a.y_stride + nw + n + i] = v[i];
+                            else reinterpret_cast<bf16_t*>(a.y)[to * a.y_stride + nw + n + i] = f2bf(v[i]);
+                        }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();                           // (LDS serves a wave in order: its next writes come behind these reads)
         }
     }
 #endif
