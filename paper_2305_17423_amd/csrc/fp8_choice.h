@@ -5,17 +5,35 @@
 
 namespace fise {
 
-enum { FP8_FORM_256 = 0, FP8_FORM_128 = 1, FP8_FORM_32 = 2 };          // 256 x 256, 128 x 128, 32 tokens x 128 outputs
+enum { FP8_FORM_256 = 0, FP8_FORM_128 = 1, FP8_FORM_32 = 2, FP8_FORM_FEW = 3, FP8_FORM_64 = 4 };      // 256 x 256, 128 x 128, 32 tokens x 128 outputs; weights streamed past up to 64 rows
 
-struct Fp8Choice { int form, bm, bn; int64_t m_tiles, n_tiles; };
+struct Fp8Choice {
+    int form, bm, bn; int64_t m_tiles, n_tiles;
+    int waves;                  // FEW: of a workgroup
+    bool make_rows;             // x is put in 8 bits by a launch in front
+};
 
 // exact: products in bf16 (float results), whose operands leave no room for the largest tile
-inline Fp8Choice fp8_choose(int64_t M, int64_t N, bool exact) {
+inline Fp8Choice fp8_choose(int64_t M, int64_t N, int64_t K, bool exact, bool codes) {
     Fp8Choice c{};
     auto set = [&](int form, int bm, int bn) { c.form = form; c.bm = bm; c.bn = bn; c.m_tiles = (M + bm - 1) / bm; c.n_tiles = (N + bn - 1) / bn; };
+    c.make_rows = !codes && M > 0;
+    // Few rows: streaming the weights past them is bound by the trips; more rows for many outputs read rows and turn codes into bf16 too often for that.  us, streamed and tiles:
+    // 64 rows 4096 x 4096: 13.7 and 23.6, 8192 x 8192: 42 and 43.5, 10240 x 1280: 15.2 and 10.0, 28672 x 8192: 144 and 70; 32 rows 8192 x 8192: 25 and 38, 10240 x 1280: 9.9 and 8.6,
+    // 28672 x 8192: 96 and 65; 16 rows 28672 x 8192: 59 and 63
+    if (M <= 16 || (M <= 64 && N <= 8192)) {
+        set(FP8_FORM_FEW, 64, 16);
+        const int64_t blocks = (K + 127) / 128;
+        c.waves = (int)std::min<int64_t>(16, blocks);
+        // Each workgroup puts the rows in 8 bits for itself where that is one piece of sixteen rows a wave (16 rows, 1280 columns: 5.3 us, one launch); more is made once (54 rows of 5136
+        // columns for 1283 outputs: 30 and 14.5 us)
+        c.make_rows = !codes && M > 0 && !(M <= 16 && blocks <= 16);
+        return c;
+    }
     set(FP8_FORM_256, 256, 256);
+    if (M <= 32) { set(FP8_FORM_32, 32, 128); return c; }
+    if (M <= 64) { set(FP8_FORM_64, 64, 128); return c; }
     if (exact || c.m_tiles * c.n_tiles < 200) set(FP8_FORM_128, 128, 128);
-    if (M <= 32) set(FP8_FORM_32, 32, 128);
     return c;
 }
 

@@ -91,8 +91,9 @@ template <> struct Fp8Operand<false> {
 };
 template <> struct Fp8Operand<true> {
     bf16x8_t v[4];
-    __device__ __forceinline__ void ld(const unsigned char* row, int at0, int at1) {
-        const i32x4_t c[2] = {*reinterpret_cast<const i32x4_t*>(row + at0), *reinterpret_cast<const i32x4_t*>(row + at1)};
+    __device__ __forceinline__ void ld(const unsigned char* row, int at0, int at1) { of(*reinterpret_cast<const i32x4_t*>(row + at0), *reinterpret_cast<const i32x4_t*>(row + at1)); }
+    __device__ __forceinline__ void of(i32x4_t lo, i32x4_t hi) {
+        const i32x4_t c[2] = {lo, hi};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u32x4_t w;

@@ -2,7 +2,8 @@
 // experts' order.
 //
 // Reading the logits once bounds it for many tokens, a launch for few.  Sixteen lanes (64 for more than 256 experts) share a token, each with neighbouring experts in
-// registers; k rounds take the largest key, the lowest expert among equal ones.  Which expert is chosen is a whole number, so keys are compared as they are in 64 bits.
+// registers; k rounds take the largest key, the lowest expert among equal ones.  Which expert is chosen is a whole number, so keys are compared as they are in 64 bits: in float first, and
+// again in 64 bits where two keys are closer than float's error explains (all in 64 bits: 249 us for 65536 tokens of 256 experts).
 // The order of the pairs is that of a counting sort: a wave gives each of its pairs its rank among those of the same expert (ballots of the expert's bits find the lanes that
 // share it), the workgroup adds up its waves, and further launches add the workgroups, all in order, so that nothing depends on the run.  Few tokens are one workgroup and one launch.
 #include <algorithm>
@@ -18,18 +19,150 @@ struct RouteArgs {
     const float* bias; float scale;
     int* ids; float* weights; int* offsets; int* slots;
     unsigned* pairs; int* hist; int* total;
-    int wave_tokens, chunks, bits;
+    int wave_tokens, chunks, bits, wide;
 };
 
-__device__ __forceinline__ double route_shfl(double v, int lane) { return __shfl(v, lane); }
-
-// The largest key of a token's lanes, the lowest lane among equal ones: all its lanes get both.
-template <int L> __device__ __forceinline__ void route_first(double& key, int& lane) {
+// over the L neighbouring lanes of a token; all of them get the result
+template <int L> __device__ __forceinline__ float route_max(float v) {
+    // rotations within sixteen lanes
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false)));
+    if constexpr (L == 64) { v = fmaxf(v, __shfl_xor(v, 16)); v = fmaxf(v, __shfl_xor(v, 32)); }
+    return v;
+}
+template <int L> __device__ __forceinline__ double route_max(double v) {
 #pragma unroll
-    for (int o = 1; o < L; o <<= 1) {
-        const double k2 = __shfl_xor(key, o);
-        const int l2 = __shfl_xor(lane, o);
-        if (k2 > key || (k2 == key && l2 < lane)) { key = k2; lane = l2; }
+    for (int o = 1; o < L; o <<= 1) v = fmax(v, __shfl_xor(v, o));
+    return v;
+}
+template <int L> __device__ __forceinline__ double route_sum(double v) {
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+// the lowest of a token's lanes for which it holds, L if there is none
+template <int L> __device__ __forceinline__ int route_lowest(bool holds, int part) {
+    const unsigned long long all = __ballot(holds);
+    if constexpr (L == 64) return all ? __ffsll(all) - 1 : 64;
+    const unsigned mine = (unsigned)(all >> (part * L)) & ((1u << L) - 1);
+    return mine ? __ffs((int)mine) - 1 : L;
+}
+__device__ __forceinline__ float route_exp(float x) { return __expf(x); }
+__device__ __forceinline__ double route_exp(double x) { return exp(x); }
+__device__ __forceinline__ float route_inverse(float x) { return __builtin_amdgcn_rcpf(x); }
+__device__ __forceinline__ double route_inverse(double x) { return 1.0 / x; }
+
+// The experts of a token from its logits l, V neighbouring ones a lane: lane `sub` gets the expert of place `sub` (-1: none) and its logit.
+// K double: as the definition says.  K float: the same where the keys are the logits themselves (the order of the scores is theirs); otherwise scores are off by `off` at most, and
+// `close` says that two keys, of which the order matters, are no further apart than that explains.
+template <int L, int V, typename K>
+__device__ __forceinline__ void route_choose_experts(const RouteArgs& a, const float* l, float top, int sub, int part, bool& bad, bool& close, int& id, float& logit) {
+    const K none = -INFINITY;
+    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);
+    K key[V], off = 0;
+    if (direct) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = (K)l[i];
+    } else {
+        if (a.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) key[i] = route_inverse((K)1 + route_exp(-(K)l[i]));
+            off = (K)0x1p-19;                                          // s (1 - s) (|l| 2^-23 + 2^-21) of the exponential, two roundings
+        } else {
+            K sum = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { key[i] = l[i] == -INFINITY ? (K)0 : route_exp((K)l[i] - (K)top); sum += key[i]; }
+            const K one = (K)1 / (K)route_sum<L>((double)sum);         // (a token without experts: not used)
+#pragma unroll
+            for (int i = 0; i < V; ++i) key[i] *= one;
+            off = one * (K)0x1p-19;                                    // p (|x| 2^-23 + 2^-21) with p = e^-|x|, of the exponential and the sum
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = sub * V + i;
+            if (a.bias && e < a.E) key[i] += (K)a.bias[e];
+            if (l[i] == -INFINITY) key[i] = none;
+            bad = bad || key[i] != key[i];
+        }
+    }
+    auto near = [&](K high, K low) { return !direct && sizeof(K) == 4 && low > none && high - low <= 4 * off + (K)0x1p-21 * (high < 0 ? -high : high); };
+    close = false;
+    if (a.groups > 1) {
+        const int size = a.E / a.groups;
+        K mine = none;                                                 // of group `sub`
+        if (size % V == 0 && ((size / V) & (size / V - 1)) == 0 && size / V <= L) {      // groups of whole lanes, a power of two of them
+            K m1 = none, m2 = none;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const K k = key[i]; m2 = k > m1 ? m1 : k > m2 ? k : m2; m1 = k > m1 ? k : m1; }
+            for (int o = 1; o < size / V; o <<= 1) {
+                const K n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o), low = m1 < n1 ? m1 : n1, second = m2 > n2 ? m2 : n2;
+                m1 = m1 > n1 ? m1 : n1;
+                m2 = low > second ? low : second;
+            }
+            if (a.group_top > 1 && m2 > none) m1 += m2;
+            mine = __shfl(m1, part * L + min(sub * (size / V), L - 1));
+            if (sub >= a.groups) mine = none;
+        } else
+            for (int g = 0; g < a.groups; ++g) {
+                K m1 = none, m2 = none;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int e = sub * V + i;
+                    if (e < g * size || e >= (g + 1) * size) continue;
+                    const K k = key[i];
+                    m2 = k > m1 ? m1 : k > m2 ? k : m2;
+                    m1 = k > m1 ? k : m1;
+                }
+                for (int o = 1; o < L; o <<= 1) {
+                    const K n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o), low = m1 < n1 ? m1 : n1, second = m2 > n2 ? m2 : n2;
+                    m1 = m1 > n1 ? m1 : n1;
+                    m2 = low > second ? low : second;
+                }
+                if (a.group_top > 1 && m2 > none) m1 += m2;
+                if (sub == g) mine = m1;
+            }
+        unsigned long long kept = 0;
+        K last = none;
+        for (int j = 0; j <= a.top_groups && j < a.groups; ++j) {
+            const K best = route_max<L>(mine);
+            if (j == a.top_groups) { close = close || near(last, best); break; }
+            const int g = route_lowest<L>(mine == best, part);
+            if (best > none) kept |= 1ull << g;
+            if (sub == g) mine = none;
+            last = best;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (!(kept >> (min(sub * V + i, a.E - 1) / size) & 1)) key[i] = none;
+    }
+    id = -1;
+    logit = 0.f;
+    K last = INFINITY;
+    for (int j = 0; j <= a.k; ++j) {
+        K m = key[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) m = key[i] > m ? key[i] : m;
+        const K best = route_max<L>(m);
+        if (j > 0) close = close || near(last, best);
+        if (j == a.k || !__any(best > none)) break;
+        const int from = route_lowest<L>(m == best, part);
+        int at = 0;
+        float value = 0.f;
+        bool open = sub == from;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const bool hit = open && key[i] == best;
+            at = hit ? i : at;
+            value = hit ? l[i] : value;
+            key[i] = hit ? none : key[i];
+            open = open && !hit;
+        }
+        const int lane = part * L + min(from, L - 1), e = from * V + __shfl(at, lane);
+        value = __shfl(value, lane);
+        if (best > none && sub == j) { id = e; logit = value; }
+        last = best;
     }
 }
 
@@ -41,104 +174,63 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
     int* const count = route_lds + wave * a.E;
     unsigned* const held = reinterpret_cast<unsigned*>(route_lds + WAVES * a.E);
     const long long first = ((long long)blockIdx.x * WAVES + wave) * a.wave_tokens;
-    const double none = -INFINITY;
     if (a.lists)
         for (int e = lane; e < a.E; e += 64) count[e] = 0;
     for (int r0 = 0; r0 < a.wave_tokens; r0 += AT_ONCE) {
         const long long t = first + r0 + part;
         const bool there = t < a.T;
-        float l[V];
+        if (!__any(there)) break;
+        float l[V], top = -INFINITY;
         bool bad = false;
 #pragma unroll
+        for (int i0 = 0; i0 < V; i0 += 4) {
+            const int e = sub * V + i0;
+            if (a.wide && there && e + 4 <= a.E) {
+                if (a.f32) {
+                    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.logits) + t * a.stride + e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l[i0 + i] = v[i];
+                } else {
+                    const u32x2_t v = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const bf16_t*>(a.logits) + t * a.stride + e);
+                    l[i0] = lo16(v[0]); l[i0 + 1] = hi16(v[0]); l[i0 + 2] = lo16(v[1]); l[i0 + 3] = hi16(v[1]);
+                }
+            } else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    l[i0 + i] = -INFINITY;
+                    if (there && e + i < a.E) l[i0 + i] = a.f32 ? reinterpret_cast<const float*>(a.logits)[t * a.stride + e + i] : bf2f(reinterpret_cast<const bf16_t*>(a.logits)[t * a.stride + e + i]);
+                }
+        }
+#pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int e = sub * V + i;
-            l[i] = -INFINITY;
-            if (there && e < a.E) l[i] = a.f32 ? reinterpret_cast<const float*>(a.logits)[t * a.stride + e] : bf2f(reinterpret_cast<const bf16_t*>(a.logits)[t * a.stride + e]);
             bad = bad || l[i] != l[i] || (!a.sigmoid && l[i] == INFINITY);
+            top = fmaxf(top, l[i]);
         }
-        double score[V], key[V];
-        if (a.sigmoid) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) score[i] = 1.0 / (1.0 + exp(-(double)l[i]));
-        } else {
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < V; ++i) top = fmaxf(top, l[i]);
-#pragma unroll
-            for (int o = 1; o < L; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-            double sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) { score[i] = l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)top); sum += score[i]; }
-#pragma unroll
-            for (int o = 1; o < L; o <<= 1) sum += __shfl_xor(sum, o);
-#pragma unroll
-            for (int i = 0; i < V; ++i) score[i] = sum > 0.0 ? score[i] / sum : 0.0;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = sub * V + i;
-            key[i] = l[i] == -INFINITY || e >= a.E ? none : a.bias ? score[i] + (double)a.bias[e] : (a.groups > 1 && a.group_top > 1) ? score[i] : (double)l[i];
-            bad = bad || key[i] != key[i];
+        top = route_max<L>(top);
+        int id;
+        float logit;
+        bool close, broken = bad;
+        route_choose_experts<L, V, float>(a, l, top, sub, part, broken, close, id, logit);
+        if (__any(close)) {                                            // keys next to each other: all of it in 64 bits
+            broken = bad;
+            route_choose_experts<L, V, double>(a, l, top, sub, part, broken, close, id, logit);
         }
         const unsigned long long mask = L == 64 ? ~0ull : ((1ull << L) - 1) << (part * L);
-        bad = (__ballot(bad) & mask) != 0;
-        if (a.groups > 1) {
-            const int size = a.E / a.groups;
-            double mine = none;                                        // of group `sub`
-            for (int g = 0; g < a.groups; ++g) {
-                double m1 = none, m2 = none;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int e = sub * V + i;
-                    if (e < g * size || e >= (g + 1) * size) continue;
-                    if (key[i] > m1) { m2 = m1; m1 = key[i]; }
-                    else if (key[i] > m2) m2 = key[i];
-                }
-#pragma unroll
-                for (int o = 1; o < L; o <<= 1) {
-                    const double n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o);
-                    m2 = fmax(fmin(m1, n1), fmax(m2, n2));
-                    m1 = fmax(m1, n1);
-                }
-                if (a.group_top > 1 && m2 > none) m1 += m2;
-                if (sub == g) mine = m1;
-            }
-            unsigned long long kept = 0;
-            for (int j = 0; j < a.top_groups; ++j) {
-                double best = mine;
-                int g = sub;
-                route_first<L>(best, g);
-                if (best > none) kept |= 1ull << g;
-                if (sub == g) mine = none;
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (!(kept >> ((sub * V + i) / size) & 1)) key[i] = none;
-        }
-        int id = -1;                                                   // of place `sub`
-        double w = 0.0;
-        for (int j = 0; j < a.k; ++j) {
-            double best = none, s = 0.0;
-            int at = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (key[i] > best) { best = key[i]; s = score[i]; at = i; }
-            int from = sub;
-            route_first<L>(best, from);
-            const int e = from * V + __shfl(at, part * L + from);
-            s = route_shfl(s, part * L + from);
-            if (best > none && sub == j) { id = e; w = s; }
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (sub == from && i == at) key[i] = none;
-        }
-        if (bad) id = -1;
+        bad = (__ballot(broken) & mask) != 0;
+        // the chosen ones' scores in 64 bits, one a lane; a softmax' sum where it does not drop out
+        const double x = a.sigmoid ? -(double)logit : (double)logit - (double)top, p = exp(x);
+        double w = id < 0 ? 0.0 : a.sigmoid ? 1.0 / (1.0 + p) : p;
         if (a.renorm) {
-            double sum = w;
+            const double sum = route_sum<L>(w);
+            w = sum > 0.0 ? w / sum : 0.0;
+        } else if (!a.sigmoid) {
+            double sum = 0.0;
 #pragma unroll
-            for (int o = 1; o < L; o <<= 1) sum += __shfl_xor(sum, o);
+            for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : (double)__expf(l[i] - top);      // (2^-20 of the sum)
+            sum = route_sum<L>(sum);
             w = sum > 0.0 ? w / sum : 0.0;
         }
+        if (bad) id = -1;
         const bool out = there && sub < a.k;
         if (out) {
             a.ids[t * a.k + sub] = id;
@@ -307,6 +399,7 @@ extern "C" int fise_route_experts(const fise_route_args* g, void* workspace, siz
     a.pairs = (unsigned*)workspace; a.hist = (int*)((unsigned char*)workspace + c.hist_off); a.total = (int*)((unsigned char*)workspace + c.total_off);
     a.wave_tokens = c.wave_tokens; a.chunks = c.chunks;
     while ((1 << a.bits) < a.E) ++a.bits;
+    a.wide = g->dtype == FISE_F32 ? aligned16(g->logits) && g->stride % 4 == 0 : (uintptr_t)g->logits % 8 == 0 && g->stride % 4 == 0;
     const hipStream_t st = as_stream(stream);
     if (int e = c.lanes == 64 ? launch_route<64, 16>(a, c, st) : c.values == 4 ? launch_route<16, 4>(a, c, st) : launch_route<16, 16>(a, c, st)) return e;
     if (!lists || c.single) return FISE_OK;

@@ -92,17 +92,17 @@ CODES = {"x_dtype": 2, "x_scale": A, "x_scale_stride": 0}
                                          ({"x_stride": 240}, -2), ({"w_stride": 240}, -2), ({"y_stride": 63}, -2), ({"residual": A, "residual_stride": 63}, -2), ({"w_stride": (1 << 22) + 16}, -2),
                                          ({"x_stride": (1 << 22) + 16}, -2), ({**CODES, "M": 4, "x_scale_stride": 3}, -2), ({"K": 248}, -4), ({"x_stride": 260}, -4), ({**CODES, "x_stride": 264}, -4),
                                          ({"x_stride": 264}, 0), ({"w_stride": 264}, -4), ({"x": A + 8}, -4), ({"w": A + 8}, -4), ({"y": A + 1}, -4), ({"bias": A + 2, "bias_dtype": 0}, -4),
-                                         ({"w_scale": A + 2}, -4), ({"M": 3}, -5)])
+                                         ({"w_scale": A + 2}, -4), ({"M": 65}, -5)])
 def test_fp8_linear(change, code):
     refused("fise_fp8_linear", fp8, change, code, None, 0, None)
 
 
 def test_fp8_linear_workspace():
-    L, a = fb.lib(), set_all(fp8(), M=3)
+    L, a = fb.lib(), set_all(fp8(), M=65)
     need = L.fise_fp8_linear_workspace_bytes(ctypes.byref(a))
-    assert need == 768 + 256
+    assert need == 65 * 256 + 768 and L.fise_fp8_linear_workspace_bytes(ctypes.byref(set_all(fp8(), M=3))) == 0      # (few rows are put in 8 bits in registers)
     assert L.fise_fp8_linear(ctypes.byref(a), A, need - 1, None) == -5 and L.fise_fp8_linear(ctypes.byref(a), A + 64, need, None) == -4
-    assert L.fise_fp8_linear_workspace_bytes(ctypes.byref(set_all(fp8(), M=3, **CODES))) == 0 and L.fise_fp8_linear_workspace_bytes(None) == 0
+    assert L.fise_fp8_linear_workspace_bytes(ctypes.byref(set_all(fp8(), M=65, **CODES))) == 0 and L.fise_fp8_linear_workspace_bytes(None) == 0
     assert L.fise_fp8_linear_workspace_bytes(ctypes.byref(set_all(fp8(), N=0))) == 0 and L.fise_fp8_linear(None, None, 0, None) == -1
 
 
