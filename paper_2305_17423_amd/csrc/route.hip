@@ -23,13 +23,13 @@ struct RouteArgs {
 };
 
 // over the L neighbouring lanes of a token; all of them get the result
-template <int L> __device__ __forceinline__ float route_max(float v) {
+template <int L> __device__ __forceinline__ int route_max(int v) {
     // rotations within sixteen lanes
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false)));
-    if constexpr (L == 64) { v = fmaxf(v, __shfl_xor(v, 16)); v = fmaxf(v, __shfl_xor(v, 32)); }
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false));
+    if constexpr (L == 64) { v = max(v, __shfl_xor(v, 16)); v = max(v, __shfl_xor(v, 32)); }
     return v;
 }
 template <int L> __device__ __forceinline__ double route_max(double v) {
@@ -49,133 +49,216 @@ template <int L> __device__ __forceinline__ int route_lowest(bool holds, int par
     const unsigned mine = (unsigned)(all >> (part * L)) & ((1u << L) - 1);
     return mine ? __ffs((int)mine) - 1 : L;
 }
-__device__ __forceinline__ float route_exp(float x) { return __expf(x); }
-__device__ __forceinline__ double route_exp(double x) { return exp(x); }
-__device__ __forceinline__ float route_inverse(float x) { return __builtin_amdgcn_rcpf(x); }
-__device__ __forceinline__ double route_inverse(double x) { return 1.0 / x; }
+__device__ __forceinline__ float route_logit(const RouteArgs& a, long long t, int e) {
+    return a.f32 ? reinterpret_cast<const float*>(a.logits)[t * a.stride + e] : bf2f(reinterpret_cast<const bf16_t*>(a.logits)[t * a.stride + e]);
+}
+// floats in the order of whole numbers (both zeros are one), and back
+__device__ __forceinline__ int route_code(float v) { const int b = __float_as_int(v + 0.f); return b ^ ((b >> 31) & 0x7fffffff); }
+__device__ __forceinline__ float route_float(int c) { return __int_as_float(c ^ ((c >> 31) & 0x7fffffff)); }
+constexpr int ROUTE_NONE = (int)0x80000000;
 
-// The experts of a token from its logits l, V neighbouring ones a lane: lane `sub` gets the expert of place `sub` (-1: none) and its logit.
-// K double: as the definition says.  K float: the same where the keys are the logits themselves (the order of the scores is theirs); otherwise scores are off by `off` at most, and
-// `close` says that two keys, of which the order matters, are no further apart than that explains.
-template <int L, int V, typename K>
-__device__ __forceinline__ void route_choose_experts(const RouteArgs& a, const float* l, float top, int sub, int part, bool& bad, bool& close, int& id, float& logit) {
-    const K none = -INFINITY;
-    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);
-    K key[V], off = 0;
+// One token by a whole wave in 64 bits, as the definition says: lane j gets the expert of place j (-1: none).  `broken`: a key is not a number.
+template <int V> __device__ __forceinline__ int route_exact(const RouteArgs& a, long long t, bool& broken) {
+    const int lane = threadIdx.x & 63;
+    const double none = -INFINITY;
+    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);      // the order of the scores is that of the logits
+    float l[V], top = -INFINITY;
+    double key[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = lane * V + i;
+        l[i] = e < a.E ? route_logit(a, t, e) : -INFINITY;
+        top = fmaxf(top, l[i]);
+    }
     if (direct) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = (K)l[i];
+        for (int i = 0; i < V; ++i) key[i] = (double)l[i];
     } else {
-        if (a.sigmoid) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) key[i] = route_inverse((K)1 + route_exp(-(K)l[i]));
-            off = (K)0x1p-19;                                          // s (1 - s) (|l| 2^-23 + 2^-21) of the exponential, two roundings
-        } else {
-            K sum = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) { key[i] = l[i] == -INFINITY ? (K)0 : route_exp((K)l[i] - (K)top); sum += key[i]; }
-            const K one = (K)1 / (K)route_sum<L>((double)sum);         // (a token without experts: not used)
-#pragma unroll
-            for (int i = 0; i < V; ++i) key[i] *= one;
-            off = one * (K)0x1p-19;                                    // p (|x| 2^-23 + 2^-21) with p = e^-|x|, of the exponential and the sum
-        }
+        top = route_float(route_max<64>(route_code(top)));
+        double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int e = sub * V + i;
-            if (a.bias && e < a.E) key[i] += (K)a.bias[e];
+            key[i] = l[i] == -INFINITY ? 0.0 : exp(a.sigmoid ? -(double)l[i] : (double)l[i] - (double)top);
+            sum += key[i];
+        }
+        sum = a.sigmoid ? 1.0 : route_sum<64>(sum);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = lane * V + i;
+            key[i] = a.sigmoid ? 1.0 / (1.0 + key[i]) : key[i] / sum;
+            if (a.bias && e < a.E) key[i] += (double)a.bias[e];
             if (l[i] == -INFINITY) key[i] = none;
-            bad = bad || key[i] != key[i];
+            broken = broken || key[i] != key[i];
         }
     }
-    auto near = [&](K high, K low) { return !direct && sizeof(K) == 4 && low > none && high - low <= 4 * off + (K)0x1p-21 * (high < 0 ? -high : high); };
-    close = false;
     if (a.groups > 1) {
         const int size = a.E / a.groups;
-        K mine = none;                                                 // of group `sub`
-        if (size % V == 0 && ((size / V) & (size / V - 1)) == 0 && size / V <= L) {      // groups of whole lanes, a power of two of them
-            K m1 = none, m2 = none;
+        double mine = none;                                            // of group `lane`
+        for (int g = 0; g < a.groups; ++g) {
+            double m1 = none, m2 = none;
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const K k = key[i]; m2 = k > m1 ? m1 : k > m2 ? k : m2; m1 = k > m1 ? k : m1; }
-            for (int o = 1; o < size / V; o <<= 1) {
-                const K n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o), low = m1 < n1 ? m1 : n1, second = m2 > n2 ? m2 : n2;
-                m1 = m1 > n1 ? m1 : n1;
-                m2 = low > second ? low : second;
+            for (int i = 0; i < V; ++i) {
+                const int e = lane * V + i;
+                if (e < g * size || e >= (g + 1) * size) continue;
+                m2 = key[i] > m1 ? m1 : key[i] > m2 ? key[i] : m2;
+                m1 = key[i] > m1 ? key[i] : m1;
+            }
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const double n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o);
+                m2 = fmax(fmin(m1, n1), fmax(m2, n2));
+                m1 = fmax(m1, n1);
             }
             if (a.group_top > 1 && m2 > none) m1 += m2;
-            mine = __shfl(m1, part * L + min(sub * (size / V), L - 1));
-            if (sub >= a.groups) mine = none;
-        } else
-            for (int g = 0; g < a.groups; ++g) {
-                K m1 = none, m2 = none;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int e = sub * V + i;
-                    if (e < g * size || e >= (g + 1) * size) continue;
-                    const K k = key[i];
-                    m2 = k > m1 ? m1 : k > m2 ? k : m2;
-                    m1 = k > m1 ? k : m1;
-                }
-                for (int o = 1; o < L; o <<= 1) {
-                    const K n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o), low = m1 < n1 ? m1 : n1, second = m2 > n2 ? m2 : n2;
-                    m1 = m1 > n1 ? m1 : n1;
-                    m2 = low > second ? low : second;
-                }
-                if (a.group_top > 1 && m2 > none) m1 += m2;
-                if (sub == g) mine = m1;
-            }
+            if (lane == g) mine = m1;
+        }
         unsigned long long kept = 0;
-        K last = none;
-        for (int j = 0; j <= a.top_groups && j < a.groups; ++j) {
-            const K best = route_max<L>(mine);
-            if (j == a.top_groups) { close = close || near(last, best); break; }
-            const int g = route_lowest<L>(mine == best, part);
-            if (best > none) kept |= 1ull << g;
-            if (sub == g) mine = none;
-            last = best;
+        for (int j = 0; j < a.top_groups; ++j) {
+            const double best = route_max<64>(mine);
+            if (!(best > none)) break;
+            const int g = route_lowest<64>(mine == best, 0) & 63;
+            kept |= 1ull << g;
+            if (lane == g) mine = none;
         }
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (!(kept >> (min(sub * V + i, a.E - 1) / size) & 1)) key[i] = none;
+            if (!(kept >> (min(lane * V + i, a.E - 1) / size) & 1)) key[i] = none;
     }
-    id = -1;
-    logit = 0.f;
-    K last = INFINITY;
-    for (int j = 0; j <= a.k; ++j) {
-        K m = key[0];
+    int id = -1;
+    for (int j = 0; j < a.k; ++j) {
+        double m = key[0];
 #pragma unroll
         for (int i = 1; i < V; ++i) m = key[i] > m ? key[i] : m;
-        const K best = route_max<L>(m);
-        if (j > 0) close = close || near(last, best);
-        if (j == a.k || !__any(best > none)) break;
-        const int from = route_lowest<L>(m == best, part);
+        const double best = route_max<64>(m);
+        if (!(best > none)) break;
+        const int from = route_lowest<64>(m == best, 0) & 63;
         int at = 0;
-        float value = 0.f;
-        bool open = sub == from;
+        bool open = lane == from;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const bool hit = open && key[i] == best;
             at = hit ? i : at;
-            value = hit ? l[i] : value;
             key[i] = hit ? none : key[i];
             open = open && !hit;
         }
-        const int lane = part * L + min(from, L - 1), e = from * V + __shfl(at, lane);
-        value = __shfl(value, lane);
-        if (best > none && sub == j) { id = e; logit = value; }
+        at = __shfl(at, from);
+        if (lane == j) id = from * V + at;
+    }
+    return id;
+}
+
+// The same by L lanes with keys in float, their order as whole numbers of which the last four bits are the place among a lane's V (the first has the largest).  `close`: two keys of which the
+// order matters are no further apart than their errors and those four bits explain, so the token needs route_exact.  ids[j]: the expert of place j, from the lane that has it.
+template <int L, int V>
+__device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, const float* bias, int sub, int part, volatile int* ids, bool& broken, bool& close) {
+    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);
+    float off = 0.f;
+    int key[V];
+    if (direct) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = route_code(l[i]);
+    } else {
+        float v[V];
+        if (a.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
+            off = 0x1p-19f;                                            // s (1 - s) (|l| 2^-23 + 2^-21) of the exponential, three roundings
+        } else {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = fmaxf(top, l[i]);
+            top = route_float(route_max<L>(route_code(top)));
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { v[i] = l[i] == -INFINITY ? 0.f : __expf(l[i] - top); sum += (double)v[i]; }
+            const float one = 1.f / (float)route_sum<L>(sum);          // (a token without experts: not used)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] *= one;
+            off = one * 0x1p-19f;                                      // p (|x| 2^-23 + 2^-21) with p = e^-|x|, of the exponential and the sum
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (a.bias) v[i] += bias[i];
+            broken = broken || (l[i] != -INFINITY && v[i] != v[i]);
+            key[i] = l[i] == -INFINITY ? ROUTE_NONE : route_code(v[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = key[i] <= route_code(-INFINITY) ? ROUTE_NONE : (key[i] & ~15) | (15 - i);
+    // keys as whole numbers without their places, which takes up to 2^-19 of them; bf16 logits lose nothing.  (Of the sum of two, that is of the largest key there is.)
+    auto near = [&](int high, int low, float large) {
+        if (low == ROUTE_NONE) return false;
+        if (direct) return a.f32 && high == low;
+        const float h = route_float(high), w = route_float(low);
+        return !(h - w > 4.f * off + 0x1p-17f * fmaxf(large, fmaxf(fabsf(h), fabsf(w))));
+    };
+    close = false;
+    if (a.groups > 1) {                                                // groups of whole lanes, a power of two of them (others take route_exact)
+        const int lanes = a.E / a.groups / V;
+        int m1 = ROUTE_NONE, m2 = ROUTE_NONE;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { m2 = max(m2, min(m1, key[i])); m1 = max(m1, key[i]); }
+        for (int o = 1; o < lanes; o <<= 1) {
+            const int n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o);
+            m2 = max(min(m1, n1), max(m2, n2));
+            m1 = max(m1, n1);
+        }
+        m1 &= ~15; m2 &= ~15;
+        if (a.group_top > 1 && m2 != ROUTE_NONE) m1 = route_code(route_float(m1) + route_float(m2));
+        float large = 0.f;
+        if (!direct) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) if (key[i] != ROUTE_NONE) large = fmaxf(large, fabsf(route_float(key[i])));
+            large = 2.f * __int_as_float(route_max<L>(__float_as_int(large)));
+        }
+        int mine = sub % lanes == 0 && sub / lanes < a.groups ? m1 : ROUTE_NONE;      // in the group's first lane
+        unsigned kept = 0;
+        int last = ROUTE_NONE;
+        for (int j = 0; j <= a.top_groups && j < a.groups; ++j) {
+            const int best = route_max<L>(mine);
+            if (j == a.top_groups) { close = near(last, best, large); break; }
+            const int from = route_lowest<L>(mine == best, part);
+            if (best != ROUTE_NONE && sub / lanes == from / lanes) kept = 1;
+            if (sub == from) mine = ROUTE_NONE;
+            last = best;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = kept ? key[i] : ROUTE_NONE;
+    }
+    int last = 0x7fffffff;
+    for (int j = 0; j <= a.k; ++j) {
+        int m = key[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) m = max(m, key[i]);
+        const int mine = m & ~15, best = route_max<L>(mine);
+        if (j > 0) close = close || near(last, best, 0.f);
+        if (j == a.k || !__any(best != ROUTE_NONE)) break;
+        if (sub == route_lowest<L>(mine == best, part) && best != ROUTE_NONE) {
+            ids[j] = sub * V + 15 - (m & 15);
+#pragma unroll
+            for (int i = 0; i < V; ++i) key[i] = key[i] == m ? ROUTE_NONE : key[i];
+        }
         last = best;
     }
 }
 
 template <int L, int V, bool SINGLE>
 __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a) {
-    extern __shared__ int route_lds[];                                 // [wave][E] counts, then (single) the pairs
+    extern __shared__ int route_lds[];                                 // [wave][E] counts, [wave][64] ids, then (single) the pairs
     constexpr int WAVES = SINGLE ? ROUTE_SINGLE_WAVES : ROUTE_WAVES, AT_ONCE = 64 / L;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane % L, part = lane / L;
-    int* const count = route_lds + wave * a.E;
-    unsigned* const held = reinterpret_cast<unsigned*>(route_lds + WAVES * a.E);
+    // lanes read what others of their wave wrote: LDS serves a wave in order, and the compiler keeps that order
+    volatile int* const count = route_lds + wave * a.E;
+    volatile int* const ids = route_lds + WAVES * a.E + wave * 64 + part * L;
+    unsigned* const held = reinterpret_cast<unsigned*>(route_lds + WAVES * (a.E + 64));
     const long long first = ((long long)blockIdx.x * WAVES + wave) * a.wave_tokens;
     if (a.lists)
         for (int e = lane; e < a.E; e += 64) count[e] = 0;
+    const int size = a.E / a.groups, lanes = size / V;
+    const bool odd_groups = a.groups > 1 && (size % V != 0 || (lanes & (lanes - 1)) != 0);
+    float bias[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) bias[i] = a.bias && sub * V + i < a.E ? a.bias[sub * V + i] : 0.f;
     for (int r0 = 0; r0 < a.wave_tokens; r0 += AT_ONCE) {
         const long long t = first + r0 + part;
         const bool there = t < a.T;
@@ -196,42 +279,46 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
                 }
             } else
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    l[i0 + i] = -INFINITY;
-                    if (there && e + i < a.E) l[i0 + i] = a.f32 ? reinterpret_cast<const float*>(a.logits)[t * a.stride + e + i] : bf2f(reinterpret_cast<const bf16_t*>(a.logits)[t * a.stride + e + i]);
-                }
+                for (int i = 0; i < 4; ++i) l[i0 + i] = there && e + i < a.E ? route_logit(a, t, e + i) : -INFINITY;
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             bad = bad || l[i] != l[i] || (!a.sigmoid && l[i] == INFINITY);
             top = fmaxf(top, l[i]);
         }
-        top = route_max<L>(top);
-        int id;
-        float logit;
-        bool close, broken = bad;
-        route_choose_experts<L, V, float>(a, l, top, sub, part, broken, close, id, logit);
-        if (__any(close)) {                                            // keys next to each other: all of it in 64 bits
-            broken = bad;
-            route_choose_experts<L, V, double>(a, l, top, sub, part, broken, close, id, logit);
-        }
+        bool close = odd_groups;
+        ids[sub] = -1;
+        if (!odd_groups) route_fast<L, V>(a, l, bias, sub, part, ids, bad, close);
         const unsigned long long mask = L == 64 ? ~0ull : ((1ull << L) - 1) << (part * L);
-        bad = (__ballot(broken) & mask) != 0;
+        bad = (__ballot(bad) & mask) != 0;
+        int id = ids[sub];
+        for (unsigned long long again = __ballot(close && there && !bad); again;) {
+            const int p = (__ffsll(again) - 1) / L;
+            again &= L == 64 ? 0ull : ~(((1ull << L) - 1) << (p * L));
+            bool broken = false;
+            const int exact = route_exact<L * V / 64>(a, first + r0 + p, broken);
+            broken = __any(broken);
+            const int moved = __shfl(exact, sub);
+            if (part == p) { id = moved; bad = bad || broken; }
+        }
+        if (bad) id = -1;
         // the chosen ones' scores in 64 bits, one a lane; a softmax' sum where it does not drop out
-        const double x = a.sigmoid ? -(double)logit : (double)logit - (double)top, p = exp(x);
-        double w = id < 0 ? 0.0 : a.sigmoid ? 1.0 / (1.0 + p) : p;
-        if (a.renorm) {
-            const double sum = route_sum<L>(w);
-            w = sum > 0.0 ? w / sum : 0.0;
-        } else if (!a.sigmoid) {
-            double sum = 0.0;
+        const bool out = there && sub < a.k;
+        const double logit = out && id >= 0 ? (double)route_logit(a, t, id) : 0.0;
+        double w = 0.0;
+        top = a.sigmoid ? 0.f : route_float(route_max<L>(route_code(top)));
+        const double p = exp(a.sigmoid ? -logit : logit - (double)top);
+        if (out && id >= 0) w = a.sigmoid ? 1.0 / (1.0 + p) : p;
+        if (a.renorm || !a.sigmoid) {
+            double sum = w;
+            if (!a.renorm) {
+                sum = 0.0;
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : (double)__expf(l[i] - top);      // (2^-20 of the sum)
+                for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : (double)__expf(l[i] - top);      // (2^-20 of the sum)
+            }
             sum = route_sum<L>(sum);
             w = sum > 0.0 ? w / sum : 0.0;
         }
-        if (bad) id = -1;
-        const bool out = there && sub < a.k;
         if (out) {
             a.ids[t * a.k + sub] = id;
             a.weights[t * a.k + sub] = bad ? NAN : (float)(w * (double)a.scale);
@@ -296,20 +383,28 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
     }
 }
 
-// Counts of an expert in all chunks become starts among its pairs: a wave an expert.
-__global__ __launch_bounds__(64) void route_scan_kernel(int* hist, int* total, int chunks) {
+// Counts of an expert in all chunks become starts among its pairs: a workgroup an expert, a lane neighbouring chunks.
+__global__ __launch_bounds__(256) void route_scan_kernel(int* hist, int* total, int chunks) {
+    __shared__ int sums[4];
     int* const h = hist + (long long)blockIdx.x * chunks;
-    const int lane = threadIdx.x;
-    int sum = 0;
-    for (int c0 = 0; c0 < chunks; c0 += 64) {
-        const int n = c0 + lane < chunks ? h[c0 + lane] : 0;
-        int up = n;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0;
+    for (int c0 = 0; c0 < chunks; c0 += 2048) {
+        int n[8], mine = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const int c = c0 + tid * 8 + i; n[i] = c < chunks ? h[c] : 0; mine += n[i]; }
+        int up = mine;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) { const int m = __shfl_up(up, o); if (lane >= o) up += m; }
-        if (c0 + lane < chunks) h[c0 + lane] = sum + up - n;
-        sum += __shfl(up, 63);
+        if (lane == 63) sums[wave] = up;
+        __syncthreads();
+        int at = before + up - mine;
+        for (int w = 0; w < 4; ++w) { if (w < wave) at += sums[w]; before += sums[w]; }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const int c = c0 + tid * 8 + i; if (c < chunks) h[c] = at; at += n[i]; }
+        __syncthreads();
     }
-    if (lane == 0) total[blockIdx.x] = sum;
+    if (tid == 0) total[blockIdx.x] = before;
 }
 
 __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a) {
@@ -347,10 +442,10 @@ __global__ __launch_bounds__(256) void route_place_kernel(RouteArgs a) {
 }
 
 template <int L, int V> static int launch_route(const RouteArgs& a, const RouteChoice& c, hipStream_t st) {
-    const int lds = (c.waves * a.E + (c.single ? a.T * a.k + 16 : 0)) * 4;
+    const int lds = (c.waves * (a.E + 64) + (c.single ? a.T * a.k + 16 : 0)) * 4;
     if (c.single) {
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&route_kernel<L, V, true>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                           (ROUTE_SINGLE_WAVES * L * V + ROUTE_SINGLE_PAIRS + 16) * 4);
+                                                           (ROUTE_SINGLE_WAVES * (L * V + 64) + ROUTE_SINGLE_PAIRS + 16) * 4);
         if (attr != hipSuccess) return fail(FISE_ERR_HIP, "fise_route_experts: cannot raise the dynamic LDS limit");
         hipLaunchKernelGGL((route_kernel<L, V, true>), dim3(1), dim3(1024), (size_t)lds, st, a);
     } else hipLaunchKernelGGL((route_kernel<L, V, false>), dim3((unsigned)c.chunks), dim3(256), (size_t)lds, st, a);
@@ -403,7 +498,7 @@ extern "C" int fise_route_experts(const fise_route_args* g, void* workspace, siz
     const hipStream_t st = as_stream(stream);
     if (int e = c.lanes == 64 ? launch_route<64, 16>(a, c, st) : c.values == 4 ? launch_route<16, 4>(a, c, st) : launch_route<16, 16>(a, c, st)) return e;
     if (!lists || c.single) return FISE_OK;
-    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)a.E), dim3(64), 0, st, a.hist, a.total, a.chunks);
+    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)a.E), dim3(256), 0, st, a.hist, a.total, a.chunks);
     FISE_CHECK_LAUNCH(fn);
     hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)(((long long)a.T * a.k + 1023) / 1024)), dim3(256), 0, st, a);
     FISE_CHECK_LAUNCH(fn);

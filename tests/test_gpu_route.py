@@ -167,3 +167,15 @@ def test_rows_with_gaps_and_none(fb):
     o = torch.full((34,), 5, dtype=torch.int32, device=DEV)
     fb.fise_route_experts(fb.route_args(logits[:0, 3:36], ids[:0], w[:0], o, ids.view(-1)[:0]))
     assert bool((o == 5).all())
+
+
+@pytest.mark.parametrize("type", ["bf16", "f32"])
+def test_zeros_of_both_signs_and_negative_ties(fb, type):
+    """Zeros of both signs are one number, negative logits tie like positive ones; keys that cancel in a group's sum."""
+    g = torch.Generator().manual_seed(21)
+    z = torch.where(torch.rand((60, 32), generator=g) < 0.5, 0.0, -0.0).to(T_[type])
+    check(fb, z, None, 5)
+    check(fb, -torch.randint(0, 4, (60, 32), generator=g).to(T_[type]), None, 7, "sigmoid")
+    b = torch.cat((torch.full((16,), -1.0), torch.zeros(16)))[torch.randperm(32, generator=g)]
+    check(fb, torch.randn((300, 32), generator=g).to(T_[type]), b, 4, "sigmoid", 8, 3, 2, True, 1.0)
+    check(fb, torch.randn((300, 32), generator=g).to(T_[type]), b * 1e4, 4, "softmax", 8, 3, 2, False, 1.0)
