@@ -147,6 +147,24 @@ template <int V> __device__ __forceinline__ int route_exact(const RouteArgs& a, 
     return id;
 }
 
+// Steps of the network: key x and the one D behind it, for all x; then the shorter distances among sorted runs of P keys, and the longer runs.  (Templates, not loops: the compiler
+// took the loops' indices for numbers of its run time and searched the keys for each.)
+template <int V, int P, int D, int X> __device__ __forceinline__ void route_sort(int (&key)[V]) {
+    if constexpr (X >= D % P && (X - D % P) / D % 2 == 0 && X / (2 * P) == (X + D) / (2 * P)) {
+        const int high = max(key[X], key[X + D]), low = min(key[X], key[X + D]);
+        key[X] = high;
+        key[X + D] = low;
+    }
+    if constexpr (X + 1 < V - D) route_sort<V, P, D, X + 1>(key);
+    else if constexpr (D > 1) route_sort<V, P, D / 2, 0>(key);
+    else if constexpr (2 * P < V) route_sort<V, 2 * P, 2 * P, 0>(key);
+}
+// the first key goes, the others move up
+template <int V, int X> __device__ __forceinline__ void route_shift(int (&key)[V], bool really) {
+    key[X] = really ? (X + 1 < V ? key[X + 1 < V ? X + 1 : X] : ROUTE_NONE) : key[X];
+    if constexpr (X + 1 < V) route_shift<V, X + 1>(key, really);
+}
+
 // The same by L lanes with keys in float, their order as whole numbers of which the last four bits are the place among a lane's V (the first has the largest).  `close`: two keys of which the
 // order matters are no further apart than their errors and those four bits explain, so the token needs route_exact.  ids[j]: the expert of place j, from the lane that has it.
 template <int L, int V>
@@ -225,19 +243,16 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
 #pragma unroll
         for (int i = 0; i < V; ++i) key[i] = kept ? key[i] : ROUTE_NONE;
     }
+    // each lane's keys in descending order (a network of compare-and-exchange steps that merges sorted halves); then the largest of the lanes' first ones, k times
+    route_sort<V, 1, 1, 0>(key);
     int last = 0x7fffffff;
     for (int j = 0; j <= a.k; ++j) {
-        int m = key[0];
-#pragma unroll
-        for (int i = 1; i < V; ++i) m = max(m, key[i]);
-        const int mine = m & ~15, best = route_max<L>(mine);
+        const int mine = key[0] & ~15, best = route_max<L>(mine);
         if (j > 0) close = close || near(last, best, 0.f);
         if (j == a.k || !__any(best != ROUTE_NONE)) break;
-        if (sub == route_lowest<L>(mine == best, part) && best != ROUTE_NONE) {
-            ids[j] = sub * V + 15 - (m & 15);
-#pragma unroll
-            for (int i = 0; i < V; ++i) key[i] = key[i] == m ? ROUTE_NONE : key[i];
-        }
+        const bool won = sub == route_lowest<L>(mine == best, part) && best != ROUTE_NONE;
+        if (won) ids[j] = sub * V + 15 - (key[0] & 15);
+        route_shift<V, 0>(key, won);
         last = best;
     }
 }
