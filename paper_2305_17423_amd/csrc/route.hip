@@ -32,11 +32,6 @@ template <int L> __device__ __forceinline__ int route_max(int v) {
     if constexpr (L == 64) { v = max(v, __shfl_xor(v, 16)); v = max(v, __shfl_xor(v, 32)); }
     return v;
 }
-template <int L> __device__ __forceinline__ double route_max(double v) {
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) v = fmax(v, __shfl_xor(v, o));
-    return v;
-}
 template <int L> __device__ __forceinline__ double route_sum(double v) {
 #pragma unroll
     for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o);
@@ -57,92 +52,102 @@ __device__ __forceinline__ int route_code(float v) { const int b = __float_as_in
 __device__ __forceinline__ float route_float(int c) { return __int_as_float(c ^ ((c >> 31) & 0x7fffffff)); }
 constexpr int ROUTE_NONE = (int)0x80000000;
 
+// Doubles in the order of whole numbers, and back; the largest of a wave's, and the lowest lane that has it.  (By rotations within sixteen lanes and four scalar reads: shuffles through LDS,
+// one behind the other, made a token that comes here take 10 us.)
+__device__ __forceinline__ long long route_code64(double v) { const long long b = __double_as_longlong(v + 0.0); return b ^ ((b >> 63) & 0x7fffffffffffffffLL); }
+__device__ __forceinline__ double route_double(long long c) { return __longlong_as_double(c ^ ((c >> 63) & 0x7fffffffffffffffLL)); }
+constexpr long long ROUTE_NONE64 = (long long)0x8000000000000000ULL;
+__device__ __forceinline__ int route_wave_max(int v) {
+    v = route_max<16>(v);
+    return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+__device__ __forceinline__ long long route_first64(long long key, int& lane) {
+    const int high = (int)(key >> 32), low = (int)((unsigned)key ^ 0x80000000u), top = route_wave_max(high), then = route_wave_max(high == top ? low : (int)0x80000000);
+    lane = __ffsll(__ballot(high == top && low == then)) - 1;
+    return (long long)(((unsigned long long)(unsigned)top << 32) | ((unsigned)then ^ 0x80000000u));
+}
+
 // One token by a whole wave in 64 bits, as the definition says: lane j gets the expert of place j (-1: none).  `broken`: a key is not a number.
 template <int V> __device__ __forceinline__ int route_exact(const RouteArgs& a, long long t, bool& broken) {
     const int lane = threadIdx.x & 63;
-    const double none = -INFINITY;
     const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);      // the order of the scores is that of the logits
     float l[V], top = -INFINITY;
-    double key[V];
+    double score[V];
+    long long key[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = lane * V + i;
         l[i] = e < a.E ? route_logit(a, t, e) : -INFINITY;
         top = fmaxf(top, l[i]);
+        score[i] = (double)l[i];
     }
-    if (direct) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = (double)l[i];
-    } else {
-        top = route_float(route_max<64>(route_code(top)));
+    if (!direct) {
+        top = route_float(route_wave_max(route_code(top)));
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            key[i] = l[i] == -INFINITY ? 0.0 : exp(a.sigmoid ? -(double)l[i] : (double)l[i] - (double)top);
-            sum += key[i];
+            score[i] = l[i] == -INFINITY ? 0.0 : exp(a.sigmoid ? -score[i] : score[i] - (double)top);
+            sum += score[i];
         }
         sum = a.sigmoid ? 1.0 : route_sum<64>(sum);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int e = lane * V + i;
-            key[i] = a.sigmoid ? 1.0 / (1.0 + key[i]) : key[i] / sum;
-            if (a.bias && e < a.E) key[i] += (double)a.bias[e];
-            if (l[i] == -INFINITY) key[i] = none;
-            broken = broken || key[i] != key[i];
+            score[i] = a.sigmoid ? 1.0 / (1.0 + score[i]) : score[i] / sum;
+            if (a.bias && e < a.E) score[i] += (double)a.bias[e];
+            broken = broken || (l[i] != -INFINITY && score[i] != score[i]);
         }
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = l[i] == -INFINITY || score[i] == -INFINITY ? ROUTE_NONE64 : route_code64(score[i]);
     if (a.groups > 1) {
         const int size = a.E / a.groups;
-        double mine = none;                                            // of group `lane`
+        long long mine = ROUTE_NONE64;                                 // of group `lane`
         for (int g = 0; g < a.groups; ++g) {
-            double m1 = none, m2 = none;
+            long long m1 = ROUTE_NONE64;
+            int at = -1, from;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int e = lane * V + i;
-                if (e < g * size || e >= (g + 1) * size) continue;
-                m2 = key[i] > m1 ? m1 : key[i] > m2 ? key[i] : m2;
-                m1 = key[i] > m1 ? key[i] : m1;
+                if (e >= g * size && e < (g + 1) * size && key[i] > m1) { m1 = key[i]; at = i; }
             }
+            long long best = route_first64(m1, from);
+            if (a.group_top > 1 && best != ROUTE_NONE64) {
+                long long m2 = ROUTE_NONE64;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const double n1 = __shfl_xor(m1, o), n2 = __shfl_xor(m2, o);
-                m2 = fmax(fmin(m1, n1), fmax(m2, n2));
-                m1 = fmax(m1, n1);
+                for (int i = 0; i < V; ++i) {
+                    const int e = lane * V + i;
+                    if (e >= g * size && e < (g + 1) * size && key[i] > m2 && !(lane == from && i == at)) m2 = key[i];
+                }
+                const long long second = route_first64(m2, from);
+                if (second != ROUTE_NONE64) best = route_code64(route_double(best) + route_double(second));
             }
-            if (a.group_top > 1 && m2 > none) m1 += m2;
-            if (lane == g) mine = m1;
+            if (lane == g) mine = best;
         }
         unsigned long long kept = 0;
         for (int j = 0; j < a.top_groups; ++j) {
-            const double best = route_max<64>(mine);
-            if (!(best > none)) break;
-            const int g = route_lowest<64>(mine == best, 0) & 63;
+            int g;
+            if (route_first64(mine, g) == ROUTE_NONE64) break;
             kept |= 1ull << g;
-            if (lane == g) mine = none;
+            if (lane == g) mine = ROUTE_NONE64;
         }
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (!(kept >> (min(lane * V + i, a.E - 1) / size) & 1)) key[i] = none;
+            if (!(kept >> (min(lane * V + i, a.E - 1) / size) & 1)) key[i] = ROUTE_NONE64;
     }
     int id = -1;
     for (int j = 0; j < a.k; ++j) {
-        double m = key[0];
+        long long m = key[0];
+        int at = 0, from;
 #pragma unroll
-        for (int i = 1; i < V; ++i) m = key[i] > m ? key[i] : m;
-        const double best = route_max<64>(m);
-        if (!(best > none)) break;
-        const int from = route_lowest<64>(m == best, 0) & 63;
-        int at = 0;
-        bool open = lane == from;
+        for (int i = 1; i < V; ++i)
+            if (key[i] > m) { m = key[i]; at = i; }
+        if (route_first64(m, from) == ROUTE_NONE64) break;
+        const int e = from * V + __builtin_amdgcn_readlane(at, from);
+        if (lane == j) id = e;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const bool hit = open && key[i] == best;
-            at = hit ? i : at;
-            key[i] = hit ? none : key[i];
-            open = open && !hit;
-        }
-        at = __shfl(at, from);
-        if (lane == j) id = from * V + at;
+        for (int i = 0; i < V; ++i)
+            if (lane == from && i == at) key[i] = ROUTE_NONE64;
     }
     return id;
 }
@@ -168,9 +173,9 @@ template <int V, int X> __device__ __forceinline__ void route_shift(int (&key)[V
 // The same by L lanes with keys in float, their order as whole numbers of which the last four bits are the place among a lane's V (the first has the largest).  `close`: two keys of which the
 // order matters are no further apart than their errors and those four bits explain, so the token needs route_exact.  ids[j]: the expert of place j, from the lane that has it.
 template <int L, int V>
-__device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, const float* bias, int sub, int part, volatile int* ids, bool& broken, bool& close) {
+__device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, const float* bias, bool odd_bias, int sub, int part, volatile int* ids, bool& broken, bool& close) {
     const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);
-    float off = 0.f;
+    float off = 0.f, large = 0.f;
     int key[V];
     if (direct) {
 #pragma unroll
@@ -180,7 +185,7 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
         if (a.sigmoid) {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
-            off = 0x1p-19f;                                            // s (1 - s) (|l| 2^-23 + 2^-21) of the exponential, three roundings
+            off = 0x1p-21f;                                            // s (1 - s) (|l| 2^-23 + 2^-21) of the exponential, which is below 2^-22.3, and three roundings of s
         } else {
             float top = -INFINITY;
 #pragma unroll
@@ -192,23 +197,27 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
             const float one = 1.f / (float)route_sum<L>(sum);          // (a token without experts: not used)
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] *= one;
-            off = one * 0x1p-19f;                                      // p (|x| 2^-23 + 2^-21) with p = e^-|x|, of the exponential and the sum
+            off = one * 0x1p-19f;                                      // p (|x| 2^-23 + 2^-21) with p = e^-|x|, of the exponential, which is below 2^-20.8; as much of the sum; two roundings
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (a.bias) v[i] += bias[i];
-            broken = broken || (l[i] != -INFINITY && v[i] != v[i]);
+            large = fmaxf(large, fabsf(v[i]));
             key[i] = l[i] == -INFINITY ? ROUTE_NONE : route_code(v[i]);
         }
+        if (odd_bias)
+#pragma unroll
+            for (int i = 0; i < V; ++i) broken = broken || (l[i] != -INFINITY && v[i] != v[i]);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = key[i] <= route_code(-INFINITY) ? ROUTE_NONE : (key[i] & ~15) | (15 - i);
-    // keys as whole numbers without their places, which takes up to 2^-19 of them; bf16 logits lose nothing.  (Of the sum of two, that is of the largest key there is.)
-    auto near = [&](int high, int low, float large) {
+    // Keys as whole numbers without their places, which takes less than 2^-19 off them (bf16 logits: nothing).  Two are in order where they are further apart than that, the errors of both
+    // scores and the roundings of their biases.  (For sums of two keys `large` is twice the largest key there is, and their errors are those of two.)
+    auto near = [&](int high, int low, float large, float errors) {
         if (low == ROUTE_NONE) return false;
         if (direct) return a.f32 && high == low;
         const float h = route_float(high), w = route_float(low);
-        return !(h - w > 4.f * off + 0x1p-17f * fmaxf(large, fmaxf(fabsf(h), fabsf(w))));
+        return !(h - w > errors * off + (0x1p-19f + 0x1p-21f) * fmaxf(large, fmaxf(fabsf(h), fabsf(w))));
     };
     close = false;
     if (a.groups > 1) {                                                // groups of whole lanes, a power of two of them (others take route_exact)
@@ -223,18 +232,13 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
         }
         m1 &= ~15; m2 &= ~15;
         if (a.group_top > 1 && m2 != ROUTE_NONE) m1 = route_code(route_float(m1) + route_float(m2));
-        float large = 0.f;
-        if (!direct) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) if (key[i] != ROUTE_NONE) large = fmaxf(large, fabsf(route_float(key[i])));
-            large = 2.f * __int_as_float(route_max<L>(__float_as_int(large)));
-        }
+        large = 2.f * __int_as_float(route_max<L>(__float_as_int(large)));
         int mine = sub % lanes == 0 && sub / lanes < a.groups ? m1 : ROUTE_NONE;      // in the group's first lane
         unsigned kept = 0;
         int last = ROUTE_NONE;
         for (int j = 0; j <= a.top_groups && j < a.groups; ++j) {
             const int best = route_max<L>(mine);
-            if (j == a.top_groups) { close = near(last, best, large); break; }
+            if (j == a.top_groups) { close = near(last, best, 2.f * large, 4.f); break; }
             const int from = route_lowest<L>(mine == best, part);
             if (best != ROUTE_NONE && sub / lanes == from / lanes) kept = 1;
             if (sub == from) mine = ROUTE_NONE;
@@ -245,16 +249,20 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
     }
     // each lane's keys in descending order (a network of compare-and-exchange steps that merges sorted halves); then the largest of the lanes' first ones, k times
     route_sort<V, 1, 1, 0>(key);
-    int last = 0x7fffffff;
+    int taken = ROUTE_NONE, after = ROUTE_NONE;                        // the key of place `sub`, and the first that is not taken
     for (int j = 0; j <= a.k; ++j) {
         const int mine = key[0] & ~15, best = route_max<L>(mine);
-        if (j > 0) close = close || near(last, best, 0.f);
+        if (j == a.k) after = best;
         if (j == a.k || !__any(best != ROUTE_NONE)) break;
+        if (sub == j) taken = best;
         const bool won = sub == route_lowest<L>(mine == best, part) && best != ROUTE_NONE;
         if (won) ids[j] = sub * V + 15 - (key[0] & 15);
         route_shift<V, 0>(key, won);
-        last = best;
     }
+    // each place against the next
+    int next = __shfl_down(taken, 1, L);
+    if (sub == a.k - 1) next = after;
+    if (sub < a.k && near(taken, next, 0.f, 2.f)) close = true;
 }
 
 template <int L, int V, bool SINGLE>
@@ -272,8 +280,30 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
     const int size = a.E / a.groups, lanes = size / V;
     const bool odd_groups = a.groups > 1 && (size % V != 0 || (lanes & (lanes - 1)) != 0);
     float bias[V];
+    bool odd_bias = false;                                             // one that is not a number
 #pragma unroll
-    for (int i = 0; i < V; ++i) bias[i] = a.bias && sub * V + i < a.E ? a.bias[sub * V + i] : 0.f;
+    for (int i = 0; i < V; ++i) { bias[i] = a.bias && sub * V + i < a.E ? a.bias[sub * V + i] : 0.f; odd_bias = odd_bias || bias[i] != bias[i]; }
+    odd_bias = __any(odd_bias);
+    float ahead[V];                                                    // the next tokens' logits are on their way while these are worked on
+    auto fetch = [&](long long t) {
+#pragma unroll
+        for (int i0 = 0; i0 < V; i0 += 4) {
+            const int e = sub * V + i0;
+            if (a.wide && t < a.T && e + 4 <= a.E) {
+                if (a.f32) {
+                    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.logits) + t * a.stride + e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ahead[i0 + i] = v[i];
+                } else {
+                    const u32x2_t v = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const bf16_t*>(a.logits) + t * a.stride + e);
+                    ahead[i0] = lo16(v[0]); ahead[i0 + 1] = hi16(v[0]); ahead[i0 + 2] = lo16(v[1]); ahead[i0 + 3] = hi16(v[1]);
+                }
+            } else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ahead[i0 + i] = t < a.T && e + i < a.E ? route_logit(a, t, e + i) : -INFINITY;
+        }
+    };
+    fetch(first + part);
     for (int r0 = 0; r0 < a.wave_tokens; r0 += AT_ONCE) {
         const long long t = first + r0 + part;
         const bool there = t < a.T;
@@ -281,21 +311,8 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
         float l[V], top = -INFINITY;
         bool bad = false;
 #pragma unroll
-        for (int i0 = 0; i0 < V; i0 += 4) {
-            const int e = sub * V + i0;
-            if (a.wide && there && e + 4 <= a.E) {
-                if (a.f32) {
-                    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.logits) + t * a.stride + e);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) l[i0 + i] = v[i];
-                } else {
-                    const u32x2_t v = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const bf16_t*>(a.logits) + t * a.stride + e);
-                    l[i0] = lo16(v[0]); l[i0 + 1] = hi16(v[0]); l[i0 + 2] = lo16(v[1]); l[i0 + 3] = hi16(v[1]);
-                }
-            } else
-#pragma unroll
-                for (int i = 0; i < 4; ++i) l[i0 + i] = there && e + i < a.E ? route_logit(a, t, e + i) : -INFINITY;
-        }
+        for (int i = 0; i < V; ++i) l[i] = ahead[i];
+        if (r0 + AT_ONCE < a.wave_tokens) fetch(t + AT_ONCE);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             bad = bad || l[i] != l[i] || (!a.sigmoid && l[i] == INFINITY);
@@ -303,7 +320,7 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
         }
         bool close = odd_groups;
         ids[sub] = -1;
-        if (!odd_groups) route_fast<L, V>(a, l, bias, sub, part, ids, bad, close);
+        if (!odd_groups) route_fast<L, V>(a, l, bias, odd_bias, sub, part, ids, bad, close);
         const unsigned long long mask = L == 64 ? ~0ull : ((1ull << L) - 1) << (part * L);
         bad = (__ballot(bad) & mask) != 0;
         int id = ids[sub];
