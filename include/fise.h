@@ -663,8 +663,8 @@ int fise_route_experts(const fise_route_args* a /* host */, void* workspace, siz
  *   h = silu(Wg[e] x_t) * (Wu[e] x_t),   y[t] = sum_j weights[t, j] * Wo[e] h (+ residual[t]),   e = ids[t, j]
  * Products as in fise_fp8_linear for y in bf16: x and h are put in 8 bits with a power of two for 128 channels; sums float,
  * and for y in bf16 an expert's result is rounded to bf16 before its weight (y float: not rounded).  A
- * pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots as fise_route_experts leaves them (pairs
- * in offsets / slots decide which expert's product a pair gets; places out of range are skipped).
+ * pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots belong together, as fise_route_experts leaves them (pairs
+ * whose places are out of range or contradict each other get no defined result; nothing outside the buffers is touched).
  * w_in codes [E, 2, I, K] (gate, up), w_in_scale [E, 2, ceil(I / 128), ceil(K / 128)]; w_out codes [E, N, I],
  * w_out_scale [E, ceil(N / 128), ceil(I / 128)]; 16-byte aligned.  x float or bf16 [T, K], rows x_stride apart; y,
  * residual [T, N], 16-byte aligned, strides multiples of 8.  K, I multiples of 16, N of 8, each at most 2^16; E 1..1024; T * k < 2^24;
@@ -679,7 +679,7 @@ typedef struct {
     const void* residual; int64_t residual_stride;
     void* y; int y_dtype; int64_t y_stride;
 } fise_expert_mlp_args;
-size_t fise_expert_mlp_workspace_bytes(const fise_expert_mlp_args* a /* host; sizes and types only */);
+size_t fise_expert_mlp_workspace_bytes(const fise_expert_mlp_args* a /* host; sizes, strides and types only */);
 int fise_expert_mlp(const fise_expert_mlp_args* a /* host */, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------

@@ -1,8 +1,9 @@
 // The feed-forward of the chosen experts: h = silu(Wg x) * (Wu x) and Wo h for every pair (token, expert) in the experts' order, then a token's weighted sum.
 //
-// Four launches: rows of x into 8 bits, with the table of tiles (a tile has rows of one expert); gate and up of a tile side by side in a wave, so that h leaves the
+// A few tokens: two launches that stream the weights past them (fp8_few.h), a workgroup a pair, then a token, h in float in between.  (Rows of an expert streamed past like that, 64 tokens of
+// 6 among 64 experts: 303 us, 124 on tiles.)  More: four launches: rows of x into 8 bits, with the table of tiles (a tile has rows of one expert); gate and up of a tile side by side in a wave, so that h leaves the
 // accumulators in 8 bits with the scale of its 128 channels; Wo; and the sum, which reads a pair's row where its token's list says it is.  No atomics: a result depends on its arguments only.
-#include "fp8.h"
+#include "fp8_few.h"
 #include "fp8_choice.h"
 
 namespace fise {
@@ -55,6 +56,87 @@ template <typename T> __global__ __launch_bounds__(256) void experts_rows_kernel
     fp8_quantize_unit((const T*)a.x, a.x_stride, a.T, a.K, a.units, a.units * 8, a.codes, a.code_stride, a.scale, (long long)a.T, (long long)(blockIdx.x - 1) * 256 + threadIdx.x);
 }
 
+// ---- a few tokens ----
+// silu(gate) * up of sixteen channels of one pair, the token in the first of the product's sixteen rows.
+template <int X>
+__global__ __launch_bounds__(1024) void experts_token_in_kernel(ExpertsFewArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    extern __shared__ __align__(16) float few_lds[];                   // [wave][gate, up][16]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, l16 = lane & 15, lq = lane >> 4;
+    const int i0 = blockIdx.x * 16, p = blockIdx.y, blocks = (a.K + FP8_BLOCK - 1) / FP8_BLOCK, i_blocks = (a.I + FP8_BLOCK - 1) / FP8_BLOCK;
+    const int expert = __builtin_amdgcn_readfirstlane(a.ids[p]);
+    if ((unsigned)expert >= (unsigned)a.E) return;
+    constexpr int es = X == FP8_X_BF16 ? 2 : 4;
+    const unsigned char* const wg = a.w_in + ((long long)expert * 2 * a.I + i0) * a.K;
+    const unsigned w_bytes = (unsigned)(min(16, a.I - i0) * a.K);
+    const auto from_g = buf(wg, w_bytes), from_u = buf(wg + (long long)a.I * a.K, w_bytes), from_x = buf(a.x, a.x_bytes);
+    const unsigned w_row = i0 + l16 < a.I ? (unsigned)(l16 * a.K) : FP8_FEW_NO_ROW, x_row = l16 == 0 ? (unsigned)(p / a.k * a.x_stride * es) : FP8_FEW_NO_ROW;
+    const float* const sg = a.w_in_scale + ((long long)expert * 2 * i_blocks + i0 / FP8_BLOCK) * blocks;
+    const float* const su = sg + (long long)i_blocks * blocks;
+    f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    Fp8FewWeights g, u;
+    if (wave < blocks) { g.ld(from_g, w_row, sg, wave, lq, a.K); u.ld(from_u, w_row, su, wave, lq, a.K); }
+    for (int kb = wave; kb < blocks; kb += waves) {
+        Fp8Operand<true> vg, vu, x;
+        vg.of(g.lo, g.hi);
+        vu.of(u.lo, u.hi);
+        const float kg = g.scale, ku = u.scale;
+        if (kb + waves < blocks) { g.ld(from_g, w_row, sg, kb + waves, lq, a.K); u.ld(from_u, w_row, su, kb + waves, lq, a.K); }
+        float xk;
+        fp8_few_rows<X>(from_x, x_row, kb, lq, a.K, x, xk);
+        const f32x4_t q = fp8_product(vg, x), r = fp8_product(vu, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { acc[0][i] = fmaf(q[i], xk * kg, acc[0][i]); acc[1][i] = fmaf(r[i], xk * ku, acc[1][i]); }
+    }
+    if (l16 == 0)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<f32x4_t*>(few_lds + (wave * 2 + j) * 16 + lq * 4) = acc[j];
+    __syncthreads();
+    if (tid < 16 && i0 + tid < a.I) {
+        float gate = 0.f, up = 0.f;
+        for (int k = 0; k < waves; ++k) { gate += few_lds[k * 32 + tid]; up += few_lds[k * 32 + 16 + tid]; }
+        a.h[(long long)p * a.I + i0 + tid] = gate / (1.f + expf(-gate)) * up;
+    }
+#endif
+}
+// Sixteen outputs of one token, all its experts: the waves share (place, block of columns).
+__global__ __launch_bounds__(1024) void experts_token_out_kernel(ExpertsFewArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    extern __shared__ __align__(16) float few_lds[];                   // [wave][16]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, l16 = lane & 15, lq = lane >> 4;
+    const int n0 = blockIdx.x * 16, t = blockIdx.y, blocks = (a.I + FP8_BLOCK - 1) / FP8_BLOCK, n_blocks = (a.N + FP8_BLOCK - 1) / FP8_BLOCK;
+    const auto from_h = buf(a.h, a.h_bytes);
+    const unsigned w_row = n0 + l16 < a.N ? (unsigned)(l16 * a.I) : FP8_FEW_NO_ROW;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int it = wave; it < a.k * blocks; it += waves) {
+        const int j = it / blocks, kb = it - j * blocks, p = t * a.k + j, expert = __builtin_amdgcn_readfirstlane(a.ids[p]);
+        if ((unsigned)expert >= (unsigned)a.E) continue;
+        const auto from_w = buf(a.w_out + ((long long)expert * a.N + n0) * a.I, (unsigned)(min(16, a.N - n0) * a.I));
+        Fp8FewWeights w;
+        w.ld(from_w, w_row, a.w_out_scale + ((long long)expert * n_blocks + n0 / FP8_BLOCK) * blocks, kb, lq, a.I);
+        Fp8Operand<true> v, x;
+        float xk;
+        fp8_few_rows<FP8_X_F32>(from_h, l16 == 0 ? (unsigned)p * (unsigned)(a.I * 4) : FP8_FEW_NO_ROW, kb, lq, a.I, x, xk);
+        v.of(w.lo, w.hi);
+        const f32x4_t r = fp8_product(v, x);
+        const float f = a.weights[p];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, r[i] * (xk * w.scale), acc[i]);
+    }
+    if (l16 == 0) *reinterpret_cast<f32x4_t*>(few_lds + wave * 16 + lq * 4) = acc;
+    __syncthreads();
+    if (tid < 16 && n0 + tid < a.N) {
+        const int n = n0 + tid;
+        float v = a.residual ? fp8_value(a.residual, a.y_f32, t * a.residual_stride + n) : 0.f;
+        for (int j = 0; j < a.k; ++j) if ((unsigned)a.ids[t * a.k + j] >= (unsigned)a.E) v = fmaf(a.weights[t * a.k + j], 0.f, v);
+        for (int k = 0; k < waves; ++k) v += few_lds[k * 16 + tid];
+        if (a.y_f32) reinterpret_cast<float*>(a.y)[t * a.y_stride + n] = v;
+        else reinterpret_cast<bf16_t*>(a.y)[t * a.y_stride + n] = f2bf(v);
+    }
+#endif
+}
+
+// ---- the sum ----
 struct ExpertsSum {
     const void* rows; const int* ids; const float* weights; const void* residual; long long residual_stride; void* y; long long y_stride;
     int T, k, N, units;
@@ -98,7 +180,7 @@ extern "C" size_t fise_expert_mlp_workspace_bytes(const fise_expert_mlp_args* g)
     const char* fn = "fise_expert_mlp";
     if (!g) { fail(FISE_ERR_NULL, "%s: null pointer", fn); return 0; }
     if (expert_sizes(fn, g)) return 0;
-    return (size_t)expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, g->y_dtype == FISE_F32 ? 4 : 2).bytes;
+    return (size_t)expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, g->x_stride * (g->x_dtype == FISE_F32 ? 4 : 2), g->y_dtype == FISE_F32 ? 4 : 2).bytes;
 }
 
 extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, size_t workspace_bytes, void* stream) {
@@ -110,14 +192,38 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     if (g->x_stride % 8 || g->y_stride % 8 || (g->residual && g->residual_stride % 8) || !aligned16(g->x) || !aligned16(g->y) || !aligned16(g->residual) || !aligned16(g->w_in) || !aligned16(g->w_out) ||
         ((uintptr_t)g->ids | (uintptr_t)g->weights | (uintptr_t)g->offsets | (uintptr_t)g->slots | (uintptr_t)g->w_in_scale | (uintptr_t)g->w_out_scale) & 3)
         return fail(FISE_ERR_ALIGN, "%s: rows and codes must be 16-byte aligned, strides multiples of 8, lists and scales aligned to their type", fn);
-    const int es = g->y_dtype == FISE_F32 ? 4 : 2;
-    const ExpertChoice c = expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, es);
+    const int es = g->y_dtype == FISE_F32 ? 4 : 2, xs = g->x_dtype == FISE_F32 ? 4 : 2;
+    const ExpertChoice c = expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, g->x_stride * xs, es);
     if (g->T && (!workspace || workspace_bytes < (size_t)c.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)c.bytes);
     if ((uintptr_t)workspace & 255) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
     if (g->T == 0) return FISE_OK;
+    ExpertsSum s{};
+    s.ids = g->ids; s.weights = g->weights; s.residual = g->residual; s.residual_stride = g->residual_stride; s.y = g->y; s.y_stride = g->y_stride;
+    s.T = g->T; s.k = g->k; s.N = g->N; s.units = g->N / 8;
+    const dim3 sum_grid((unsigned)(((long long)g->T * s.units + 255) / 256));
+    const hipStream_t st = as_stream(stream);
+    if (c.form == EXPERTS_TOKENS) {
+        ExpertsFewArgs f{};
+        f.x = g->x; f.x_stride = g->x_stride; f.x_bytes = (unsigned)(((g->T - 1) * g->x_stride + g->K) * xs);
+        f.ids = g->ids; f.weights = g->weights; f.T = g->T; f.k = g->k; f.E = g->E; f.K = g->K; f.I = g->I; f.N = g->N;
+        f.w_in = g->w_in; f.w_in_scale = g->w_in_scale; f.w_out = g->w_out; f.w_out_scale = g->w_out_scale;
+        f.h = (float*)workspace; f.h_bytes = (unsigned)((long long)g->T * g->k * g->I * 4);
+        f.residual = g->residual; f.residual_stride = g->residual_stride; f.y = g->y; f.y_stride = g->y_stride; f.y_f32 = es == 4;
+        const int n = g->T * g->k;
+        {
+            ProfileScope prof(PROF_ROWS_GEMM, 4.0 * n * g->I * g->K, 2.0 * n * g->I * g->K + 4.0 * n * g->I, st);
+            const dim3 grid((unsigned)ceil_div(g->I, 16), (unsigned)n), block(64u * c.waves_in);
+            if (xs == 4) hipLaunchKernelGGL((experts_token_in_kernel<FP8_X_F32>), grid, block, (size_t)c.waves_in * 128, st, f);
+            else hipLaunchKernelGGL((experts_token_in_kernel<FP8_X_BF16>), grid, block, (size_t)c.waves_in * 128, st, f);
+            FISE_CHECK_LAUNCH(fn);
+        }
+        ProfileScope prof(PROF_ROWS_GEMM, 2.0 * n * g->I * g->N, (double)n * g->I * (g->N + 4.0), st);
+        hipLaunchKernelGGL(experts_token_out_kernel, dim3((unsigned)ceil_div(g->N, 16), (unsigned)g->T), dim3(64u * c.waves_out), (size_t)c.waves_out * 64, st, f);
+        FISE_CHECK_LAUNCH(fn);
+        return FISE_OK;
+    }
     const int blocks_i = (g->I + FP8_BLOCK - 1) / FP8_BLOCK, blocks_k = (g->K + FP8_BLOCK - 1) / FP8_BLOCK, blocks_n = (g->N + FP8_BLOCK - 1) / FP8_BLOCK, n_tiles = (g->N + 255) / 256;
     if (c.m_tiles * std::max(blocks_i, n_tiles) > 0x7fffffff) return fail(FISE_ERR_SHAPE, "%s: more tiles than a launch holds", fn);
-    const hipStream_t st = as_stream(stream);
     unsigned char* const ws = (unsigned char*)workspace;
     const int pairs = g->T * g->k;
     ExpertsArgs r{};
@@ -135,7 +241,7 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.h = ws + c.h_off; a.h_stride = c.h_stride; a.h_scale = (float*)(ws + c.h_scale_off); a.h_scale_stride = pairs;
     {
         ProfileScope prof(PROF_IGEMM_GEGLU, 4.0 * pairs * g->I * g->K, 2.0 * std::min(g->E, pairs) * g->I * g->K + (double)pairs * (g->K + g->I), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_GATED>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED>(a, fn, st)) return e;
+        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_GATED>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED, true>(a, fn, st)) return e;
     }
     a.x = a.h; a.x_stride = c.h_stride; a.x_scale = a.h_scale; a.x_scale_stride = pairs;
     a.w = g->w_out; a.w_stride = g->I; a.w_expert = (long long)g->N * g->I; a.w_scale = g->w_out_scale; a.w_scale_expert = blocks_n * blocks_i;
@@ -143,14 +249,11 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4;
     {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * pairs * g->I * g->N, (double)std::min(g->E, pairs) * g->I * g->N + (double)pairs * (g->I + g->N * es), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS>(a, fn, st)) return e;
+        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
     }
-    ExpertsSum s{};
-    s.rows = a.y; s.ids = g->ids; s.weights = g->weights; s.residual = g->residual; s.residual_stride = g->residual_stride; s.y = g->y; s.y_stride = g->y_stride;
-    s.T = g->T; s.k = g->k; s.N = g->N; s.units = g->N / 8;
-    const dim3 sum_grid((unsigned)(((long long)g->T * s.units + 255) / 256));
-    if (es == 4) hipLaunchKernelGGL(experts_sum_kernel<float>, sum_grid, dim3(256), 0, st, s);
-    else hipLaunchKernelGGL(experts_sum_kernel<bf16_t>, sum_grid, dim3(256), 0, st, s);
+    s.rows = a.y;
+    if (es == 4) hipLaunchKernelGGL((experts_sum_kernel<float>), sum_grid, dim3(256), 0, st, s);
+    else hipLaunchKernelGGL((experts_sum_kernel<bf16_t>), sum_grid, dim3(256), 0, st, s);
     FISE_CHECK_LAUNCH(fn);
     return FISE_OK;
 }

@@ -48,15 +48,29 @@ inline Fp8Space fp8_space(int64_t M, int64_t K) {
     return s;
 }
 
-// The experts' feed-forward: tokens of a tile, an upper bound of the tiles, and the workspace.
+// The experts' feed-forward: its form, tokens of a tile, an upper bound of the tiles, and the workspace.
+// TOKENS: a workgroup has a pair, then a token's sum.  TILES: rows in 8 bits, tiles of an expert's rows through LDS.
+enum { EXPERTS_TOKENS = 0, EXPERTS_TILES = 1 };
 struct ExpertChoice {
-    int bm; int64_t m_tiles;
+    int form, bm; int64_t m_tiles;
+    int waves_in, waves_out;    // of a workgroup (TOKENS)
     int64_t x_stride, x_scale_off, h_off, h_stride, h_scale_off, out_off, table_off, bytes;
 };
-inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, int64_t E, int64_t k, int y_bytes) {
+inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, int64_t E, int64_t k, int64_t x_row_bytes, int y_bytes) {
     ExpertChoice c{};
-    const int64_t P = T * k;
+    const int64_t P = T * k, blocks_k = (K + 127) / 128, blocks_i = (I + 127) / 128;
     auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
+    // Two launches instead of four, but each pair reads its expert's weights and each workgroup puts its token in 8 bits, a block of columns for sixteen channels at a time.  us, TOKENS and TILES:
+    // one token, 2 of 16, 1280 x 640: 10.4 and 23.5; 8 of 128, 2048 x 768: 24 and 33; 8 of 64, 4096 x 1536: 51 and 53; four, 6 of 64, 2048 x 1408: 78 and 61
+    const bool fits = T * x_row_bytes < (1 << 30) && P * I * 4 < (1 << 30);      // offsets of these kernels
+    if (fits && T <= 4 && P * blocks_k * ((I + 15) / 16) <= 24576) {
+        c.form = EXPERTS_TOKENS;
+        c.waves_in = (int)std::min<int64_t>(16, blocks_k);
+        c.waves_out = (int)std::min<int64_t>(16, blocks_i * k);
+        c.bytes = up(P * I * 4);
+        return c;
+    }
+    c.form = EXPERTS_TILES;
     c.bm = P >= 512 * E ? 256 : P >= 64 * E ? 128 : 32;
     c.m_tiles = P / c.bm + std::min(E, P);
     const Fp8Space x = fp8_space(T, K), h = fp8_space(P, I);

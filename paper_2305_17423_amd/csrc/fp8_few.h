@@ -76,6 +76,16 @@ struct Fp8FewCodes {
 __device__ __forceinline__ int fp8_few_at(int n, int m) { return ((n >> 2) * 16 + m) * 4 + (n & 3); }
 #endif
 
+// A few tokens and their experts.
+struct ExpertsFewArgs {
+    const void* x; long long x_stride; unsigned x_bytes;               // [T, K]
+    const int* ids; const float* weights;
+    int T, k, E, K, I, N;
+    const unsigned char* w_in; const float* w_in_scale; const unsigned char* w_out; const float* w_out_scale;
+    float* h; unsigned h_bytes;                                        // [T k, I]
+    const void* residual; long long residual_stride; void* y; long long y_stride; int y_f32;
+};
+
 constexpr unsigned FP8_FEW_NO_ROW = 0x40000000u;   // behind every buffer of these kernels
 
 }  // namespace fise

@@ -143,9 +143,10 @@ def test_expert_mlp(change, code):
 
 
 def test_expert_mlp_workspace():
-    L, a = fb.lib(), set_all(experts(), T=3)
+    L, a = fb.lib(), set_all(experts(), T=30)
     need = L.fise_expert_mlp_workspace_bytes(ctypes.byref(a))
-    assert need > 3 * 256 + 6 * 128 + 6 * 128 * 2
+    assert need > 30 * 256 + 60 * 128 + 60 * 128 * 2 and L.fise_expert_mlp_workspace_bytes(ctypes.byref(set_all(experts(), T=3))) == 6 * 64 * 4
+    a.T = 30
     assert L.fise_expert_mlp(ctypes.byref(a), A, need - 1, None) == -5 and L.fise_expert_mlp(ctypes.byref(a), A + 16, need, None) == -4
     assert L.fise_expert_mlp_workspace_bytes(ctypes.byref(set_all(experts(), K=8))) == 0 and L.fise_expert_mlp_workspace_bytes(None) == 0 and L.fise_expert_mlp(None, None, 0, None) == -1
 
