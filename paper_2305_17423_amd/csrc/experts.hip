@@ -138,7 +138,7 @@ __global__ __launch_bounds__(1024) void experts_token_out_kernel(ExpertsFewArgs 
 
 // ---- the sum ----
 struct ExpertsSum {
-    const void* rows; const int* ids; const float* weights; const void* residual; long long residual_stride; void* y; long long y_stride;
+    const void* rows; const unsigned char* row_exp; const int* ids; const float* weights; const void* residual; long long residual_stride; void* y; long long y_stride;
     int T, k, N, units;
 };
 template <typename T> __global__ __launch_bounds__(256) void experts_sum_kernel(ExpertsSum a) {
@@ -151,7 +151,15 @@ template <typename T> __global__ __launch_bounds__(256) void experts_sum_kernel(
         const long long p = t * a.k + j;
         const float w = a.weights[p];
         float r[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (a.ids[p] >= 0) fp8_load8((const T*)a.rows + p * a.N + n, r);
+        if (a.ids[p] >= 0) {
+            if constexpr (sizeof(T) == 4) fp8_load8((const float*)a.rows + p * a.N + n, r);
+            else {                                                     // 16-bit floats times a power of two (fp8_tile.h)
+                const f16x8_t half = *reinterpret_cast<const f16x8_t*>((const _Float16*)a.rows + p * a.N + n);
+                const float f = fp8_power((int)a.row_exp[p * ((a.N + FP8_ROW_SHARE - 1) / FP8_ROW_SHARE) + n / FP8_ROW_SHARE] - 127);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[i] = (float)half[i] * f;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(w, r[i], v[i]);
     }
@@ -246,12 +254,12 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.x = a.h; a.x_stride = c.h_stride; a.x_scale = a.h_scale; a.x_scale_stride = pairs;
     a.w = g->w_out; a.w_stride = g->I; a.w_expert = (long long)g->N * g->I; a.w_scale = g->w_out_scale; a.w_scale_expert = blocks_n * blocks_i;
     a.N = g->N; a.K = g->I; a.n_tiles = n_tiles;
-    a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4;
+    a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4; a.row_exp = ws + c.row_exp_off;
     {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * pairs * g->I * g->N, (double)std::min(g->E, pairs) * g->I * g->N + (double)pairs * (g->I + g->N * es), st);
         if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
     }
-    s.rows = a.y;
+    s.rows = a.y; s.row_exp = a.row_exp;
     if (es == 4) hipLaunchKernelGGL((experts_sum_kernel<float>), sum_grid, dim3(256), 0, st, s);
     else hipLaunchKernelGGL((experts_sum_kernel<bf16_t>), sum_grid, dim3(256), 0, st, s);
     FISE_CHECK_LAUNCH(fn);

@@ -3,7 +3,7 @@
 Tolerance, from arithmetic.  A sum over the columns of codes is off by d = (2^-10 + 2 (128 + 3 K / 128 + 4) 2^-24) of the magnitudes' sum at most (what the matrix unit drops of
 eight products, and float roundings).  gate and up carry that into h: |dh| <= |silu(g)'|max |dg| |u| + |silu(g)| |du| with a slope of at most 1.1, and 2^-20 of h for SiLU in float.
 A code of h is the nearest one, so it lies between the codes of h - dh and of h + dh; the difference of those two, times the weights' magnitudes, bounds what a result is off by, with the second
-sum's own d, the rounding of an expert's result (half a step; bf16 results), and the output's."""
+sum's own d, the rounding of an expert's result (half a step; where the output is bf16 that is no more than 2^-12 of it, held to bf16's), and the output's."""
 import math
 
 import pytest
