@@ -54,7 +54,7 @@ enum { EXPERTS_TOKENS = 0, EXPERTS_TILES = 1 };
 struct ExpertChoice {
     int form, bm; int64_t m_tiles;
     int waves_in, waves_out;    // of a workgroup (TOKENS)
-    int64_t x_stride, x_scale_off, h_off, h_stride, h_scale_off, out_off, row_exp_off, table_off, bytes;
+    int64_t x_stride, x_scale_off, h_off, h_stride, h_scale_off, out_off, row_exp_off, table_off, place_off, bytes;
 };
 inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, int64_t E, int64_t k, int64_t x_row_bytes, int y_bytes) {
     ExpertChoice c{};
@@ -79,7 +79,8 @@ inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, in
     c.out_off = c.h_off + h.bytes;
     c.row_exp_off = c.out_off + up(P * N * y_bytes);
     c.table_off = c.row_exp_off + (y_bytes == 4 ? 0 : up(P * ((N + 63) / 64)));
-    c.bytes = c.table_off + up(c.m_tiles * 8);
+    c.place_off = c.table_off + up(c.m_tiles * 8);
+    c.bytes = c.place_off + up(P * 4);
     return c;
 }
 

@@ -55,7 +55,7 @@ __device__ __forceinline__ void fp8_load8(const bf16_t* p, float* v) {
 // What a tile kernel works on.  Rows of x are codes padded with zeros to whole blocks where the library made them.
 enum { FP8_LINEAR = 0,      // y[m, n] of rows 0..M-1
        FP8_GATED = 1,       // rows of pairs, gate and up: silu(gate) * up in 8 bits again
-       FP8_PAIRS = 2 };     // rows of those, to the pair's row of a scratch
+       FP8_PAIRS = 2 };     // rows of those, in the same order
 struct Fp8TileArgs {
     const unsigned char* x; long long x_stride; long long x_bytes;     // rows of codes (GATED: of tokens, in one buffer of x_bytes)
     const float* x_scale; long long x_scale_stride;                    // [block][row]
@@ -342,13 +342,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
             auto row_to = [&](int r, long long& to) {                  // where the wave's row r goes
                 const int row = (wm * MF + b) * 16 + r;
                 to = m0 + row;
-                if (row >= rows) return false;
-                if constexpr (KIND == FP8_PAIRS) {
-                    const unsigned p = (unsigned)a.slots[m0 + row];
-                    if (p >= (unsigned)a.pairs) return false;
-                    to = p;
-                }
-                return true;
+                return row < rows;
             };
             constexpr int LANES = W / 8, AT_ONCE = 64 / LANES;         // eight outputs a lane
             const int n = lane % LANES * 8;

@@ -172,7 +172,7 @@ def test_lists_that_do_not_fit(fb):
     good = call(fb, ex, x.cpu(), ids, w, None, torch.bfloat16)
     s2 = s.clone()
     n1 = int(o[1])
-    s2[0], s2[1] = -5, 10 ** 9                                                  # two pairs of expert 0 get lost: their rows of the scratch are what they were, here zeros
+    s2[0], s2[1] = -5, 10 ** 9                                                  # two pairs of expert 0 get lost: their tokens have no defined result
     for offsets, slots in ((o, s2), (o * 0 + 10 ** 9, s), (torch.flip(o, (0,)).contiguous(), s), (o - 10 ** 6, s)):
         a = fb.expert_mlp_args(x, ids.to(DEV), w.to(DEV), offsets, slots, *ex.dev, y)
         ws = torch.zeros(fb.fise_expert_mlp_workspace_bytes(a) + 4096, dtype=torch.uint8, device=DEV)
