@@ -623,7 +623,7 @@ def _here(args, workspace=None):
     d = args.device
     if d.type != "cuda" or (workspace is not None and workspace.device != d):
         raise ValueError(f"tensors on {d}, workspace on {None if workspace is None else workspace.device}: a call works on one GPU")
-    if d.index != torch.cuda.current_device():
+    if d.index != (_device() if _initialized() else torch.cuda.current_device()):
         raise ValueError(f"tensors on {d}, which is not the current device")
     if workspace is None:
         return None, 0
