@@ -29,7 +29,7 @@ inline RouteChoice route_choose(int64_t T, int E, int k, int groups, bool lists)
     if (c.single) {
         const int64_t rounds = (T + c.waves * at_once - 1) / (c.waves * at_once);
         c.wave_tokens = (int)(rounds > 0 ? rounds : 1) * at_once;
-    } else c.wave_tokens = 16;
+    } else c.wave_tokens = 12;      // (65536 tokens of 256 experts: 87 us, 91 with 16, 89 with 8)
     c.chunks = (int)((T + c.waves * c.wave_tokens - 1) / (c.waves * c.wave_tokens));
     if (lists && !c.single) {
         c.hist_off = (T * k * 4 + 255) / 256 * 256;

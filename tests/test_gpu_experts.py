@@ -109,7 +109,8 @@ def call(fb, ex, x, ids, w, residual, y_type, fill=0x7f):
 CASES = [(1, 16, 1280, 640, 1280, 2, 0, "bf16", "bf16", True), (1, 1, 16, 16, 8, 1, 0, "f32", "f32", False), (2, 4, 144, 48, 40, 4, 0, "bf16", "bf16", False),
          (7, 8, 320, 208, 328, 3, 8, "f32", "bf16", True), (33, 4, 640, 272, 264, 2, 0, "bf16", "f32", True), (64, 64, 512, 256, 512, 6, 3, "bf16", "bf16", True),
          (300, 3, 208, 144, 392, 2, 20, "bf16", "bf16", False), (520, 2, 128, 128, 128, 1, 100, "f32", "bf16", True), (257, 5, 400, 656, 520, 5, 0, "bf16", "bf16", True),
-         (1000, 8, 256, 384, 256, 2, 4, "bf16", "bf16", True), (90, 256, 128, 64, 128, 8, 2, "bf16", "bf16", True), (3, 1024, 64, 32, 64, 64, 0, "bf16", "bf16", False)]
+         (1000, 8, 256, 384, 256, 2, 4, "bf16", "bf16", True), (90, 256, 128, 64, 128, 8, 2, "bf16", "bf16", True),
+         (1300, 2, 144, 272, 200, 1, 1, "bf16", "bf16", True), (2100, 4, 272, 144, 264, 2, 1, "f32", "f32", False), (4, 8, 272, 144, 72, 8, 0, "f32", "bf16", True), (3, 1024, 64, 32, 64, 64, 0, "bf16", "bf16", False)]
 
 
 @pytest.mark.parametrize("T,E,K,I,N,k,skew,xt,yt,res", CASES)

@@ -116,7 +116,10 @@ CASES = [(1, 1280, 320, "f32", "f32", True, False), (1, 1, 16, "bf16", "f32", Fa
          (17, 1283, 1296, "bf16", "bf16", True, True), (33, 100, 128, "bf16", "f32", True, False), (54, 1283, 5136, "bf16", "bf16", True, True), (64, 640, 2048, "e4m3", "bf16", False, False),
          (65, 257, 272, "e4m3", "f32", True, True), (129, 255, 1280, "bf16", "bf16", True, False), (256, 129, 112, "f32", "f32", False, True), (300, 513, 400, "e4m3", "bf16", True, False),
          (1000, 2000, 528, "bf16", "bf16", True, True), (5, 4000, 4096, "e4m3", "bf16", True, False), (2049, 8200, 272, "bf16", "bf16", True, True), (4100, 4099, 144, "e4m3", "f32", True, False),
-         (8, 30, 16384, "bf16", "f32", False, False), (700, 5, 640, "bf16", "bf16", True, False), (4096, 3840, 656, "bf16", "f32", False, True)]
+         (8, 30, 16384, "bf16", "f32", False, False), (700, 5, 640, "bf16", "bf16", True, False), (4096, 3840, 656, "bf16", "f32", False, True),
+         # few rows for many outputs
+         (20, 8300, 400, "bf16", "bf16", True, True), (32, 10000, 144, "e4m3", "f32", True, False), (50, 9001, 272, "f32", "bf16", True, False), (64, 8208, 1040, "e4m3", "f32", False, True),
+         (40, 8200, 2064, "bf16", "bf16", True, False), (12, 700, 2064, "f32", "f32", True, True), (30, 333, 4112, "e4m3", "bf16", True, False)]
 
 
 @pytest.mark.parametrize("M,N,K,xt,yt,bias,res", CASES)
