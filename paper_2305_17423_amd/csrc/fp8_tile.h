@@ -268,13 +268,14 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
         if (NF * MF >= 2) add(NF * MF - 2);
         add(NF * MF - 1);
     }
+    // the last block's step has sent for one more, of zeros: it must have arrived before LDS is used for something else, and all waves must be done with their operands
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if constexpr (KIND == FP8_GATED) {
         // silu(gate) * up, the largest magnitude of a token's 128 channels over pieces, lanes and waves, codes
         constexpr int PITCH = FP8_BLOCK + 16;
         static_assert(WN * BM * 4 + BM * PITCH <= 2 * STAGE, "magnitudes and codes in LDS");
         unsigned* const largest = reinterpret_cast<unsigned*>(fp8_lds);      // [WN][BM]
         unsigned char* const codes = fp8_lds + WN * BM * 4;            // [BM], rows 16 bytes off the banks' round
-        __syncthreads();
 #pragma unroll
         for (int b = 0; b < MF; ++b) {
             unsigned top = 0;
@@ -326,7 +327,6 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
                     bias[f][i] = a.bias && n < n_left ? fp8_value(a.bias, a.bias_f32, nw + n) : 0.f;
                 }
         }
-        __syncthreads();
 #pragma unroll
         for (int b = 0; b < MF; ++b) {
 #pragma unroll

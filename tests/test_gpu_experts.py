@@ -209,3 +209,28 @@ def test_no_tokens(fb):
     ids, w = torch.zeros((0, 1), dtype=torch.int32, device=DEV), torch.zeros((0, 1), device=DEV)
     a = fb.expert_mlp_args(torch.zeros((0, 16), device=DEV), ids, w, torch.zeros(3, dtype=torch.int32, device=DEV), ids.view(-1), *ex.dev, torch.zeros((0, 8), device=DEV))
     fb.fise_expert_mlp(a, torch.zeros(256, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("T,E,K,I,N,k", [(48, 16, 1024, 640, 512, 4), (400, 4, 640, 384, 264, 1), (1200, 2, 384, 256, 512, 1)])
+def test_calls_between_other_kernels(fb, T, E, K, I, N, k):
+    """The first call and calls behind other kernels, whose code and LDS contents are what the next one finds: all alike, and the definition's.  (Loads still under way when LDS gets its
+    second use show only where a kernel's code is not in the caches yet.)"""
+    g = torch.Generator().manual_seed(T)
+    ex = Experts(g, E, K, I, N)
+    x = torch.randn((T, K), generator=g).bfloat16()
+    ids, w = pick(g, T, E, k, 0)
+    o, s = lists(ids, E)
+    y = [torch.full((T, N), math.nan, dtype=torch.bfloat16, device=DEV) for _ in range(6)]
+    xd, idd, wd, ws = x.to(DEV), ids.to(DEV), w.to(DEV), None
+    noise = torch.randn((1 << 20,), device=DEV)
+    for i, out in enumerate(y):
+        a = fb.expert_mlp_args(xd, idd, wd, o, s, *ex.dev, out)
+        if ws is None:
+            ws = torch.empty(fb.fise_expert_mlp_workspace_bytes(a), dtype=torch.uint8, device=DEV)
+        ws.fill_(0xFF)
+        fb.fise_expert_mlp(a, ws)
+        for f in (torch.sort, torch.fft.rfft, torch.erfinv, torch.lgamma, lambda t: t.view(1024, 1024) @ t.view(1024, 1024), lambda t: t.view(-1, 16).softmax(1), lambda t: t.topk(50)):
+            f(noise)
+    want, tol = ex.want(x, ids, w, None, torch.bfloat16)
+    assert bool(((y[0].double().cpu() - want).abs() <= tol).all())
+    assert all(torch.equal(y[0], t) for t in y[1:])
