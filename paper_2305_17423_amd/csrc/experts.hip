@@ -262,7 +262,7 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.h = ws + c.h_off; a.h_stride = c.h_stride; a.h_scale = (float*)(ws + c.h_scale_off); a.h_scale_stride = pairs;
     {
         ProfileScope prof(PROF_IGEMM_GEGLU, 4.0 * pairs * g->I * g->K, 2.0 * std::min(g->E, pairs) * g->I * g->K + (double)pairs * (g->K + g->I), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_GATED>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED, true>(a, fn, st)) return e;
+        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_GATED>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED, true>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED, true>(a, fn, st)) return e;
     }
     a.x = a.h; a.x_stride = c.h_stride; a.x_scale = a.h_scale; a.x_scale_stride = pairs;
     a.w = g->w_out; a.w_stride = g->I; a.w_expert = (long long)g->N * g->I; a.w_scale = g->w_out_scale; a.w_scale_expert = blocks_n * blocks_i;
@@ -270,7 +270,7 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4; a.row_exp = ws + c.row_exp_off;
     {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * pairs * g->I * g->N, (double)std::min(g->E, pairs) * g->I * g->N + (double)pairs * (g->I + g->N * es), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
+        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS, true>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
     }
     s.rows = a.y; s.row_exp = a.row_exp; s.place = r.place; s.pairs = pairs;
     if (es == 4) hipLaunchKernelGGL((experts_sum_kernel<float>), sum_grid, dim3(256), 0, st, s);
