@@ -661,10 +661,11 @@ int fise_route_experts(const fise_route_args* a /* host */, void* workspace, siz
 
 /* The feed-forward of the chosen experts and its weighted sum:
  *   h = silu(Wg[e] x_t) * (Wu[e] x_t),   y[t] = sum_j weights[t, j] * Wo[e] h (+ residual[t]),   e = ids[t, j]
- * Products as in fise_fp8_linear, with its sums for y in bf16 from 512 pairs an expert on, for float below: x and h are put in 8 bits with a power of two for 128 channels; sums float,
- * and for y in bf16 an expert's result keeps eleven bits before its weight (y float: all).  A
- * pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots belong together, as fise_route_experts leaves them (pairs
- * whose places are out of range or contradict each other get no defined result; nothing outside the buffers is touched).
+ * Products as in fise_fp8_linear: x and h are put in 8 bits with a power of two for 128 channels; sums float, but
+ * from 512 pairs an expert on (on average) as for y in bf16 there.  For y in bf16 a pair's result keeps eleven bits
+ * before its weight (y float: all).  A pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots belong
+ * together, as fise_route_experts leaves them (pairs whose places are out of range or contradict each other
+ * get no defined result; nothing outside the buffers is touched).
  * w_in codes [E, 2, I, K] (gate, up), w_in_scale [E, 2, ceil(I / 128), ceil(K / 128)]; w_out codes [E, N, I],
  * w_out_scale [E, ceil(N / 128), ceil(I / 128)]; 16-byte aligned.  x float or bf16 [T, K], rows x_stride apart; y,
  * residual [T, N], 16-byte aligned, strides multiples of 8.  K, I multiples of 16, N of 8, each at most 2^16; E 1..1024; T * k < 2^24;
@@ -689,18 +690,20 @@ int fise_expert_mlp(const fise_expert_mlp_args* a /* host */, void* workspace, s
  * events and returns the summed event time (ms), algorithmic FLOPs and bytes
  * and the number of launches recorded for `kind`:
  *   0 gathered GEMM over maps (and over 2048 - 4095 compact rows of one output)
- *   1 gathered GEMM with the GEGLU epilogue
+ *   1 gathered GEMM with the GEGLU epilogue, gate and up of experts on tiles
  *   2 attention (main kernels), of latent vectors too
- *   3 gathered GEMM, 64x128 tiles (>= 4096 compact rows); keys and values made of latent vectors
+ *   3 gathered GEMM, 64x128 tiles (>= 4096 compact rows); keys and values made of latent vectors; 8-bit
+ *     products on tiles, those of the experts' results among them
  *   4 split-K reduce launches           5 gathered GEMM, 32x128 tiles (<= 32 rows of odd widths)
  *   6 gathered GEMM with the GroupNorm prologue / 32-wide K steps, and four columns under a 3x3
  *     kernel behind a GroupNorm
  *   7 attention merge launches, with the latent vectors' values weights where they are one launch
  *   8 empty brackets (fise_profile_calibrate)
  *   9 gathered GEMM over compact rows (fewer than 2048, or several outputs), cross-attention
- *     that is one launch with the products beside it, and products with 4-bit weights
- * (masked norms, the packing of 4-bit weights and the queries' launch of attention over latent
- * vectors are not recorded)
+ *     that is one launch with the products beside it, products with 4-bit weights, 8-bit products of few
+ *     rows and of experts of a few tokens
+ * (masked norms, the packing of 4-bit weights, the queries' launch of attention over latent
+ * vectors, rows put in 8 bits, rotary positions, routing and the sum of the experts' results are not recorded)
  * kind = -1 clears the log.  fise_profile_calibrate records n brackets with no
  * launch inside on `stream`: their average is what a bracket itself adds to every
  * figure above.  All pointers host.  Not thread safe.

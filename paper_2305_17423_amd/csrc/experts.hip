@@ -150,7 +150,7 @@ __global__ __launch_bounds__(1024) void experts_token_out_kernel(ExpertsFewArgs 
 // ---- the sum ----
 struct ExpertsSum {
     const void* rows; const unsigned char* row_exp; const int* place; int pairs; const int* ids; const float* weights; const void* residual; long long residual_stride; void* y; long long y_stride;
-    int T, k, N, units;
+    int T, k, N, units, share;                                         // share: outputs with one power of two
 };
 template <typename T> __global__ __launch_bounds__(256) void experts_sum_kernel(ExpertsSum a) {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x, t = id / a.units;
@@ -167,7 +167,7 @@ template <typename T> __global__ __launch_bounds__(256) void experts_sum_kernel(
             if constexpr (sizeof(T) == 4) fp8_load8((const float*)a.rows + at * a.N + n, r);
             else {                                                     // 16-bit floats times a power of two (fp8_tile.h)
                 const f16x8_t half = *reinterpret_cast<const f16x8_t*>((const _Float16*)a.rows + at * a.N + n);
-                const float f = fp8_power((int)a.row_exp[at * ((a.N + FP8_ROW_SHARE - 1) / FP8_ROW_SHARE) + n / FP8_ROW_SHARE] - 127);
+                const float f = fp8_power((int)a.row_exp[at * ((a.N + a.share - 1) / a.share) + n / a.share] - 127);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) r[i] = (float)half[i] * f;
             }
@@ -242,7 +242,7 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
         FISE_CHECK_LAUNCH(fn);
         return FISE_OK;
     }
-    const int blocks_i = (g->I + FP8_BLOCK - 1) / FP8_BLOCK, blocks_k = (g->K + FP8_BLOCK - 1) / FP8_BLOCK, blocks_n = (g->N + FP8_BLOCK - 1) / FP8_BLOCK, n_tiles = (g->N + 255) / 256;
+    const int blocks_i = (g->I + FP8_BLOCK - 1) / FP8_BLOCK, blocks_k = (g->K + FP8_BLOCK - 1) / FP8_BLOCK, blocks_n = (g->N + FP8_BLOCK - 1) / FP8_BLOCK, n_tiles = ceil_div(g->N, c.bm == 32 ? 128 : 256);      // (32 rows: more workgroups on their way at once)
     if (c.m_tiles * std::max(blocks_i, n_tiles) > 0x7fffffff) return fail(FISE_ERR_SHAPE, "%s: more tiles than a launch holds", fn);
     unsigned char* const ws = (unsigned char*)workspace;
     const int pairs = g->T * g->k;
@@ -270,9 +270,9 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4; a.row_exp = ws + c.row_exp_off;
     {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * pairs * g->I * g->N, (double)std::min(g->E, pairs) * g->I * g->N + (double)pairs * (g->I + g->N * es), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS, true>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
+        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS, true>(a, fn, st) : launch_fp8_tile<2, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
     }
-    s.rows = a.y; s.row_exp = a.row_exp; s.place = r.place; s.pairs = pairs;
+    s.rows = a.y; s.row_exp = a.row_exp; s.place = r.place; s.pairs = pairs; s.share = c.bm == 32 ? 32 : 64;
     if (es == 4) hipLaunchKernelGGL((experts_sum_kernel<float>), sum_grid, dim3(256), 0, st, s);
     else hipLaunchKernelGGL((experts_sum_kernel<bf16_t>), sum_grid, dim3(256), 0, st, s);
     FISE_CHECK_LAUNCH(fn);

@@ -192,7 +192,7 @@ extern "C" int fise_fp8_linear(const fise_fp8_linear_args* g, void* workspace, s
     a.M = g->M; a.N = g->N; a.K = g->K; a.m_tiles = (int)c.m_tiles; a.n_tiles = (int)c.n_tiles;
     a.bias = g->bias; a.bias_f32 = g->bias_dtype == FISE_F32; a.residual = g->residual; a.residual_stride = g->residual_stride;
     a.y = g->y; a.y_stride = g->y_stride; a.y_f32 = g->y_dtype == FISE_F32;
-    ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * g->M * g->N * g->K, (double)g->N * g->K + (double)g->M * g->K + (double)g->M * g->N * ye, st);
+    ProfileScope prof(c.form == FP8_FORM_FEW ? PROF_ROWS_GEMM : PROF_IGEMM_WIDE, 2.0 * g->M * g->N * g->K, (double)g->N * g->K + (double)g->M * g->K + (double)g->M * g->N * ye, st);
     switch (c.form) {
         case FP8_FORM_256: return launch_fp8_tile<8, 4, 2, 4, FP8_LINEAR>(a, fn, st);
         case FP8_FORM_128: return a.y_f32 ? launch_fp8_tile<4, 4, 2, 2, FP8_LINEAR, true>(a, fn, st) : launch_fp8_tile<4, 4, 2, 2, FP8_LINEAR>(a, fn, st);

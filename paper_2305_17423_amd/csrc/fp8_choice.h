@@ -80,7 +80,7 @@ inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, in
     c.h_off = x.bytes; c.h_stride = h.stride; c.h_scale_off = c.h_off + h.scale_off;
     c.out_off = c.h_off + h.bytes;
     c.row_exp_off = c.out_off + up(P * N * y_bytes);
-    c.table_off = c.row_exp_off + (y_bytes == 4 ? 0 : up(P * ((N + 63) / 64)));
+    c.table_off = c.row_exp_off + (y_bytes == 4 ? 0 : up(P * ((N + 31) / 32)));
     c.place_off = c.table_off + up(c.m_tiles * 8);
     c.bytes = c.place_off + up(P * 4);
     return c;

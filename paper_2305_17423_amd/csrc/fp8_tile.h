@@ -69,9 +69,8 @@ struct Fp8TileArgs {
     const int* table; int pairs, k;                                    // table[tile] = expert << 24 ..., see experts.hip
     const int* slots;
     unsigned char* h; long long h_stride; float* h_scale; long long h_scale_stride;
-    unsigned char* row_exp;                                            // PAIRS that are not float: 16-bit floats times 2^(this - 127), for 64 outputs of a pair
+    unsigned char* row_exp;                                            // PAIRS that are not float: 16-bit floats times 2^(this - 127), for 64 outputs of a pair (32 where a wave has no more)
 };
-constexpr int FP8_ROW_SHARE = 64;
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -313,6 +312,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
         // sixteen tokens at a time through LDS, a part of it for each wave, so that a wave's outputs of a token are stored side by side; its rows are 16 bytes off the banks' round
         constexpr int W = NF * 16, PITCH = W * 4 + 16;
         static_assert(WAVES * 16 * PITCH <= 2 * STAGE, "the results of sixteen tokens in LDS");
+        constexpr int SHARE = W < 64 ? W : 64;                         // (a power of two belongs to one row of a wave)
         unsigned char* const mine = fp8_lds + wave * 16 * PITCH;
         const int es = a.y_f32 ? 4 : 2, nw = n0 + wn * W, n_left = min(W, a.N - nw);      // (n_left may be negative)
         bool wide = (((uintptr_t)a.y | (uintptr_t)(a.y_stride * es)) & 15) == 0;
@@ -354,13 +354,13 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                 if constexpr (KIND == FP8_PAIRS)
                     if (!a.y_f32) {
-                        // Results that meet others in a sum keep eleven bits: 16-bit floats times a power of two for eight lanes' outputs, which brings the largest to 2^14 .. 2^15.  (bf16 made the
+                        // Results that meet others in a sum keep eleven bits: 16-bit floats times a power of two for SHARE outputs, which brings the largest to 2^14 .. 2^15.  (bf16 made the
                         // sums 2.5e-3 off in the root mean square instead of 2.2e-3, of which 1.7e-3 is the sums' own rounding; floats move twice the bytes.)
                         unsigned top = 0;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) top = max(top, fp8_magnitude(v[i]));
 #pragma unroll
-                        for (int o = 1; o < FP8_ROW_SHARE / 8; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
+                        for (int o = 1; o < SHARE / 8; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
                         const int e = max((int)(top >> 23) - 141, -126);
                         const float inv = fp8_power(-e);
                         if (!row_to(r, to) || n >= n_left) continue;
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) half[i] = (_Float16)(v[i] * inv);
                         *reinterpret_cast<f16x8_t*>(reinterpret_cast<_Float16*>(a.y) + to * a.y_stride + nw + n) = half;
-                        if ((lane & (FP8_ROW_SHARE / 8 - 1)) == 0) a.row_exp[to * ((a.N + FP8_ROW_SHARE - 1) / FP8_ROW_SHARE) + (nw + n) / FP8_ROW_SHARE] = (unsigned char)(e + 127);
+                        if ((lane & (SHARE / 8 - 1)) == 0) a.row_exp[to * ((a.N + SHARE - 1) / SHARE) + (nw + n) / SHARE] = (unsigned char)(e + 127);
                         continue;
                     }
                 if (!row_to(r, to) || n >= n_left) continue;

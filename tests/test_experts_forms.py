@@ -96,7 +96,7 @@ def test_what_holds_for_any_size(ask):
             counts[rng.randrange(E)] += 1
         assert sum(-(-n // c["bm"]) for n in counts) <= c["m_tiles"]
         offs = [c[n] for n in ("x_scale_off", "h_off", "h_scale_off", "out_off", "row_exp_off", "table_off", "place_off", "bytes")]
-        need = [T * c["x_stride"], 4 * T * (c["x_stride"] // 128), P * c["h_stride"], 4 * P * (c["h_stride"] // 128), P * N * y, 0 if y == 4 else P * -(-N // 64), 8 * c["m_tiles"], 4 * P]
+        need = [T * c["x_stride"], 4 * T * (c["x_stride"] // 128), P * c["h_stride"], 4 * P * (c["h_stride"] // 128), P * N * y, 0 if y == 4 else P * -(-N // 32), 8 * c["m_tiles"], 4 * P]
         for begin, end, n in zip([0] + offs, offs, need):
             assert end - begin >= n and begin % 256 == 0
     cases = [(size(22), E, min(size(6), E, 64), rng.choice([g for g in (1, 2, 4, 8, 16, 64) if E % g == 0]), 1) for E in (size(10) for _ in range(2000))]
