@@ -216,6 +216,7 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     const ExpertChoice c = expert_choose(g->T, g->K, g->I, g->N, g->E, g->k, g->x_stride * xs, es);
     if (g->T && (!workspace || workspace_bytes < (size_t)c.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)c.bytes);
     if ((uintptr_t)workspace & 255) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
+    if ((long long)g->T * g->N >= 1LL << 34) return fail(FISE_ERR_SHAPE, "%s: T=%d N=%d: more results than a launch holds", fn, g->T, g->N);
     if (g->T == 0) return FISE_OK;
     ExpertsSum s{};
     s.ids = g->ids; s.weights = g->weights; s.residual = g->residual; s.residual_stride = g->residual_stride; s.y = g->y; s.y_stride = g->y_stride;
@@ -243,7 +244,7 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
         return FISE_OK;
     }
     const int blocks_i = (g->I + FP8_BLOCK - 1) / FP8_BLOCK, blocks_k = (g->K + FP8_BLOCK - 1) / FP8_BLOCK, blocks_n = (g->N + FP8_BLOCK - 1) / FP8_BLOCK, n_tiles = ceil_div(g->N, c.bm == 32 ? 128 : 256);      // (32 rows: more workgroups on their way at once)
-    if (c.m_tiles * std::max(blocks_i, n_tiles) > 0x7fffffff) return fail(FISE_ERR_SHAPE, "%s: more tiles than a launch holds", fn);
+    if (c.m_tiles * std::max(blocks_i, n_tiles) >= 1 << 23) return fail(FISE_ERR_SHAPE, "%s: more tiles than a launch holds", fn);
     unsigned char* const ws = (unsigned char*)workspace;
     const int pairs = g->T * g->k;
     ExpertsArgs r{};

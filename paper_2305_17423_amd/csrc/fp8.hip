@@ -111,13 +111,18 @@ template <int MT, int X> static int launch_few(const Fp8TileArgs& a, int waves, 
     FISE_CHECK_LAUNCH(fn);
     return FISE_OK;
 }
+// (a launch has fewer than 2^32 lanes: more rows go in several)
 static int fp8_rows(const char* fn, const void* x, int dtype, long long x_stride, int M, int K, int written, unsigned char* codes, long long code_stride, float* scale,
                     long long scale_stride, hipStream_t st) {
-    const int units = (K + FP8_BLOCK - 1) / FP8_BLOCK * 16;
-    const dim3 grid((unsigned)(((long long)M * units + 255) / 256));
-    if (dtype == FISE_F32) hipLaunchKernelGGL(fp8_rows_kernel<float>, grid, dim3(256), 0, st, (const float*)x, x_stride, M, K, units, written, codes, code_stride, scale, scale_stride);
-    else hipLaunchKernelGGL(fp8_rows_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)x, x_stride, M, K, units, written, codes, code_stride, scale, scale_stride);
-    FISE_CHECK_LAUNCH(fn);
+    const int units = (K + FP8_BLOCK - 1) / FP8_BLOCK * 16, step = std::max(1, (1 << 30) / units);
+    for (int r0 = 0; r0 < M; r0 += std::min(step, M - r0)) {
+        const int rows = std::min(step, M - r0);
+        const dim3 grid((unsigned)(((long long)rows * units + 255) / 256));
+        unsigned char* const c = codes + r0 * code_stride;
+        if (dtype == FISE_F32) hipLaunchKernelGGL(fp8_rows_kernel<float>, grid, dim3(256), 0, st, (const float*)x + r0 * x_stride, x_stride, rows, K, units, written, c, code_stride, scale + r0, scale_stride);
+        else hipLaunchKernelGGL(fp8_rows_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t*)x + r0 * x_stride, x_stride, rows, K, units, written, c, code_stride, scale + r0, scale_stride);
+        FISE_CHECK_LAUNCH(fn);
+    }
     return FISE_OK;
 }
 
@@ -138,10 +143,17 @@ extern "C" int fise_fp8_quantize(const void* x, int dtype, int64_t x_stride, int
         return fail(FISE_ERR_ALIGN, "%s: K and the strides of x and of the codes must be multiples of 8, x 16-byte, codes 8-byte aligned", fn);
     if (M == 0) return FISE_OK;
     if (block_rows == 1) return fp8_rows(fn, x, dtype, x_stride, M, K, K, codes, code_stride, scale, scale_stride, as_stream(stream));
-    const dim3 grid((unsigned)(((long long)M + 127) / 128 * blocks));
-    if (dtype == FISE_F32) hipLaunchKernelGGL(fp8_block_kernel<float>, grid, dim3(256), 0, as_stream(stream), (const float*)x, (long long)x_stride, M, K, (int)blocks, codes, (long long)code_stride, scale, (long long)scale_stride);
-    else hipLaunchKernelGGL(fp8_block_kernel<bf16_t>, grid, dim3(256), 0, as_stream(stream), (const bf16_t*)x, (long long)x_stride, M, K, (int)blocks, codes, (long long)code_stride, scale, (long long)scale_stride);
-    FISE_CHECK_LAUNCH(fn);
+    const int high = (int)(((long long)M + 127) / 128), step = (int)std::max<long long>(1, (1 << 22) / blocks);      // rows of blocks, and those of a launch
+    for (int b0 = 0; b0 < high; b0 += std::min(step, high - b0)) {
+        const long long r0 = (long long)b0 * FP8_BLOCK;
+        const dim3 grid((unsigned)(std::min(step, high - b0) * blocks));
+        const int rows = (int)(M - r0);
+        uint8_t* const c = codes + r0 * code_stride;
+        float* const s = scale + b0 * scale_stride;
+        if (dtype == FISE_F32) hipLaunchKernelGGL(fp8_block_kernel<float>, grid, dim3(256), 0, as_stream(stream), (const float*)x + r0 * x_stride, (long long)x_stride, rows, K, (int)blocks, c, (long long)code_stride, s, (long long)scale_stride);
+        else hipLaunchKernelGGL(fp8_block_kernel<bf16_t>, grid, dim3(256), 0, as_stream(stream), (const bf16_t*)x + r0 * x_stride, (long long)x_stride, rows, K, (int)blocks, c, (long long)code_stride, s, (long long)scale_stride);
+        FISE_CHECK_LAUNCH(fn);
+    }
     return FISE_OK;
 }
 
@@ -178,7 +190,7 @@ extern "C" int fise_fp8_linear(const fise_fp8_linear_args* g, void* workspace, s
     const Fp8Space space = c.make_rows ? fp8_space(g->M, g->K) : Fp8Space{};
     if (space.bytes && (!workspace || workspace_bytes < (size_t)space.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)space.bytes);
     if (space.bytes && ((uintptr_t)workspace & 255)) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
-    if (c.m_tiles * c.n_tiles > 0x7fffffff) return fail(FISE_ERR_SHAPE, "%s: M=%d N=%d: more tiles than a launch holds", fn, g->M, g->N);
+    if (c.m_tiles * c.n_tiles >= 1 << 23) return fail(FISE_ERR_SHAPE, "%s: M=%d N=%d: more tiles than a launch holds", fn, g->M, g->N);
     if (g->M == 0) return FISE_OK;
     const hipStream_t st = as_stream(stream);
     Fp8TileArgs a{};

@@ -181,7 +181,7 @@ extern "C" int fise_rotary(const fise_rotary_args* g, void* stream) {
     for (int i = 0; i < g->n_tensors; ++i) maps = maps || g->t[i].x_is_map || g->t[i].y_is_map;
     const bool grid = !g->pos || maps || g->tile;
     if (grid) {
-        if (g->T < 1 || g->H < 1 || g->W < 1 || (long long)g->T * g->H * g->W > 0x7fffffffLL) return fail(FISE_ERR_SHAPE, "%s: grid %d x %d x %d", fn, g->T, g->H, g->W);
+        if (g->T < 1 || g->H < 1 || g->W < 1 || (long long)g->T * g->H > 0x7fffffffLL || (long long)g->T * g->H * g->W > 0x7fffffffLL) return fail(FISE_ERR_SHAPE, "%s: grid %d x %d x %d", fn, g->T, g->H, g->W);
         if (!g->pos && g->n_axes > 3) return fail(FISE_ERR_SHAPE, "%s: a grid has at most 3 axes", fn);
         if (g->tile < 0 || (g->tile && (g->H % g->tile || g->W % g->tile))) return fail(FISE_ERR_SHAPE, "%s: tile %d on a %d x %d map", fn, g->tile, g->H, g->W);
         const long long tokens = (long long)g->T * g->H * g->W;
@@ -231,7 +231,7 @@ extern "C" int fise_rotary(const fise_rotary_args* g, void* stream) {
         const long long n = ((long long)a.rows * p.units * p.slices + 255) / 256;
         blocks = std::max(blocks, n);
     }
-    if (blocks > 0x7fffffffLL) return fail(FISE_ERR_SHAPE, "%s: more pairs than a launch holds", fn);
+    if (blocks >= 1 << 24) return fail(FISE_ERR_SHAPE, "%s: more pairs than a launch holds", fn);
     const dim3 dims((unsigned)blocks, (unsigned)g->n_tensors);
     const hipStream_t st = as_stream(stream);
     if (g->dtype == FISE_F32) {

@@ -515,6 +515,7 @@ extern "C" int fise_route_experts(const fise_route_args* g, void* workspace, siz
         return fail(FISE_ERR_ALIGN, "%s: pointers must be aligned to their type", fn);
     const bool lists = g->offsets != nullptr;
     const RouteChoice c = route_choose(g->T, g->E, g->k, g->groups, lists);
+    if (c.chunks >= 1 << 24) return fail(FISE_ERR_SHAPE, "%s: T=%d: more tokens than a launch holds", fn, g->T);
     if (c.bytes && (!workspace || workspace_bytes < (size_t)c.bytes)) return fail(FISE_ERR_CAPACITY, "%s: workspace of %zu bytes, %lld needed", fn, workspace ? workspace_bytes : 0, (long long)c.bytes);
     if (c.bytes && ((uintptr_t)workspace & 255)) return fail(FISE_ERR_ALIGN, "%s: workspace must be 256-byte aligned", fn);
     if (g->T == 0) return FISE_OK;

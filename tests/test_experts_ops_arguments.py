@@ -37,7 +37,7 @@ def rotary(**kw):
 @pytest.mark.parametrize("change,code", [({}, 0), ({"n_tensors": 0}, -2), ({"n_tensors": 3}, -2), ({"n_tensors": 2}, -1), ({"dtype": 2}, -3), ({"n_axes": 0}, -2), ({"n_axes": 5}, -2),
                                          ({"pairing": 3}, -2), ({"pairing": -1}, -2), ({"B": 0}, -2), ({"M": -1}, -2), ({"M": 5}, -2), ({"T": 0}, -2), ({"H": 6}, -2), ({"tile": 3}, -2), ({"tile": -4}, -2),
                                          ({"n_active": 5, "M": 80}, -5), ({"n_active": -1}, -5), ({"n_active": 1}, -2), ({"n_active": 1, "M": 16, "tile_idx": None}, -1),
-                                         ({"pos": A, "pos_B": 3}, -2), ({"pos": A + 2, "pos_B": 1}, -4), ({"T": 1 << 20, "H": 1 << 10, "W": 1 << 10}, -2)])
+                                         ({"pos": A, "pos_B": 3}, -2), ({"pos": A + 2, "pos_B": 1}, -4), ({"T": 1 << 20, "H": 1 << 10, "W": 1 << 10}, -2), ({"T": 1 << 30, "H": 1 << 30, "W": 1 << 30}, -2)])
 def test_rotary(change, code):
     refused("fise_rotary", rotary, change, code, None)
 
@@ -92,7 +92,7 @@ CODES = {"x_dtype": 2, "x_scale": A, "x_scale_stride": 0}
                                          ({"x_stride": 240}, -2), ({"w_stride": 240}, -2), ({"y_stride": 63}, -2), ({"residual": A, "residual_stride": 63}, -2), ({"w_stride": (1 << 22) + 16}, -2),
                                          ({"x_stride": (1 << 22) + 16}, -2), ({**CODES, "M": 4, "x_scale_stride": 3}, -2), ({"K": 248}, -4), ({"x_stride": 260}, -4), ({**CODES, "x_stride": 264}, -4),
                                          ({"x_stride": 264}, 0), ({"w_stride": 264}, -4), ({"x": A + 8}, -4), ({"w": A + 8}, -4), ({"y": A + 1}, -4), ({"bias": A + 2, "bias_dtype": 0}, -4),
-                                         ({"w_scale": A + 2}, -4), ({"M": 65}, -5)])
+                                         ({"w_scale": A + 2}, -4), ({"M": 65}, -5), ({**CODES, "M": 1 << 20, "N": 1 << 20, "y_stride": 1 << 20, "x_scale_stride": 1 << 20}, -2)])
 def test_fp8_linear(change, code):
     refused("fise_fp8_linear", fp8, change, code, None, 0, None)
 
@@ -114,7 +114,7 @@ def route():
                                          ({"dtype": 2}, -3), ({"E": 0}, -2), ({"E": 1025, "stride": 2000}, -2), ({"k": 0}, -2), ({"k": 65}, -2), ({"E": 3}, -2), ({"T": -1}, -2), ({"T": 1 << 30}, -2), ({"stride": 63}, -2),
                                          ({"score": 2}, -2), ({"score": -1}, -2), ({"groups": 0}, -2), ({"groups": 5}, -2), ({"groups": 4, "top_groups": 5}, -2), ({"groups": 4, "top_groups": 0}, -2),
                                          ({"groups": 4, "group_top": 3}, -2), ({"groups": 4, "group_top": 0}, -2), ({"groups": 4, "top_groups": 2, "group_top": 2}, 0), ({"logits": A + 2}, -4), ({"logits": A + 2, "dtype": 1}, 0),
-                                         ({"ids": A + 1}, -4), ({"bias": A + 2}, -4), ({"T": 1000}, -5)])
+                                         ({"ids": A + 1}, -4), ({"bias": A + 2}, -4), ({"T": 1000}, -5), ({"T": 1 << 30, "k": 1}, -2)])
 def test_route(change, code):
     refused("fise_route_experts", route, change, code, None, 0, None)
 
@@ -137,7 +137,7 @@ def experts():
                          [({"x_dtype": 2}, -3), ({"y_dtype": 2}, -3), ({"T": -1}, -2), ({"K": 0}, -2), ({"I": 0}, -2), ({"N": 0}, -2), ({"E": 0}, -2), ({"E": 1025}, -2), ({"k": 0}, -2), ({"k": 65}, -2),
                           ({"K": 65552, "x_stride": 65552}, -2), ({"I": 65552}, -2), ({"N": 65544, "y_stride": 65544}, -2), ({"T": 1 << 23}, -2), ({"T": 1 << 22, "k": 1}, -2), ({"K": 248}, -4), ({"I": 72}, -4),
                           ({"N": 124}, -4), ({"x_stride": 248}, -2), ({"y_stride": 120}, -2), ({"residual": A, "residual_stride": 120}, -2), ({"x_stride": 260}, -4), ({"y_stride": 132}, -4),
-                          ({"residual": A, "residual_stride": 132}, -4), ({"x": A + 8}, -4), ({"y": A + 8}, -4), ({"w_in": A + 8}, -4), ({"w_out": A + 4}, -4), ({"ids": A + 2}, -4), ({"w_in_scale": A + 2}, -4), ({"T": 1}, -5)])
+                          ({"residual": A, "residual_stride": 132}, -4), ({"x": A + 8}, -4), ({"y": A + 8}, -4), ({"w_in": A + 8}, -4), ({"w_out": A + 4}, -4), ({"ids": A + 2}, -4), ({"w_in_scale": A + 2}, -4), ({"T": 1}, -5), ({"T": 1 << 21, "N": 1 << 13, "y_stride": 1 << 13}, -5)])
 def test_expert_mlp(change, code):
     refused("fise_expert_mlp", experts, change, code, None, 0, None)
 
