@@ -132,11 +132,12 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
     static_assert(KIND != FP8_GATED || (BN == 256 && NF % 2 == 0), "gate and up of one block of 128");
     extern __shared__ __align__(16) unsigned char fp8_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave / WM, wm = wave % WM;
-    // workgroup w runs on XCD w mod 8, which gets a run of tiles: bands of six tiles of tokens, all outputs of a band before the next, so that the tiles at work in an XCD
-    // share rows of both sides in its L2
+    // workgroup w runs on XCD w mod 8, which gets a run of tiles: bands of a few tiles of tokens, all outputs of a band before the next, so that the tiles at work in an
+    // XCD share rows of both sides in its L2 (8192 x 8192 x 8192, bands of 4, 6, 8: 469, 461, 470 us; 131072 pairs of 64 experts, where a band's tiles may be of two of them, 3, 6, 12: 3.27, 3.33, 3.37 ms)
     int w = blockIdx.x;
     { const int chunk = gridDim.x >> 3; if (w < chunk << 3) w = (w & 7) * chunk + (w >> 3); }
-    const int band = w / (6 * a.n_tiles), in = w - band * 6 * a.n_tiles, high = min(6, a.m_tiles - band * 6), nt = in / high, mt = band * 6 + in - nt * high;
+    constexpr int BAND = KIND == FP8_LINEAR ? 6 : 3;
+    const int band = w / (BAND * a.n_tiles), in = w - band * BAND * a.n_tiles, high = min(BAND, a.m_tiles - band * BAND), nt = in / high, mt = band * BAND + in - nt * high;
     int m0 = mt * BM, rows = min(BM, a.M - m0), expert = 0;
     if constexpr (KIND != FP8_LINEAR) {
         const int first = a.table[2 * mt], info = a.table[2 * mt + 1];
