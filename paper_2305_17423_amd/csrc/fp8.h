@@ -12,16 +12,12 @@ __device__ __forceinline__ void fp8_quantize_unit(const T* x, long long x_stride
     const long long row = id / units;
     const int col = (int)(id - row * units) * 8;
     float v[8];
-    unsigned top = 0;
     const bool in = row < M && col < K;
     if (in) fp8_load8(x + row * x_stride + col, v);
+    else
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (!in) v[i] = 0.f;
-        top = max(top, fp8_magnitude(v[i]));
-    }
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    const unsigned top = fp8_over<16>(fp8_largest<8>(v));
     if (row >= M) return;
     const int e = fp8_exponent(top);
     const float inv = fp8_inverse(e);

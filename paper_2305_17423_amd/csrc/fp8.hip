@@ -1,7 +1,7 @@
 // 8-bit floating point (e4m3) with a scale for each block of 128 columns: rows and weights into codes, and the product of the two.
 //
 // Scales that the library makes are powers of two: dividing by one is exact, so a code is the value rounded once, and the largest of a block uses the format's range to
-// within a factor of two, which costs none of the three bits of mantissa.
+// within a factor of two, which costs none of the three bits of mantissa.  Rows into codes are bound by their bytes: 8192 x 8192 in bf16, 35 us (5.7 TB/s) among other launches.
 #include "fp8_few.h"
 #include "fp8_choice.h"
 
@@ -29,8 +29,7 @@ __global__ __launch_bounds__(256) void fp8_block_kernel(const T* x, long long x_
         else
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, fp8_magnitude(v[j][i]));
+        top = max(top, fp8_largest<8>(v[j]));
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));

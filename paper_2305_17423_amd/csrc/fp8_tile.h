@@ -6,6 +6,8 @@
 // The 8-bit instruction adds its products eight at a time and drops of each what is below 2^-13 of the largest of the eight (measured: eight of 2^14 and 2^1 add up exactly, those of 2^0
 // are gone); 16x16x32, of half its rate, does the same.  That is up to 2^-10 of the magnitudes' sum, next to 2^-8 of a bf16 result, so bf16 results and the experts take it; float results
 // (EXACT) are made of the same codes as bf16, whose instruction keeps all of a product, at half the rate.
+// 8192 x 8192 x 8192, rows in 8 bits: 461 - 490 us by the card, 2.2 - 2.4 PFLOP/s (a library's product with one scale a matrix: 414), matrix units busy 56 % of the time.  Steps on the way there, us: products added up
+// where they were made and the next block's loads waited for, 770; scales loaded a block ahead, 608; products added up two behind, 516; pieces without bank conflicts, 499; loads between the products, 470.
 #pragma once
 #include "common.h"
 #include "latent.h"
@@ -23,20 +25,32 @@ __device__ __forceinline__ int fp8_exponent(unsigned bits) {
     return max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -126);
 }
 __device__ __forceinline__ float fp8_power(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
-// magnitude for the scale: what is not finite does not count
-__device__ __forceinline__ unsigned fp8_magnitude(float v) {
-    const unsigned b = __float_as_uint(v) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0u;
-}
-// four values times `inverse`, a power of two that brings them to 448 at most, as codes; what is not finite is NaN (there is no infinity)
-__device__ __forceinline__ unsigned fp8_codes(float a, float b, float c, float d, float inverse) {
-    const float v[4] = {a * inverse, b * inverse, c * inverse, d * inverse};
-    int w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
+// The largest magnitude of N values (its bits); what is not finite does not count.  (NaN drops out of a maximum by itself, an infinity is looked for once.)
+template <int N> __device__ __forceinline__ unsigned fp8_largest(const float* v) {
+    float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!(fabsf(v[i]) <= 448.f)) w |= 0x7f << (8 * i);
+    for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(v[i]));
+    if (m > 3.402823466e38f) {
+        m = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fabsf(v[i]) <= 3.402823466e38f ? fmaxf(m, fabsf(v[i])) : m;
+    }
+    return __float_as_uint(m);
+}
+// the largest of such numbers over the LANES (4, 8 or 16) neighbouring lanes of a block of lanes
+template <int LANES> __device__ __forceinline__ unsigned fp8_over(unsigned v) {
+    int m = (int)v;                                                    // (not negative)
+    m = max(m, __builtin_amdgcn_update_dpp(0, m, 0xb1, 0xf, 0xf, false));      // lane ^ 1
+    m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x4e, 0xf, 0xf, false));      // lane ^ 2
+    if constexpr (LANES >= 8) m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x141, 0xf, 0xf, false));      // eight lanes mirrored
+    if constexpr (LANES >= 16) m = max(m, __builtin_amdgcn_update_dpp(0, m, 0x140, 0xf, 0xf, false));     // sixteen
+    return (unsigned)m;
+}
+// Four values times `inverse`, a power of two that brings what is finite to 448 at most, as codes: rounded to the nearest, ties to even; the conversion makes NaN of what is beyond (there is no infinity).
+__device__ __forceinline__ unsigned fp8_codes(float a, float b, float c, float d, float inverse) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
     return (unsigned)w;
 }
 __device__ __forceinline__ float fp8_inverse(int e) { return fp8_power(-e); }      // (e is between -126 and 119)
@@ -66,7 +80,7 @@ struct Fp8TileArgs {
     const void* bias; int bias_f32; const void* residual; long long residual_stride;
     void* y; long long y_stride; int y_f32;
     // experts
-    const int* table; int pairs, k;                                    // table[tile] = expert << 24 ..., see experts.hip
+    const int* table; int pairs, k;                                    // a tile's first row, and its expert << 16 | rows
     const int* slots;
     unsigned char* h; long long h_stride; float* h_scale; long long h_scale_stride;
     unsigned char* row_exp;                                            // PAIRS that are not float: 16-bit floats times 2^(this - 127), for 64 outputs of a pair (32 where a wave has no more)
@@ -278,15 +292,12 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
         unsigned char* const codes = fp8_lds + WN * BM * 4;            // [BM], rows 16 bytes off the banks' round
 #pragma unroll
         for (int b = 0; b < MF; ++b) {
-            unsigned top = 0;
+            float h[NF * 2];
 #pragma unroll
             for (int f = 0; f < NF / 2; ++f)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float g = acc[f][b][i];
-                    acc[f][b][i] = g / (1.f + __expf(-g)) * acc[f + NF / 2][b][i];
-                    top = max(top, fp8_magnitude(acc[f][b][i]));
-                }
+                for (int i = 0; i < 4; ++i) h[f * 4 + i] = acc[f][b][i] = silu_f(acc[f][b][i]) * acc[f + NF / 2][b][i];
+            unsigned top = fp8_largest<NF * 2>(h);
             top = max(top, (unsigned)__shfl_xor((int)top, 16));
             top = max(top, (unsigned)__shfl_xor((int)top, 32));
             if (lq == 0) largest[wn * BM + (wm * MF + b) * 16 + l16] = top;
@@ -357,11 +368,7 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
                     if (!a.y_f32) {
                         // Results that meet others in a sum keep eleven bits: 16-bit floats times a power of two for SHARE outputs, which brings the largest to 2^14 .. 2^15.  (bf16 made the
                         // sums 2.5e-3 off in the root mean square instead of 2.2e-3, of which 1.7e-3 is the sums' own rounding; floats move twice the bytes.)
-                        unsigned top = 0;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) top = max(top, fp8_magnitude(v[i]));
-#pragma unroll
-                        for (int o = 1; o < SHARE / 8; o <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
+                        const unsigned top = fp8_over<SHARE / 8>(fp8_largest<8>(v));
                         const int e = max((int)(top >> 23) - 141, -126);
                         const float inv = fp8_power(-e);
                         if (!row_to(r, to) || n >= n_left) continue;
