@@ -47,11 +47,12 @@ __global__ __launch_bounds__(256) void fp8_block_kernel(const T* x, long long x_
     if (tid == 0) scale[bm * scale_stride + bk] = fp8_power(e);
 }
 
-// At most 16 MT rows: a workgroup has sixteen outputs (fp8_few.h).
-template <int MT, int X>
+// At most 16 MT rows: a workgroup has sixteen outputs (fp8_few.h).  More than sixteen rows for bf16 results take the 8-bit instruction (fp8_tile.h): 54 rows, 1283 outputs of
+// 5136 columns, without turning codes into bf16 11.2 -> 10.4 us.
+template <int MT, int X, bool EXACT>
 __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    extern __shared__ __align__(16) float few_lds[];                   // [wave][MT][256]
+    extern __shared__ __align__(16) float few_lds[];                   // [wave][MT][FP8_FEW_PIECE]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, l16 = lane & 15, lq = lane >> 4;
     const int n0 = blockIdx.x * 16, blocks = (a.K + FP8_BLOCK - 1) / FP8_BLOCK;
     constexpr int es = X == FP8_X_CODES ? 1 : X == FP8_X_BF16 ? 2 : 4;
@@ -62,6 +63,16 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
 #pragma unroll
     for (int b = 0; b < MT; ++b) x_row[b] = b * 16 + l16 < a.M ? (unsigned)((b * 16 + l16) * a.x_stride * es) : FP8_FEW_NO_ROW;
     const float* const ws = a.w_scale + (long long)(n0 / FP8_BLOCK) * blocks;
+    // what is added to a lane's first result: asked for at the start, not behind the sums
+    auto added = [&](int i) {
+        const int n = n0 + (i & 15), m = i >> 4;
+        float v = 0.f;
+        if (m >= a.M || n >= a.N) return v;
+        if (a.bias) v += fp8_value(a.bias, a.bias_f32, n);
+        if (a.residual) v += fp8_value(a.residual, a.y_f32, m * a.residual_stride + n);
+        return v;
+    };
+    const float first = added(tid);
     f32x4_t acc[MT];
 #pragma unroll
     for (int b = 0; b < MT; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -69,7 +80,7 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
     Fp8FewWeights w;
     if (wave < blocks) w.ld(from_w, w_row, ws, wave, lq, a.K);
     for (int kb = wave; kb < blocks; kb += waves) {
-        Fp8Operand<true> v;
+        Fp8Operand<EXACT> v;
         const float wk = w.scale;
         v.of(w.lo, w.hi);
         if (kb + waves < blocks) w.ld(from_w, w_row, ws, kb + waves, lq, a.K);
@@ -79,7 +90,7 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
             for (int b = 0; b < MT; ++b) c[b].ld(from_x, x_row[b], a.x_scale + kb * a.x_scale_stride, b * 16 + l16, b * 16 + l16 < a.M, kb, lq, a.K);
 #pragma unroll
         for (int b = 0; b < MT; ++b) {
-            Fp8Operand<true> x;
+            Fp8Operand<EXACT> x;
             float xk;
             if constexpr (X == FP8_X_CODES) { x.of(c[b].lo, c[b].hi); xk = c[b].scale; }
             else fp8_few_rows<X>(from_x, x_row[b], kb, lq, a.K, x, xk);
@@ -89,24 +100,23 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
         }
     }
 #pragma unroll
-    for (int b = 0; b < MT; ++b) *reinterpret_cast<f32x4_t*>(few_lds + (wave * MT + b) * 256 + lane * 4) = acc[b];
+    for (int b = 0; b < MT; ++b) *reinterpret_cast<f32x4_t*>(few_lds + (wave * MT + b) * FP8_FEW_PIECE + (lq * 17 + l16) * 4) = acc[b];
     __syncthreads();
     for (int i = tid; i < a.M * 16; i += blockDim.x) {
         const int n = i & 15, m = i >> 4;
         if (n0 + n >= a.N) continue;
         float v = 0.f;
-        for (int k = 0; k < waves; ++k) v += few_lds[(k * MT + (m >> 4)) * 256 + fp8_few_at(n, m & 15)];
-        if (a.bias) v += fp8_value(a.bias, a.bias_f32, n0 + n);
-        if (a.residual) v += fp8_value(a.residual, a.y_f32, m * a.residual_stride + n0 + n);
+        for (int k = 0; k < waves; ++k) v += few_lds[(k * MT + (m >> 4)) * FP8_FEW_PIECE + fp8_few_at(n, m & 15)];
+        v += i == tid ? first : added(i);
         if (a.y_f32) reinterpret_cast<float*>(a.y)[m * a.y_stride + n0 + n] = v;
         else reinterpret_cast<bf16_t*>(a.y)[m * a.y_stride + n0 + n] = f2bf(v);
     }
 #endif
 }
-template <int MT, int X> static int launch_few(const Fp8TileArgs& a, int waves, const char* fn, hipStream_t st) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_few_kernel<MT, X>), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * MT * 1024);
+template <int MT, int X, bool EXACT = true> static int launch_few(const Fp8TileArgs& a, int waves, const char* fn, hipStream_t st) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_few_kernel<MT, X, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * MT * FP8_FEW_PIECE * 4);
     if (attr != hipSuccess) return fail(FISE_ERR_HIP, "%s: cannot raise the dynamic LDS limit", fn);
-    hipLaunchKernelGGL((fp8_few_kernel<MT, X>), dim3((unsigned)ceil_div(a.N, 16)), dim3(64u * waves), (size_t)waves * MT * 1024, st, a);
+    hipLaunchKernelGGL((fp8_few_kernel<MT, X, EXACT>), dim3((unsigned)ceil_div(a.N, 16)), dim3(64u * waves), (size_t)waves * MT * FP8_FEW_PIECE * 4, st, a);
     FISE_CHECK_LAUNCH(fn);
     return FISE_OK;
 }
@@ -211,6 +221,8 @@ extern "C" int fise_fp8_linear(const fise_fp8_linear_args* g, void* workspace, s
         case FP8_FORM_32: return a.y_f32 ? launch_fp8_tile<2, 2, 4, 1, FP8_LINEAR, true>(a, fn, st) : launch_fp8_tile<2, 2, 4, 1, FP8_LINEAR>(a, fn, st);
         default:
             if (!codes && !c.make_rows) return g->x_dtype == FISE_F32 ? launch_few<1, FP8_X_F32>(a, c.waves, fn, st) : launch_few<1, FP8_X_BF16>(a, c.waves, fn, st);
-            return a.M <= 16 ? launch_few<1, FP8_X_CODES>(a, c.waves, fn, st) : a.M <= 32 ? launch_few<2, FP8_X_CODES>(a, c.waves, fn, st) : launch_few<4, FP8_X_CODES>(a, c.waves, fn, st);
+            if (a.M <= 16) return launch_few<1, FP8_X_CODES>(a, c.waves, fn, st);
+            if (a.M <= 32) return a.y_f32 ? launch_few<2, FP8_X_CODES>(a, c.waves, fn, st) : launch_few<2, FP8_X_CODES, false>(a, c.waves, fn, st);
+            return a.y_f32 ? launch_few<4, FP8_X_CODES>(a, c.waves, fn, st) : launch_few<4, FP8_X_CODES, false>(a, c.waves, fn, st);
     }
 }

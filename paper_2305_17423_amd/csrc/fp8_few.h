@@ -2,8 +2,9 @@
 //
 // The weights' bytes and the trips to memory bound it, not products: a workgroup has sixteen outputs (experts: of gate and of up), its waves share the columns block by block, a
 // wave's loads are the lines of sixteen rows, and the waves' sums meet in LDS, added in their order.  Rows that are not in 8 bits yet are put there in registers: a lane has 32 columns of a
-// block of its token, four lanes the block.  The codes go to the products as bf16, whose sums lose nothing (fp8_tile.h).
-// One row, 1280 outputs of 320 columns: 5 us, a launch; 54 rows, 1283 of 5136: 12 us behind the 4 of the launch that puts them in 8 bits; 16 rows in 8 bits, 28672 of 8192: 59 us, 4.0 TB/s.
+// block of its token, four lanes the block.  Up to sixteen rows, and float results, have their codes turned into
+// bf16, whose sums lose nothing (fp8_tile.h).
+// One row, 1280 outputs of 320 columns: 5 us, a launch; 54 rows, 1283 of 5136: 10.4 us behind the 4 of the launch that puts them in 8 bits; 16 rows in 8 bits, 28672 of 8192: 59 us, 4.0 TB/s.
 #pragma once
 #include "fp8.h"
 
@@ -72,8 +73,8 @@ struct Fp8FewCodes {
         scale = there ? scales[at] : 0.f;
     }
 };
-// where result (output n of sixteen, row m of a piece) is among the 256 values of a piece, lane by lane
-__device__ __forceinline__ int fp8_few_at(int n, int m) { return ((n >> 2) * 16 + m) * 4 + (n & 3); }
+// where result (output n of sixteen, row m of a piece) is among the values of a piece, lane by lane, sixteen lanes 16 bytes off the banks' round
+__device__ __forceinline__ int fp8_few_at(int n, int m) { return ((n >> 2) * 17 + m) * 4 + (n & 3); }
 #endif
 
 // A few tokens and their experts.
@@ -86,6 +87,7 @@ struct ExpertsFewArgs {
     const void* residual; long long residual_stride; void* y; long long y_stride; int y_f32;
 };
 
+constexpr int FP8_FEW_PIECE = 4 * 17 * 4;            // values of a piece in LDS
 constexpr unsigned FP8_FEW_NO_ROW = 0x40000000u;   // behind every buffer of these kernels
 
 }  // namespace fise
