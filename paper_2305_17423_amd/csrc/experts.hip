@@ -4,7 +4,8 @@
 // 6 among 64 experts: 303 us, 124 on tiles.)  More: four launches: rows of x into 8 bits, with the table of tiles (a tile has rows of one expert); gate and up of a tile side by side in a wave, so that h leaves the
 // accumulators in 8 bits with the scale of its 128 channels; Wo; and the sum, which reads a pair's row where it is in the experts' order (rows stored where the pair is among
 // the tokens, 131072 rows of 4096: 1219 us instead of 1133).  No atomics: a result depends on its arguments only.
-// One token, 2 of 16 experts, 1280 x 640: 10.3 us; 64 tokens, 6 of 64, 2048 x 1408: 125 us, 4.4 TB/s of weights; 16384 tokens, 8 of 64, 4096 x 1536: 3.15 ms, 1.57 PFLOP/s (gate and up 1.8, the second product 1.1, the sum 0.29 ms).
+// One token, 2 of 16 experts, 1280 x 640: 9.2 us; 64 tokens, 6 of 64, 2048 x 1408: 124 us, 4.5 TB/s of weights; 16384 tokens, 8 of 64, 4096 x 1536: 3.06 - 3.15 ms, 1.6 PFLOP/s (gate and up 1.8 ms, the second
+// product 1.0, the sum 0.29).
 #include "fp8_few.h"
 #include "fp8_choice.h"
 
