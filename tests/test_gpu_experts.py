@@ -234,3 +234,17 @@ def test_calls_between_other_kernels(fb, T, E, K, I, N, k):
     want, tol = ex.want(x, ids, w, None, torch.bfloat16)
     assert bool(((y[0].double().cpu() - want).abs() <= tol).all())
     assert all(torch.equal(y[0], t) for t in y[1:])
+
+
+@pytest.mark.parametrize("T", [2, 30, 700])
+def test_an_expert_twice(fb, T):
+    """A token that lists an expert twice gets it with both weights; weights of zero, negative and large ones."""
+    g = torch.Generator().manual_seed(T)
+    ex = Experts(g, 3, 144, 80, 72)
+    x = torch.randn((T, 144), generator=g).bfloat16()
+    ids = torch.randint(0, 3, (T, 1), generator=g).to(torch.int32).expand(T, 3).contiguous()
+    w = torch.tensor([[0.0, -2.0, 1e4]]).expand(T, 3).contiguous()
+    residual = torch.randn((T, 72), generator=g).bfloat16()
+    y = call(fb, ex, x, ids, w, residual, torch.bfloat16)
+    want, tol = ex.want(x, ids, w, residual, torch.bfloat16)
+    assert bool(((y.double().cpu() - want).abs() <= tol).all())

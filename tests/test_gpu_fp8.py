@@ -217,3 +217,22 @@ def test_weights_made_here(fb):
     (xq, xe), (wq, we) = in_eight(x, 1), in_eight(pad, 128)
     v, u = xq * torch.exp2(xe).repeat_interleave(128, 1)[:, :272], wq * torch.exp2(we).repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :272]
     check(y, v @ u.t(), v.abs() @ u.abs().t(), 272)
+
+
+@pytest.mark.parametrize("M,yt", [(3, "f32"), (3, "bf16"), (40, "bf16"), (140, "f32"), (140, "bf16")])
+@pytest.mark.parametrize("low,high", [(0, 8), (0, 128), (1, 2), (0x78, 0x7f)])
+def test_codes_of_every_size(fb, M, yt, low, high):
+    """The smallest codes, which have no leading one, alone; all codes; the smallest of all; the largest: sums as of the values they stand for."""
+    g = torch.Generator().manual_seed(low * 7 + M)
+    N, K = 70, 400
+
+    def draw(m):
+        c = torch.randint(low, high, (m, K), generator=g)
+        c[c == 0x7f] = 0x7e
+        return (c + 128 * torch.randint(0, 2, c.shape, generator=g)).to(torch.uint8)
+    x, w = draw(M), draw(N)
+    xs, ws = torch.rand((blocks(K), M), generator=g) + 0.5, torch.rand((1, blocks(K)), generator=g) + 0.5
+    y = torch.zeros((M, N), dtype=T[yt], device=DEV)
+    fb.fise_fp8_linear(fb.fp8_linear_args(x.to(DEV), w.to(DEV), ws.to(DEV), y, x_scale=xs.to(DEV)))
+    v, u = x.view(E4M3).double() * xs.double().t().repeat_interleave(128, 1)[:, :K], wide(w.view(E4M3), ws)
+    check(y, v @ u.t(), v.abs() @ u.abs().t(), K)

@@ -157,3 +157,26 @@ def test_values_that_are_not_finite_and_another_stream(fb):
     fb.fise_rotary(fb.rotary_args([fb.rotary_tensor(x, y)], [8], 10.0, grid=(1, 2, 2)), stream=s)
     torch.cuda.current_stream().wait_stream(s)
     assert (~torch.isfinite(y)).nonzero().tolist() == [[0, 1, 0, 2], [0, 1, 0, 3], [0, 2, 0, 4], [0, 2, 0, 5]]
+
+
+@pytest.mark.parametrize("pairing", ["adjacent", "halves", "axis_halves"])
+@pytest.mark.parametrize("type,axes", [("bf16", [6, 4, 2, 20]), ("f32", [2, 2, 2, 2]), ("bf16", [2, 14, 8, 8]), ("f32", [16, 8, 24, 16])])
+@pytest.mark.parametrize("shared", [False, True])
+def test_four_axes_with_borders_inside_a_thread(fb, type, axes, pairing, shared):
+    """Four axes with positions of their own; axes of one pair; borders of axes anywhere among the pairs of a thread; a row of positions for each batch element."""
+    g = torch.Generator().manual_seed(sum(axes))
+    theta, offset = [10000.0, 7.0, 0.5, 1.0], [1.0, 0.0, -2.5, 100.0]
+    pos = 500 * torch.randn((3, 5, 4), generator=g)
+    x = torch.randn((3, 5, 2, sum(axes)), generator=g).to(T[type])
+    y = torch.zeros_like(x, device=DEV)
+    fb.fise_rotary(fb.rotary_args([fb.rotary_tensor(x.to(DEV), y)], axes, theta, pos=pos.to(DEV), offset=offset, pairing=pairing, shared_frequencies=shared))
+    close(y, *turn(x.double(), pos.double(), 0, axes, theta, pairing, shared, False, offset))
+
+
+def test_a_tile_listed_twice(fb):
+    x = torch.randn((1, 8, 2, 16), device=DEV)
+    x[:, 4:] = x[:, :4]
+    y = torch.zeros((1, 16, 2, 16), device=DEV)
+    idx = torch.tensor([2, 2], dtype=torch.int32, device=DEV)
+    fb.fise_rotary(fb.rotary_args([fb.rotary_tensor(x, y, y_is_map=True)], [8, 8], 10.0, grid=(1, 4, 4), tile_idx=idx, n_active=2, tile=2))
+    close(y[:, tile_tokens([2], (1, 4, 4), 2)], *turn(x[:, :4].double().cpu(), places((1, 4, 4), 2, tile_tokens([2], (1, 4, 4), 2))[None], 0, [8, 8], [10.0] * 2, "adjacent", False, False, [0, 0]))
