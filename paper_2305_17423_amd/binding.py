@@ -703,7 +703,7 @@ def fise_fp8_quantize(x, codes, scale, block_rows=1, stream=None):
     if M == 1:
         x_stride = code_stride = -(-K // 16) * 16
     _here(a)
-    _ck(lib().fise_fp8_quantize(_pn(x), _dt(x), x_stride, M, K, block_rows, _pn(codes), code_stride, _pn(scale), max(scale_stride, M if block_rows == 1 else blocks), _stream(stream)))
+    _ck(lib().fise_fp8_quantize(_pn(x), _dt(x), x_stride, M, K, block_rows, _pn(codes), code_stride, _pn(scale), scale_stride, _stream(stream)))
 
 
 def fp8_linear_args(x, w, w_scale, y, x_scale=None, bias=None, residual=None):
@@ -720,7 +720,7 @@ def fp8_linear_args(x, w, w_scale, y, x_scale=None, bias=None, residual=None):
     if x_scale is not None:
         if x_scale.dtype != torch.float32:
             raise ValueError(f"x_scale: {x_scale.dtype}, expected float")
-        a.x_scale, a.x_scale_stride = _pn(x_scale), max(_rows_of("x_scale", x_scale, (-(-K // 128), M)), M)
+        a.x_scale, a.x_scale_stride = _pn(x_scale), _rows_of("x_scale", x_scale, (-(-K // 128), M))
     a.w, a.w_stride = _p(w), _rows_of("w", w, (N, K))
     if N == 1:
         a.w_stride = -(-K // 16) * 16
@@ -756,7 +756,7 @@ def route_args(logits, ids, weights, offsets=None, slots=None, score="softmax", 
     T, E = logits.shape
     k = ids.shape[1]
     a = fise_route_args()
-    a.logits, a.dtype, a.stride = _pn(logits), _dt(logits), max(_rows_of("logits", logits, (T, E)), E)
+    a.logits, a.dtype, a.stride = _pn(logits), _dt(logits), _rows_of("logits", logits, (T, E))
     _like("ids", ids, (T, k), (torch.int32,))
     _like("weights", weights, (T, k), (torch.float32,))
     if (offsets is None) != (slots is None):
@@ -792,7 +792,7 @@ def expert_mlp_args(x, ids, weights, offsets, slots, w_in, w_in_scale, w_out, w_
     N, k = w_out.shape[1], ids.shape[1]
     blocks = lambda n: -(-n // 128)
     a = fise_expert_mlp_args()
-    a.x, a.x_dtype, a.x_stride = _pn(x), _dt(x), max(_rows_of("x", x, (T, K)), K)
+    a.x, a.x_dtype, a.x_stride = _pn(x), _dt(x), _rows_of("x", x, (T, K))
     if T == 1:
         a.x_stride = -(-K // 8) * 8
     _like("ids", ids, (T, k), (torch.int32,))
@@ -806,13 +806,13 @@ def expert_mlp_args(x, ids, weights, offsets, slots, w_in, w_in_scale, w_out, w_
     a.ids, a.weights, a.offsets, a.slots = _pn(ids), _pn(weights), _p(offsets), _pn(slots)
     a.T, a.K, a.k, a.E, a.I, a.N = T, K, k, E, I, N
     a.w_in, a.w_in_scale, a.w_out, a.w_out_scale = _p(w_in), _p(w_in_scale), _p(w_out), _p(w_out_scale)
-    a.y, a.y_dtype, a.y_stride = _pn(y), _dt(y), max(_rows_of("y", y, (T, N)), N)
+    a.y, a.y_dtype, a.y_stride = _pn(y), _dt(y), _rows_of("y", y, (T, N))
     if T == 1:
         a.y_stride = -(-N // 8) * 8
     if residual is not None:
         if residual.dtype != y.dtype:
             raise ValueError(f"residual is {residual.dtype}, y {y.dtype}")
-        a.residual, a.residual_stride = _pn(residual), max(_rows_of("residual", residual, (T, N)), N)
+        a.residual, a.residual_stride = _pn(residual), _rows_of("residual", residual, (T, N))
         if T == 1:
             a.residual_stride = a.y_stride
     _one_device(a, x, ids, weights, offsets, slots, w_in, w_in_scale, w_out, w_out_scale, residual, y)
