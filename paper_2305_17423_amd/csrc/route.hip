@@ -70,9 +70,8 @@ __device__ __forceinline__ long long route_first64(long long key, int& lane) {
 // One token by a whole wave in 64 bits, as the definition says: lane j gets the expert of place j (-1: none).  `broken`: a key is not a number.
 template <int V> __device__ __forceinline__ int route_exact(const RouteArgs& a, long long t, bool& broken) {
     const int lane = threadIdx.x & 63;
-    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);      // the order of the scores is that of the logits
     float l[V], top = -INFINITY;
-    double score[V];
+    double score[V], sum = 0.0;
     long long key[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -81,22 +80,19 @@ template <int V> __device__ __forceinline__ int route_exact(const RouteArgs& a, 
         top = fmaxf(top, l[i]);
         score[i] = (double)l[i];
     }
-    if (!direct) {
-        top = route_float(route_wave_max(route_code(top)));
-        double sum = 0.0;
+    top = route_float(route_wave_max(route_code(top)));
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            score[i] = l[i] == -INFINITY ? 0.0 : exp(a.sigmoid ? -score[i] : score[i] - (double)top);
-            sum += score[i];
-        }
-        sum = a.sigmoid ? 1.0 : route_sum<64>(sum);
+    for (int i = 0; i < V; ++i) {
+        score[i] = l[i] == -INFINITY ? 0.0 : exp(a.sigmoid ? -score[i] : score[i] - (double)top);
+        sum += score[i];
+    }
+    sum = a.sigmoid ? 1.0 : route_sum<64>(sum);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = lane * V + i;
-            score[i] = a.sigmoid ? 1.0 / (1.0 + score[i]) : score[i] / sum;
-            if (a.bias && e < a.E) score[i] += (double)a.bias[e];
-            broken = broken || (l[i] != -INFINITY && score[i] != score[i]);
-        }
+    for (int i = 0; i < V; ++i) {
+        const int e = lane * V + i;
+        score[i] = a.sigmoid ? 1.0 / (1.0 + score[i]) : score[i] / sum;
+        if (a.bias && e < a.E) score[i] += (double)a.bias[e];
+        broken = broken || (l[i] != -INFINITY && score[i] != score[i]);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = l[i] == -INFINITY || score[i] == -INFINITY ? ROUTE_NONE64 : route_code64(score[i]);
@@ -173,8 +169,8 @@ template <int V, int X> __device__ __forceinline__ void route_shift(int (&key)[V
 // The same by L lanes with keys in float, their order as whole numbers of which the last four bits are the place among a lane's V (the first has the largest).  `close`: two keys of which the
 // order matters are no further apart than their errors and those four bits explain, so the token needs route_exact.  ids[j]: the expert of place j, from the lane that has it.
 template <int L, int V>
-__device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, const float* bias, bool odd_bias, int sub, int part, volatile int* ids, bool& broken, bool& close) {
-    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);
+__device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, float top, const float* bias, bool odd_bias, int sub, int part, volatile int* ids, bool& broken, bool& close) {
+    const bool direct = !a.bias && (a.groups == 1 || a.group_top == 1);      // the logits are the keys: larger ones have larger scores, or (close) the same in 64 bits
     float off = 0.f, large = 0.f;
     int key[V];
     if (direct) {
@@ -187,10 +183,6 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
             for (int i = 0; i < V; ++i) v[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
             off = 0x1p-21f;                                            // s (1 - s) (|l| 2^-23 + 2^-21) of the exponential, which is below 2^-22.3, and three roundings of s
         } else {
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < V; ++i) top = fmaxf(top, l[i]);
-            top = route_float(route_max<L>(route_code(top)));
             double sum = 0.0;
 #pragma unroll
             for (int i = 0; i < V; ++i) { v[i] = l[i] == -INFINITY ? 0.f : __expf(l[i] - top); sum += (double)v[i]; }
@@ -215,8 +207,11 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
     // scores and the roundings of their biases.  (For sums of two keys `large` is twice the largest key there is, and their errors are those of two.)
     auto near = [&](int high, int low, float large, float errors) {
         if (low == ROUTE_NONE) return false;
-        if (direct) return a.f32 && high == low;
         const float h = route_float(high), w = route_float(low);
+        // Logits that are no further apart than this may have one score in 64 bits.  A score moves by (1 - s) dx of itself, with 1 - s >= 1 / (1 + e^x); under softmax by dx, where x - top is a
+        // difference in 64 bits.  2^-50 of that is behind every rounding of the score, and a difference of float keys without their places at most 32 times that of the logits.  Below
+        // -700 the exponential leaves the normal numbers.
+        if (direct) return high == low ? a.f32 != 0 : a.sigmoid ? !(h > -700.f && h - w > 0x1p-45f * (1.f + __expf(h))) : !(h - top > -690.f && h - w > 0x1p-45f * (1.f + (top - h)));
         return !(h - w > errors * off + (0x1p-19f + 0x1p-21f) * fmaxf(large, fmaxf(fabsf(h), fabsf(w))));
     };
     close = false;
@@ -238,7 +233,14 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
         int last = ROUTE_NONE;
         for (int j = 0; j <= a.top_groups && j < a.groups; ++j) {
             const int best = route_max<L>(mine);
-            if (j == a.top_groups) { close = near(last, best, 2.f * large, 4.f); break; }
+            if (j == a.top_groups) {
+                close = near(last, best, 2.f * large, 4.f);
+                if (direct && __any(best == last)) {                   // equal logits, and a lower one behind them with their score
+                    const int lower = route_max<L>(mine < best ? mine : ROUTE_NONE);
+                    close = close || (best == last && near(best, lower, 0.f, 0.f));
+                }
+                break;
+            }
             const int from = route_lowest<L>(mine == best, part);
             if (best != ROUTE_NONE && sub / lanes == from / lanes) kept = 1;
             if (sub == from) mine = ROUTE_NONE;
@@ -263,6 +265,16 @@ __device__ __forceinline__ void route_fast(const RouteArgs& a, const float* l, c
     int next = __shfl_down(taken, 1, L);
     if (sub == a.k - 1) next = after;
     if (sub < a.k && near(taken, next, 0.f, 2.f)) close = true;
+    if (direct) {                                                      // the last place's logit once more among those left over, and a lower one behind it with its score
+        const bool again = sub == a.k - 1 && taken == after && after != ROUTE_NONE;
+        if (__any(again)) {
+            int lower = ROUTE_NONE;
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const int v = key[i] & ~15; lower = max(lower, v < after ? v : ROUTE_NONE); }
+            lower = route_max<L>(lower);
+            if (again && near(after, lower, 0.f, 0.f)) close = true;
+        }
+    }
 }
 
 template <int L, int V, bool SINGLE>
@@ -318,9 +330,10 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
             bad = bad || l[i] != l[i] || (!a.sigmoid && l[i] == INFINITY);
             top = fmaxf(top, l[i]);
         }
+        top = route_float(route_max<L>(route_code(top)));
         bool close = odd_groups;
         ids[sub] = -1;
-        if (!odd_groups) route_fast<L, V>(a, l, bias, odd_bias, sub, part, ids, bad, close);
+        if (!odd_groups) route_fast<L, V>(a, l, top, bias, odd_bias, sub, part, ids, bad, close);
         const unsigned long long mask = L == 64 ? ~0ull : ((1ull << L) - 1) << (part * L);
         bad = (__ballot(bad) & mask) != 0;
         int id = ids[sub];
@@ -338,7 +351,6 @@ __global__ __launch_bounds__(SINGLE ? 1024 : 256) void route_kernel(RouteArgs a)
         const bool out = there && sub < a.k;
         const double logit = out && id >= 0 ? (double)route_logit(a, t, id) : 0.0;
         double w = 0.0;
-        top = a.sigmoid ? 0.f : route_float(route_max<L>(route_code(top)));
         const double p = exp(a.sigmoid ? -logit : logit - (double)top);
         if (out && id >= 0) w = a.sigmoid ? 1.0 / (1.0 + p) : p;
         if (a.renorm || !a.sigmoid) {
