@@ -72,8 +72,9 @@ inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, in
     }
     c.form = EXPERTS_TILES;
     // Tiles of 256 rows take the 8-bit instruction, which is what bounds them (131072 pairs, 4096 x 1536: 3.3 ms, with exact sums 5.4); smaller ones have exact sums, which cost them less (4096 tokens of 4
-    // among 64, 4096 x 1536: 864 and 952 us) and leave codes of h next to a border where they belong (error of the result without residual 2.6e-3 and 1.7e-3, its rounding)
-    c.bm = P >= 512 * E ? 256 : P >= 64 * E ? 128 : 32;
+    // among 64, 4096 x 1536: 864 and 952 us) and leave codes of h next to a border where they belong (error of the result without residual 2.6e-3 and 1.7e-3, its rounding).  Float results have
+    // exact sums at any size, as those of one product have (131072 pairs 5.75 ms, by the 8-bit instruction 3.46)
+    c.bm = P >= 512 * E && y_bytes != 4 ? 256 : P >= 64 * E ? 128 : 32;
     c.m_tiles = P / c.bm + std::min(E, P);
     const Fp8Space x = fp8_space(T, K), h = fp8_space(P, I);
     c.x_stride = x.stride; c.x_scale_off = x.scale_off;
