@@ -47,9 +47,9 @@ __global__ __launch_bounds__(256) void fp8_block_kernel(const T* x, long long x_
     if (tid == 0) scale[bm * scale_stride + bk] = fp8_power(e);
 }
 
-// At most 16 MT rows: a workgroup has sixteen outputs (fp8_few.h).  More than sixteen rows for bf16 results take the 8-bit instruction (fp8_tile.h): 54 rows, 1283 outputs of
-// 5136 columns, without turning codes into bf16 11.2 -> 10.4 us.
-template <int MT, int X, bool EXACT>
+// At most 16 MT rows: a workgroup has sixteen outputs (fp8_few.h).  The products' sums keep everything, for bf16 results too: with the 8-bit instruction (fp8_tile.h) 54 rows, 1283 outputs of 5136
+// columns take 14.7 us a call instead of 14.9, 32 rows, 8192 x 8192 25.4 instead of 27.1, and lose what is small beside products that cancel.
+template <int MT, int X>
 __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     extern __shared__ __align__(16) float few_lds[];                   // [wave][MT][FP8_FEW_PIECE]
@@ -76,11 +76,11 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
     f32x4_t acc[MT];
 #pragma unroll
     for (int b = 0; b < MT; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    // a block's weights are on their way while the one before is worked on (rows that are codes too: 32 rows, 8192 x 8192: 27 instead of 25 us)
+    // a block's weights are on their way while the one before is worked on (rows that are codes too: 32 rows, 8192 x 8192: 8 % slower)
     Fp8FewWeights w;
     if (wave < blocks) w.ld(from_w, w_row, ws, wave, lq, a.K);
     for (int kb = wave; kb < blocks; kb += waves) {
-        Fp8Operand<EXACT> v;
+        Fp8Operand<true> v;
         const float wk = w.scale;
         v.of(w.lo, w.hi);
         if (kb + waves < blocks) w.ld(from_w, w_row, ws, kb + waves, lq, a.K);
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
             for (int b = 0; b < MT; ++b) c[b].ld(from_x, x_row[b], a.x_scale + kb * a.x_scale_stride, b * 16 + l16, b * 16 + l16 < a.M, kb, lq, a.K);
 #pragma unroll
         for (int b = 0; b < MT; ++b) {
-            Fp8Operand<EXACT> x;
+            Fp8Operand<true> x;
             float xk;
             if constexpr (X == FP8_X_CODES) { x.of(c[b].lo, c[b].hi); xk = c[b].scale; }
             else fp8_few_rows<X>(from_x, x_row[b], kb, lq, a.K, x, xk);
@@ -113,10 +113,10 @@ __global__ __launch_bounds__(1024) void fp8_few_kernel(Fp8TileArgs a) {
     }
 #endif
 }
-template <int MT, int X, bool EXACT = true> static int launch_few(const Fp8TileArgs& a, int waves, const char* fn, hipStream_t st) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_few_kernel<MT, X, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * MT * FP8_FEW_PIECE * 4);
+template <int MT, int X> static int launch_few(const Fp8TileArgs& a, int waves, const char* fn, hipStream_t st) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&fp8_few_kernel<MT, X>), hipFuncAttributeMaxDynamicSharedMemorySize, 16 * MT * FP8_FEW_PIECE * 4);
     if (attr != hipSuccess) return fail(FISE_ERR_HIP, "%s: cannot raise the dynamic LDS limit", fn);
-    hipLaunchKernelGGL((fp8_few_kernel<MT, X, EXACT>), dim3((unsigned)ceil_div(a.N, 16)), dim3(64u * waves), (size_t)waves * MT * FP8_FEW_PIECE * 4, st, a);
+    hipLaunchKernelGGL((fp8_few_kernel<MT, X>), dim3((unsigned)ceil_div(a.N, 16)), dim3(64u * waves), (size_t)waves * MT * FP8_FEW_PIECE * 4, st, a);
     FISE_CHECK_LAUNCH(fn);
     return FISE_OK;
 }
@@ -221,8 +221,6 @@ extern "C" int fise_fp8_linear(const fise_fp8_linear_args* g, void* workspace, s
         case FP8_FORM_32: return a.y_f32 ? launch_fp8_tile<2, 2, 4, 1, FP8_LINEAR, true>(a, fn, st) : launch_fp8_tile<2, 2, 4, 1, FP8_LINEAR>(a, fn, st);
         default:
             if (!codes && !c.make_rows) return g->x_dtype == FISE_F32 ? launch_few<1, FP8_X_F32>(a, c.waves, fn, st) : launch_few<1, FP8_X_BF16>(a, c.waves, fn, st);
-            if (a.M <= 16) return launch_few<1, FP8_X_CODES>(a, c.waves, fn, st);
-            if (a.M <= 32) return a.y_f32 ? launch_few<2, FP8_X_CODES>(a, c.waves, fn, st) : launch_few<2, FP8_X_CODES, false>(a, c.waves, fn, st);
-            return a.y_f32 ? launch_few<4, FP8_X_CODES>(a, c.waves, fn, st) : launch_few<4, FP8_X_CODES, false>(a, c.waves, fn, st);
+            return a.M <= 16 ? launch_few<1, FP8_X_CODES>(a, c.waves, fn, st) : a.M <= 32 ? launch_few<2, FP8_X_CODES>(a, c.waves, fn, st) : launch_few<4, FP8_X_CODES>(a, c.waves, fn, st);
     }
 }

@@ -19,7 +19,7 @@ inline Fp8Choice fp8_choose(int64_t M, int64_t N, int64_t K, bool exact, bool co
     auto set = [&](int form, int bm, int bn) { c.form = form; c.bm = bm; c.bn = bn; c.m_tiles = (M + bm - 1) / bm; c.n_tiles = (N + bn - 1) / bn; };
     c.make_rows = !codes && M > 0;
     // Few rows: streaming the weights past them is bound by the trips; more rows for many outputs read rows and turn codes into bf16 too often for that.  us, streamed and tiles:
-    // 64 rows 4096 x 4096: 13.7 and 23.6, 8192 x 8192: 42 and 43.5, 10240 x 1280: 15.2 and 10.0, 28672 x 8192: 144 and 70; 32 rows 8192 x 8192: 25 and 38, 10240 x 1280: 9.9 and 8.6,
+    // 64 rows 4096 x 4096: 13.3 and 23.6, 8192 x 8192: 42 and 43.5, 10240 x 1280: 15.2 and 10.0, 28672 x 8192: 144 and 70; 32 rows 8192 x 8192: 27 and 38, 10240 x 1280: 9.9 and 8.6,
     // 28672 x 8192: 96 and 65; 16 rows 28672 x 8192: 59 and 63
     if (M <= 16 || (M <= 64 && N <= 8192)) {
         set(FP8_FORM_FEW, 64, 16);

@@ -2,9 +2,8 @@
 //
 // The weights' bytes and the trips to memory bound it, not products: a workgroup has sixteen outputs (experts: of gate and of up), its waves share the columns block by block, a
 // wave's loads are the lines of sixteen rows, and the waves' sums meet in LDS, added in their order.  Rows that are not in 8 bits yet are put there in registers: a lane has 32 columns of a
-// block of its token, four lanes the block.  Up to sixteen rows, and float results, have their codes turned into
-// bf16, whose sums lose nothing (fp8_tile.h).
-// One row, 1280 outputs of 320 columns: 5 us, a launch; 54 rows, 1283 of 5136: 10.4 us behind the 4 of the launch that puts them in 8 bits; 16 rows in 8 bits, 28672 of 8192: 59 us, 4.0 TB/s.
+// block of its token, four lanes the block.  The codes go to the products as bf16, whose sums lose nothing (fp8_tile.h).
+// One row, 1280 outputs of 320 columns: 5 us, a launch; 54 rows, 1283 of 5136: 11 us behind the 4 of the launch that puts them in 8 bits; 16 rows in 8 bits, 28672 of 8192: 59 us, 4.0 TB/s.
 #pragma once
 #include "fp8.h"
 

@@ -5,7 +5,7 @@
 // the lane's) and four neighbouring outputs.
 // The 8-bit instruction adds its products eight at a time and drops of each what is below 2^-13 of the largest of the eight (measured: eight of 2^14 and 2^1 add up exactly, those of 2^0
 // are gone); 16x16x32, of half its rate, does the same.  That is up to 2^-10 of the magnitudes' sum, next to 2^-8 of a bf16 result, so bf16 results and experts of many rows take it; float results
-// (EXACT) are made of the same codes as bf16, whose instruction keeps all of a product, at half the rate.
+// and experts of few rows (EXACT) are made of the same codes as bf16, whose instruction keeps all of a product, at half the rate.
 // 8192 x 8192 x 8192, rows in 8 bits: 461 - 490 us by the card, 2.2 - 2.4 PFLOP/s (a library's product with one scale a matrix: 414), matrix units busy 56 % of the time.  Steps on the way there, us: products added up
 // where they were made and the next block's loads waited for, 770; scales loaded a block ahead, 608; products added up two behind, 516; pieces without bank conflicts, 499; loads between the products, 470.
 #pragma once
