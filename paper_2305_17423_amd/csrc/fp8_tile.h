@@ -53,7 +53,7 @@ __device__ __forceinline__ unsigned fp8_codes(float a, float b, float c, float d
     w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
     return (unsigned)w;
 }
-__device__ __forceinline__ float fp8_inverse(int e) { return fp8_power(-e); }      // (e is between -126 and 119)
+__device__ __forceinline__ float fp8_inverse(int e) { return fp8_power(-e); }      // (e is between -126 and 120, of values beyond 1.75 * 2^127: 2^-120 is a normal number)
 
 __device__ __forceinline__ void fp8_load8(const float* p, float* v) {
     const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p), b = *reinterpret_cast<const f32x4_t*>(p + 4);
