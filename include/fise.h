@@ -663,8 +663,8 @@ int fise_route_experts(const fise_route_args* a /* host */, void* workspace, siz
 /* The feed-forward of the chosen experts and its weighted sum:
  *   h = silu(Wg[e] x_t) * (Wu[e] x_t),   y[t] = sum_j weights[t, j] * Wo[e] h (+ residual[t]),   e = ids[t, j]
  * Products as in fise_fp8_linear: x and h are put in 8 bits with a power of two for 128 channels; sums float, but
- * for y in bf16 from 512 pairs an expert on (on average) as for many rows there.  For y in bf16 a pair's result
- * keeps eleven bits before its weight (y float: all).  A pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots belong
+ * for y in bf16 from 512 pairs an expert on (on average) those of Wo as for many rows there.  For y in bf16 a pair's
+ * result keeps eleven bits before its weight (y float: all).  A pair with id -1 adds weights[t, j] * 0.  ids, weights, offsets and slots belong
  * together, as fise_route_experts leaves them (pairs whose places are out of range or contradict each other
  * get no defined result; nothing outside the buffers is touched).
  * w_in codes [E, 2, I, K] (gate, up), w_in_scale [E, 2, ceil(I / 128), ceil(K / 128)]; w_out codes [E, N, I],

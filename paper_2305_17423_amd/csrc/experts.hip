@@ -1,11 +1,12 @@
 // The feed-forward of the chosen experts: h = silu(Wg x) * (Wu x) and Wo h for every pair (token, expert) in the experts' order, then a token's weighted sum.
 //
 // A few tokens: two launches that stream the weights past them (fp8_few.h), a workgroup a pair, then a token, h in float in between.  (Rows of an expert streamed past like that, 64 tokens of
-// 6 among 64 experts: 303 us, 124 on tiles.)  More: four launches: rows of x into 8 bits, with the table of tiles (a tile has rows of one expert); gate and up of a tile side by side in a wave, so that h leaves the
+// 6 among 64 experts: 303 us, 124 on tiles.)  More: four launches: rows of x into 8 bits, with the tables of tiles (a tile has rows of one expert); gate and up of a tile side by side in a wave, so that h leaves the
 // accumulators in 8 bits with the scale of its 128 channels; Wo; and the sum, which reads a pair's row where it is in the experts' order (rows stored where the pair is among
 // the tokens, 131072 rows of 4096: 1219 us instead of 1133).  No atomics: a result depends on its arguments only.
-// One token, 2 of 16 experts, 1280 x 640: 9.2 us; 64 tokens, 6 of 64, 2048 x 1408: 124 us, 4.5 TB/s of weights; 16384 tokens, 8 of 64, 4096 x 1536: 3.06 - 3.15 ms, 1.6 PFLOP/s (gate and up 1.8 ms, the second
-// product 1.0, the sum 0.29).
+// Gate and up have exact sums (fp8_tile.h): h is put in 8 bits, and a code next to a border is moved by very little.
+// One token, 2 of 16 experts, 1280 x 640: 9.2 us; 64 tokens, 6 of 64, 2048 x 1408: 124 us, 4.5 TB/s of weights; 16384 tokens, 8 of 64, 4096 x 1536: 4.55 ms, 1.1 PFLOP/s (gate and up 3.25 ms, 1.0 PFLOP/s of a
+// library's 1.2 - 1.36 in bf16, the second product 1.0, the sum 0.28).
 #include "fp8_few.h"
 #include "fp8_choice.h"
 
@@ -14,13 +15,14 @@ namespace fise {
 struct ExpertsArgs {
     const void* x; long long x_stride; int T, K, units;
     unsigned char* codes; long long code_stride; float* scale;
-    const int* offsets; int E, pairs, bm, m_tiles; int* table;
+    const int* offsets; int E, pairs;
+    int tables, bm[2], m_tiles[2]; int* table[2];                      // of the second product, and of gate and up where theirs is another
     const int* slots; int* place;                                      // place[pair]: where it is in the experts' order
     int place_blocks;
 };
 
 // table[2 t] = first row of tile t in the experts' order, table[2 t + 1] = expert << 16 | rows (0: no such tile).  Offsets that do not ascend or leave 0..pairs count as the nearest that do not.
-__device__ void experts_table(const ExpertsArgs& a) {
+__device__ void experts_table(const ExpertsArgs& a, int bm, int m_tiles, int* table) {
     __shared__ int sums[2][4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (a.E + 255) / 256, e0 = min(tid * each, a.E), e1 = min(e0 + each, a.E);
@@ -40,8 +42,8 @@ __device__ void experts_table(const ExpertsArgs& a) {
         for (int e = e0; e < e1; ++e) {
             start = max(start, min(max(a.offsets[e], 0), a.pairs));
             const int end = max(start, min(max(a.offsets[e + 1], 0), a.pairs));
-            for (int r = start; r < end; r += a.bm, ++at)
-                if (write && at < a.m_tiles) { a.table[2 * at] = r; a.table[2 * at + 1] = e << 16 | min(a.bm, end - r); }
+            for (int r = start; r < end; r += bm, ++at)
+                if (write && at < m_tiles) { table[2 * at] = r; table[2 * at + 1] = e << 16 | min(bm, end - r); }
         }
         return at;
     };
@@ -53,20 +55,25 @@ __device__ void experts_table(const ExpertsArgs& a) {
     int at = upto - n, all = 0;
     for (int w = 0; w < 4; ++w) { if (w < wave) at += sums[1][w]; all += sums[1][w]; }
     tiles_from(at, true);
-    for (int t = all + tid; t < a.m_tiles; t += 256) { a.table[2 * t] = 0; a.table[2 * t + 1] = 0; }
+    for (int t = all + tid; t < m_tiles; t += 256) { table[2 * t] = 0; table[2 * t + 1] = 0; }
 }
 
 template <typename T> __global__ __launch_bounds__(256) void experts_rows_kernel(ExpertsArgs a) {
-    if (blockIdx.x == 0) { experts_table(a); return; }
-    if ((int)blockIdx.x <= a.place_blocks) {
-        const int s = (blockIdx.x - 1) * 256 + threadIdx.x;
+    const int block = (int)blockIdx.x - a.tables;
+    if (block < 0) {
+        const int w = blockIdx.x;
+        experts_table(a, w ? a.bm[1] : a.bm[0], w ? a.m_tiles[1] : a.m_tiles[0], w ? a.table[1] : a.table[0]);
+        return;
+    }
+    if (block < a.place_blocks) {
+        const int s = block * 256 + threadIdx.x;
         if (s < min(max(a.offsets[a.E], 0), a.pairs)) {
             const int p = a.slots[s];
             if ((unsigned)p < (unsigned)a.pairs) a.place[p] = s;
         }
         return;
     }
-    fp8_quantize_unit((const T*)a.x, a.x_stride, a.T, a.K, a.units, a.units * 8, a.codes, a.code_stride, a.scale, (long long)a.T, (long long)(blockIdx.x - 1 - a.place_blocks) * 256 + threadIdx.x);
+    fp8_quantize_unit((const T*)a.x, a.x_stride, a.T, a.K, a.units, a.units * 8, a.codes, a.code_stride, a.scale, (long long)a.T, (long long)(block - a.place_blocks) * 256 + threadIdx.x);
 }
 
 // ---- a few tokens ----
@@ -246,26 +253,37 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
         return FISE_OK;
     }
     const int blocks_i = (g->I + FP8_BLOCK - 1) / FP8_BLOCK, blocks_k = (g->K + FP8_BLOCK - 1) / FP8_BLOCK, blocks_n = (g->N + FP8_BLOCK - 1) / FP8_BLOCK, n_tiles = ceil_div(g->N, c.bm == 32 ? 128 : 256);      // (32 rows: more workgroups on their way at once)
-    if (c.m_tiles * std::max(blocks_i, n_tiles) >= 1 << 23) return fail(FISE_ERR_SHAPE, "%s: more tiles than a launch holds", fn);
     unsigned char* const ws = (unsigned char*)workspace;
     const int pairs = g->T * g->k;
     ExpertsArgs r{};
     r.x = g->x; r.x_stride = g->x_stride; r.T = g->T; r.K = g->K; r.units = blocks_k * 16; r.codes = ws; r.code_stride = c.x_stride; r.scale = (float*)(ws + c.x_scale_off);
-    r.offsets = g->offsets; r.E = g->E; r.pairs = pairs; r.bm = c.bm; r.m_tiles = (int)c.m_tiles; r.table = (int*)(ws + c.table_off);
+    r.offsets = g->offsets; r.E = g->E; r.pairs = pairs;
+    r.tables = c.bm_in == c.bm ? 1 : 2;
+    r.bm[0] = c.bm; r.m_tiles[0] = (int)c.m_tiles; r.table[0] = (int*)(ws + c.table_off);
+    r.bm[1] = c.bm_in; r.m_tiles[1] = (int)c.m_tiles_in; r.table[1] = (int*)(ws + c.table_in_off);
     r.slots = g->slots; r.place = (int*)(ws + c.place_off); r.place_blocks = ceil_div(pairs, 256);
-    const dim3 rows_grid((unsigned)(1 + r.place_blocks + ((long long)g->T * r.units + 255) / 256));
+    const dim3 rows_grid((unsigned)(r.tables + r.place_blocks + ((long long)g->T * r.units + 255) / 256));
     if (g->x_dtype == FISE_F32) hipLaunchKernelGGL(experts_rows_kernel<float>, rows_grid, dim3(256), 0, st, r);
     else hipLaunchKernelGGL(experts_rows_kernel<bf16_t>, rows_grid, dim3(256), 0, st, r);
     FISE_CHECK_LAUNCH(fn);
     Fp8TileArgs a{};
-    a.table = r.table; a.pairs = pairs; a.k = g->k; a.slots = g->slots; a.M = pairs; a.m_tiles = (int)c.m_tiles;
+    // (a launch has fewer than 2^32 lanes: more tiles go in several)
+    auto tiles = [&](const int* table, int64_t n, auto launch) {
+        const int64_t step = (1 << 22) / a.n_tiles;
+        for (int64_t t0 = 0; t0 < n; t0 += step) {
+            a.table = table + 2 * t0; a.m_tiles = (int)std::min(step, n - t0);
+            if (int e = launch()) return e;
+        }
+        return (int)FISE_OK;
+    };
+    a.pairs = pairs; a.k = g->k; a.slots = g->slots; a.M = pairs;
     a.x = ws; a.x_stride = c.x_stride; a.x_bytes = (long long)g->T * c.x_stride; a.x_scale = r.scale; a.x_scale_stride = g->T;
     a.w = g->w_in; a.w_stride = g->K; a.w_expert = 2LL * g->I * g->K; a.w_scale = g->w_in_scale; a.w_scale_expert = 2 * blocks_i * blocks_k;
     a.N = g->I; a.K = g->K; a.n_tiles = blocks_i;
     a.h = ws + c.h_off; a.h_stride = c.h_stride; a.h_scale = (float*)(ws + c.h_scale_off); a.h_scale_stride = pairs;
     {
         ProfileScope prof(PROF_IGEMM_GEGLU, 4.0 * pairs * g->I * g->K, 2.0 * std::min(g->E, pairs) * g->I * g->K + (double)pairs * (g->K + g->I), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_GATED>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED, true>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED, true>(a, fn, st)) return e;
+        if (int e = tiles(r.table[1], c.m_tiles_in, [&] { return c.bm_in == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_GATED, true>(a, fn, st) : launch_fp8_tile<4, 2, 4, 1, FP8_GATED, true>(a, fn, st); })) return e;
     }
     a.x = a.h; a.x_stride = c.h_stride; a.x_scale = a.h_scale; a.x_scale_stride = pairs;
     a.w = g->w_out; a.w_stride = g->I; a.w_expert = (long long)g->N * g->I; a.w_scale = g->w_out_scale; a.w_scale_expert = blocks_n * blocks_i;
@@ -273,7 +291,9 @@ extern "C" int fise_expert_mlp(const fise_expert_mlp_args* g, void* workspace, s
     a.y = ws + c.out_off; a.y_stride = g->N; a.y_f32 = es == 4; a.row_exp = ws + c.row_exp_off;
     {
         ProfileScope prof(PROF_IGEMM_WIDE, 2.0 * pairs * g->I * g->N, (double)std::min(g->E, pairs) * g->I * g->N + (double)pairs * (g->I + g->N * es), st);
-        if (int e = c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS, true>(a, fn, st) : launch_fp8_tile<2, 2, 4, 1, FP8_PAIRS, true>(a, fn, st)) return e;
+        if (int e = tiles(r.table[0], c.m_tiles, [&] {
+                return c.bm == 256 ? launch_fp8_tile<8, 4, 2, 4, FP8_PAIRS>(a, fn, st) : c.bm == 128 ? launch_fp8_tile<4, 4, 4, 2, FP8_PAIRS, true>(a, fn, st) : launch_fp8_tile<2, 2, 4, 1, FP8_PAIRS, true>(a, fn, st); }))
+            return e;
     }
     s.rows = a.y; s.row_exp = a.row_exp; s.place = r.place; s.pairs = pairs; s.share = c.bm == 32 ? 32 : 64;
     if (es == 4) hipLaunchKernelGGL((experts_sum_kernel<float>), sum_grid, dim3(256), 0, st, s);

@@ -52,9 +52,9 @@ inline Fp8Space fp8_space(int64_t M, int64_t K) {
 // TOKENS: a workgroup has a pair, then a token's sum.  TILES: rows in 8 bits, tiles of an expert's rows through LDS.
 enum { EXPERTS_TOKENS = 0, EXPERTS_TILES = 1 };
 struct ExpertChoice {
-    int form, bm; int64_t m_tiles;
+    int form, bm, bm_in; int64_t m_tiles, m_tiles_in;                  // TILES: of the second product, of gate and up
     int waves_in, waves_out;    // of a workgroup (TOKENS)
-    int64_t x_stride, x_scale_off, h_off, h_stride, h_scale_off, out_off, row_exp_off, table_off, place_off, bytes;
+    int64_t x_stride, x_scale_off, h_off, h_stride, h_scale_off, out_off, row_exp_off, table_off, place_off, table_in_off, bytes;
 };
 inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, int64_t E, int64_t k, int64_t x_row_bytes, int y_bytes) {
     ExpertChoice c{};
@@ -71,11 +71,14 @@ inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, in
         return c;
     }
     c.form = EXPERTS_TILES;
-    // Tiles of 256 rows take the 8-bit instruction, which is what bounds them (131072 pairs, 4096 x 1536: 3.3 ms, with exact sums 5.4); smaller ones have exact sums, which cost them less (4096 tokens of 4
-    // among 64, 4096 x 1536: 864 and 952 us) and leave codes of h next to a border where they belong (error of the result without residual 2.6e-3 and 1.7e-3, its rounding).  Float results have
-    // exact sums at any size, as those of one product have (131072 pairs 5.75 ms, by the 8-bit instruction 3.46)
+    // Gate and up have exact sums (fp8_tile.h) in every form, on 128 rows at most: what the 8-bit instruction drops of them moves codes of h that are next to a border, one in a thousand
+    // (131072 pairs, 4096 x 1536: 1.75 ms instead of 3.3, but the result's error without residual 2.6e-3 instead of 1.7e-3, its rounding).  For the second product, behind which nothing is put in
+    // 8 bits, bf16 results of many rows take that instruction, on tiles of 256 rows (1.0 ms, with exact sums on 128 rows 1.8); with fewer exact sums cost less (4096 tokens of 4 among 64,
+    // 4096 x 1536: the call 864 us and 952).  Float results have exact sums at any size, as those of one product have
     c.bm = P >= 512 * E && y_bytes != 4 ? 256 : P >= 64 * E ? 128 : 32;
+    c.bm_in = std::min(c.bm, 128);
     c.m_tiles = P / c.bm + std::min(E, P);
+    c.m_tiles_in = P / c.bm_in + std::min(E, P);
     const Fp8Space x = fp8_space(T, K), h = fp8_space(P, I);
     c.x_stride = x.stride; c.x_scale_off = x.scale_off;
     c.h_off = x.bytes; c.h_stride = h.stride; c.h_scale_off = c.h_off + h.scale_off;
@@ -83,7 +86,8 @@ inline ExpertChoice expert_choose(int64_t T, int64_t K, int64_t I, int64_t N, in
     c.row_exp_off = c.out_off + up(P * N * y_bytes);
     c.table_off = c.row_exp_off + (y_bytes == 4 ? 0 : up(P * ((N + 31) / 32)));
     c.place_off = c.table_off + up(c.m_tiles * 8);
-    c.bytes = c.place_off + up(P * 4);
+    c.table_in_off = c.bm_in == c.bm ? c.table_off : c.place_off + up(P * 4);      // (one table where the tiles are the same)
+    c.bytes = c.place_off + up(P * 4) + (c.bm_in == c.bm ? 0 : up(c.m_tiles_in * 8));
     return c;
 }
 

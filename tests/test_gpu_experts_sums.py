@@ -1,5 +1,5 @@
-"""GPU checks of what the experts' sums lose: nothing but float's roundings for float results, and below 512 pairs an expert; products below 2^-13 of the largest of eight, for bf16 results
-of more.
+"""GPU checks of what the experts' sums lose: nothing but float's roundings in gate and up, for float results, and below 512 pairs an expert; products below 2^-13 of the largest of eight
+in the second product, for bf16 results of more.
 
 Tolerance: as in the other tests of the experts, but the matrix unit's 2^-10 of the magnitudes only where the 8-bit instruction is the documented one, and 2^-11 for a pair's result on
 its way to a sum in bf16 (eleven bits; 2^-39 of the largest it shares a power of two with), none for float."""
@@ -31,7 +31,7 @@ def want(ex, x, ids, weight, residual, y_type):
     E, K, I, N = ex.dims
     T, k = ids.shape
     drop = 2.0 ** -10 if y_type == torch.bfloat16 and T * k >= 512 * E else 0.0
-    sums = lambda n: drop + 2 * (128 + 3 * n / 128 + 4) * 2.0 ** -24
+    sums = lambda n: 2 * (128 + 3 * n / 128 + 4) * 2.0 ** -24
     c, e = in_eight(x, 1)
     v = (c * torch.exp2(e).repeat_interleave(128, 1)[:, :K]).to(DEV)
     y = torch.zeros((T, N), dtype=torch.float64, device=DEV) if residual is None else residual.double().to(DEV)
@@ -56,7 +56,7 @@ def want(ex, x, ids, weight, residual, y_type):
             lo, hi = torch.where(may, torch.minimum(lo, a), lo), torch.where(may, torch.maximum(hi, b), hi)
         w = ex.outs[i]
         f = hq @ w.t()
-        off = torch.maximum(hi - hq, hq - lo) @ w.abs().t() + sums(I) * (hq.abs() @ w.abs().t())
+        off = torch.maximum(hi - hq, hq - lo) @ w.abs().t() + (drop + sums(I)) * (hq.abs() @ w.abs().t())
         if y_type == torch.bfloat16:
             off = off + 2.0 ** -11 * (f.abs() + off) + 2.0 ** -39 * (f.abs() + off).amax(1, keepdim=True)
         p = weight[t, j][:, None]
