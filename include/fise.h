@@ -583,7 +583,9 @@ int fise_latent_attention(const fise_latent_attention_args* a /* host */, void* 
  * (ids outside the grid: rows left out).  M is the number of rows.
  * x is [B, rows, heads, d] with neighbouring channels and any strides (in elements, at least 0; of y
  * without overlap); x_is_map / y_is_map: its rows are tokens of the whole map, else 0..M-1.  The other
- * channels of a head are copied.  y may be x with the same strides and form (in place); nothing else may overlap. */
+ * channels of a head are copied.  y may be x with the same strides and form (in place); nothing else may overlap.
+ * Ids of a list differ: of a tile listed twice a map gets either of its rows, and in place over a map its rows would be
+ * turned more than once, or in part. */
 enum { FISE_ROTARY_ADJACENT = 0, FISE_ROTARY_HALVES = 1, FISE_ROTARY_AXIS_HALVES = 2 };
 typedef struct {
     const void* x; void* y;

@@ -2,9 +2,9 @@
 //
 // Every channel is read and written once, which bounds it.  A thread owns VE pairs (one 16-byte vector of each side; one pair where strides or alignment do not
 // allow that) of one row, works out their sines and cosines once and turns those pairs of several heads with them.
-// The angle is taken in 64 bits and in turns, so that its whole part drops out without error and a position of 10^6 has the same angle as in
-// exact arithmetic to 2^-30 turns; sine and cosine of what is left are float.
-// Queries and keys of 65536 tokens, 16 heads of 128 channels each, bf16 (1.07 GB): 212 us, 5.1 TB/s, which is a large copy's rate.
+// The angle is taken in 64 bits and in turns, so that its whole part drops out without error and what is left of a position of 10^6 is that of
+// exact arithmetic to 2^-30 turns; rounded to float it is within 2^-26 turns, and sine and cosine are float.
+// Queries and keys of 65536 tokens, 16 heads of 128 channels each, bf16 (1.07 GB): 205 us, 5.2 TB/s, which is a large copy's rate.
 #include <cmath>
 #include "common.h"
 
@@ -224,7 +224,7 @@ extern "C" int fise_rotary(const fise_rotary_args* g, void* stream) {
         p.heads = t.heads; p.start = t.start; p.x_is_map = t.x_is_map != 0; p.y_is_map = t.y_is_map != 0;
         p.rot_units = a.half / ve;
         p.units = p.rot_units + (t.x == t.y ? 0 : (t.d - rot) / ve);
-        // heads that share a thread's sines: as many as leave two waves on each of the 1024 SIMDs, up to eight (65536 tokens, 16 heads of 128, us at 2, 4, 8, 16: 322, 231, 212, 256)
+        // heads that share a thread's sines: as many as leave two waves on each of the 1024 SIMDs, up to eight (65536 tokens, 16 heads of 128, us at 2, 4, 8, 16: 211, 202, 205, 234)
         const long long all = (long long)a.rows * p.units * t.heads;
         p.per_thread = (int)std::min<long long>(std::min(t.heads, 8), std::max<long long>(1, all / 131072));
         p.slices = ceil_div(t.heads, p.per_thread);

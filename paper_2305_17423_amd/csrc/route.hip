@@ -1,9 +1,10 @@
 // Routing of tokens to experts: keys (a score by softmax or sigmoid, and a bias), groups, the k largest, their weights, and the pairs (token, place) in the
 // experts' order.
 //
-// Reading the logits once bounds it for many tokens, a launch for few.  Sixteen lanes (64 for more than 256 experts) share a token, each with neighbouring experts in
+// Reading the logits once bounds it for many tokens, a launch for few.  Sixteen lanes (64 for more than 256 experts, sixteen places or sixteen groups) share a token, each with neighbouring experts in
 // registers; k rounds take the largest key, the lowest expert among equal ones.  Which expert is chosen is a whole number, so keys are compared as they are in 64 bits: in float first, and
-// again in 64 bits where two keys are closer than float's error explains (65536 tokens of 256 experts, 8 of 4 of 8 groups: 87 us; all in 64 bits 249).
+// again in 64 bits where two keys are closer than float's error explains (65536 tokens of 256 experts, 8 of 4 of 8 groups: 87 us; all in 64 bits 249).  Without a
+// bias, and groups by their largest key, the logits are the float keys, and two of them close where their scores may be one number of 64 bits.
 // The order of the pairs is that of a counting sort: a wave gives each of its pairs its rank among those of the same expert (ballots of the expert's bits find the lanes that
 // share it), the workgroup adds up its waves, and further launches add the workgroups, all in order, so that nothing depends on the run.  Few tokens are one workgroup and one launch.
 #include <algorithm>
