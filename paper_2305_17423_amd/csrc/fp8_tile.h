@@ -367,8 +367,8 @@ __global__ __launch_bounds__(64 * WN * WM) void fp8_tile_kernel(Fp8TileArgs a) {
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                 if constexpr (KIND == FP8_PAIRS)
                     if (!a.y_f32) {
-                        // Results that meet others in a sum keep eleven bits: 16-bit floats times a power of two for SHARE outputs, which brings the largest to 2^14 .. 2^15.  (bf16 made the
-                        // sums 2.5e-3 off in the root mean square instead of 2.2e-3, of which 1.7e-3 is the sums' own rounding; floats move twice the bytes.)
+                        // Results that meet others in a sum keep eleven bits: 16-bit floats times a power of two for SHARE outputs, which brings the largest to 2^14 .. 2^15.  (bf16
+                        // made the sums half as far again from 64 bits in the root mean square, where 1.7e-3 is their own rounding; floats move twice the bytes.)
                         const unsigned top = fp8_over<SHARE / 8>(fp8_largest<8>(v));
                         const int e = max((int)(top >> 23) - 141, -126);
                         const float inv = fp8_power(-e);
